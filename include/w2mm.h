@@ -321,6 +321,135 @@ W2_API int w2_matmul_a16_epi(const void* packed, int64_t K, int64_t N, int G, co
 W2_API int w2_workspace_size(int64_t M, int64_t K, int64_t N, int G, int a16, size_t* bytes);
 
 /* ------------------------------------------------------------------------
+ * The operators between the projections of an attention block, for serving:
+ * adapters of many requests beside a projection, norm and rotation of queries
+ * and keys with the keys and values written into a paged cache, and attention
+ * of each request's drafted tokens over that cache.  The conventions at the
+ * top of this file hold for them too.  Numbers inside device arrays (adapters,
+ * positions, slots, pages, lengths) cannot be checked on the host: what an
+ * out-of-range one means is said below, and no such number makes a kernel
+ * leave the buffers that the host-side arguments describe.
+ * ------------------------------------------------------------------------ */
+
+/* Low-rank adapters of many requests beside a shared projection X [M,K] ->
+ * base [M,N].  Adapter a of row m, part p of the columns (Q, K and V of a fused
+ * projection, gate and up), rank r < rank[a]:
+ *   T[m,p,r] = sum_k X[m,k] A[a,p,r,k]                               (fp32)
+ *   z[m,n]   = base[m,n] + scale[a] * sum_r T[m,p(n),r] B[a,n,r]      (fp32)
+ *   Y        = bf16 of z, silu(z), or silu(z_gate) z_up               (one rounding)
+ * A       dev, bf16, adapter a's row p*max_rank + r at A + a*a_stride + (p*max_rank + r)*K
+ * B       dev, bf16, adapter a's column n at B + a*b_stride + n*max_rank
+ * rank    dev, int32 [n_adapters], or NULL: every adapter has rank max_rank.  Entries of A and B at r >= rank[a]
+ *         do not reach the result whatever they are; rank[a] is clamped to 0..max_rank.
+ * scale   dev, fp32 [n_adapters], or NULL: 1
+ * n_parts 1..4; part p is the columns part_end[p-1] .. part_end[p]-1, part_end[n_parts-1] == N, the other ends
+ *         multiples of 16; gated != 0: two parts instead, which alternate by 16 columns (gate, up, gate, up ...: the
+ *         order of W2_ACT_SILU_MUL), n_parts and part_end not read.
+ * max_rank: a multiple of 8 up to 128; A and B 16-byte aligned, strides multiples of 8. */
+typedef struct {
+    const uint16_t* A;
+    const uint16_t* B;
+    const int32_t* rank;
+    const float* scale;
+    int64_t a_stride, b_stride;
+    int64_t part_end[4];
+    int n_adapters, max_rank, n_parts, gated;
+} w2_lora_t;
+
+/* Bytes of workspace (host out-pointer) that w2_lora_add needs for M rows. */
+W2_API int w2_lora_workspace_size(const w2_lora_t* lora, int64_t M, int64_t K, int64_t N, size_t* bytes);
+
+/* X        dev, fp32 or bf16 [M][K], row stride ldx
+ * adapter  dev, int32 [M]: the adapter of each row, in any order; a number outside 0..n_adapters-1 (-1): none,
+ *          the row is act(base)
+ * base     dev, bf16 [M][N], row stride ldb: the projection's result before its activation (a bias included), or
+ *          NULL: zero
+ * Y        dev, bf16 [M][N] ([M][N/2] for W2_ACT_SILU_MUL), row stride ldy; may be base itself except for
+ *          W2_ACT_SILU_MUL
+ * act      w2_act_t
+ * workspace  dev, 16-byte aligned, w2_lora_workspace_size bytes, contents undefined before and after
+ * K % 256 == 0, N % 8 == 0, as for the projections. */
+W2_API int w2_lora_add(const w2_lora_t* lora, int64_t K, int64_t N, const void* X, w2_dtype_t x_dtype, int64_t ldx,
+                       int64_t M, const int32_t* adapter, const uint16_t* base, int64_t ldb, uint16_t* Y, int64_t ldy,
+                       int act, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rotary positions.  Pair i of the first rotary_dim numbers of a head is
+ * (i, i + rotary_dim/2), or (2i, 2i+1) with interleaved != 0, and is turned by
+ * position * phase[i] / 2^64 turns:
+ *   (a, b) -> mscale * (a cos - b sin, b cos + a sin)
+ * phase (dev, [rotary_dim/2]) holds the frequencies as 64-bit fractions of a turn per position: whole turns drop out
+ * of the integer product, so the angle is as exact at position 2^31 - 1 as at 1.  rotary_dim % 4 == 0. */
+typedef struct {
+    const uint64_t* phase;
+    int rotary_dim, interleaved;
+    float mscale;
+} w2_rope_t;
+
+/* Scaled frequencies for contexts longer than the one trained on.  theta_i = base^(-2i/rotary_dim) per position;
+ *   NONE    theta_i
+ *   LINEAR  theta_i / factor
+ *   NTK     base is raised to base * factor^(rotary_dim / (rotary_dim - 2))
+ *   BANDS   by how many turns u = original_len * theta_i / 2 pi a pair makes in the original context: u <= low:
+ *           theta_i / factor; u >= high: theta_i; between: the mean of the two with weight (u - low)/(high - low) on
+ *           theta_i (arXiv 2309.00071, section 3.2; used there with mscale = 0.1 ln(factor) + 1) */
+typedef enum { W2_ROPE_NONE = 0, W2_ROPE_LINEAR = 1, W2_ROPE_NTK = 2, W2_ROPE_BANDS = 3 } w2_rope_scaling_t;
+
+/* phase: HOST, [rotary_dim/2], written on the host in 64 bits; the caller copies it to the device. */
+W2_API int w2_rope_phases(double base, int rotary_dim, w2_rope_scaling_t scaling, double factor, double original_len,
+                          double low, double high, uint64_t* phase);
+
+/* A paged cache of keys and values.  Page p, place t of it, head h: k + p*k_page_stride + t*k_slot_stride +
+ * h*k_head_stride, head_dim numbers in a row (bf16); v likewise.  Strides in elements, multiples of 8; k and v 16-byte
+ * aligned; any page_size; n_pages * page_size < 2^31. */
+typedef struct {
+    uint16_t *k, *v;
+    int64_t n_pages, page_size;
+    int64_t k_page_stride, k_slot_stride, k_head_stride;
+    int64_t v_page_stride, v_slot_stride, v_head_stride;
+    int n_heads, head_dim;
+} w2_kv_cache_t;
+
+/* One pass over the rows of a fused QKV projection: RMS norm of every query and key head, rotation, queries to q, keys
+ * and values into the cache.  All in fp32, one rounding to bf16.
+ * x          dev, bf16 [M][(n_q + 2 n_heads) * head_dim], row stride ldx: queries, keys, values
+ * q_weight, k_weight  dev, bf16 [head_dim], or NULL: not normed.  x_d -> x_d / sqrt(mean(x^2) + eps) * w_d over a head
+ * rope       NULL: no rotation;  positions  dev, int32 [M], >= 0
+ * q          dev, bf16 [M][n_q * head_dim], row stride ldq; may be x itself (ldq == ldx)
+ * slots      dev, int64 [M]: page * page_size + place of each row's key and value; a number outside the cache (-1):
+ *            not written.  NULL: row m goes to slot m.  No two rows may name the same slot.
+ * head_dim a multiple of 8 up to 256; x, q 16-byte aligned, ldx, ldq multiples of 8. */
+W2_API int w2_qk_norm_rope(const uint16_t* x, int64_t ldx, int64_t M, int n_q, const uint16_t* q_weight,
+                           const uint16_t* k_weight, float eps, const w2_rope_t* rope, const int32_t* positions,
+                           uint16_t* q, int64_t ldq, const w2_kv_cache_t* cache, const int64_t* slots, void* stream);
+
+/* Attention of drafted tokens over the cache.  Request r owns the rows row_start[r] .. row_start[r+1]-1 (T_r of them)
+ * and the keys 0 .. kv_len[r]-1, key c in place c % page_size of page page_table[r][c / page_size]; its drafted tokens
+ * are the last T_r keys, whose keys and values are in the cache already.  Row i of the request sees key c iff
+ *   c < kv_len[r] - T_r, or bit j = c - (kv_len[r] - T_r) of the row's mask is set      (mask == NULL: j <= i)
+ *   out = sum_c softmax_c(scale * q.k_c) v_c      lse = ln sum_c exp(scale * q.k_c)
+ * over the keys seen, query heads in equal groups per cache head; a row that sees none: out 0, lse -infinity.  Keys
+ * that no row of the request can see reach no result whatever their contents; a drafted token's own key and value are
+ * multiplied by zero in the rows that do not see it, so they have to be finite.  T_r = 1 is plain decoding; no mask is
+ * a causal chunk of a prompt.
+ * q          dev, bf16 [M][n_q * head_dim], row stride ldq;  out  the same with ldo;  lse  dev, fp32 [M][n_q] or NULL
+ * page_table dev, int32 [n_requests][table_cols], row stride ld_table; a number outside 0..n_pages-1: the keys of that
+ *            page are not seen
+ * row_start  dev, int32 [n_requests + 1], not decreasing, at most M;  kv_len  dev, int32 [n_requests]
+ * max_rows, max_len  at least every T_r and kv_len[r] (the launch is planned by them; rows and keys past them are left
+ *            out);  total_len  the sum of kv_len, or 0: not known
+ * mask       dev, [M][mask_words] words of 64 bits, bit j in word j / 64; NULL: causal
+ * workspace  optional (NULL / 0: none), 16-byte aligned: with w2_tree_attention_workspace_size bytes the keys of a
+ *            request are shared out over several workgroups where the batch is small, and a second launch joins them
+ * head_dim a multiple of 8 up to 256; n_q a multiple of the cache's n_heads; all pointers of bf16 16-byte aligned. */
+W2_API int w2_tree_attention_workspace_size(int64_t n_requests, int64_t M, int n_q, int n_heads, int head_dim,
+                                            int64_t max_rows, int64_t max_len, int64_t total_len, size_t* bytes);
+W2_API int w2_tree_attention(const uint16_t* q, int64_t ldq, int64_t M, int n_q, const w2_kv_cache_t* cache,
+                             const int32_t* page_table, int64_t table_cols, int64_t ld_table, const int32_t* row_start,
+                             const int32_t* kv_len, int64_t n_requests, int64_t max_rows, int64_t max_len,
+                             int64_t total_len, const uint64_t* mask, int mask_words, float scale, uint16_t* out,
+                             int64_t ldo, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Test-only exports.
  * w2_debug_group_acc_a8: the int32 group accumulators acc[M][K/G][N] (dense)
  *   exactly as the chosen kernel family holds them before the dequant step.

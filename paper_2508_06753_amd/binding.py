@@ -30,6 +30,7 @@ if not os.path.exists(LIB_PATH):
 _lib = ctypes.CDLL(LIB_PATH)
 
 _i64, _int, _sz, _vp = ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, ctypes.c_void_p
+_dbl = ctypes.c_double
 _SIGS = {
     "w2_packed_size": [_i64, _i64, _int, ctypes.POINTER(_sz)],
     "w2_prepack": [_vp, _vp, _i64, _i64, _int, _int, _vp, _sz, _vp, _vp],
@@ -49,6 +50,13 @@ _SIGS = {
     "w2_matmul_a8_epi": [_vp, _i64, _i64, _int, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp, _vp],
     "w2_matmul_a16_epi": [_vp, _i64, _i64, _int, _vp, _i64, _i64, _vp, _i64, _vp, _vp, _sz, _vp, _vp],
     "w2_matmul_a8_fused_epi": [_vp, _i64, _i64, _int, _vp, _int, _i64, _i64, _vp, _i64, _vp, _vp, _sz, _vp, _vp],
+    "w2_lora_workspace_size": [_vp, _i64, _i64, _i64, ctypes.POINTER(_sz)],
+    "w2_lora_add": [_vp, _i64, _i64, _vp, _int, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _int, _vp, _sz, _vp],
+    "w2_rope_phases": [_dbl, _int, _int, _dbl, _dbl, _dbl, _dbl, _vp],
+    "w2_qk_norm_rope": [_vp, _i64, _i64, _int, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _i64, _vp, _vp, _vp],
+    "w2_tree_attention_workspace_size": [_i64, _i64, _int, _int, _int, _i64, _i64, _i64, ctypes.POINTER(_sz)],
+    "w2_tree_attention": [_vp, _i64, _i64, _int, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _vp, _int,
+                          ctypes.c_float, _vp, _i64, _vp, _vp, _sz, _vp],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -345,6 +353,212 @@ def matmul_a16(packed, K, N, G, X, out=None, variant=VARIANT_AUTO, workspace=Non
     _check("w2_matmul_a16", _lib.w2_matmul_a16_ex(_ptr(packed), K, N, G, _ptr(X), ldx, M, _ptr(Y),
                                                   ldy, wp, wb, _tp(t), _stream()))
     return Y
+
+
+# ---- the operators between the projections of an attention block
+
+class _LoraStruct(ctypes.Structure):
+    _fields_ = [("A", _vp), ("B", _vp), ("rank", _vp), ("scale", _vp), ("a_stride", _i64), ("b_stride", _i64),
+                ("part_end", _i64 * 4), ("n_adapters", _int), ("max_rank", _int), ("n_parts", _int), ("gated", _int)]
+
+
+class Lora:
+    """Low-rank adapters of one projection [K -> N], laid out once (w2_lora_t).
+
+    A bf16 [n_adapters, parts * max_rank, K], B bf16 [n_adapters, N, max_rank]; rank int32 / scale fp32 [n_adapters] on
+    the device or None.  `parts`: the widths of the column ranges that have an A of their own (default: one);
+    gated=True: gate and up columns alternate by 16 instead."""
+
+    def __init__(self, A, B, rank=None, scale=None, parts=None, gated=False):
+        _dev(A, torch.bfloat16, "A")
+        _dev(B, torch.bfloat16, "B")
+        if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[0] < 1:
+            raise ValueError("A must be [n_adapters, parts * max_rank, K] and B [n_adapters, N, max_rank]")
+        n, N, R = B.shape
+        if gated and parts is not None:
+            raise ValueError("gated adapters have their two parts by blocks of 16 columns: give no widths")
+        widths = [N] if parts is None else [int(w) for w in parts]
+        n_parts = 2 if gated else len(widths)
+        if not 1 <= n_parts <= 4 or sum(widths) != N or min(widths) <= 0:
+            raise ValueError("parts must be one to four positive widths that add up to N")
+        if A.shape[1] != n_parts * R:
+            raise ValueError("A must have parts * max_rank rows")
+        if A.stride(2) != 1 or A.stride(1) != A.shape[2] or B.stride(2) != 1 or B.stride(1) != R:
+            raise ValueError("A and B must be dense within an adapter")
+        for t, dt, name in ((rank, torch.int32, "rank"), (scale, torch.float32, "scale")):
+            if t is not None and (_dev(t, dt, name).shape != (n,) or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous [n_adapters]")
+        self.A, self.B, self.rank, self.scale = A, B, rank, scale
+        self.K, self.N, self.max_rank, self.n_adapters, self.n_parts, self.gated = A.shape[2], N, R, n, n_parts, gated
+        ends = [sum(widths[:i + 1]) for i in range(len(widths))] + [0] * (4 - len(widths))
+        self._c = _LoraStruct(_ptr(A), _ptr(B), _ptr(rank), _ptr(scale), A.stride(0), B.stride(0), (_i64 * 4)(*ends), n, R,
+                              n_parts, int(gated))
+        self._ref = ctypes.byref(self._c)
+
+
+def lora_workspace_size(lora, M):
+    out = _sz(0)
+    _check("w2_lora_workspace_size", _lib.w2_lora_workspace_size(lora._ref, M, lora.K, lora.N, ctypes.byref(out)))
+    return out.value
+
+
+def lora_add(lora, X, adapter, base, act=ACT_NONE, out=None, workspace=None):
+    """Y bf16 = act(base + scale * (X A^T) B^T), each row of X (fp32 or bf16 [M,K]) with the adapter that `adapter` (int32
+    [M], -1: none) names.  `base`: bf16 [M,N], the projection's result before its activation, or None for zero.
+    `workspace`: a uint8 device tensor of lora_workspace_size(lora, M) bytes; allocated here if None."""
+    if X.dtype == torch.float32:
+        dt = DT_F32
+    elif X.dtype == torch.bfloat16:
+        dt = DT_BF16
+    else:
+        raise ValueError("X must be float32 or bfloat16")
+    M, K, N = X.shape[0], lora.K, lora.N
+    if not X.is_cuda or X.dim() != 2 or X.shape[1] != K or X.stride(1) != 1:
+        raise ValueError("X must be a device tensor [M,K] with unit inner stride")
+    _dev(adapter, torch.int32, "adapter")
+    if adapter.shape != (M,) or not adapter.is_contiguous():
+        raise ValueError("adapter must be contiguous [M]")
+    n_out = N // 2 if act == ACT_SILU_MUL else N
+    if base is not None:
+        _dev(base, torch.bfloat16, "base")
+        if base.shape != (M, N) or base.stride(1) != 1:
+            raise ValueError("base must be [M,N] with unit inner stride")
+    Y = out if out is not None else torch.empty((M, n_out), dtype=torch.bfloat16, device=X.device)
+    if out is not None and (_dev(Y, torch.bfloat16, "out").shape != (M, n_out) or Y.stride(1) != 1):
+        raise ValueError("out must be [M, number of output columns] with unit inner stride")
+    if workspace is None:
+        workspace = torch.empty(lora_workspace_size(lora, M), dtype=torch.uint8, device=X.device)
+    wp, wb = _ws(workspace)
+    _check("w2_lora_add", _lib.w2_lora_add(
+        lora._ref, K, N, X.data_ptr(), dt, X.stride(0) if M > 1 else K, M, adapter.data_ptr(), _ptr(base),
+        base.stride(0) if base is not None and M > 1 else N, Y.data_ptr(), Y.stride(0) if M > 1 else n_out, act, wp, wb,
+        _stream()))
+    return Y
+
+
+ROPE_NONE, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS = 0, 1, 2, 3
+
+
+class _RopeStruct(ctypes.Structure):
+    _fields_ = [("phase", _vp), ("rotary_dim", _int), ("interleaved", _int), ("mscale", ctypes.c_float)]
+
+
+def rope_phases(rotary_dim, base=10000.0, scaling=None):
+    """The frequencies of the rotated pairs as 64-bit fractions of a turn per position: int64 [rotary_dim/2] on the host.
+
+    scaling: None, ("linear", factor), ("ntk", factor) or ("bands", factor, original_len, low, high)."""
+    kind, args = ROPE_NONE, ()
+    if scaling is not None:
+        kinds = {"linear": (ROPE_LINEAR, 1), "ntk": (ROPE_NTK, 1), "bands": (ROPE_BANDS, 4)}
+        if scaling[0] not in kinds or len(scaling) - 1 != kinds[scaling[0]][1]:
+            raise ValueError("scaling must be ('linear', factor), ('ntk', factor) or ('bands', factor, original_len, low, high)")
+        kind, args = kinds[scaling[0]][0], scaling[1:]
+    factor, original_len, low, high = (tuple(float(a) for a in args) + (1.0, 0.0, 0.0, 0.0)[len(args):])
+    phase = torch.empty(max(1, rotary_dim // 2), dtype=torch.int64)
+    _check("w2_rope_phases", _lib.w2_rope_phases(base, rotary_dim, kind, factor, original_len, low, high, _ptr(phase)))
+    return phase
+
+
+class Rope:
+    """Rotary positions (w2_rope_t): the frequencies on the device and how a head's numbers pair up."""
+
+    def __init__(self, rotary_dim, base=10000.0, interleaved=False, scaling=None, mscale=1.0, device="cuda"):
+        self.rotary_dim, self.interleaved, self.mscale = rotary_dim, bool(interleaved), float(mscale)
+        self.phase = rope_phases(rotary_dim, base, scaling).to(device)
+        self._c = _RopeStruct(_ptr(self.phase), rotary_dim, int(self.interleaved), self.mscale)
+        self._ref = ctypes.byref(self._c)
+
+
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("n_pages", _i64), ("page_size", _i64),
+                ("k_page_stride", _i64), ("k_slot_stride", _i64), ("k_head_stride", _i64),
+                ("v_page_stride", _i64), ("v_slot_stride", _i64), ("v_head_stride", _i64),
+                ("n_heads", _int), ("head_dim", _int)]
+
+
+class KVCache:
+    """A paged cache (w2_kv_cache_t): k and v bf16 [pages, page_size, heads, head_dim], any strides with a unit inner one
+    (a cache stored [pages, heads, page_size, head_dim] is passed transposed)."""
+
+    def __init__(self, k, v):
+        _dev(k, torch.bfloat16, "k")
+        _dev(v, torch.bfloat16, "v")
+        if k.dim() != 4 or k.shape != v.shape or k.stride(3) != 1 or v.stride(3) != 1:
+            raise ValueError("k and v must be [pages, page_size, heads, head_dim] with unit inner stride")
+        self.k, self.v = k, v
+        self.n_pages, self.page_size, self.n_heads, self.head_dim = k.shape
+        self._c = _CacheStruct(_ptr(k), _ptr(v), k.shape[0], k.shape[1], *k.stride()[:3], *v.stride()[:3], k.shape[2], k.shape[3])
+        self._ref = ctypes.byref(self._c)
+
+
+def qk_norm_rope(x, n_q, rope, positions, cache, slots=None, q_weight=None, k_weight=None, eps=1e-6, out=None):
+    """Norm and rotation of the heads of x (bf16 [M, (n_q + 2 * cache.n_heads) * head_dim], a fused QKV projection's rows):
+    returns the queries, bf16 [M, n_q, head_dim]; keys and values go to the cache's `slots` (int64 [M], page * page_size +
+    place; -1: not written; None: row m to slot m).  rope None: no rotation; a weight None: not normed."""
+    _dev(x, torch.bfloat16, "x")
+    D, M = cache.head_dim, x.shape[0]
+    if x.dim() != 2 or x.shape[1] != (n_q + 2 * cache.n_heads) * D or x.stride(1) != 1:
+        raise ValueError("x must be [M, (n_q + 2 n_kv) * head_dim] with unit inner stride")
+    for t, dt, name in ((positions, torch.int32, "positions"), (slots, torch.int64, "slots")):
+        if t is not None and (_dev(t, dt, name).shape != (M,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous [M]")
+    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if t is not None and (_dev(t, torch.bfloat16, name).shape != (D,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous [head_dim]")
+    q = out if out is not None else torch.empty((M, n_q, D), dtype=torch.bfloat16, device=x.device)
+    if out is not None and (_dev(q, torch.bfloat16, "out").shape != (M, n_q, D) or q.stride(2) != 1 or q.stride(1) != D):
+        raise ValueError("out must be [M, n_q, head_dim], dense within a row")
+    _check("w2_qk_norm_rope", _lib.w2_qk_norm_rope(
+        x.data_ptr(), x.stride(0) if M > 1 else x.shape[1], M, n_q, _ptr(q_weight), _ptr(k_weight), eps,
+        rope._ref if rope is not None else None, _ptr(positions), q.data_ptr(), q.stride(0) if M > 1 else n_q * D,
+        cache._ref, _ptr(slots), _stream()))
+    return q
+
+
+def tree_attention_workspace_size(n_requests, M, n_q, cache, max_rows, max_len, total_len=0):
+    out = _sz(0)
+    _check("w2_tree_attention_workspace_size", _lib.w2_tree_attention_workspace_size(
+        n_requests, M, n_q, cache.n_heads, cache.head_dim, max_rows, max_len, total_len, ctypes.byref(out)))
+    return out.value
+
+
+def tree_attention(q, cache, page_table, row_start, kv_len, max_rows, max_len, mask=None, scale=None, total_len=0, out=None,
+                   lse=None, workspace=None):
+    """Attention of the rows q (bf16 [M, n_q, head_dim]) of every request over its keys in the cache: out like q.
+
+    page_table int32 [requests, pages], row_start int32 [requests + 1], kv_len int32 [requests]; mask int64 [M, words], bit
+    j: the row sees its request's drafted token j (None: causal); scale None: 1/sqrt(head_dim).  lse: fp32 [M, n_q], written
+    if given.  `workspace`: a uint8 device tensor of tree_attention_workspace_size bytes; None: the keys of a request are
+    not shared out over workgroups."""
+    _dev(q, torch.bfloat16, "q")
+    M, n_q, D = q.shape
+    if D != cache.head_dim or q.stride(2) != 1 or (n_q > 1 and q.stride(1) != D):
+        raise ValueError("q must be [M, n_q, head_dim], dense within a row")
+    _dev(page_table, torch.int32, "page_table")
+    _dev(row_start, torch.int32, "row_start")
+    _dev(kv_len, torch.int32, "kv_len")
+    R = kv_len.shape[0]
+    if page_table.dim() != 2 or page_table.shape[0] != R or page_table.stride(1) != 1 or row_start.shape != (R + 1,) or \
+            not row_start.is_contiguous() or not kv_len.is_contiguous():
+        raise ValueError("page_table must be [requests, pages], row_start [requests + 1], kv_len [requests]")
+    words = 0
+    if mask is not None:
+        _dev(mask, torch.int64, "mask")
+        if mask.dim() != 2 or mask.shape[0] != M or not mask.is_contiguous():
+            raise ValueError("mask must be contiguous [M, words]")
+        words = mask.shape[1]
+    o = out if out is not None else torch.empty((M, n_q, D), dtype=torch.bfloat16, device=q.device)
+    if out is not None and (_dev(o, torch.bfloat16, "out").shape != q.shape or o.stride(2) != 1 or (n_q > 1 and o.stride(1) != D)):
+        raise ValueError("out must be like q, dense within a row")
+    if lse is not None and (_dev(lse, torch.float32, "lse").shape != (M, n_q) or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous [M, n_q]")
+    wp, wb = _ws(workspace)
+    _check("w2_tree_attention", _lib.w2_tree_attention(
+        q.data_ptr(), q.stride(0) if M > 1 else n_q * D, M, n_q, cache._ref, page_table.data_ptr(), page_table.shape[1],
+        page_table.stride(0) if R > 1 else page_table.shape[1], row_start.data_ptr(), kv_len.data_ptr(), R, max_rows, max_len,
+        total_len, _ptr(mask), words, D ** -0.5 if scale is None else scale, o.data_ptr(), o.stride(0) if M > 1 else n_q * D,
+        _ptr(lse), wp, wb, _stream()))
+    return o
 
 
 def debug_group_acc_a8(packed, K, N, G, xq, variant=VARIANT_AUTO, tune=None):

@@ -109,7 +109,7 @@ int launch_stream_read(const void* src, size_t bytes, uint32_t* sink, const w2_t
     return check_launch("w2_debug_stream_read");
 }
 
-static int fail(int code, const char* fmt, ...)
+int fail(int code, const char* fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);

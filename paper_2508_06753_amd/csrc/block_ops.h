@@ -1,0 +1,95 @@
+// Arguments of the operators between the projections (lora.hip, qk_norm_rope.hip, tree_attention.hip), checked by
+// block_api.hip before anything is launched.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "w2_internal.h"
+
+namespace w2 {
+
+__device__ __forceinline__ float bf16_f32(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+
+// round to nearest even; a NaN stays one
+__device__ __forceinline__ uint16_t f32_bf16(float f)
+{
+    uint32_t u = __float_as_uint(f);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40);
+    return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+}
+
+// n / d for 0 <= n < 2^31 by a multiply and a shift.  With s = ceil(log2 d) and m = ceil(2^(31+s) / d), the error
+// e = m d - 2^(31+s) is below d <= 2^s, so n e < 2^(31+s) and the quotient is exact.
+struct Divider {
+    uint32_t m;
+    int s;
+};
+inline Divider make_divider(uint32_t d)
+{
+    int s = 0;
+    while (((uint64_t)1 << s) < d) ++s;
+    return {(uint32_t)((((uint64_t)1 << (31 + s)) + d - 1) / d), 31 + s};
+}
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divider& v) { return (uint32_t)(((uint64_t)n * v.m) >> v.s); }
+
+struct LoraArgs {
+    const uint16_t *A, *B;
+    const int32_t* rank;
+    const float* scale;
+    int64_t a_stride, b_stride;
+    int n_adapters, R, n_parts, gated;
+    int end16[4];                       // the parts' ends in blocks of 16 columns
+    const void* X;
+    int x_f32;
+    const int32_t* adapter;
+    const uint16_t* base;
+    uint16_t* Y;
+    int64_t K, N, M, ldx, ldb, ldy;
+    int act;
+    float* T;                           // the workspace: [K ranges][M][parts * R]
+};
+size_t lora_workspace_bytes(int n_parts, int R, int64_t M, int64_t K, int64_t N);
+int launch_lora(const LoraArgs& a, hipStream_t stream);
+
+struct RopeArgs {
+    const uint16_t* x;
+    int64_t ldx, M;
+    int n_q, n_kv, D;
+    const uint16_t *qw, *kw;
+    float eps;
+    const uint64_t* phase;
+    int rd, interleaved;
+    float mscale;
+    const int32_t* positions;
+    uint16_t* q;
+    int64_t ldq;
+    w2_kv_cache_t cache;
+    Divider page;
+    const int64_t* slots;
+};
+int launch_qk_norm_rope(const RopeArgs& a, hipStream_t stream);
+
+struct TreeArgs {
+    const uint16_t* q;
+    int64_t ldq, M;
+    int n_q, G, D;                      // G query heads share a cache head
+    w2_kv_cache_t cache;
+    Divider page;
+    const int32_t* table;
+    int64_t table_cols, ld_table;
+    const int32_t *row_start, *kv_len;
+    int64_t n_requests, max_rows, max_len, total_len;
+    const uint64_t* mask;
+    int mask_words;
+    float scale;
+    uint16_t* out;
+    int64_t ldo;
+    float* lse;
+    void* workspace;
+    size_t workspace_bytes;
+};
+size_t tree_workspace_bytes(int64_t n_requests, int64_t M, int n_q, int n_kv, int D, int64_t max_rows, int64_t max_len,
+                            int64_t total_len);
+int launch_tree_attention(const TreeArgs& a, hipStream_t stream);
+
+}  // namespace w2

@@ -38,6 +38,7 @@ __device__ __forceinline__ float wave_max_f32(float m)
 // preceding launches failed; returns a w2_status_t.
 int check_launch(const char* what);
 void set_error(const char* fmt, ...);
+int fail(int code, const char* fmt, ...);      // set_error, and `code` back
 
 int launch_prepack(const uint8_t* codes, const uint16_t* scales, const Layout& L, int codec,
                    void* packed, int32_t* bad_codes, hipStream_t stream);
