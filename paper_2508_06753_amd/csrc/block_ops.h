@@ -48,7 +48,7 @@ struct LoraArgs {
     int act;
     float* T;                           // the workspace: [K ranges][M][parts * R]
 };
-size_t lora_workspace_bytes(int n_parts, int R, int64_t M, int64_t K, int64_t N);
+size_t lora_workspace_bytes(int n_parts, int R, int n_adapters, int64_t M, int64_t K, int64_t N);
 int launch_lora(const LoraArgs& a, hipStream_t stream);
 
 struct RopeArgs {
