@@ -399,8 +399,8 @@ W2_API int w2_rope_phases(double base, int rotary_dim, w2_rope_scaling_t scaling
                           double low, double high, uint64_t* phase);
 
 /* A paged cache of keys and values.  Page p, place t of it, head h: k + p*k_page_stride + t*k_slot_stride +
- * h*k_head_stride, head_dim numbers in a row (bf16); v likewise.  Strides in elements, multiples of 8; k and v 16-byte
- * aligned; any page_size; n_pages * page_size < 2^31. */
+ * h*k_head_stride, head_dim numbers in a row (bf16); v likewise.  Strides in elements, multiples of 8 below 2^31; k and v
+ * 16-byte aligned; any page_size; n_pages * page_size < 2^31. */
 typedef struct {
     uint16_t *k, *v;
     int64_t n_pages, page_size;

@@ -54,6 +54,8 @@ int check_cache(const char* fn, const w2_kv_cache_t* c)
     const int64_t st[6] = {c->k_page_stride, c->k_slot_stride, c->k_head_stride, c->v_page_stride, c->v_slot_stride, c->v_head_stride};
     for (int i = 0; i < 6; ++i)
         if (st[i] < 0 || st[i] % 8) return fail(W2_ERR_MISALIGNED, "%s: the cache's strides must be multiples of 8, not negative", fn);
+    for (int i = 0; i < 6; ++i)
+        if (st[i] > 0x7fffffff) return fail(W2_ERR_UNSUPPORTED_SHAPE, "%s: the cache's strides are limited to 2^31 - 1 elements", fn);
     return W2_OK;
 }
 

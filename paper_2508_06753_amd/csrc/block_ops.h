@@ -19,7 +19,7 @@ __device__ __forceinline__ uint16_t f32_bf16(float f)
 }
 
 // n / d for 0 <= n < 2^31 by a multiply and a shift.  With s = ceil(log2 d) and m = ceil(2^(31+s) / d), the error
-// e = m d - 2^(31+s) is below d <= 2^s, so n e < 2^(31+s) and the quotient is exact.
+// e = m d - 2^(31+s) is below d <= 2^s, so n e < 2^(31+s) and the quotient, n m / 2^(31+s), is exact.
 struct Divider {
     uint32_t m;
     int s;
@@ -28,9 +28,9 @@ inline Divider make_divider(uint32_t d)
 {
     int s = 0;
     while (((uint64_t)1 << s) < d) ++s;
-    return {(uint32_t)((((uint64_t)1 << (31 + s)) + d - 1) / d), 31 + s};
+    return {(uint32_t)((((uint64_t)1 << (31 + s)) + d - 1) / d), s};
 }
-__device__ __forceinline__ uint32_t divide(uint32_t n, const Divider& v) { return (uint32_t)(((uint64_t)n * v.m) >> v.s); }
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divider& v) { return __umulhi(2 * n, v.m) >> v.s; }
 
 struct LoraArgs {
     const uint16_t *A, *B;

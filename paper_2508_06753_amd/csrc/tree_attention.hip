@@ -17,6 +17,7 @@
 #include <algorithm>
 
 #include "block_ops.h"
+#include "w2_small_common.h"
 
 namespace w2 {
 
@@ -38,6 +39,28 @@ __device__ __forceinline__ v4f mfma(const v4i& a, const v4i& b, const v4f& c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
 }
 
+// 16 bytes a lane from wherever the lane says to local memory, lane after lane from dst on
+// (CACHE 2: read once, not to be kept)
+template <int CACHE>
+__device__ __forceinline__ void load_lds(const void* src, char* dst)
+{
+    asm volatile("" : "+v"(src));                            // (one load from a chosen address, not a choice of two loads: they are counted)
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, CACHE);
+}
+__device__ __forceinline__ void load_lds4(const void* src, char* dst)        // 4 bytes a lane
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
+}
+
+// every read of local memory that was issued has delivered (what it read may be overwritten)
+__device__ __forceinline__ void wait_reads()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xc07f);                      // lgkmcnt 0
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // two floats to bf16, round to nearest even
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
@@ -46,10 +69,68 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){lo, hi}, v2bf));
 }
 
-// 16-byte pieces of a row of DT numbers are stored XORed by this, so that 16 rows at one piece lie in 16 different places
-// of the 256 bytes that local memory delivers at once
+// 16-byte pieces of a row of DT numbers are stored XORed by this: 16 rows at one piece (scores) lie in 16 different places of
+// the 256 bytes that local memory delivers at once, and 8 rows at a pair of pieces (values) in 8 different pairs
 template <int DT>
-__device__ __forceinline__ int swizzle(int key) { return DT == 64 ? (key >> 1) & 7 : key & 15; }
+__device__ __forceinline__ int swizzle(int key) { return DT == 64 ? ((key & 6) | ((key >> 3) & 1)) : (((key & 7) << 1) | ((key >> 3) & 1)); }
+
+// (fmaxf makes sure of every operand first, one instruction each)
+__device__ __forceinline__ float max2(float a, float b)
+{
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// V^T operands of four blocks of 16 numbers: lane (q, l16) gets numbers 16 d + l16 of keys 4q ..+ 3 of both tiles.  Rows of
+// the cache are read transposed, 4 keys by 16 numbers for 16 lanes.  One block with its own wait: the compiler would wait
+// here for every load to local memory that is under way, since it cannot tell that they go elsewhere.
+template <int TILE_STEP>
+__device__ __forceinline__ void read_vt(const uint32_t (&at)[4], v4i (&out)[4])
+{
+    uint2 a0, a1, b0, b1, c0, c1, d0, d1;
+    asm volatile("ds_read_b64_tr_b16 %0, %8\n\t"
+                 "ds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %2, %9\n\t"
+                 "ds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %4, %10\n\t"
+                 "ds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %6, %11\n\t"
+                 "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(a0), "=&v"(a1), "=&v"(b0), "=&v"(b1), "=&v"(c0), "=&v"(c1), "=&v"(d0), "=&v"(d1)
+                 : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(TILE_STEP)
+                 : "memory");
+    out[0] = (v4i){(int)a0.x, (int)a0.y, (int)a1.x, (int)a1.y};
+    out[1] = (v4i){(int)b0.x, (int)b0.y, (int)b1.x, (int)b1.y};
+    out[2] = (v4i){(int)c0.x, (int)c0.y, (int)c1.x, (int)c1.y};
+    out[3] = (v4i){(int)d0.x, (int)d0.y, (int)d1.x, (int)d1.y};
+}
+
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
+
+// Where a lane reads V^T of block d from: its key of a tile, the piece's place in the row
+template <int DT>
+__device__ __forceinline__ uint32_t vt_offset(int d, int q, int l16)
+{
+    const int key = 4 * q + (l16 >> 2), piece = 2 * d + ((l16 >> 1) & 1);
+    return (uint32_t)(key * DT * 2 + ((piece ^ swizzle<DT>(key)) << 4) + 8 * (l16 & 1));
+}
+
+// Maximum, sum over the four lanes that hold a query row (lane & 15)
+__device__ __forceinline__ float max_over_q(float x)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    const float y = max2(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+    return max2(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 
 struct Plan {
     int few;                             // tree_few_kernel, else tree_tile_kernel
@@ -66,15 +147,15 @@ Plan make_plan(int64_t n_requests, int64_t max_rows, int G, int n_kv, int D, int
     const int64_t rows = max_rows * G;
     p.dt = D <= 64 ? 64 : D <= 128 ? 128 : 256;
     p.few = rows <= (p.dt < 256 ? 32 : 16);
-    p.rt = p.few ? (rows <= 16 ? 1 : 2) : p.dt < 256 && (rows % 128 == 0 || rows % 128 > 64 || rows > 640) ? 2 : 1;
-    const int rows_per_wg = p.few ? 16 * p.rt : 64 * p.rt;
+    p.rt = p.few && rows <= 16 ? 1 : 2;
+    const int rows_per_wg = p.few ? 16 * p.rt : 128;
     p.tiles = (int)((rows + rows_per_wg - 1) / rows_per_wg);
     if (total_len <= 0 || total_len > n_requests * max_len) total_len = n_requests * max_len;
     // workgroups for about two on every CU, of at least 128 (few) or 256 keys each
-    const int64_t least = p.few ? 128 : 256, want = 512;
+    const int64_t least = p.few ? 128 : 256, want = p.few ? 2048 : 512;
     int64_t chunk = (total_len * n_kv * p.tiles + want - 1) / want;
     chunk = std::max(chunk, (max_len + MAX_CHUNKS - 1) / MAX_CHUNKS);
-    if (max_rows * G * n_kv >= (int64_t)1 << 26) chunk = std::max(chunk, max_len);     // (more than a grid of the join counts)
+    if (max_rows * G * n_kv >= (int64_t)1 << 24) chunk = std::max(chunk, max_len);     // (more than a grid of the join counts)
     chunk = (std::max(chunk, least) + 127) / 128 * 128;
     p.chunk = (int)std::min<int64_t>(chunk, (int64_t)1 << 31 >> 1);
     p.chunks = (int)std::max<int64_t>(1, (max_len + p.chunk - 1) / p.chunk);
@@ -98,6 +179,7 @@ struct Work {
     Divider by_g, by_tiles;
     float c;                             // |scale| * log2 e
     int flip;                            // scale < 0: queries change sign
+    int same;                            // K and V have the same strides
     int tiles, chunk, chunks, n_kv;
     float* part_o;
     float2* part_ml;
@@ -124,33 +206,42 @@ __device__ __forceinline__ Span make_span(const Work& w, int r)
     return s;
 }
 
+// Workgroups that are eight apart run on one die: a die that saw one head only would ask one or two of its cache's channels
+// for everything, since a head's rows lie a whole key apart.  The head of a workgroup turns with its chunk and request.
+__device__ __forceinline__ int head_of(const Work& w, uint32_t unit, int chunk, int r)
+{
+    return (int)((unit + (uint32_t)chunk + (uint32_t)r) % (uint32_t)w.n_kv);
+}
+
 // Which of the keys base .. base + 3 (base a multiple of 4 from a tile's start on) the row sees, as 4 bits.
 __device__ __forceinline__ uint32_t seen4(const TreeArgs& a, const Span& sp, int64_t row, int t, uint64_t word0, uint32_t base)
 {
     const int j = (int)(base - (uint32_t)sp.ctx);            // drafted number of the first key
     if (!a.mask) return j > t ? 0u : t - j >= 3 ? 15u : (2u << (t - j)) - 1u;
-    uint32_t bits = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        bool on = true;
-        if (j + i >= 0) {
-            const int w = (j + i) >> 6;
-            on = w < a.mask_words;
-            if (on) on = ((w == 0 ? word0 : a.mask[row * a.mask_words + w]) >> ((j + i) & 63)) & 1;
-        }
-        bits |= (uint32_t)on << i;
-    }
-    return bits;
+    if (j <= -4) return 15u;
+    if (j < 0) return (uint32_t)((word0 << -j) | ((1u << -j) - 1u)) & 15u;
+    const uint64_t* const words = a.mask + row * a.mask_words;
+    const int at = j >> 6, shift = j & 63;
+    uint64_t bits = (at == 0 ? word0 : at < a.mask_words ? words[at] : 0) >> shift;
+    if (shift > 60 && at + 1 < a.mask_words) bits |= words[at + 1] << (64 - shift);
+    return (uint32_t)bits & 15u;
 }
 
-// Where a key's row of the cache lies, in elements, without its head; `valid` false: not seen, a safe place.
-__device__ __forceinline__ void locate(const TreeArgs& a, uint32_t key, int page, bool valid, int64_t* k_off, int64_t* v_off)
+// Where a key's row of the cache lies, in elements, without its head; `valid` false: not seen, a safe place.  (Strides are
+// below 2^31: one 32 x 32 -> 64 bit product each.)
+__device__ __forceinline__ void locate(const Work& w, uint32_t key, int page, bool valid, uint64_t& k_off, uint64_t& v_off)
 {
-    const uint32_t at = divide(key, a.page);
-    const int64_t place = key - (int64_t)at * a.cache.page_size;
-    const int64_t p = valid ? page : 0;
-    *k_off = p * a.cache.k_page_stride + place * a.cache.k_slot_stride;
-    *v_off = p * a.cache.v_page_stride + place * a.cache.v_slot_stride;
+    const w2_kv_cache_t& c = w.a.cache;
+    const uint32_t at = divide(key, w.a.page), place = key - at * (uint32_t)c.page_size, p = valid ? page : 0;
+    k_off = (uint64_t)p * (uint32_t)c.k_page_stride + (uint64_t)place * (uint32_t)c.k_slot_stride;
+    v_off = k_off;
+    if (!w.same) v_off = (uint64_t)p * (uint32_t)c.v_page_stride + (uint64_t)place * (uint32_t)c.v_slot_stride;
+}
+
+// a 64-bit number of another lane
+__device__ __forceinline__ uint64_t from_lane(uint64_t x, int lane)
+{
+    return (uint64_t)(uint32_t)__shfl((int)(x >> 32), lane) << 32 | (uint32_t)__shfl((int)x, lane);
 }
 
 template <int RT>
@@ -196,28 +287,63 @@ __device__ __forceinline__ void load_q(const Work& w, const Rows<RT>& x, int q, 
         }
 }
 
-// Weights of 32 keys (tiles s[0], s[1]) for one row tile; updates m, l and tells by how much the outputs shrink.
-__device__ __forceinline__ float softmax_step(v4f (&s)[2], float c, float& m, float& l)
+// Scores of the 32 keys at kb against RT row tiles
+template <int DT, int RT>
+__device__ __forceinline__ void scores(const char* kb, int l16, int q, const v4i (&qf)[RT][DT / 32], v4f (&s)[RT][2])
 {
-    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    float shrink = 1.0f;
-    if (__any((mx - m) * c > SLACK || (m == -INFINITY && mx != -INFINITY))) {
-        const float up = fmaxf(m, mx);
-        shrink = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - up) * c);
-        l *= shrink;
-        m = up;
+    constexpr int KS = DT / 32;
+    v4i kf[2][KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int key = 16 * t + l16;
+            kf[t][ks] = *reinterpret_cast<const v4i*>(kb + key * DT * 2 + (((4 * ks + q) ^ swizzle<DT>(key)) << 4));
+        }
+    __builtin_amdgcn_sched_barrier(0);                       // all reads first, then the products as they arrive
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) s[rt][t] = (v4f){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) s[rt][t] = mfma(kf[t][ks], qf[rt][ks], s[rt][t]);
+}
+
+// The running maximum (times c; -infinity: nothing seen yet), what is added to scores before the exponential, the lane's
+// part of the sum.
+struct Running {
+    float top = -INFINITY, off = 0.0f, sum = 0.0f;
+};
+
+// Weights of 32 keys (tiles s[0], s[1]) for one row tile.
+template <int N>
+__device__ __forceinline__ void softmax_step(v4f (&s)[2], float c, Running& run, v4f (&o)[N])
+{
+    float mx = max3(s[0][0], s[0][1], s[0][2]);
+    mx = max3(mx, s[0][3], s[1][0]);
+    mx = max3(mx, s[1][1], s[1][2]);
+    mx = max_over_q(max2(mx, s[1][3]));
+    // (a maximum of -infinity has no difference from itself: not a number, no change)
+    if (__builtin_amdgcn_ballot_w64(fmaf(mx, c, -run.top) > SLACK)) {
+        const float up = fmaxf(run.top, mx * c);
+        const float shrink = run.top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(run.top - up);
+        run.sum *= shrink;
+        run.top = up;
+        run.off = up == -INFINITY ? 0.0f : -up;
+#pragma unroll
+        for (int d = 0; d < N; ++d) o[d] *= shrink;
     }
-    const float off = m == -INFINITY ? 0.0f : -m * c;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], c, off));
-            l += s[t][i];
+            s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], c, run.off));
+            run.sum += s[t][i];
         }
-    return shrink;
 }
 
 // The result of packed row (row, head), numbers d .. d + 3: rounded to q's type, or a chunk's part of it.
@@ -237,109 +363,93 @@ __device__ __forceinline__ void store4(const Work& w, bool whole, int chunk, int
 __device__ __forceinline__ void store_stats(const Work& w, bool whole, int chunk, int64_t row, int head, float m, float l)
 {
     if (!whole) w.part_ml[((int64_t)chunk * w.a.M + row) * w.a.n_q + head] = make_float2(m, l);
-    else if (w.a.lse) w.a.lse[row * w.a.n_q + head] = l == 0.0f ? -INFINITY : (m * w.c + __log2f(l)) * (1.0f / LOG2E);
+    else if (w.a.lse) w.a.lse[row * w.a.n_q + head] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * (1.0f / LOG2E);
 }
 
 // ---------------------------------------------------------------------------------------------- few rows
 constexpr int FEW_WAVES = 4;
 
 template <int DT, int RT>
-__global__ void __launch_bounds__(64 * FEW_WAVES) tree_few_kernel(Work w)
+__global__ void __launch_bounds__(64 * FEW_WAVES, DT == 256 ? 1 : 2) tree_few_kernel(Work w)
 {
     constexpr int KS = DT / 32;
-    constexpr int TILE = 32 * DT * 2;                        // a wave's 32 keys of V
+    constexpr int TILE = 32 * DT * 2;                        // a wave's 32 keys of K, and of V again
+    constexpr int LOADS = TILE / 1024, PIECES = DT / 8;
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int hk = blockIdx.x % w.n_kv, chunk = blockIdx.x / w.n_kv, r = blockIdx.y;
+    const int chunk = blockIdx.x / w.n_kv, r = blockIdx.y, hk = head_of(w, blockIdx.x, chunk, r);
     const Span sp = make_span(w, r);
     if (sp.rows == 0 || chunk >= sp.n_chunks) return;
     const uint32_t k0 = (uint32_t)chunk * w.chunk, k1 = min((uint32_t)sp.len, k0 + w.chunk);
     const uint32_t ctx = max(sp.ctx, 0);
-    const Rows<RT> x = make_rows<RT>(w, sp, 0, hk, l16);
-    v4i qf[RT][KS];
-    load_q<DT, RT>(w, x, q, qf);
 
     const uint16_t* const kh = w.a.cache.k + hk * w.a.cache.k_head_stride;
     const uint16_t* const vh = w.a.cache.v + hk * w.a.cache.v_head_stride;
     const int32_t* const table = w.a.table + r * w.a.ld_table;
-    char* const vs = smem + wave * TILE;
+    char* const kb = smem + wave * 2 * TILE;
+    char* const vb = kb + TILE;
 
-    float m[RT], l[RT];
-    v4f o[RT][DT / 16];
+    // lane = key of a step (twice), for its page
+    auto page_of = [&](uint32_t base) { return table[divide(min(base + (lane & 31), k1 - 1), w.a.page)]; };
+    uint32_t valid = 0, valid_next = 0;
+    uint64_t koff = 0, voff = 0;
+    auto place = [&](uint32_t base, int id) {
+        const uint32_t key = base + (lane & 31);
+        const bool ok = key < k1 && id >= 0 && id < w.a.cache.n_pages;
+        locate(w, min(key, k1 - 1), id, ok, koff, voff);
+        valid_next = (uint32_t)__ballot(ok);
+    };
+    // whole rows of the cache side by side, 1 KiB an instruction; rows that nobody sees come from a place that holds zeros
+    auto fetch = [&](const uint16_t* head, uint64_t off, char* dst) {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        m[rt] = -INFINITY;
-        l[rt] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < DT / 16; ++d) o[rt][d] = (v4f){0.f, 0.f, 0.f, 0.f};
-    }
-
-    // a lane's keys of a step: l16 and 16 + l16
-    auto page_of = [&](uint32_t base, int t) { return table[divide(min(base + 16 * t + l16, k1 - 1), w.a.page)]; };
-    v4i kf[2][KS], vf[2][KS];
-    int ids[2];
-    uint32_t valid_next = 0, valid;
-    int64_t voff[2];
-    auto place = [&](uint32_t base, int64_t (&koff)[2]) {
-        valid_next = 0;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const uint32_t key = base + 16 * t + l16;
-            const bool ok = key < k1 && ids[t] >= 0 && ids[t] < w.a.cache.n_pages;
-            valid_next |= ((uint32_t)__ballot(ok) & 0xffffu) << (16 * t);
-            locate(w.a, min(key, k1 - 1), ids[t], ok, &koff[t], &voff[t]);
+        for (int j = 0; j < LOADS; ++j) {
+            const int at = j * 64 + lane, row = at / PIECES, slot = at % PIECES;
+            const int d = (slot ^ swizzle<DT>(row)) * 8;
+            const uint64_t o = from_lane(off, row);
+            load_lds<2>((valid_next >> row & 1) && d < w.a.D ? (const void*)(head + d + o) : (const void*)g_zeros, dst + j * 1024);
         }
     };
-    auto load_k = [&](const int64_t (&koff)[2]) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int d = 32 * ks + 8 * q;
-                kf[t][ks] = *reinterpret_cast<const v4i*>(kh + koff[t] + (d < w.a.D ? d : 0));
-            }
-    };
-    auto load_v = [&]() {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int d = 32 * ks + 8 * q;
-                vf[t][ks] = *reinterpret_cast<const v4i*>(vh + voff[t] + (d < w.a.D ? d : 0));
-            }
-    };
 
-    uint32_t base = k0 + 32 * wave;
     constexpr uint32_t STEP = 32 * FEW_WAVES;
+    uint32_t base = k0 + 32 * wave;
+    int id = 0;
     if (base < k1) {
-        int64_t koff[2];
-        ids[0] = page_of(base, 0);
-        ids[1] = page_of(base, 1);
-        place(base, koff);
-        ids[0] = page_of(base + STEP, 0);
-        ids[1] = page_of(base + STEP, 1);
-        load_k(koff);
-        load_v();
+        const int first = page_of(base);
+        id = page_of(base + STEP);
+        place(base, first);
+        fetch(kh, koff, kb);
+        fetch(vh, voff, vb);
         valid = valid_next;
     }
-    for (; base < k1; base += STEP) {
-        v4f s[RT][2];
+    uint32_t vat[DT / 16];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+    for (int d = 0; d < DT / 16; ++d) vat[d] = lds_address(vb) + vt_offset<DT>(d, q, l16);
+    const Rows<RT> x = make_rows<RT>(w, sp, 0, hk, l16);
+    v4i qf[RT][KS];
+    load_q<DT, RT>(w, x, q, qf);
+    Running run[RT];
+    v4f o[RT][DT / 16];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                s[rt][t] = (v4f){0.f, 0.f, 0.f, 0.f};
+    for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) s[rt][t] = mfma(kf[t][ks], qf[rt][ks], s[rt][t]);
-            }
-        // the next keys are asked for as soon as these have met the queries (past the end: the last ones again)
-        int64_t koff[2];
-        place(base + STEP, koff);
-        ids[0] = page_of(base + 2 * STEP, 0);
-        ids[1] = page_of(base + 2 * STEP, 1);
-        load_k(koff);
+        for (int d = 0; d < DT / 16; ++d) o[rt][d] = (v4f){0.f, 0.f, 0.f, 0.f};
+    if (base < k1) wait_loads<0>();                          // (the queries stand behind the first keys)
 
+    // K of the next step is asked for as soon as this step's has met the queries, V when this step's has met the weights:
+    // one buffer each.  Loads complete in order; what may be under way behind the one waited for is counted.
+    for (; base < k1; base += STEP) {
+        const bool more = base + STEP < k1;
+        if (base != k0 + 32 * wave) wait_loads<LOADS>();     // K is there (V under way)
+        v4f s[RT][2];
+        scores<DT, RT>(kb, l16, q, qf, s);
+        if (more) {
+            const int next = id;
+            id = page_of(base + 2 * STEP);
+            place(base + STEP, next);
+            wait_reads();
+            fetch(kh, koff, kb);
+        }
         if (valid != 0xffffffffu || base + 32 > ctx) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
@@ -354,10 +464,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) tree_few_kernel(Work w)
         v4i hi[RT], lo[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            const float shrink = softmax_step(s[rt], w.c, m[rt], l[rt]);
-            if (__any(shrink != 1.0f))
-#pragma unroll
-                for (int d = 0; d < DT / 16; ++d) o[rt][d] *= shrink;
+            softmax_step(s[rt], w.c, run[rt], o[rt]);
             // weights in two bf16 parts: 16 bits of them meet V; the matrix pipe has the room
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -369,41 +476,26 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) tree_few_kernel(Work w)
                                                            s[rt][t][i + 1] - __uint_as_float(h & 0xffff0000u));
                 }
         }
-        // V to local memory, rows that are not seen by anybody as zeros
+        if (more) wait_loads<LOADS>();                       // V is there (the next K under way)
+        else wait_loads<0>();
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int key = 16 * t + l16;
-            const bool ok = valid >> key & 1;
+        for (int g = 0; g < DT / 64; ++g) {
+            const uint32_t at[4] = {vat[4 * g], vat[4 * g + 1], vat[4 * g + 2], vat[4 * g + 3]};
+            v4i vt[4];
+            read_vt<16 * DT * 2>(at, vt);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int piece = 4 * ks + q;
-                v4i v = vf[t][ks];
-                if (!ok || 8 * piece >= w.a.D) v = (v4i){0, 0, 0, 0};
-                *reinterpret_cast<v4i*>(vs + key * DT * 2 + ((piece ^ swizzle<DT>(key)) << 4)) = v;
-            }
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    o[rt][4 * g + e] = mfma(vt[e], hi[rt], o[rt][4 * g + e]);
+                    o[rt][4 * g + e] = mfma(vt[e], lo[rt], o[rt][4 * g + e]);
+                }
         }
-        load_v();
+        if (more) {
+            wait_reads();
+            fetch(vh, voff, vb);
+        }
         valid = valid_next;
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int d = 0; d < DT / 16; ++d) {
-            v4i vt;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int key = 16 * t + 4 * q + (l16 >> 2), piece = 2 * d + ((l16 >> 1) & 1);
-                const v4s p = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(
-                    vs + key * DT * 2 + ((piece ^ swizzle<DT>(key)) << 4) + 8 * (l16 & 1)));
-                const uint2 u = __builtin_bit_cast(uint2, p);
-                vt[2 * t] = (int)u.x;
-                vt[2 * t + 1] = (int)u.y;
-            }
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                o[rt][d] = mfma(vt, hi[rt], o[rt][d]);
-                o[rt][d] = mfma(vt, lo[rt], o[rt][d]);
-            }
-        }
-        __builtin_amdgcn_wave_barrier();
     }
 
     // the waves' parts meet in local memory, one row tile at a time
@@ -414,12 +506,12 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) tree_few_kernel(Work w)
     const bool whole = sp.n_chunks == 1;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        float sum = l[rt];
+        float sum = run[rt].sum;
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         __syncthreads();
         if (q == 0) {
-            ms[wave * 16 + l16] = m[rt];
+            ms[wave * 16 + l16] = run[rt].top;
             ls[wave * 16 + l16] = sum;
         }
 #pragma unroll
@@ -436,7 +528,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) tree_few_kernel(Work w)
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int v = 0; v < FEW_WAVES; ++v) {
-                const float mv = ms[v * 16 + n], f = mv == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mv - top) * w.c);
+                const float mv = ms[v * 16 + n], f = mv == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mv - top);
                 const float4 ov = *reinterpret_cast<const float4*>(os + (v * 16 + n) * LD + d);
                 if (mv != -INFINITY) {
                     all = fmaf(ls[v * 16 + n], f, all);
@@ -456,179 +548,273 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) tree_few_kernel(Work w)
 }
 
 // ---------------------------------------------------------------------------------------------- many rows
-constexpr int TILE_WAVES = 4;
-template <int DT> constexpr int stage_keys() { return DT == 256 ? 32 : 64; }
-template <int DT> constexpr int stage_bytes() { return stage_keys<DT>() * DT * 2; }          // of K, and of V again
+constexpr int TILE_WAVES = 4;                                // of 32 packed rows each
+constexpr int RING = 4;                                      // stages of 32 keys in local memory
+template <int DT> constexpr int stage_bytes() { return 32 * DT * 2; }                        // of K, and of V again
+constexpr int ID_SLOTS = 8;                                  // a wave's pages of so many stages, 256 bytes each
+template <int DT> constexpr int tile_lds() { return RING * 2 * stage_bytes<DT>() + TILE_WAVES * ID_SLOTS * 256; }
 
-template <int DT, int RT>
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ v16f mfma32(const v4i& a, const v4i& b, const v16f& c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
+
+// As swizzle(): here 4 rows at four pieces (values) have to lie in different places too
+template <int DT>
+__device__ __forceinline__ int swizzle32(int key) { return DT == 64 ? ((key & 2) << 1 | ((key >> 2) & 3)) : (((key & 3) << 2) | ((key >> 2) & 3)); }
+
+// V^T operands of two blocks of 32 numbers, for the first and the second 16 keys of a stage.  at[block][j]: rows 8 j + 4 h ..
+template <int HALF>
+__device__ __forceinline__ void read_vt32(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, v4i (&out)[2][2])
+{
+    uint2 x0, x1, x2, x3, y0, y1, y2, y3;
+    asm volatile("ds_read_b64_tr_b16 %0, %8\n\t"
+                 "ds_read_b64_tr_b16 %1, %9\n\t"
+                 "ds_read_b64_tr_b16 %2, %8 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %4, %10\n\t"
+                 "ds_read_b64_tr_b16 %5, %11\n\t"
+                 "ds_read_b64_tr_b16 %6, %10 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+                 "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(x0), "=&v"(x1), "=&v"(x2), "=&v"(x3), "=&v"(y0), "=&v"(y1), "=&v"(y2), "=&v"(y3)
+                 : "v"(a0), "v"(a1), "v"(b0), "v"(b1), "n"(HALF)
+                 : "memory");
+    out[0][0] = (v4i){(int)x0.x, (int)x0.y, (int)x1.x, (int)x1.y};
+    out[0][1] = (v4i){(int)x2.x, (int)x2.y, (int)x3.x, (int)x3.y};
+    out[1][0] = (v4i){(int)y0.x, (int)y0.y, (int)y1.x, (int)y1.y};
+    out[1][1] = (v4i){(int)y2.x, (int)y2.y, (int)y3.x, (int)y3.y};
+}
+
+// A wave holds 32 packed rows, one in lanes l and l + 32.  Scores: lane half h has keys 8 b + 4 h + i (b, i = 0..3) of a
+// stage, which are slots 4 b + i of the weights' operands.  The scores of the next stage are multiplied while this stage's
+// weights are made: matrix and vector instructions of one wave side by side.
+template <int DT>
 __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_kernel(Work w)
 {
-    constexpr int KS = DT / 32, SK = stage_keys<DT>(), SB = stage_bytes<DT>();
+    constexpr int KS = DT / 16, SB = stage_bytes<DT>();
     constexpr int LOADS = SB / 1024 / TILE_WAVES;            // of 64 pieces of 16 bytes, of K and of V, a wave and stage
     constexpr int PIECES = DT / 8;                           // of a row
-    extern __shared__ __align__(16) char smem[];             // two stages of K and V
-    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+    extern __shared__ __align__(16) char smem[];             // RING stages of K and V, pages
+    const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // eight units (head, chunk) of a request side by side, then their next row tile: the tiles of a unit read the same keys, and
     // workgroups that are eight apart share an L2
     const uint32_t side = w.n_kv * w.chunks % 8 == 0 ? 3 : 0;
     const uint32_t group = divide(blockIdx.x >> side, w.by_tiles);
-    const int tile = (blockIdx.x >> side) - group * w.tiles, unit = (group << side) + (blockIdx.x & ((1 << side) - 1));
-    const int hk = unit % w.n_kv, chunk = unit / w.n_kv, r = blockIdx.y;
+    const int tile = w.tiles - 1 - (int)((blockIdx.x >> side) - group * w.tiles);            // (causal: the longest first)
+    const int unit = (group << side) + (blockIdx.x & ((1 << side) - 1));
+    const int chunk = unit / w.n_kv, r = blockIdx.y;
+    const int hk = head_of(w, unit, chunk, r);
     const Span sp = make_span(w, r);
-    const int rho_wg = tile * 64 * RT;
+    const int rho_wg = tile * 32 * TILE_WAVES;
     if (rho_wg >= sp.rows || chunk >= sp.n_chunks) return;
-    const int rho0 = rho_wg + wave * 16 * RT;
     const uint32_t k0 = (uint32_t)chunk * w.chunk, ctx = max(sp.ctx, 0);
     uint32_t k1 = min((uint32_t)sp.len, k0 + w.chunk);
     if (!w.a.mask) {                                         // causal: nothing past the tile's last token
-        const int last = (int)divide((uint32_t)min(rho_wg + 64 * RT, sp.rows) - 1, w.by_g);
+        const int last = (int)divide((uint32_t)min(rho_wg + 32 * TILE_WAVES, sp.rows) - 1, w.by_g);
         k1 = max(k0, min(k1, (uint32_t)max(sp.ctx + last + 1, 0)));
     }
-    const Rows<RT> x = make_rows<RT>(w, sp, rho0, hk, l16);
-    v4i qf[RT][KS];
-    load_q<DT, RT>(w, x, q, qf);
-
+    const int stages = (int)((k1 - k0 + 31) / 32);
     const uint16_t* const kh = w.a.cache.k + hk * w.a.cache.k_head_stride;
     const uint16_t* const vh = w.a.cache.v + hk * w.a.cache.v_head_stride;
     const int32_t* const table = w.a.table + r * w.a.ld_table;
 
-    float m[RT], l[RT];
-    v4f o[RT][DT / 16];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        m[rt] = -INFINITY;
-        l[rt] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < DT / 16; ++d) o[rt][d] = (v4f){0.f, 0.f, 0.f, 0.f};
-    }
-
-    // lane = key of a stage, for its page
-    auto page_of = [&](uint32_t base) { return table[divide(min(base + (lane & (SK - 1)), k1 - 1), w.a.page)]; };
-    auto fetch = [&](uint32_t base, int id, char* buf) -> uint64_t {
-        const uint32_t key = base + (lane & (SK - 1));
+    // Pages of a stage go to local memory like its keys (lane = key), RING - 1 stages before they are needed: a wave that
+    // waited for them in registers would wait for every load of keys before them too.
+    char* const ids = smem + RING * 2 * SB + wave * ID_SLOTS * 256;
+    auto fetch_pages = [&](int st) {
+        const uint32_t key = min(k0 + (uint32_t)st * 32 + l32, k1 - 1);
+        load_lds4(table + divide(key, w.a.page), ids + (st & (ID_SLOTS - 1)) * 256);
+    };
+    auto fetch = [&](int st, int buf) -> uint32_t {
+        char* const dst = smem + buf * 2 * SB;
+        const uint32_t key = k0 + (uint32_t)st * 32 + l32;
+        const int id = *reinterpret_cast<const int*>(ids + (st & (ID_SLOTS - 1)) * 256 + lane * 4);
         const bool ok = key < k1 && id >= 0 && id < w.a.cache.n_pages;
-        int64_t koff, voff;
-        locate(w.a, min(key, k1 - 1), id, ok, &koff, &voff);
-        const uint64_t valid = __ballot(ok);
+        uint64_t koff, voff;
+        locate(w, min(key, k1 - 1), id, ok, koff, voff);
+        const uint32_t valid = (uint32_t)__builtin_amdgcn_ballot_w64(ok);
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int at = (wave * LOADS + j) * 64 + lane, row = at / PIECES, slot = at % PIECES;
-            const int d = (slot ^ swizzle<DT>(row)) * 8;
-            const int64_t ko = ((int64_t)__shfl((int)(koff >> 32), row) << 32) | (uint32_t)__shfl((int)koff, row);
-            const int64_t vo = ((int64_t)__shfl((int)(voff >> 32), row) << 32) | (uint32_t)__shfl((int)voff, row);
+            const int d = (slot ^ swizzle32<DT>(row)) * 8;
+            const uint64_t ko = from_lane(koff, row), vo = w.same ? ko : from_lane(voff, row);
             const bool there = (valid >> row & 1) && d < w.a.D;
-            const void* const ka = there ? (const void*)(kh + ko + d) : (const void*)g_zeros;
-            const void* const va = there ? (const void*)(vh + vo + d) : (const void*)g_zeros;
-            char* const kd = buf + (wave * LOADS + j) * 1024;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)ka, (__attribute__((address_space(3))) void*)kd, 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)va, (__attribute__((address_space(3))) void*)(kd + SB), 16, 0, 0);
+            char* const to = dst + (wave * LOADS + j) * 1024;
+            load_lds<0>(there ? (const void*)(kh + d + ko) : (const void*)g_zeros, to);
+            load_lds<0>(there ? (const void*)(vh + d + vo) : (const void*)g_zeros, to + SB);
         }
         return valid;
     };
-
-    uint64_t valid = 0, valid_next = 0;
-    int id = 0;
-    if (k0 < k1) {
-        id = page_of(k0);
-        valid = fetch(k0, id, smem);
-        id = page_of(k0 + SK);
+    uint32_t valid[RING] = {};
+    if (stages > 0) {
+#pragma unroll
+        for (int st = 0; st < 2 * (RING - 1); ++st) fetch_pages(st);
+        wait_loads<0>();
+#pragma unroll
+        for (int st = 0; st < RING - 1; ++st)
+            if (st < stages) valid[st] = fetch(st, st);
     }
-    int buf = 0;
-    for (uint32_t base = k0; base < k1; base += SK, buf ^= 1) {
-        char* const ks_ = smem + buf * 2 * SB;
-        char* const vs = ks_ + SB;
-        __syncthreads();                                     // (waits for this stage's loads) every wave's part of the stage is there
-        if (base + SK < k1) {
-            valid_next = fetch(base + SK, id, smem + (buf ^ 1) * 2 * SB);
-            id = page_of(base + 2 * SK);
+
+    // the lane's query row, its operands: numbers 16 ks + 8 h ..+ 7
+    const int rho = rho_wg + wave * 32 + l32;
+    const bool live = rho < sp.rows;
+    const int t = (int)divide((uint32_t)(live ? rho : 0), w.by_g), head = hk * w.a.G + (live ? rho : 0) - t * w.a.G;
+    const int64_t row = sp.first + t;
+    const uint64_t word = w.a.mask ? w.a.mask[row * w.a.mask_words] : 0;
+    v4i qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int d = 16 * ks + 8 * h;
+        qf[ks] = (v4i){0, 0, 0, 0};
+        if (live && d < w.a.D) qf[ks] = *reinterpret_cast<const v4i*>(w.a.q + row * w.a.ldq + (int64_t)head * w.a.D + d);
+        if (w.flip)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) qf[ks][e] ^= 0x80008000;
+    }
+    Running run;
+    v16f o[DT / 32];
+#pragma unroll
+    for (int d = 0; d < DT / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+
+    // addresses within a stage: K, pieces 2 ks + h of key l32; V^T, block d, rows 8 j + 4 h ..
+    uint32_t kat[KS], vat[DT / 32][2];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kat[ks] = l32 * DT * 2 + (((2 * ks + h) ^ swizzle32<DT>(l32)) << 4);
+#pragma unroll
+    for (int d = 0; d < DT / 32; ++d)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int key = 8 * j + 4 * h + ((lane >> 2) & 3), piece = 4 * d + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+            vat[d][j] = lds_address(smem + SB) + key * DT * 2 + ((piece ^ swizzle32<DT>(key)) << 4) + 8 * (lane & 1);
+        }
+    auto read_k = [&](const char* kb, v4i (&kf)[KS]) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const v4i*>(kb + kat[ks]);
+    };
+    auto zero = [](v16f& s) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+    };
+
+    v16f s, sn;
+    zero(s);
+    if (stages > 0) {
+        if (stages > 2) wait_loads<4 * LOADS>();
+        else if (stages > 1) wait_loads<2 * LOADS>();
+        else wait_loads<0>();
+        bare_barrier();
+        v4i kf[KS];
+        read_k(smem, kf);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mfma32(kf[ks], qf[ks], s);
+    }
+    for (int st0 = 0; st0 < stages; st0 += RING)
+#pragma unroll
+    for (int b = 0; b < RING; ++b) {
+        const int st = st0 + b;
+        if (st >= stages) break;
+        const uint32_t base = k0 + (uint32_t)st * 32;
+        // the next stage is there; one behind it is under way
+        if (st + 2 < stages) wait_loads<2 * LOADS>();
+        else wait_loads<0>();
+        bare_barrier();                                      // every wave's part of it, and no wave reads the stage before this one any more
+        if (st + RING - 1 < stages) {
+            fetch_pages(st + 2 * (RING - 1));
+            valid[(b + RING - 1) % RING] = fetch(st + RING - 1, (b + RING - 1) % RING);
+        }
+        if (valid[b] != 0xffffffffu || base + 32 > ctx) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t on = valid[b] >> (8 * e + 4 * h) & 15u;
+                if (base + 32 > ctx) on &= seen4(w.a, sp, row, t, word, base + 8 * e + 4 * h);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[4 * e + i] = on >> i & 1 ? s[4 * e + i] : -INFINITY;
+            }
+        }
+        float mx = max3(s[0], s[1], s[2]);
+#pragma unroll
+        for (int i = 3; i < 15; i += 2) mx = max3(mx, s[i], s[i + 1]);
+        mx = max2(mx, s[15]);
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = max2(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+        if (__builtin_amdgcn_ballot_w64(fmaf(mx, w.c, -run.top) > SLACK)) {
+            const float up = fmaxf(run.top, mx * w.c);
+            const float shrink = run.top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(run.top - up);
+            run.sum *= shrink;
+            run.top = up;
+            run.off = up == -INFINITY ? 0.0f : -up;
+#pragma unroll
+            for (int d = 0; d < DT / 32; ++d) o[d] *= shrink;
+        }
+        // (past the last stage: the scores of a stage that is there once more, which nobody uses)
+        v4i kf[KS];
+        __builtin_amdgcn_sched_barrier(0);
+        read_k(smem + (st + 1 < stages ? (b + 1) % RING : b) * 2 * SB, kf);
+        zero(sn);
+        v4i p[2];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sn = mfma32(kf[ks], qf[ks], sn);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], w.c, run.off));
+            run.sum += s[i];
         }
 #pragma unroll
-        for (int half = 0; half < SK / 32; ++half) {
-            const uint32_t kb = base + 32 * half;
-            v4f s[RT][2];
+        for (int i = 0; i < 16; i += 2) p[i >> 3][(i & 7) >> 1] = (int)pack_bf16(s[i], s[i + 1]);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int key = 32 * half + 16 * t + l16;
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) s[rt][t] = (v4f){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const v4i kf = *reinterpret_cast<const v4i*>(ks_ + key * DT * 2 + (((4 * ks + q) ^ swizzle<DT>(key)) << 4));
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) s[rt][t] = mfma(kf, qf[rt][ks], s[rt][t]);
-                }
-            }
-            const uint32_t v32 = (uint32_t)(valid >> (32 * half));
-            if (v32 != 0xffffffffu || kb + 32 > ctx) {
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        uint32_t on = v32 >> (16 * t + 4 * q) & 15u;
-                        if (kb + 32 > ctx) on &= seen4(w.a, sp, x.row[rt], x.t[rt], x.word[rt], kb + 16 * t + 4 * q);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) s[rt][t][i] = on >> i & 1 ? s[rt][t][i] : -INFINITY;
-                    }
-            }
-            v4i p[RT];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const float shrink = softmax_step(s[rt], w.c, m[rt], l[rt]);
-                if (__any(shrink != 1.0f))
-#pragma unroll
-                    for (int d = 0; d < DT / 16; ++d) o[rt][d] *= shrink;
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; i += 2) p[rt][2 * t + i / 2] = (int)pack_bf16(s[rt][t][i], s[rt][t][i + 1]);
-            }
-#pragma unroll
-            for (int d = 0; d < DT / 16; ++d) {
-                v4i vt;
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int key = 32 * half + 16 * t + 4 * q + (l16 >> 2), piece = 2 * d + ((l16 >> 1) & 1);
-                    const v4s u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(
-                        vs + key * DT * 2 + ((piece ^ swizzle<DT>(key)) << 4) + 8 * (l16 & 1)));
-                    const uint2 u2 = __builtin_bit_cast(uint2, u);
-                    vt[2 * t] = (int)u2.x;
-                    vt[2 * t + 1] = (int)u2.y;
-                }
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) o[rt][d] = mfma(vt, p[rt], o[rt][d]);
-            }
+        for (int ks = 0; ks < KS; ++ks) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, 56 / KS, 0);
         }
-        valid = valid_next;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < DT / 64; ++g) {
+            v4i vt[2][2];
+            const uint32_t off = b * 2 * SB;
+            read_vt32<16 * DT * 2>(vat[2 * g][0] + off, vat[2 * g][1] + off, vat[2 * g + 1][0] + off, vat[2 * g + 1][1] + off, vt);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) o[2 * g + e] = mfma32(vt[e][k], p[k], o[2 * g + e]);
+        }
+        s = sn;
+        // (the stage's reads have all delivered: the scores have been used, and the values wait for themselves)
     }
 
     const bool whole = sp.n_chunks == 1;
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(run.sum), __float_as_uint(run.sum), false, false);
+    const float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (!live) return;
+    const float inv = !whole ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        float sum = l[rt];
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (!x.live[rt]) continue;
-        const float inv = !whole ? 1.0f : sum == 0.0f ? 0.0f : 1.0f / sum;
+    for (int d = 0; d < DT / 32; ++d)
 #pragma unroll
-        for (int d = 0; d < DT / 16; ++d)
-            store4(w, whole, chunk, x.row[rt], x.head[rt], 16 * d + 4 * q,
-                   make_float4(o[rt][d][0] * inv, o[rt][d][1] * inv, o[rt][d][2] * inv, o[rt][d][3] * inv));
-        if (q == 0) store_stats(w, whole, chunk, x.row[rt], x.head[rt], m[rt], sum);
-    }
+        for (int e = 0; e < 4; ++e)
+            store4(w, whole, chunk, row, head, 32 * d + 8 * e + 4 * h,
+                   make_float4(o[d][4 * e] * inv, o[d][4 * e + 1] * inv, o[d][4 * e + 2] * inv, o[d][4 * e + 3] * inv));
+    if (h == 0) store_stats(w, whole, chunk, row, head, run.top, sum);
 }
 
 // ---------------------------------------------------------------------------------------------- chunks of a request joined
-// One wave per (row, query head) of a request; a lane holds 4 numbers.
-__global__ void __launch_bounds__(256) tree_join_kernel(Work w)
+// A workgroup per (row, query head) of a request.  D / 4 lanes (rounded up to a power of two, `width`) hold a row's numbers,
+// the 256 / width groups of them take turns at the chunks.
+__global__ void __launch_bounds__(256) tree_join_kernel(Work w, int width)
 {
+    __shared__ float4 sums[256];
+    __shared__ float weight[MAX_CHUNKS];
     const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int head = (int)(unit % w.a.n_q), i = (int)(unit / w.a.n_q);
+    const int head = (int)(blockIdx.x % w.a.n_q), i = (int)(blockIdx.x / w.a.n_q);
     const Span sp = make_span(w, blockIdx.y);
     if (i >= sp.T || i >= w.a.max_rows || sp.n_chunks < 2) return;
     const int64_t row = sp.first + i;
     const int64_t at = row * w.a.n_q + head, step = w.a.M * w.a.n_q;
+    // every wave for itself: the chunks' maxima and sums
     float top = -INFINITY;
     float2 mine[MAX_CHUNKS / 64];
 #pragma unroll
@@ -638,48 +824,63 @@ __global__ void __launch_bounds__(256) tree_join_kernel(Work w)
         top = fmaxf(top, mine[e].x);
     }
     top = wave_max_f32(top);
-    float all = 0.0f, f[MAX_CHUNKS / 64];
+    float all = 0.0f;
 #pragma unroll
     for (int e = 0; e < MAX_CHUNKS / 64; ++e) {
-        f[e] = mine[e].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mine[e].x - top) * w.c);
-        all = fmaf(mine[e].y, f[e], all);
+        const float f = mine[e].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine[e].x - top);
+        all = fmaf(mine[e].y, f, all);
+        if (threadIdx.x < 64) weight[e * 64 + lane] = f;
     }
 #pragma unroll
     for (int off = 32; off; off >>= 1) all += __shfl_xor(all, off);
+    __syncthreads();
+    const int d = 4 * (threadIdx.x & (width - 1)), groups = 256 / width;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int d = 4 * lane;
-    for (int c = 0; c < sp.n_chunks; ++c) {
-        const float g = __shfl(c < 64 ? f[0] : f[1], c & 63);
-        if (g == 0.0f || d >= w.a.D) continue;
-        const float4 v = *reinterpret_cast<const float4*>(w.part_o + ((int64_t)c * step + at) * w.a.D + d);
-        acc.x = fmaf(v.x, g, acc.x);
-        acc.y = fmaf(v.y, g, acc.y);
-        acc.z = fmaf(v.z, g, acc.z);
-        acc.w = fmaf(v.w, g, acc.w);
+    if (d < w.a.D) {
+        const float* src = w.part_o + at * w.a.D + d;
+#pragma unroll 4
+        for (int c = threadIdx.x / width; c < sp.n_chunks; c += groups) {
+            const float g = weight[c];                       // (0: the chunk saw nothing, its sums are zeros)
+            const float4 v = *reinterpret_cast<const float4*>(src + (int64_t)c * step * w.a.D);
+            acc.x = fmaf(v.x, g, acc.x);
+            acc.y = fmaf(v.y, g, acc.y);
+            acc.z = fmaf(v.z, g, acc.z);
+            acc.w = fmaf(v.w, g, acc.w);
+        }
+    }
+    sums[threadIdx.x] = acc;
+    __syncthreads();
+    if (threadIdx.x >= width) return;
+    for (int g = 1; g < groups; ++g) {
+        const float4 v = sums[g * width + threadIdx.x];
+        acc.x += v.x;
+        acc.y += v.y;
+        acc.z += v.z;
+        acc.w += v.w;
     }
     const float inv = all == 0.0f ? 0.0f : 1.0f / all;
     store4(w, true, 0, row, head, d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-    if (lane == 0) store_stats(w, true, 0, row, head, top, all);
+    if (threadIdx.x == 0) store_stats(w, true, 0, row, head, top, all);
 }
 
 template <int DT, int RT>
 int launch_few(const Work& w, hipStream_t stream)
 {
-    constexpr int merge = FEW_WAVES * 16 * (DT + 4) * 4 + 2 * FEW_WAVES * 16 * 4, tiles = FEW_WAVES * 32 * DT * 2;
+    constexpr int merge = FEW_WAVES * 16 * (DT + 4) * 4 + 2 * FEW_WAVES * 16 * 4, tiles = FEW_WAVES * 2 * 32 * DT * 2;
     constexpr int lds = merge > tiles ? merge : tiles;
     if (int rc = ensure_dynamic_lds((const void*)tree_few_kernel<DT, RT>, lds, "w2_tree_attention")) return rc;
     hipLaunchKernelGGL((tree_few_kernel<DT, RT>), dim3(w.chunks * w.n_kv, (unsigned)w.a.n_requests), dim3(64 * FEW_WAVES), lds, stream, w);
     return check_launch("w2_tree_attention");
 }
 
-template <int DT, int RT>
+template <int DT>
 int launch_tile(const Work& w, hipStream_t stream)
 {
-    constexpr int lds = 4 * stage_bytes<DT>();
-    if (int rc = ensure_dynamic_lds((const void*)tree_tile_kernel<DT, RT>, lds, "w2_tree_attention")) return rc;
+    constexpr int lds = tile_lds<DT>();
+    if (int rc = ensure_dynamic_lds((const void*)tree_tile_kernel<DT>, lds, "w2_tree_attention")) return rc;
     const int64_t blocks = (int64_t)w.chunks * w.n_kv * w.tiles;
     if (blocks >= (int64_t)1 << 24) return fail(W2_ERR_UNSUPPORTED_SHAPE, "w2_tree_attention: a request's rows are more than a grid counts");
-    hipLaunchKernelGGL((tree_tile_kernel<DT, RT>), dim3((unsigned)blocks, (unsigned)w.a.n_requests), dim3(64 * TILE_WAVES), lds, stream, w);
+    hipLaunchKernelGGL((tree_tile_kernel<DT>), dim3((unsigned)blocks, (unsigned)w.a.n_requests), dim3(64 * TILE_WAVES), lds, stream, w);
     return check_launch("w2_tree_attention");
 }
 
@@ -706,6 +907,7 @@ int launch_tree_attention(const TreeArgs& a, hipStream_t stream)
     // (a scale of zero as the smallest number: unseen keys stay at -infinity)
     w.c = std::max(fabsf(a.scale) * LOG2E, 1e-30f);
     w.flip = a.scale < 0.0f;
+    w.same = a.cache.k_page_stride == a.cache.v_page_stride && a.cache.k_slot_stride == a.cache.v_slot_stride;
     w.tiles = p.tiles;
     w.chunk = p.chunk;
     w.chunks = p.chunks;
@@ -718,13 +920,12 @@ int launch_tree_attention(const TreeArgs& a, hipStream_t stream)
         else if (p.dt == 128) rc = p.rt == 1 ? launch_few<128, 1>(w, stream) : launch_few<128, 2>(w, stream);
         else rc = launch_few<256, 1>(w, stream);
     } else {
-        if (p.dt == 64) rc = p.rt == 1 ? launch_tile<64, 1>(w, stream) : launch_tile<64, 2>(w, stream);
-        else if (p.dt == 128) rc = p.rt == 1 ? launch_tile<128, 1>(w, stream) : launch_tile<128, 2>(w, stream);
-        else rc = launch_tile<256, 1>(w, stream);
+        rc = p.dt == 64 ? launch_tile<64>(w, stream) : p.dt == 128 ? launch_tile<128>(w, stream) : launch_tile<256>(w, stream);
     }
     if (rc || p.chunks < 2) return rc;
-    const int64_t waves = a.max_rows * a.n_q;
-    hipLaunchKernelGGL(tree_join_kernel, dim3((unsigned)((waves + 3) / 4), (unsigned)a.n_requests), dim3(256), 0, stream, w);
+    int width = 1;
+    while (4 * width < a.D) width *= 2;
+    hipLaunchKernelGGL(tree_join_kernel, dim3((unsigned)(a.max_rows * a.n_q), (unsigned)a.n_requests), dim3(256), 0, stream, w, width);
     return check_launch("w2_tree_attention");
 }
 
