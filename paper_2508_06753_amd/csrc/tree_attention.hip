@@ -15,6 +15,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "block_ops.h"
 #include "w2_small_common.h"
@@ -34,6 +35,10 @@ constexpr int MAX_CHUNKS = 128;
 
 __device__ __align__(16) const uint32_t g_zeros[4] = {0, 0, 0, 0};
 
+// an index that is the same in every lane, by the scalar unit
+typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
+__device__ __forceinline__ int scalar_load(const int32_t* p, int64_t i) { return ((scalar_ptr)(uintptr_t)p)[i]; }
+
 __device__ __forceinline__ v4f mfma(const v4i& a, const v4i& b, const v4f& c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
@@ -46,6 +51,12 @@ __device__ __forceinline__ void load_lds(const void* src, char* dst)
 {
     asm volatile("" : "+v"(src));                            // (one load from a chosen address, not a choice of two loads: they are counted)
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, CACHE);
+}
+// from a place that is the same in every lane, `off` bytes on
+template <int CACHE>
+__device__ __forceinline__ void load_lds_run(const char* run, uint32_t off, char* dst)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) char*)run + off, (__attribute__((address_space(3))) void*)dst, 16, 0, CACHE);
 }
 __device__ __forceinline__ void load_lds4(const void* src, char* dst)        // 4 bytes a lane
 {
@@ -81,10 +92,15 @@ __device__ __forceinline__ float max2(float a, float b)
     asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
     return r;
 }
-__device__ __forceinline__ float max3(float a, float b, float c)
+// (the numbers may come straight from a matrix instruction: it is given the time that it needs, which the compiler does not
+// see to for such a block)
+__device__ __forceinline__ float max8(const v4f& a, const v4f& b)
 {
     float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    asm("s_nop 15\n\ts_nop 7\n\t"
+        "v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max_f32 %0, %0, %8"
+        : "=&v"(r)
+        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]));
     return r;
 }
 
@@ -180,6 +196,7 @@ struct Work {
     float c;                             // |scale| * log2 e
     int flip;                            // scale < 0: queries change sign
     int same;                            // K and V have the same strides
+    uint32_t n_pages;
     int tiles, chunk, chunks, n_kv;
     float* part_o;
     float2* part_ml;
@@ -195,11 +212,11 @@ struct Span {
 __device__ __forceinline__ Span make_span(const Work& w, int r)
 {
     Span s;
-    const int64_t lo = max((int64_t)w.a.row_start[r], (int64_t)0), hi = min((int64_t)w.a.row_start[r + 1], w.a.M);
+    const int64_t lo = max((int64_t)scalar_load(w.a.row_start, r), (int64_t)0), hi = min((int64_t)scalar_load(w.a.row_start, r + 1), w.a.M);
     s.first = lo;
     s.T = (int)max(min(hi - lo, w.a.M), (int64_t)0);
     s.rows = (int)min((int64_t)s.T, w.a.max_rows) * w.a.G;
-    const int64_t len = min(min((int64_t)w.a.kv_len[r], w.a.max_len), w.a.table_cols * w.a.cache.page_size);
+    const int64_t len = min(min((int64_t)scalar_load(w.a.kv_len, r), w.a.max_len), w.a.table_cols * w.a.cache.page_size);
     s.len = (int)max(len, (int64_t)0);
     s.ctx = s.len - s.T;
     s.n_chunks = max(1, (int)(((uint32_t)s.len + (uint32_t)w.chunk - 1) / (uint32_t)w.chunk));
@@ -236,6 +253,36 @@ __device__ __forceinline__ void locate(const Work& w, uint32_t key, int page, bo
     k_off = (uint64_t)p * (uint32_t)c.k_page_stride + (uint64_t)place * (uint32_t)c.k_slot_stride;
     v_off = k_off;
     if (!w.same) v_off = (uint64_t)p * (uint32_t)c.v_page_stride + (uint64_t)place * (uint32_t)c.v_slot_stride;
+}
+
+// Pages of a multiple of 16 places (P16): 16 keys from a multiple of 16 on lie in one page, and an instruction that loads rows
+// to local memory takes rows of one such run: where the two runs of a step begin is worked out by the scalar unit, a lane
+// adds where its 16 bytes lie in a run, the same for every step.
+// Where, in bytes, the run that starts at `key` lies in the cache, without its head
+struct Run {
+    uint64_t k, v;
+};
+__device__ __forceinline__ Run make_run(const Work& w, uint32_t key, uint32_t page)
+{
+    const w2_kv_cache_t& c = w.a.cache;
+    const uint32_t place = key - divide(key, w.a.page) * (uint32_t)c.page_size;
+    Run x;
+    x.k = x.v = ((uint64_t)page * (uint32_t)c.k_page_stride + (uint64_t)place * (uint32_t)c.k_slot_stride) * 2;
+    if (!w.same) x.v = ((uint64_t)page * (uint32_t)c.v_page_stride + (uint64_t)place * (uint32_t)c.v_slot_stride) * 2;
+    return x;
+}
+
+// Which of the 32 keys from base on are there, their two runs in pages id[0] and id[1]
+__device__ __forceinline__ uint32_t valid_keys(const Work& w, uint32_t base, uint32_t k1, const int (&id)[2])
+{
+    if (base + 32 <= k1 && (uint32_t)id[0] < w.n_pages && (uint32_t)id[1] < w.n_pages) return 0xffffffffu;
+    uint32_t valid = 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const uint32_t key = base + 16 * t;
+        if (key < k1 && (uint32_t)id[t] < w.n_pages) valid |= (k1 - key >= 16 ? 0xffffu : (1u << (k1 - key)) - 1u) << (16 * t);
+    }
+    return valid;
 }
 
 // a 64-bit number of another lane
@@ -323,10 +370,7 @@ struct Running {
 template <int N>
 __device__ __forceinline__ void softmax_step(v4f (&s)[2], float c, Running& run, v4f (&o)[N])
 {
-    float mx = max3(s[0][0], s[0][1], s[0][2]);
-    mx = max3(mx, s[0][3], s[1][0]);
-    mx = max3(mx, s[1][1], s[1][2]);
-    mx = max_over_q(max2(mx, s[1][3]));
+    const float mx = max_over_q(max8(s[0], s[1]));
     // (a maximum of -infinity has no difference from itself: not a number, no change)
     if (__builtin_amdgcn_ballot_w64(fmaf(mx, c, -run.top) > SLACK)) {
         const float up = fmaxf(run.top, mx * c);
@@ -369,7 +413,7 @@ __device__ __forceinline__ void store_stats(const Work& w, bool whole, int chunk
 // ---------------------------------------------------------------------------------------------- few rows
 constexpr int FEW_WAVES = 4;
 
-template <int DT, int RT>
+template <int DT, int RT, bool P16>
 __global__ void __launch_bounds__(64 * FEW_WAVES, DT == 256 ? 1 : 2) tree_few_kernel(Work w)
 {
     constexpr int KS = DT / 32;
@@ -390,36 +434,65 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DT == 256 ? 1 : 2) tree_few_ke
     char* const kb = smem + wave * 2 * TILE;
     char* const vb = kb + TILE;
 
-    // lane = key of a step (twice), for its page
-    auto page_of = [&](uint32_t base) { return table[divide(min(base + (lane & 31), k1 - 1), w.a.page)]; };
     uint32_t valid = 0, valid_next = 0;
+    // Pages of a step and, from them, where its rows lie.  Without P16: lane = key of a step (twice).
+    struct Pages { int id[2]; };
+    auto pages_of = [&](uint32_t base) {
+        Pages p = {};
+        if constexpr (P16) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) p.id[t] = scalar_load(table, divide(min(base + 16 * t, k1 - 1), w.a.page));
+        } else {
+            p.id[0] = table[divide(min(base + (lane & 31), k1 - 1), w.a.page)];
+        }
+        return p;
+    };
+    Run runs[2] = {};
     uint64_t koff = 0, voff = 0;
-    auto place = [&](uint32_t base, int id) {
-        const uint32_t key = base + (lane & 31);
-        const bool ok = key < k1 && id >= 0 && id < w.a.cache.n_pages;
-        locate(w, min(key, k1 - 1), id, ok, koff, voff);
-        valid_next = (uint32_t)__ballot(ok);
+    auto place = [&](uint32_t base, const Pages& p) {
+        if constexpr (P16) {
+            valid_next = valid_keys(w, base, k1, p.id);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)                      // (a run without a valid key: page 0, zeros are taken instead)
+                runs[t] = make_run(w, base + 16 * t, valid_next >> (16 * t) & 0xffff ? p.id[t] : 0);
+        } else {
+            const uint32_t key = base + (lane & 31);
+            const bool ok = key < k1 && (uint32_t)p.id[0] < w.n_pages;
+            locate(w, min(key, k1 - 1), p.id[0], ok, koff, voff);
+            valid_next = (uint32_t)__builtin_amdgcn_ballot_w64(ok);
+        }
     };
     // whole rows of the cache side by side, 1 KiB an instruction; rows that nobody sees come from a place that holds zeros
-    auto fetch = [&](const uint16_t* head, uint64_t off, char* dst) {
+    auto fetch = [&](bool is_v, char* dst) {
+        const uint32_t slot_bytes = 2 * (uint32_t)(is_v ? w.a.cache.v_slot_stride : w.a.cache.k_slot_stride);
+        if (P16 && valid_next == 0xffffffffu && w.a.D == DT) {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const int at = j * 64 + lane, row = at / PIECES, d = (at % PIECES ^ swizzle<DT>(row)) * 8, t = j * 64 / PIECES / 16;
+                const char* const run = (const char*)(is_v ? vh : kh) + (is_v ? runs[t].v : runs[t].k);
+                load_lds_run<2>(run, (uint32_t)(row & 15) * slot_bytes + 2 * d, dst + j * 1024);
+            }
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-            const int at = j * 64 + lane, row = at / PIECES, slot = at % PIECES;
-            const int d = (slot ^ swizzle<DT>(row)) * 8;
-            const uint64_t o = from_lane(off, row);
-            load_lds<2>((valid_next >> row & 1) && d < w.a.D ? (const void*)(head + d + o) : (const void*)g_zeros, dst + j * 1024);
+            const int at = j * 64 + lane, row = at / PIECES, d = (at % PIECES ^ swizzle<DT>(row)) * 8, t = j * 64 / PIECES / 16;
+            const char* src = (const char*)(is_v ? vh : kh) + 2 * d;
+            if constexpr (P16) src += (is_v ? runs[t].v : runs[t].k) + (uint32_t)(row & 15) * slot_bytes;
+            else src += 2 * from_lane(is_v ? voff : koff, row);
+            load_lds<2>((valid_next >> row & 1) && d < w.a.D ? (const void*)src : (const void*)g_zeros, dst + j * 1024);
         }
     };
 
     constexpr uint32_t STEP = 32 * FEW_WAVES;
     uint32_t base = k0 + 32 * wave;
-    int id = 0;
+    Pages pages = {};
     if (base < k1) {
-        const int first = page_of(base);
-        id = page_of(base + STEP);
+        const Pages first = pages_of(base);
+        pages = pages_of(base + STEP);
         place(base, first);
-        fetch(kh, koff, kb);
-        fetch(vh, voff, vb);
+        fetch(false, kb);
+        fetch(true, vb);
         valid = valid_next;
     }
     uint32_t vat[DT / 16];
@@ -444,11 +517,11 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DT == 256 ? 1 : 2) tree_few_ke
         v4f s[RT][2];
         scores<DT, RT>(kb, l16, q, qf, s);
         if (more) {
-            const int next = id;
-            id = page_of(base + 2 * STEP);
+            const Pages next = pages;
+            pages = pages_of(base + 2 * STEP);
             place(base + STEP, next);
             wait_reads();
-            fetch(kh, koff, kb);
+            fetch(false, kb);
         }
         if (valid != 0xffffffffu || base + 32 > ctx) {
 #pragma unroll
@@ -493,7 +566,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DT == 256 ? 1 : 2) tree_few_ke
         }
         if (more) {
             wait_reads();
-            fetch(vh, voff, vb);
+            fetch(true, vb);
         }
         valid = valid_next;
     }
@@ -556,6 +629,18 @@ template <int DT> constexpr int tile_lds() { return RING * 2 * stage_bytes<DT>()
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 
+__device__ __forceinline__ float max16(const v16f& s)
+{
+    float r;
+    asm("s_nop 15\n\ts_nop 7\n\t"
+        "v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max3_f32 %0, %0, %8, %9\n\t"
+        "v_max3_f32 %0, %0, %10, %11\n\tv_max3_f32 %0, %0, %12, %13\n\tv_max3_f32 %0, %0, %14, %15\n\tv_max_f32 %0, %0, %16"
+        : "=&v"(r)
+        : "v"(s[0]), "v"(s[1]), "v"(s[2]), "v"(s[3]), "v"(s[4]), "v"(s[5]), "v"(s[6]), "v"(s[7]), "v"(s[8]), "v"(s[9]), "v"(s[10]),
+          "v"(s[11]), "v"(s[12]), "v"(s[13]), "v"(s[14]), "v"(s[15]));
+    return r;
+}
+
 __device__ __forceinline__ v16f mfma32(const v4i& a, const v4i& b, const v16f& c)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
@@ -566,21 +651,21 @@ template <int DT>
 __device__ __forceinline__ int swizzle32(int key) { return DT == 64 ? ((key & 2) << 1 | ((key >> 2) & 3)) : (((key & 3) << 2) | ((key >> 2) & 3)); }
 
 // V^T operands of two blocks of 32 numbers, for the first and the second 16 keys of a stage.  at[block][j]: rows 8 j + 4 h ..
-template <int HALF>
+template <int BUF, int HALF>
 __device__ __forceinline__ void read_vt32(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, v4i (&out)[2][2])
 {
     uint2 x0, x1, x2, x3, y0, y1, y2, y3;
-    asm volatile("ds_read_b64_tr_b16 %0, %8\n\t"
-                 "ds_read_b64_tr_b16 %1, %9\n\t"
-                 "ds_read_b64_tr_b16 %2, %8 offset:%12\n\t"
-                 "ds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
-                 "ds_read_b64_tr_b16 %4, %10\n\t"
-                 "ds_read_b64_tr_b16 %5, %11\n\t"
-                 "ds_read_b64_tr_b16 %6, %10 offset:%12\n\t"
-                 "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+    asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %1, %9 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %2, %8 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %4, %10 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %5, %11 offset:%12\n\t"
+                 "ds_read_b64_tr_b16 %6, %10 offset:%13\n\t"
+                 "ds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
                  "s_waitcnt lgkmcnt(0)"
                  : "=&v"(x0), "=&v"(x1), "=&v"(x2), "=&v"(x3), "=&v"(y0), "=&v"(y1), "=&v"(y2), "=&v"(y3)
-                 : "v"(a0), "v"(a1), "v"(b0), "v"(b1), "n"(HALF)
+                 : "v"(a0), "v"(a1), "v"(b0), "v"(b1), "n"(BUF), "n"(BUF + HALF)
                  : "memory");
     out[0][0] = (v4i){(int)x0.x, (int)x0.y, (int)x1.x, (int)x1.y};
     out[0][1] = (v4i){(int)x2.x, (int)x2.y, (int)x3.x, (int)x3.y};
@@ -591,7 +676,7 @@ __device__ __forceinline__ void read_vt32(uint32_t a0, uint32_t a1, uint32_t b0,
 // A wave holds 32 packed rows, one in lanes l and l + 32.  Scores: lane half h has keys 8 b + 4 h + i (b, i = 0..3) of a
 // stage, which are slots 4 b + i of the weights' operands.  The scores of the next stage are multiplied while this stage's
 // weights are made: matrix and vector instructions of one wave side by side.
-template <int DT>
+template <int DT, bool P16>
 __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_kernel(Work w)
 {
     constexpr int KS = DT / 16, SB = stage_bytes<DT>();
@@ -622,18 +707,48 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
     const uint16_t* const vh = w.a.cache.v + hk * w.a.cache.v_head_stride;
     const int32_t* const table = w.a.table + r * w.a.ld_table;
 
-    // Pages of a stage go to local memory like its keys (lane = key), RING - 1 stages before they are needed: a wave that
-    // waited for them in registers would wait for every load of keys before them too.
+    // Pages of a stage: P16: by the scalar unit, a stage before they are needed.  Else they go to local memory like its keys
+    // (lane = key), RING - 1 stages before they are needed: a wave that waited for them in registers would wait for every load of
+    // keys before them too.
     char* const ids = smem + RING * 2 * SB + wave * ID_SLOTS * 256;
+    int next[2] = {0, 0}, page = 0;
+    const int half = wave * LOADS * 64 / PIECES >= 16;       // the run that a wave's 8 rows of a stage lie in
+    uint32_t koffs[LOADS], voffs[LOADS];                     // where a lane's pieces lie in a run
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+        const int at = (wave * LOADS + j) * 64 + lane, row = at / PIECES, d = (at % PIECES ^ swizzle32<DT>(row)) * 8;
+        koffs[j] = (uint32_t)(row & 15) * 2 * (uint32_t)w.a.cache.k_slot_stride + 2 * d;
+        voffs[j] = (uint32_t)(row & 15) * 2 * (uint32_t)w.a.cache.v_slot_stride + 2 * d;
+    }
     auto fetch_pages = [&](int st) {
-        const uint32_t key = min(k0 + (uint32_t)st * 32 + l32, k1 - 1);
-        load_lds4(table + divide(key, w.a.page), ids + (st & (ID_SLOTS - 1)) * 256);
+        if constexpr (P16) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) next[t] = scalar_load(table, divide(min(k0 + (uint32_t)st * 32 + 16 * t, k1 - 1), w.a.page));
+        } else {
+            const uint32_t key = min(k0 + (uint32_t)st * 32 + l32, k1 - 1);
+            load_lds4(table + divide(key, w.a.page), ids + (st & (ID_SLOTS - 1)) * 256);
+        }
     };
     auto fetch = [&](int st, int buf) -> uint32_t {
         char* const dst = smem + buf * 2 * SB;
+        if constexpr (P16) {
+            const uint32_t base = k0 + (uint32_t)st * 32, valid = valid_keys(w, base, k1, next);
+            const Run x = make_run(w, base + 16 * half, valid >> (16 * half) & 0xffff ? next[half] : 0);
+            const char* const kr = (const char*)kh + x.k;
+            const char* const vr = (const char*)vh + x.v;
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const int at = (wave * LOADS + j) * 64 + lane, row = at / PIECES, d = (at % PIECES ^ swizzle32<DT>(row)) * 8;
+                const bool there = (valid >> row & 1) && d < w.a.D;
+                char* const to = dst + (wave * LOADS + j) * 1024;
+                load_lds<0>(there ? (const void*)(kr + koffs[j]) : (const void*)g_zeros, to);
+                load_lds<0>(there ? (const void*)(vr + voffs[j]) : (const void*)g_zeros, to + SB);
+            }
+            return valid;
+        }
         const uint32_t key = k0 + (uint32_t)st * 32 + l32;
         const int id = *reinterpret_cast<const int*>(ids + (st & (ID_SLOTS - 1)) * 256 + lane * 4);
-        const bool ok = key < k1 && id >= 0 && id < w.a.cache.n_pages;
+        const bool ok = key < k1 && (uint32_t)id < w.n_pages;
         uint64_t koff, voff;
         locate(w, min(key, k1 - 1), id, ok, koff, voff);
         const uint32_t valid = (uint32_t)__builtin_amdgcn_ballot_w64(ok);
@@ -651,12 +766,17 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
     };
     uint32_t valid[RING] = {};
     if (stages > 0) {
+        if constexpr (!P16) {
 #pragma unroll
-        for (int st = 0; st < 2 * (RING - 1); ++st) fetch_pages(st);
-        wait_loads<0>();
+            for (int st = 0; st < 2 * (RING - 1); ++st) fetch_pages(st);
+            wait_loads<0>();
+        }
 #pragma unroll
         for (int st = 0; st < RING - 1; ++st)
-            if (st < stages) valid[st] = fetch(st, st);
+            if (st < stages) {
+                if constexpr (P16) fetch_pages(st);
+                valid[st] = fetch(st, st);
+            }
     }
 
     // the lane's query row, its operands: numbers 16 ks + 8 h ..+ 7
@@ -702,45 +822,43 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
         for (int i = 0; i < 16; ++i) s[i] = 0.0f;
     };
 
-    v16f s, sn;
-    zero(s);
-    if (stages > 0) {
-        if (stages > 2) wait_loads<4 * LOADS>();
-        else if (stages > 1) wait_loads<2 * LOADS>();
-        else wait_loads<0>();
-        bare_barrier();
-        v4i kf[KS];
-        read_k(smem, kf);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = mfma32(kf[ks], qf[ks], s);
-    }
-    for (int st0 = 0; st0 < stages; st0 += RING)
-#pragma unroll
-    for (int b = 0; b < RING; ++b) {
-        const int st = st0 + b;
-        if (st >= stages) break;
+    // INNER: a stage whose keys everybody sees, in the middle of a chunk whose pages are all there: nothing to check.
+    // cur: its scores, next: the next stage's.
+    auto stage = [&](int st, auto bc, auto inner, v16f& cur, v16f& nxt) {
+        constexpr int b = decltype(bc)::value, ahead = (b + RING - 1) % RING;
+        constexpr bool INNER = decltype(inner)::value;
         const uint32_t base = k0 + (uint32_t)st * 32;
         // the next stage is there; one behind it is under way
-        if (st + 2 < stages) wait_loads<2 * LOADS>();
+        if (INNER || st + 2 < stages) wait_loads<2 * LOADS>();
         else wait_loads<0>();
         bare_barrier();                                      // every wave's part of it, and no wave reads the stage before this one any more
-        if (st + RING - 1 < stages) {
-            fetch_pages(st + 2 * (RING - 1));
-            valid[(b + RING - 1) % RING] = fetch(st + RING - 1, (b + RING - 1) % RING);
-        }
-        if (valid[b] != 0xffffffffu || base + 32 > ctx) {
+        if constexpr (INNER) {
+            const uint32_t mine = base + 32 * (RING - 1) + 16 * half;
+            const Run x = make_run(w, mine, (uint32_t)page);
+            page = scalar_load(table, divide(mine + 32, w.a.page));      // (mine + 32 < k1)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                uint32_t on = valid[b] >> (8 * e + 4 * h) & 15u;
-                if (base + 32 > ctx) on &= seen4(w.a, sp, row, t, word, base + 8 * e + 4 * h);
+            for (int j = 0; j < LOADS; ++j) {
+                char* const to = smem + ahead * 2 * SB + (wave * LOADS + j) * 1024;
+                load_lds_run<0>((const char*)kh + x.k, koffs[j], to);
+                load_lds_run<0>((const char*)vh + x.v, voffs[j], to + SB);
+            }
+        } else {
+            if (st + RING - 1 < stages) {
+                if constexpr (P16) fetch_pages(st + RING - 1);
+                else fetch_pages(st + 2 * (RING - 1));
+                valid[ahead] = fetch(st + RING - 1, ahead);
+            }
+            if (valid[b] != 0xffffffffu || base + 32 > ctx) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[4 * e + i] = on >> i & 1 ? s[4 * e + i] : -INFINITY;
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t on = valid[b] >> (8 * e + 4 * h) & 15u;
+                    if (base + 32 > ctx) on &= seen4(w.a, sp, row, t, word, base + 8 * e + 4 * h);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) cur[4 * e + i] = on >> i & 1 ? cur[4 * e + i] : -INFINITY;
+                }
             }
         }
-        float mx = max3(s[0], s[1], s[2]);
-#pragma unroll
-        for (int i = 3; i < 15; i += 2) mx = max3(mx, s[i], s[i + 1]);
-        mx = max2(mx, s[15]);
+        float mx = max16(cur);
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         mx = max2(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
         if (__builtin_amdgcn_ballot_w64(fmaf(mx, w.c, -run.top) > SLACK)) {
@@ -752,39 +870,85 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
 #pragma unroll
             for (int d = 0; d < DT / 32; ++d) o[d] *= shrink;
         }
-        // (past the last stage: the scores of a stage that is there once more, which nobody uses)
+        // (past the last stage: scores of whatever the buffer holds, which nobody uses)
         v4i kf[KS];
         __builtin_amdgcn_sched_barrier(0);
-        read_k(smem + (st + 1 < stages ? (b + 1) % RING : b) * 2 * SB, kf);
-        zero(sn);
+        read_k(smem + (b + 1) % RING * 2 * SB, kf);
+        zero(nxt);
         v4i p[2];
+        __builtin_amdgcn_sched_barrier(0);                   // all reads first; then a product, its share of the vector instructions, a product ...
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) sn = mfma32(kf[ks], qf[ks], sn);
+        for (int ks = 0; ks < KS; ++ks) nxt = mfma32(kf[ks], qf[ks], nxt);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], w.c, run.off));
-            run.sum += s[i];
+            cur[i] = __builtin_amdgcn_exp2f(fmaf(cur[i], w.c, run.off));
+            run.sum += cur[i];
         }
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) p[i >> 3][(i & 7) >> 1] = (int)pack_bf16(s[i], s[i + 1]);
+        for (int i = 0; i < 16; i += 2) p[i >> 3][(i & 7) >> 1] = (int)pack_bf16(cur[i], cur[i + 1]);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x402, 56 / KS, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 56 / KS, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int g = 0; g < DT / 64; ++g) {
             v4i vt[2][2];
-            const uint32_t off = b * 2 * SB;
-            read_vt32<16 * DT * 2>(vat[2 * g][0] + off, vat[2 * g][1] + off, vat[2 * g + 1][0] + off, vat[2 * g + 1][1] + off, vt);
+            constexpr bool near = (b * 2 + 1) * SB < 65536;  // (within the reach of an instruction's offset)
+            constexpr uint32_t far = near ? 0 : b * 2 * SB;
+            read_vt32<near ? b * 2 * SB : 0, 16 * DT * 2>(vat[2 * g][0] + far, vat[2 * g][1] + far, vat[2 * g + 1][0] + far, vat[2 * g + 1][1] + far, vt);
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) o[2 * g + e] = mfma32(vt[e][k], p[k], o[2 * g + e]);
         }
-        s = sn;
         // (the stage's reads have all delivered: the scores have been used, and the values wait for themselves)
+    };
+    v16f sa, sb;
+    zero(sa);
+    zero(sb);
+    int inner = 0;                                           // stages of that kind, from the first on
+    if (stages > 0) {
+        if (P16 && w.a.D == DT) {
+            inner = max(min((int)((k1 - k0) / 32) - RING, (int)((min(ctx, k1) - min(ctx, k0)) / 32)), 0) / RING * RING;
+            const uint32_t p0 = divide(k0, w.a.page), p1 = divide(k1 - 1, w.a.page);
+            bool all = inner > 0;
+            if (all)
+                for (uint32_t p = p0 + lane; p <= p1; p += 64) all &= (uint32_t)table[p] < w.n_pages;
+            if (__builtin_amdgcn_ballot_w64(all) != ~(uint64_t)0) inner = 0;
+            if (inner) page = scalar_load(table, divide(k0 + 32 * (RING - 1) + 16 * half, w.a.page));
+        }
+        if (stages > 2) wait_loads<4 * LOADS>();
+        else if (stages > 1) wait_loads<2 * LOADS>();
+        else wait_loads<0>();
+        bare_barrier();
+        v4i kf[KS];
+        read_k(smem, kf);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sa = mfma32(kf[ks], qf[ks], sa);
+    }
+    static_assert(RING == 4, "the loops below");
+    typedef std::integral_constant<int, 0> B0;
+    typedef std::integral_constant<int, 1> B1;
+    typedef std::integral_constant<int, 2> B2;
+    typedef std::integral_constant<int, 3> B3;
+    int st = 0;
+    for (; st < inner; st += RING) {
+        stage(st, B0{}, std::true_type{}, sa, sb);
+        stage(st + 1, B1{}, std::true_type{}, sb, sa);
+        stage(st + 2, B2{}, std::true_type{}, sa, sb);
+        stage(st + 3, B3{}, std::true_type{}, sb, sa);
+    }
+    // (the inner stages asked for three whole stages behind them)
+    if (inner)
+#pragma unroll
+        for (int b = 0; b < RING - 1; ++b) valid[b] = 0xffffffffu;
+    for (; st < stages; st += RING) {
+        stage(st, B0{}, std::false_type{}, sa, sb);
+        if (st + 1 < stages) stage(st + 1, B1{}, std::false_type{}, sb, sa);
+        if (st + 2 < stages) stage(st + 2, B2{}, std::false_type{}, sa, sb);
+        if (st + 3 < stages) stage(st + 3, B3{}, std::false_type{}, sb, sa);
     }
 
     const bool whole = sp.n_chunks == 1;
@@ -863,25 +1027,28 @@ __global__ void __launch_bounds__(256) tree_join_kernel(Work w, int width)
     if (threadIdx.x == 0) store_stats(w, true, 0, row, head, top, all);
 }
 
-template <int DT, int RT>
-int launch_few(const Work& w, hipStream_t stream)
+template <typename Kern>
+int launch(Kern kern, const Work& w, int64_t blocks, int waves, int lds, hipStream_t stream)
 {
-    constexpr int merge = FEW_WAVES * 16 * (DT + 4) * 4 + 2 * FEW_WAVES * 16 * 4, tiles = FEW_WAVES * 2 * 32 * DT * 2;
-    constexpr int lds = merge > tiles ? merge : tiles;
-    if (int rc = ensure_dynamic_lds((const void*)tree_few_kernel<DT, RT>, lds, "w2_tree_attention")) return rc;
-    hipLaunchKernelGGL((tree_few_kernel<DT, RT>), dim3(w.chunks * w.n_kv, (unsigned)w.a.n_requests), dim3(64 * FEW_WAVES), lds, stream, w);
+    if (blocks >= (int64_t)1 << 24) return fail(W2_ERR_UNSUPPORTED_SHAPE, "w2_tree_attention: a request's rows are more than a grid counts");
+    if (int rc = ensure_dynamic_lds((const void*)kern, lds, "w2_tree_attention")) return rc;
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks, (unsigned)w.a.n_requests), dim3(64 * waves), lds, stream, w);
     return check_launch("w2_tree_attention");
 }
 
-template <int DT>
-int launch_tile(const Work& w, hipStream_t stream)
+template <int DT, int RT>
+int launch_few(const Work& w, bool p16, hipStream_t stream)
 {
-    constexpr int lds = tile_lds<DT>();
-    if (int rc = ensure_dynamic_lds((const void*)tree_tile_kernel<DT>, lds, "w2_tree_attention")) return rc;
+    constexpr int merge = FEW_WAVES * 16 * (DT + 4) * 4 + 2 * FEW_WAVES * 16 * 4, tiles = FEW_WAVES * 2 * 32 * DT * 2;
+    const int64_t blocks = (int64_t)w.chunks * w.n_kv;
+    return launch(p16 ? tree_few_kernel<DT, RT, true> : tree_few_kernel<DT, RT, false>, w, blocks, FEW_WAVES, std::max(merge, tiles), stream);
+}
+
+template <int DT>
+int launch_tile(const Work& w, bool p16, hipStream_t stream)
+{
     const int64_t blocks = (int64_t)w.chunks * w.n_kv * w.tiles;
-    if (blocks >= (int64_t)1 << 24) return fail(W2_ERR_UNSUPPORTED_SHAPE, "w2_tree_attention: a request's rows are more than a grid counts");
-    hipLaunchKernelGGL((tree_tile_kernel<DT>), dim3((unsigned)blocks, (unsigned)w.a.n_requests), dim3(64 * TILE_WAVES), lds, stream, w);
-    return check_launch("w2_tree_attention");
+    return launch(p16 ? tree_tile_kernel<DT, true> : tree_tile_kernel<DT, false>, w, blocks, TILE_WAVES, tile_lds<DT>(), stream);
 }
 
 }  // namespace
@@ -907,6 +1074,7 @@ int launch_tree_attention(const TreeArgs& a, hipStream_t stream)
     // (a scale of zero as the smallest number: unseen keys stay at -infinity)
     w.c = std::max(fabsf(a.scale) * LOG2E, 1e-30f);
     w.flip = a.scale < 0.0f;
+    w.n_pages = (uint32_t)a.cache.n_pages;
     w.same = a.cache.k_page_stride == a.cache.v_page_stride && a.cache.k_slot_stride == a.cache.v_slot_stride;
     w.tiles = p.tiles;
     w.chunk = p.chunk;
@@ -914,13 +1082,15 @@ int launch_tree_attention(const TreeArgs& a, hipStream_t stream)
     w.n_kv = n_kv;
     w.part_o = (float*)a.workspace;
     w.part_ml = (float2*)((float*)a.workspace + (size_t)p.chunks * a.M * a.n_q * a.D);
+    // (chunks begin at multiples of 128 keys; a run of 16 rows has to span less than 2^31 bytes)
+    const bool p16 = a.cache.page_size % 16 == 0 && std::max(a.cache.k_slot_stride, a.cache.v_slot_stride) < (int64_t)1 << 25;
     int rc;
     if (p.few) {
-        if (p.dt == 64) rc = p.rt == 1 ? launch_few<64, 1>(w, stream) : launch_few<64, 2>(w, stream);
-        else if (p.dt == 128) rc = p.rt == 1 ? launch_few<128, 1>(w, stream) : launch_few<128, 2>(w, stream);
-        else rc = launch_few<256, 1>(w, stream);
+        if (p.dt == 64) rc = p.rt == 1 ? launch_few<64, 1>(w, p16, stream) : launch_few<64, 2>(w, p16, stream);
+        else if (p.dt == 128) rc = p.rt == 1 ? launch_few<128, 1>(w, p16, stream) : launch_few<128, 2>(w, p16, stream);
+        else rc = launch_few<256, 1>(w, p16, stream);
     } else {
-        rc = p.dt == 64 ? launch_tile<64>(w, stream) : p.dt == 128 ? launch_tile<128>(w, stream) : launch_tile<256>(w, stream);
+        rc = p.dt == 64 ? launch_tile<64>(w, p16, stream) : p.dt == 128 ? launch_tile<128>(w, p16, stream) : launch_tile<256>(w, p16, stream);
     }
     if (rc || p.chunks < 2) return rc;
     int width = 1;
