@@ -150,7 +150,8 @@ __device__ __forceinline__ float max_over_q(float x)
 
 struct Plan {
     int few;                             // tree_few_kernel, else tree_tile_kernel
-    int rt;                              // 16-row tiles a wave
+    int rt;                              // few: 16-row tiles a wave
+    int waves;                           // many: waves of 32 rows a workgroup
     int dt;                              // head_dim padded to 64, 128 or 256
     int tiles;                           // row tiles of a request
     int chunk;                           // keys of a workgroup, a multiple of 32 * waves
@@ -164,11 +165,13 @@ Plan make_plan(int64_t n_requests, int64_t max_rows, int G, int n_kv, int D, int
     p.dt = D <= 64 ? 64 : D <= 128 ? 128 : 256;
     p.few = rows <= (p.dt < 256 ? 32 : 16);
     p.rt = p.few && rows <= 16 ? 1 : 2;
-    const int rows_per_wg = p.few ? 16 * p.rt : 128;
+    p.waves = rows <= 64 ? 2 : 4;
+    const int rows_per_wg = p.few ? 16 * p.rt : 32 * p.waves;
     p.tiles = (int)((rows + rows_per_wg - 1) / rows_per_wg);
     if (total_len <= 0 || total_len > n_requests * max_len) total_len = n_requests * max_len;
-    // workgroups for about two on every CU, of at least 128 (few) or 256 keys each
-    const int64_t least = p.few ? 128 : 256, want = p.few ? 2048 : 512;
+    // workgroups for two on every CU (few: for eight, which are done sooner), each with so many keys that the parts of its rows,
+    // written and read again in 32 bits, stay a tenth of them
+    const int64_t least = std::max<int64_t>(p.few ? 128 : 256, 20 * std::min<int64_t>(rows, rows_per_wg)), want = p.few ? 2048 : 512;
     int64_t chunk = (total_len * n_kv * p.tiles + want - 1) / want;
     chunk = std::max(chunk, (max_len + MAX_CHUNKS - 1) / MAX_CHUNKS);
     if (max_rows * G * n_kv >= (int64_t)1 << 24) chunk = std::max(chunk, max_len);     // (more than a grid of the join counts)
@@ -621,11 +624,10 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DT == 256 ? 1 : 2) tree_few_ke
 }
 
 // ---------------------------------------------------------------------------------------------- many rows
-constexpr int TILE_WAVES = 4;                                // of 32 packed rows each
 constexpr int RING = 4;                                      // stages of 32 keys in local memory
 template <int DT> constexpr int stage_bytes() { return 32 * DT * 2; }                        // of K, and of V again
 constexpr int ID_SLOTS = 8;                                  // a wave's pages of so many stages, 256 bytes each
-template <int DT> constexpr int tile_lds() { return RING * 2 * stage_bytes<DT>() + TILE_WAVES * ID_SLOTS * 256; }
+template <int DT, int W, bool P16> constexpr int tile_lds() { return RING * 2 * stage_bytes<DT>() + (P16 ? 0 : W * ID_SLOTS * 256); }
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 
@@ -676,12 +678,13 @@ __device__ __forceinline__ void read_vt32(uint32_t a0, uint32_t a1, uint32_t b0,
 // A wave holds 32 packed rows, one in lanes l and l + 32.  Scores: lane half h has keys 8 b + 4 h + i (b, i = 0..3) of a
 // stage, which are slots 4 b + i of the weights' operands.  The scores of the next stage are multiplied while this stage's
 // weights are made: matrix and vector instructions of one wave side by side.
-template <int DT, bool P16>
-__global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_kernel(Work w)
+template <int DT, int W, bool P16>
+__global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_kernel(Work w)
 {
     constexpr int KS = DT / 16, SB = stage_bytes<DT>();
-    constexpr int LOADS = SB / 1024 / TILE_WAVES;            // of 64 pieces of 16 bytes, of K and of V, a wave and stage
+    constexpr int LOADS = SB / 1024 / W;                     // of 64 pieces of 16 bytes, of K and of V, a wave and stage
     constexpr int PIECES = DT / 8;                           // of a row
+    constexpr int NT = W == 2 ? 2 : 0;                       // (up to 64 rows are one tile: nobody else reads these keys)
     extern __shared__ __align__(16) char smem[];             // RING stages of K and V, pages
     const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -694,12 +697,12 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
     const int chunk = unit / w.n_kv, r = blockIdx.y;
     const int hk = head_of(w, unit, chunk, r);
     const Span sp = make_span(w, r);
-    const int rho_wg = tile * 32 * TILE_WAVES;
+    const int rho_wg = tile * 32 * W;
     if (rho_wg >= sp.rows || chunk >= sp.n_chunks) return;
     const uint32_t k0 = (uint32_t)chunk * w.chunk, ctx = max(sp.ctx, 0);
     uint32_t k1 = min((uint32_t)sp.len, k0 + w.chunk);
     if (!w.a.mask) {                                         // causal: nothing past the tile's last token
-        const int last = (int)divide((uint32_t)min(rho_wg + 32 * TILE_WAVES, sp.rows) - 1, w.by_g);
+        const int last = (int)divide((uint32_t)min(rho_wg + 32 * W, sp.rows) - 1, w.by_g);
         k1 = max(k0, min(k1, (uint32_t)max(sp.ctx + last + 1, 0)));
     }
     const int stages = (int)((k1 - k0 + 31) / 32);
@@ -741,8 +744,8 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
                 const int at = (wave * LOADS + j) * 64 + lane, row = at / PIECES, d = (at % PIECES ^ swizzle32<DT>(row)) * 8;
                 const bool there = (valid >> row & 1) && d < w.a.D;
                 char* const to = dst + (wave * LOADS + j) * 1024;
-                load_lds<0>(there ? (const void*)(kr + koffs[j]) : (const void*)g_zeros, to);
-                load_lds<0>(there ? (const void*)(vr + voffs[j]) : (const void*)g_zeros, to + SB);
+                load_lds<NT>(there ? (const void*)(kr + koffs[j]) : (const void*)g_zeros, to);
+                load_lds<NT>(there ? (const void*)(vr + voffs[j]) : (const void*)g_zeros, to + SB);
             }
             return valid;
         }
@@ -759,8 +762,8 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
             const uint64_t ko = from_lane(koff, row), vo = w.same ? ko : from_lane(voff, row);
             const bool there = (valid >> row & 1) && d < w.a.D;
             char* const to = dst + (wave * LOADS + j) * 1024;
-            load_lds<0>(there ? (const void*)(kh + d + ko) : (const void*)g_zeros, to);
-            load_lds<0>(there ? (const void*)(vh + d + vo) : (const void*)g_zeros, to + SB);
+            load_lds<NT>(there ? (const void*)(kh + d + ko) : (const void*)g_zeros, to);
+            load_lds<NT>(there ? (const void*)(vh + d + vo) : (const void*)g_zeros, to + SB);
         }
         return valid;
     };
@@ -781,7 +784,7 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
 
     // the lane's query row, its operands: numbers 16 ks + 8 h ..+ 7
     const int rho = rho_wg + wave * 32 + l32;
-    const bool live = rho < sp.rows;
+    const bool live = rho < sp.rows, idle = rho_wg + wave * 32 >= sp.rows;       // (idle: a wave without rows, which only loads)
     const int t = (int)divide((uint32_t)(live ? rho : 0), w.by_g), head = hk * w.a.G + (live ? rho : 0) - t * w.a.G;
     const int64_t row = sp.first + t;
     const uint64_t word = w.a.mask ? w.a.mask[row * w.a.mask_words] : 0;
@@ -822,6 +825,13 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
         for (int i = 0; i < 16; ++i) s[i] = 0.0f;
     };
 
+    // V^T of blocks 2 g and 2 g + 1 of the stage in buffer bc
+    auto read_v = [&](auto bc, int g, v4i (&vt)[2][2]) {
+        constexpr int b = decltype(bc)::value;
+        constexpr bool near = (b * 2 + 1) * SB < 65536;      // (within the reach of an instruction's offset)
+        constexpr uint32_t far = near ? 0 : b * 2 * SB;
+        read_vt32<near ? b * 2 * SB : 0, 16 * DT * 2>(vat[2 * g][0] + far, vat[2 * g][1] + far, vat[2 * g + 1][0] + far, vat[2 * g + 1][1] + far, vt);
+    };
     // INNER: a stage whose keys everybody sees, in the middle of a chunk whose pages are all there: nothing to check.
     // cur: its scores, next: the next stage's.
     auto stage = [&](int st, auto bc, auto inner, v16f& cur, v16f& nxt) {
@@ -839,8 +849,8 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) {
                 char* const to = smem + ahead * 2 * SB + (wave * LOADS + j) * 1024;
-                load_lds_run<0>((const char*)kh + x.k, koffs[j], to);
-                load_lds_run<0>((const char*)vh + x.v, voffs[j], to + SB);
+                load_lds_run<NT>((const char*)kh + x.k, koffs[j], to);
+                load_lds_run<NT>((const char*)vh + x.v, voffs[j], to + SB);
             }
         } else {
             if (st + RING - 1 < stages) {
@@ -858,6 +868,7 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
                 }
             }
         }
+        if (idle) return;
         float mx = max16(cur);
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         mx = max2(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
@@ -874,6 +885,8 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
         v4i kf[KS];
         __builtin_amdgcn_sched_barrier(0);
         read_k(smem + (b + 1) % RING * 2 * SB, kf);
+        v4i vt[2][2];
+        read_v(bc, 0, vt);                                   // the first values' wait is the keys' too
         zero(nxt);
         v4i p[2];
         __builtin_amdgcn_sched_barrier(0);                   // all reads first; then a product, its share of the vector instructions, a product ...
@@ -894,10 +907,7 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int g = 0; g < DT / 64; ++g) {
-            v4i vt[2][2];
-            constexpr bool near = (b * 2 + 1) * SB < 65536;  // (within the reach of an instruction's offset)
-            constexpr uint32_t far = near ? 0 : b * 2 * SB;
-            read_vt32<near ? b * 2 * SB : 0, 16 * DT * 2>(vat[2 * g][0] + far, vat[2 * g][1] + far, vat[2 * g + 1][0] + far, vat[2 * g + 1][1] + far, vt);
+            if (g) read_v(bc, g, vt);
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -966,65 +976,74 @@ __global__ void __launch_bounds__(64 * TILE_WAVES, DT == 256 ? 1 : 2) tree_tile_
 }
 
 // ---------------------------------------------------------------------------------------------- chunks of a request joined
-// A workgroup per (row, query head) of a request.  D / 4 lanes (rounded up to a power of two, `width`) hold a row's numbers,
-// the 256 / width groups of them take turns at the chunks.
-__global__ void __launch_bounds__(256) tree_join_kernel(Work w, int width)
+// D / 4 lanes (rounded up to a power of two, `width`) hold the numbers of a (row, query head) of a request; `share` such groups
+// (a power of two) take turns at its chunks, eight at a time, and meet in local memory.
+__global__ void __launch_bounds__(256) tree_join_kernel(Work w, int width, int share)
 {
     __shared__ float4 sums[256];
-    __shared__ float weight[MAX_CHUNKS];
-    const int lane = threadIdx.x & 63;
-    const int head = (int)(blockIdx.x % w.a.n_q), i = (int)(blockIdx.x / w.a.n_q);
+    __shared__ float2 stats[256];
+    const int per = 256 / (width * share), lane = threadIdx.x & (width - 1);
+    const int sub = threadIdx.x / width & (share - 1), which = threadIdx.x / (width * share);
+    const int64_t unit = (int64_t)blockIdx.x * per + which;
+    const int i = (int)(unit / w.a.n_q), head = (int)(unit - (int64_t)i * w.a.n_q), d = 4 * lane;
     const Span sp = make_span(w, blockIdx.y);
-    if (i >= sp.T || i >= w.a.max_rows || sp.n_chunks < 2) return;
-    const int64_t row = sp.first + i;
-    const int64_t at = row * w.a.n_q + head, step = w.a.M * w.a.n_q;
-    // every wave for itself: the chunks' maxima and sums
-    float top = -INFINITY;
-    float2 mine[MAX_CHUNKS / 64];
-#pragma unroll
-    for (int e = 0; e < MAX_CHUNKS / 64; ++e) {
-        mine[e] = make_float2(-INFINITY, 0.0f);
-        if (e * 64 + lane < sp.n_chunks) mine[e] = w.part_ml[(int64_t)(e * 64 + lane) * step + at];
-        top = fmaxf(top, mine[e].x);
-    }
-    top = wave_max_f32(top);
-    float all = 0.0f;
-#pragma unroll
-    for (int e = 0; e < MAX_CHUNKS / 64; ++e) {
-        const float f = mine[e].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine[e].x - top);
-        all = fmaf(mine[e].y, f, all);
-        if (threadIdx.x < 64) weight[e * 64 + lane] = f;
-    }
-#pragma unroll
-    for (int off = 32; off; off >>= 1) all += __shfl_xor(all, off);
-    __syncthreads();
-    const int d = 4 * (threadIdx.x & (width - 1)), groups = 256 / width;
+    if (sp.n_chunks < 2 || (int)((int64_t)blockIdx.x * per / w.a.n_q) >= sp.T) return;       // (the same for the whole workgroup)
+    const bool live = i < sp.T && i < w.a.max_rows;
+    const int64_t at = (sp.first + (live ? i : 0)) * w.a.n_q + head, step = w.a.M * w.a.n_q;
+    float top = -INFINITY, all = 0.0f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (d < w.a.D) {
-        const float* src = w.part_o + at * w.a.D + d;
-#pragma unroll 4
-        for (int c = threadIdx.x / width; c < sp.n_chunks; c += groups) {
-            const float g = weight[c];                       // (0: the chunk saw nothing, its sums are zeros)
-            const float4 v = *reinterpret_cast<const float4*>(src + (int64_t)c * step * w.a.D);
-            acc.x = fmaf(v.x, g, acc.x);
-            acc.y = fmaf(v.y, g, acc.y);
-            acc.z = fmaf(v.z, g, acc.z);
-            acc.w = fmaf(v.w, g, acc.w);
+    if (live)
+        for (int c0 = sub; c0 < sp.n_chunks; c0 += 8 * share) {
+            float2 ml[8];
+            float4 v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int c = c0 + e * share;
+                ml[e] = make_float2(-INFINITY, 0.0f);
+                v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (c < sp.n_chunks) {
+                    ml[e] = w.part_ml[c * step + at];
+                    if (d < w.a.D) v[e] = *reinterpret_cast<const float4*>(w.part_o + (c * step + at) * w.a.D + d);
+                }
+            }
+            float up = top;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) up = fmaxf(up, ml[e].x);
+            const float keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - up);
+            all *= keep;
+            acc = make_float4(acc.x * keep, acc.y * keep, acc.z * keep, acc.w * keep);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float f = ml[e].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[e].x - up);
+                all = fmaf(ml[e].y, f, all);
+                acc = make_float4(fmaf(v[e].x, f, acc.x), fmaf(v[e].y, f, acc.y), fmaf(v[e].z, f, acc.z), fmaf(v[e].w, f, acc.w));
+            }
+            top = up;
         }
+    if (share > 1) {
+        sums[threadIdx.x] = acc;
+        stats[threadIdx.x] = make_float2(top, all);
+        __syncthreads();
+        if (sub) return;
+        float up = top;
+        for (int g = 1; g < share; ++g) up = fmaxf(up, stats[threadIdx.x + g * width].x);
+        float sum = 0.0f;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int g = 0; g < share; ++g) {
+            const float2 ml = stats[threadIdx.x + g * width];
+            const float4 v = sums[threadIdx.x + g * width];
+            const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - up);
+            sum = fmaf(ml.y, f, sum);
+            acc = make_float4(fmaf(v.x, f, acc.x), fmaf(v.y, f, acc.y), fmaf(v.z, f, acc.z), fmaf(v.w, f, acc.w));
+        }
+        top = up;
+        all = sum;
     }
-    sums[threadIdx.x] = acc;
-    __syncthreads();
-    if (threadIdx.x >= width) return;
-    for (int g = 1; g < groups; ++g) {
-        const float4 v = sums[g * width + threadIdx.x];
-        acc.x += v.x;
-        acc.y += v.y;
-        acc.z += v.z;
-        acc.w += v.w;
-    }
+    if (!live) return;
     const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+    const int64_t row = sp.first + i;
     store4(w, true, 0, row, head, d, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
-    if (threadIdx.x == 0) store_stats(w, true, 0, row, head, top, all);
+    if (lane == 0) store_stats(w, true, 0, row, head, top, all);
 }
 
 template <typename Kern>
@@ -1044,11 +1063,12 @@ int launch_few(const Work& w, bool p16, hipStream_t stream)
     return launch(p16 ? tree_few_kernel<DT, RT, true> : tree_few_kernel<DT, RT, false>, w, blocks, FEW_WAVES, std::max(merge, tiles), stream);
 }
 
-template <int DT>
+template <int DT, int W>
 int launch_tile(const Work& w, bool p16, hipStream_t stream)
 {
     const int64_t blocks = (int64_t)w.chunks * w.n_kv * w.tiles;
-    return launch(p16 ? tree_tile_kernel<DT, true> : tree_tile_kernel<DT, false>, w, blocks, TILE_WAVES, tile_lds<DT>(), stream);
+    return p16 ? launch(tree_tile_kernel<DT, W, true>, w, blocks, W, tile_lds<DT, W, true>(), stream)
+               : launch(tree_tile_kernel<DT, W, false>, w, blocks, W, tile_lds<DT, W, false>(), stream);
 }
 
 }  // namespace
@@ -1090,12 +1110,17 @@ int launch_tree_attention(const TreeArgs& a, hipStream_t stream)
         else if (p.dt == 128) rc = p.rt == 1 ? launch_few<128, 1>(w, p16, stream) : launch_few<128, 2>(w, p16, stream);
         else rc = launch_few<256, 1>(w, p16, stream);
     } else {
-        rc = p.dt == 64 ? launch_tile<64>(w, p16, stream) : p.dt == 128 ? launch_tile<128>(w, p16, stream) : launch_tile<256>(w, p16, stream);
+        if (p.dt == 64) rc = p.waves == 2 ? launch_tile<64, 2>(w, p16, stream) : launch_tile<64, 4>(w, p16, stream);
+        else if (p.dt == 128) rc = p.waves == 2 ? launch_tile<128, 2>(w, p16, stream) : launch_tile<128, 4>(w, p16, stream);
+        else rc = p.waves == 2 ? launch_tile<256, 2>(w, p16, stream) : launch_tile<256, 4>(w, p16, stream);
     }
     if (rc || p.chunks < 2) return rc;
     int width = 1;
     while (4 * width < a.D) width *= 2;
-    hipLaunchKernelGGL(tree_join_kernel, dim3((unsigned)(a.max_rows * a.n_q), (unsigned)a.n_requests), dim3(256), 0, stream, w, width);
+    int share = 1;
+    while (8 * share < p.chunks && 2 * share * width <= 256) share *= 2;
+    const int64_t units = 256 / (width * share), blocks = (a.max_rows * a.n_q + units - 1) / units;
+    hipLaunchKernelGGL(tree_join_kernel, dim3((unsigned)blocks, (unsigned)a.n_requests), dim3(256), 0, stream, w, width, share);
     return check_launch("w2_tree_attention");
 }
 
