@@ -368,7 +368,7 @@ W2_API int w2_lora_workspace_size(const w2_lora_t* lora, int64_t M, int64_t K, i
  *          W2_ACT_SILU_MUL
  * act      w2_act_t
  * workspace  dev, 16-byte aligned, w2_lora_workspace_size bytes, contents undefined before and after
- * K % 256 == 0, N % 8 == 0, as for the projections. */
+ * K % 256 == 0, N % 8 == 0, as for the projections; ldb and ldy below 2^25. */
 W2_API int w2_lora_add(const w2_lora_t* lora, int64_t K, int64_t N, const void* X, w2_dtype_t x_dtype, int64_t ldx,
                        int64_t M, const int32_t* adapter, const uint16_t* base, int64_t ldb, uint16_t* Y, int64_t ldy,
                        int act, void* workspace, size_t workspace_bytes, void* stream);
