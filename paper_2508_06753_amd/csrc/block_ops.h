@@ -8,14 +8,12 @@
 
 namespace w2 {
 
-__device__ __forceinline__ float bf16_f32(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
-
-// round to nearest even; a NaN stays one
-__device__ __forceinline__ uint16_t f32_bf16(float f)
+// two floats to bf16, round to nearest even
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
-    uint32_t u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40);
-    return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){lo, hi}, v2bf));
 }
 
 // n / d for 0 <= n < 2^31 by a multiply and a shift.  With s = ceil(log2 d) and m = ceil(2^(31+s) / d), the error

@@ -41,13 +41,6 @@ __device__ __forceinline__ v4f mfma(const v4i& a, const v4i& b, const v4f& c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
 }
 
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
-{
-    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-    typedef float v2f __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){lo, hi}, v2bf));
-}
-
 // eight floats as two bf16 parts whose sum has 16 bits of them
 __device__ __forceinline__ void split_bf16(const float (&f)[8], v4i& hi, v4i& lo)
 {

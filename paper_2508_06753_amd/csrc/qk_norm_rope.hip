@@ -11,43 +11,69 @@
 // instruction takes turns.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "block_ops.h"
 
 namespace w2 {
+
+namespace {
 
 template <int VEC> struct VecOf;
 template <> struct VecOf<8> { typedef uint4 type; };
 template <> struct VecOf<2> { typedef uint32_t type; };
 
 template <int VEC>
-__device__ __forceinline__ void load_vec(const uint16_t* p, uint16_t (&v)[VEC])
+struct Packed {                          // VEC bf16 numbers
+    uint32_t w[VEC / 2];
+    __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
+};
+
+template <int VEC>
+__device__ __forceinline__ Packed<VEC> load_vec(const uint16_t* p)
 {
-    typedef typename VecOf<VEC>::type V;
-    const V w = *reinterpret_cast<const V*>(p);
-    memcpy(v, &w, sizeof w);
+    const typename VecOf<VEC>::type v = *reinterpret_cast<const typename VecOf<VEC>::type*>(p);
+    Packed<VEC> r;
+    memcpy(&r, &v, sizeof r);
+    return r;
 }
 
 template <int VEC>
-__device__ __forceinline__ void store_vec(uint16_t* p, const uint16_t (&v)[VEC])
+__device__ __forceinline__ void store_vec(uint16_t* p, const Packed<VEC>& x)
 {
-    typedef typename VecOf<VEC>::type V;
-    V w;
-    memcpy(&w, v, sizeof w);
-    *reinterpret_cast<V*>(p) = w;
+    typename VecOf<VEC>::type v;
+    memcpy(&v, &x, sizeof v);
+    *reinterpret_cast<typename VecOf<VEC>::type*>(p) = v;
 }
 
-// One wave: `heads` heads of row m from head h0 on, in steps of 64 / GL.
-template <int VEC, int GL>
-__global__ void __launch_bounds__(256) qk_norm_rope_kernel(RopeArgs a, int chunks, int chunk_heads)
+// Sum over groups of GL lanes: moves within a row of 16 lanes ride on the addition
+template <int GL>
+__device__ __forceinline__ float group_sum(float v)
 {
-    const int lane = threadIdx.x & 63, j = lane & (GL - 1), sub = lane / GL;
-    const int64_t unit = (int64_t)blockIdx.x * (blockDim.x >> 6) + (threadIdx.x >> 6);
-    const int64_t m = unit / chunks;
-    if (m >= a.M) return;
-    const int H = a.n_q + 2 * a.n_kv;
-    const int h0 = (int)(unit % chunks) * chunk_heads, h1 = min(H, h0 + chunk_heads);
+    if (GL > 1) v += dpp_move_f32<0xB1>(v);                  // quad_perm [1,0,3,2]
+    if (GL > 2) v += dpp_move_f32<0x4E>(v);                  // quad_perm [2,3,0,1]
+    if (GL > 4) v += dpp_move_f32<0x141>(v);                 // row_half_mirror
+    if (GL > 8) v += dpp_move_f32<0x140>(v);                 // row_mirror
+    if (GL > 16) v += __shfl_xor(v, 16);
+    if (GL > 32) v += __shfl_xor(v, 32);
+    return v;
+}
 
-    // where the two runs of this lane lie in a head, and whether its pairs are turned
+constexpr int AHEAD = 4;                 // steps of 64 / GL heads whose loads are under way together
+
+// One wave: `per` steps of 64 / GL heads of one row.
+template <int VEC, int GL>
+__global__ void __launch_bounds__(256) qk_norm_rope_kernel(RopeArgs a, int per, Divider by_chunks, int chunks, float inv_d)
+{
+    constexpr int HEADS = 64 / GL;
+    const int lane = threadIdx.x & 63, j = lane & (GL - 1), sub = lane / GL;
+    const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t m = divide(unit, by_chunks);
+    if (m >= (uint64_t)a.M) return;
+    const int H = a.n_q + 2 * a.n_kv;
+    const int h0 = (int)(unit - m * chunks) * per * HEADS, h1 = min(H, h0 + per * HEADS);
+
+    // where the two runs of this lane lie in a head
     const int pairs = a.rd / 2;
     int at0, at1;
     if (a.interleaved) {
@@ -61,6 +87,24 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(RopeArgs a, int chunk
         at1 = at0 + VEC;
     }
     const bool has0 = at0 < a.D, has1 = at1 < a.D;
+    const uint16_t* const x = a.x + (int64_t)m * a.ldx;
+
+    Packed<VEC> u0[AHEAD], u1[AHEAD];
+    auto load = [&](int hb) {
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) {
+            const int h = hb + s * HEADS + sub;
+            u0[s] = u1[s] = Packed<VEC>{};
+            if (h < h1 && has0) u0[s] = load_vec<VEC>(x + h * a.D + at0);
+            if (h < h1 && has1) u1[s] = load_vec<VEC>(x + h * a.D + at1);
+        }
+    };
+    load(h0);
+    Packed<VEC> qw0 = {}, qw1 = {}, kw0 = {}, kw1 = {};
+    if (a.qw && has0) qw0 = load_vec<VEC>(a.qw + at0);
+    if (a.qw && has1) qw1 = load_vec<VEC>(a.qw + at1);
+    if (a.kw && has0) kw0 = load_vec<VEC>(a.kw + at0);
+    if (a.kw && has1) kw1 = load_vec<VEC>(a.kw + at1);
 
     float c[VEC], s[VEC];
     const uint32_t pos = a.rd ? (uint32_t)a.positions[m] : 0;
@@ -76,107 +120,98 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(RopeArgs a, int chunk
             s[i] = __builtin_amdgcn_sinf(t) * a.mscale;
         }
     }
-    int64_t slot = a.slots ? a.slots[m] : m;
+    const int64_t slot = a.slots ? a.slots[m] : (int64_t)m;
     const bool kept = slot >= 0 && slot < a.cache.n_pages * a.cache.page_size;
     const uint32_t page = kept ? divide((uint32_t)slot, a.page) : 0;
-    const int64_t place = kept ? slot - (int64_t)page * a.cache.page_size : 0;
+    const uint32_t place = kept ? (uint32_t)slot - page * (uint32_t)a.cache.page_size : 0;
+    uint16_t* const q = a.q + (int64_t)m * a.ldq;
+    uint16_t* const k = a.cache.k + page * a.cache.k_page_stride + place * a.cache.k_slot_stride;
+    uint16_t* const v = a.cache.v + page * a.cache.v_page_stride + place * a.cache.v_slot_stride;
 
-    for (int hb = h0; hb < h1; hb += 64 / GL) {
-        const int h = hb + sub;
-        const bool live = h < h1;
-        const uint16_t* src = a.x + m * a.ldx + (int64_t)min(h, H - 1) * a.D;
-        uint16_t u0[VEC] = {}, u1[VEC] = {};
-        if (live && has0) load_vec<VEC>(src + at0, u0);
-        if (live && has1) load_vec<VEC>(src + at1, u1);
-        const bool is_q = h < a.n_q, is_v = h >= a.n_q + a.n_kv;
-        const uint16_t* w = is_q ? a.qw : a.kw;
-        float v0[VEC], v1[VEC], sq = 0.0f;
+    for (int hb = h0; hb < h1; hb += AHEAD * HEADS) {
+        if (hb != h0) load(hb);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            v0[i] = bf16_f32(u0[i]);
-            v1[i] = bf16_f32(u1[i]);
-            sq = fmaf(v0[i], v0[i], fmaf(v1[i], v1[i], sq));
-        }
+        for (int st = 0; st < AHEAD; ++st) {
+            const int h = hb + st * HEADS + sub;
+            if (hb + st * HEADS >= h1) break;
+            const bool is_q = h < a.n_q, is_v = h >= a.n_q + a.n_kv;
+            float v0[VEC], v1[VEC], sq = 0.0f;
 #pragma unroll
-        for (int off = GL / 2; off; off >>= 1) sq += __shfl_xor(sq, off);
-        if (!is_v) {
-            if (w) {
-                const float r = rsqrtf(sq / (float)a.D + a.eps);
-                uint16_t w0[VEC] = {}, w1[VEC] = {};
-                if (has0) load_vec<VEC>(w + at0, w0);
-                if (has1) load_vec<VEC>(w + at1, w1);
+            for (int i = 0; i < VEC; ++i) {
+                v0[i] = u0[st].at(i);
+                v1[i] = u1[st].at(i);
+                sq = fmaf(v0[i], v0[i], fmaf(v1[i], v1[i], sq));
+            }
+            sq = group_sum<GL>(sq);
+            if (is_q ? a.qw != nullptr : a.kw != nullptr) {
+                const float r = rsqrtf(sq * inv_d + a.eps);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    v0[i] *= r * bf16_f32(w0[i]);
-                    v1[i] *= r * bf16_f32(w1[i]);
+                    v0[i] *= r * (is_q ? qw0.at(i) : kw0.at(i));
+                    v1[i] *= r * (is_q ? qw1.at(i) : kw1.at(i));
                 }
             }
+            float y[2 * VEC];                                // the two runs, one after the other
             if (a.interleaved) {
-                float v[2 * VEC];
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    v[i] = v0[i];
-                    v[VEC + i] = v1[i];
-                }
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const float x = v[2 * i], y = v[2 * i + 1];
-                    v[2 * i] = x * c[i] - y * s[i];
-                    v[2 * i + 1] = y * c[i] + x * s[i];
-                }
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    u0[i] = f32_bf16(v[i]);
-                    u1[i] = f32_bf16(v[VEC + i]);
+                    const float e = 2 * i < VEC ? v0[(2 * i) % VEC] : v1[(2 * i) % VEC], o = 2 * i < VEC ? v0[(2 * i + 1) % VEC] : v1[(2 * i + 1) % VEC];
+                    y[2 * i] = e * c[i] - o * s[i];
+                    y[2 * i + 1] = o * c[i] + e * s[i];
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    u0[i] = f32_bf16(v0[i] * c[i] - v1[i] * s[i]);
-                    u1[i] = f32_bf16(v1[i] * c[i] + v0[i] * s[i]);
+                    y[i] = v0[i] * c[i] - v1[i] * s[i];
+                    y[VEC + i] = v1[i] * c[i] + v0[i] * s[i];
                 }
             }
-        }
-        uint16_t* dst;
-        if (is_q) dst = a.q + m * a.ldq + (int64_t)h * a.D;
-        else if (!is_v) dst = a.cache.k + page * a.cache.k_page_stride + place * a.cache.k_slot_stride + (h - a.n_q) * a.cache.k_head_stride;
-        else dst = a.cache.v + page * a.cache.v_page_stride + place * a.cache.v_slot_stride + (h - a.n_q - a.n_kv) * a.cache.v_head_stride;
-        if (live && (is_q || kept)) {
-            if (has0) store_vec<VEC>(dst + at0, u0);
-            if (has1) store_vec<VEC>(dst + at1, u1);
+            Packed<VEC> y0 = u0[st], y1 = u1[st];            // (values stay)
+            if (!is_v)
+#pragma unroll
+                for (int i = 0; i < VEC / 2; ++i) {
+                    y0.w[i] = pack_bf16(y[2 * i], y[2 * i + 1]);
+                    y1.w[i] = pack_bf16(y[VEC + 2 * i], y[VEC + 2 * i + 1]);
+                }
+            uint16_t* const dst = is_q ? q + h * a.D : is_v ? v + (h - a.n_q - a.n_kv) * a.cache.v_head_stride : k + (h - a.n_q) * a.cache.k_head_stride;
+            if (h < h1 && (is_q || kept)) {
+                if (has0) store_vec<VEC>(dst + at0, y0);
+                if (has1) store_vec<VEC>(dst + at1, y1);
+            }
         }
     }
 }
 
-template <int VEC>
-static void launch_rope(const RopeArgs& a, int gl, hipStream_t stream)
+template <int VEC, int GL>
+void launch_rope(const RopeArgs& a, hipStream_t stream)
 {
-    const int H = a.n_q + 2 * a.n_kv, at_once = 64 / gl;
-    const int steps = (H + at_once - 1) / at_once;
-    const int64_t units = a.M * steps;
-    const int64_t blocks = (units + 3) / 4;
-#define W2_ROPE(GL) hipLaunchKernelGGL((qk_norm_rope_kernel<VEC, GL>), dim3((unsigned)blocks), dim3(256), 0, stream, a, steps, at_once)
-    switch (gl) {
-    case 1: W2_ROPE(1); break;
-    case 2: W2_ROPE(2); break;
-    case 4: W2_ROPE(4); break;
-    case 8: W2_ROPE(8); break;
-    case 16: W2_ROPE(16); break;
-    case 32: W2_ROPE(32); break;
-    default: W2_ROPE(64); break;
-    }
-#undef W2_ROPE
+    const int steps = (a.n_q + 2 * a.n_kv + 64 / GL - 1) / (64 / GL);
+    // a wave takes as much of a row as leaves 32 waves on every CU: its angles are made once, its loads overlap
+    const int per = (int)std::max<int64_t>(1, std::min<int64_t>(steps, (a.M * steps + 8191) / 8192));
+    const int chunks = (steps + per - 1) / per;
+    const int64_t blocks = (a.M * chunks + 3) / 4;
+    hipLaunchKernelGGL((qk_norm_rope_kernel<VEC, GL>), dim3((unsigned)blocks), dim3(256), 0, stream, a, per, make_divider((uint32_t)chunks), chunks,
+                       1.0f / (float)a.D);
 }
+
+template <int VEC>
+void launch_rope(const RopeArgs& a, hipStream_t stream)
+{
+    const int lanes = (a.D + 2 * VEC - 1) / (2 * VEC);
+    if (lanes <= 4) launch_rope<VEC, 4>(a, stream);
+    else if (lanes <= 8) launch_rope<VEC, 8>(a, stream);
+    else if (lanes <= 16) launch_rope<VEC, 16>(a, stream);
+    else if (lanes <= 32) launch_rope<VEC, 32>(a, stream);
+    else launch_rope<VEC, 64>(a, stream);
+}
+
+}  // namespace
 
 int launch_qk_norm_rope(const RopeArgs& a, hipStream_t stream)
 {
     // runs of 8 numbers need the second half of the rotated part, and what follows it, to start at a multiple of 8
-    const int vec = a.interleaved || a.rd % 16 == 0 ? 8 : 2;
-    const int lanes = (a.D + 2 * vec - 1) / (2 * vec);
-    int gl = 1;
-    while (gl < lanes) gl *= 2;
-    if (vec == 8) launch_rope<8>(a, gl, stream);
-    else launch_rope<2>(a, gl, stream);
+    if (a.interleaved || a.rd % 16 == 0) launch_rope<8>(a, stream);
+    else launch_rope<2>(a, stream);
     return check_launch("w2_qk_norm_rope");
 }
 

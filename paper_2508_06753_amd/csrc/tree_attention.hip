@@ -72,14 +72,6 @@ __device__ __forceinline__ void wait_reads()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// two floats to bf16, round to nearest even
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
-{
-    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-    typedef float v2f __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){lo, hi}, v2bf));
-}
-
 // 16-byte pieces of a row of DT numbers are stored XORed by this: 16 rows at one piece (scores) lie in 16 different places of
 // the 256 bytes that local memory delivers at once, and 8 rows at a pair of pieces (values) in 8 different pairs
 template <int DT>
