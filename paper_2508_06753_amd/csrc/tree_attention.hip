@@ -143,7 +143,7 @@ __device__ __forceinline__ float max_over_q(float x)
 struct Plan {
     int few;                             // tree_few_kernel, else tree_tile_kernel
     int rt;                              // few: 16-row tiles a wave
-    int waves;                           // many: waves of 32 rows a workgroup
+    int waves;                           // a workgroup
     int dt;                              // head_dim padded to 64, 128 or 256
     int tiles;                           // row tiles of a request
     int chunk;                           // keys of a workgroup, a multiple of 32 * waves
@@ -157,7 +157,7 @@ Plan make_plan(int64_t n_requests, int64_t max_rows, int G, int n_kv, int D, int
     p.dt = D <= 64 ? 64 : D <= 128 ? 128 : 256;
     p.few = rows <= (p.dt < 256 ? 32 : 16);
     p.rt = p.few && rows <= 16 ? 1 : 2;
-    p.waves = rows <= 64 ? 2 : 4;
+    p.waves = !p.few && rows <= 64 ? 2 : 4;
     const int rows_per_wg = p.few ? 16 * p.rt : 32 * p.waves;
     p.tiles = (int)((rows + rows_per_wg - 1) / rows_per_wg);
     if (total_len <= 0 || total_len > n_requests * max_len) total_len = n_requests * max_len;
@@ -168,6 +168,12 @@ Plan make_plan(int64_t n_requests, int64_t max_rows, int G, int n_kv, int D, int
     chunk = std::max(chunk, (max_len + MAX_CHUNKS - 1) / MAX_CHUNKS);
     if (max_rows * G * n_kv >= (int64_t)1 << 24) chunk = std::max(chunk, max_len);     // (more than a grid of the join counts)
     chunk = (std::max(chunk, least) + 127) / 128 * 128;
+    // a few short requests: eight waves share a request's keys and no second launch joins chunks (us, one request of 8 heads, 700
+    // keys: 9.6 against 6.1 + 3.3 and a launch, 1000 keys: 12.2 against 6.2 + 3.4; 16 requests of 1000: 13.6 against 14.3 + 3.6)
+    if (p.few && p.rt == 1 && p.dt < 256 && n_requests * n_kv <= 256 && max_len <= (n_requests * n_kv >= 64 ? 1024 : 768)) {
+        p.waves = 8;
+        chunk = 1024;
+    }
     p.chunk = (int)std::min<int64_t>(chunk, (int64_t)1 << 31 >> 1);
     p.chunks = (int)std::max<int64_t>(1, (max_len + p.chunk - 1) / p.chunk);
     return p;
@@ -406,10 +412,8 @@ __device__ __forceinline__ void store_stats(const Work& w, bool whole, int chunk
 }
 
 // ---------------------------------------------------------------------------------------------- few rows
-constexpr int FEW_WAVES = 4;
-
-template <int DT, int RT, bool P16>
-__global__ void __launch_bounds__(64 * FEW_WAVES, DT == 256 ? 1 : 2) tree_few_kernel(Work w)
+template <int DT, int RT, int W, bool P16>
+__global__ void __launch_bounds__(64 * W, DT == 256 ? 1 : 2) tree_few_kernel(Work w)
 {
     constexpr int KS = DT / 32;
     constexpr int TILE = 32 * DT * 2;                        // a wave's 32 keys of K, and of V again
@@ -479,7 +483,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DT == 256 ? 1 : 2) tree_few_ke
         }
     };
 
-    constexpr uint32_t STEP = 32 * FEW_WAVES;
+    constexpr uint32_t STEP = 32 * W;
     uint32_t base = k0 + 32 * wave;
     Pages pages = {};
     if (base < k1) {
@@ -569,8 +573,8 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DT == 256 ? 1 : 2) tree_few_ke
     // the waves' parts meet in local memory, one row tile at a time
     constexpr int LD = DT + 4;
     float* const os = reinterpret_cast<float*>(smem);                         // [wave][16][LD]
-    float* const ms = os + FEW_WAVES * 16 * LD;                               // [wave][16], then l
-    float* const ls = ms + FEW_WAVES * 16;
+    float* const ms = os + W * 16 * LD;                               // [wave][16], then l
+    float* const ls = ms + W * 16;
     const bool whole = sp.n_chunks == 1;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -586,16 +590,16 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DT == 256 ? 1 : 2) tree_few_ke
         for (int d = 0; d < DT / 16; ++d)
             *reinterpret_cast<v4f*>(os + (wave * 16 + l16) * LD + 16 * d + 4 * q) = o[rt][d];
         __syncthreads();
-        for (int e = threadIdx.x; e < 16 * DT / 4; e += 64 * FEW_WAVES) {
+        for (int e = threadIdx.x; e < 16 * DT / 4; e += 64 * W) {
             const int n = e / (DT / 4), d = e % (DT / 4) * 4;
             const int rho = 16 * rt + n;
             if (rho >= sp.rows) continue;
             float top = -INFINITY, all = 0.0f;
 #pragma unroll
-            for (int v = 0; v < FEW_WAVES; ++v) top = fmaxf(top, ms[v * 16 + n]);
+            for (int v = 0; v < W; ++v) top = fmaxf(top, ms[v * 16 + n]);
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int v = 0; v < FEW_WAVES; ++v) {
+            for (int v = 0; v < W; ++v) {
                 const float mv = ms[v * 16 + n], f = mv == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mv - top);
                 const float4 ov = *reinterpret_cast<const float4*>(os + (v * 16 + n) * LD + d);
                 if (mv != -INFINITY) {
@@ -1047,12 +1051,12 @@ int launch(Kern kern, const Work& w, int64_t blocks, int waves, int lds, hipStre
     return check_launch("w2_tree_attention");
 }
 
-template <int DT, int RT>
+template <int DT, int RT, int W>
 int launch_few(const Work& w, bool p16, hipStream_t stream)
 {
-    constexpr int merge = FEW_WAVES * 16 * (DT + 4) * 4 + 2 * FEW_WAVES * 16 * 4, tiles = FEW_WAVES * 2 * 32 * DT * 2;
+    constexpr int merge = W * 16 * (DT + 4) * 4 + 2 * W * 16 * 4, tiles = W * 2 * 32 * DT * 2;
     const int64_t blocks = (int64_t)w.chunks * w.n_kv;
-    return launch(p16 ? tree_few_kernel<DT, RT, true> : tree_few_kernel<DT, RT, false>, w, blocks, FEW_WAVES, std::max(merge, tiles), stream);
+    return launch(p16 ? tree_few_kernel<DT, RT, W, true> : tree_few_kernel<DT, RT, W, false>, w, blocks, W, std::max(merge, tiles), stream);
 }
 
 template <int DT, int W>
@@ -1098,9 +1102,10 @@ int launch_tree_attention(const TreeArgs& a, hipStream_t stream)
     const bool p16 = a.cache.page_size % 16 == 0 && std::max(a.cache.k_slot_stride, a.cache.v_slot_stride) < (int64_t)1 << 25;
     int rc;
     if (p.few) {
-        if (p.dt == 64) rc = p.rt == 1 ? launch_few<64, 1>(w, p16, stream) : launch_few<64, 2>(w, p16, stream);
-        else if (p.dt == 128) rc = p.rt == 1 ? launch_few<128, 1>(w, p16, stream) : launch_few<128, 2>(w, p16, stream);
-        else rc = launch_few<256, 1>(w, p16, stream);
+        if (p.dt == 256) rc = launch_few<256, 1, 4>(w, p16, stream);
+        else if (p.rt == 2) rc = p.dt == 64 ? launch_few<64, 2, 4>(w, p16, stream) : launch_few<128, 2, 4>(w, p16, stream);
+        else if (p.waves == 8) rc = p.dt == 64 ? launch_few<64, 1, 8>(w, p16, stream) : launch_few<128, 1, 8>(w, p16, stream);
+        else rc = p.dt == 64 ? launch_few<64, 1, 4>(w, p16, stream) : launch_few<128, 1, 4>(w, p16, stream);
     } else {
         if (p.dt == 64) rc = p.waves == 2 ? launch_tile<64, 2>(w, p16, stream) : launch_tile<64, 4>(w, p16, stream);
         else if (p.dt == 128) rc = p.waves == 2 ? launch_tile<128, 2>(w, p16, stream) : launch_tile<128, 4>(w, p16, stream);
