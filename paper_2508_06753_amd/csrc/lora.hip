@@ -13,6 +13,7 @@
 #include <type_traits>
 
 #include "block_ops.h"
+#include "w2_small_common.h"
 
 namespace w2 {
 
@@ -23,22 +24,16 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
 constexpr int WINDOW = 64;
-#ifndef LW
-#define LW 512
-#endif
-#ifndef JJ
-#define JJ 2
-#endif
-#ifndef ST
-#define ST 2048
-#endif
-#ifndef OC
-#define OC 1
-#endif
 
 __device__ __forceinline__ v4f mfma(const v4i& a, const v4i& b, const v4f& c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
+
+// 16 bytes a lane from wherever the lane says to local memory, lane after lane from dst on
+__device__ __forceinline__ void load_lds16(const void* src, char* dst)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
 // eight floats as two bf16 parts whose sum has 16 bits of them
@@ -56,6 +51,14 @@ __device__ __forceinline__ int part_of(const LoraArgs& a, int block)
 {
     if (a.gated) return block & 1;
     return (block >= a.end16[0]) + (block >= a.end16[1]) + (block >= a.end16[2]);
+}
+
+__device__ __forceinline__ void split_bf16(const v4i& x0, const v4i& x1, v4i& hi, v4i& lo)
+{
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __int_as_float(e < 4 ? x0[e & 3] : x1[e & 3]);
+    split_bf16(f, hi, lo);
 }
 
 // One adapter's rows of a window.
@@ -116,131 +119,171 @@ __device__ __forceinline__ int rank_of(const LoraArgs& a, int which)
     return a.rank ? min(max(a.rank[which], 0), a.R) : a.R;
 }
 
-// ---------------------------------------------------------------------------------------------- T = X A^T
-// A workgroup: one adapter's rows of a window, J * 16 rows of A, one of the ks ranges of K, cut again over its four waves.
-// NR: row tiles of 16 that are multiplied together.
-template <bool F32, int J, int NR>
-__device__ __forceinline__ void shrink(const LoraArgs& a, const Tile& t, int64_t m0, int j0, int row0, int kb, int ke, uint32_t turn, v4f* part, float* T)
-{
-    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int PR = a.n_parts * a.R;
-    const uint16_t* ap[J];
-#pragma unroll
-    for (int j = 0; j < J; ++j) ap[j] = a.A + t.adapter * a.a_stride + (int64_t)min(j0 + 16 * j + l16, PR - 1) * a.K + 8 * q;
-    const char* xp[NR];
-    bool live[NR];
-    int64_t row[NR];
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        live[n] = row0 + 16 * n + l16 < t.count;
-        row[n] = m0 + __shfl(t.row, (row0 + 16 * n + l16) & 63);
-        xp[n] = (const char*)a.X + (row[n] * a.ldx + 8 * q) * (F32 ? 4 : 2);
-    }
-    v4f acc[J][NR];
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int n = 0; n < NR; ++n) acc[j][n] = (v4f){0.f, 0.f, 0.f, 0.f};
-    // U steps of 32: all loads first, then the products
-    auto span = [&](int k, auto uc) {
-        constexpr int U = decltype(uc)::value;
-        v4i av[J][U], xv[NR][U * (F32 ? 2 : 1)];
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-            for (int u = 0; u < U; ++u) av[j][u] = *reinterpret_cast<const v4i*>(ap[j] + k + 32 * u);
-#pragma unroll
-        for (int n = 0; n < NR; ++n) {
-#pragma unroll
-            for (int u = 0; u < U * (F32 ? 2 : 1); ++u) xv[n][u] = (v4i){0, 0, 0, 0};
-            if (live[n])                                     // (rows that are not there cost no memory traffic)
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if constexpr (F32) {
-                        xv[n][2 * u] = *reinterpret_cast<const v4i*>(xp[n] + (int64_t)(k + 32 * u) * 4);
-                        xv[n][2 * u + 1] = *reinterpret_cast<const v4i*>(xp[n] + (int64_t)(k + 32 * u) * 4 + 16);
-                    } else {
-                        xv[n][u] = *reinterpret_cast<const v4i*>(xp[n] + (int64_t)(k + 32 * u) * 2);
-                    }
-                }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                if constexpr (F32) {
-                    float f[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e] = __int_as_float(xv[n][2 * u + e / 4][e % 4]);
-                    v4i hi, lo;
-                    split_bf16(f, hi, lo);
-#pragma unroll
-                    for (int j = 0; j < J; ++j) acc[j][n] = mfma(av[j][u], lo, mfma(av[j][u], hi, acc[j][n]));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < J; ++j) acc[j][n] = mfma(av[j][u], xv[n][u], acc[j][n]);
-                }
-            }
-    };
-    // Rows of X and A often lie a multiple of 4 KiB apart, so that what an instruction asks for is one channel of the cache's.
-    // Each wave starts somewhere else in its range, or the whole machine would go from channel to channel together.
-    constexpr int U = J * NR >= 8 ? 2 : 4;
-    const int spans = (ke - kb) / (32 * U);
-    int at = spans ? (int)(turn % (uint32_t)spans) : 0;
-    for (int i = 0; i < spans; ++i) {
-        span(kb + 32 * U * at, std::integral_constant<int, U>{});
-        at = at + 1 < spans ? at + 1 : 0;
-    }
-    for (int k = kb + 32 * U * spans; k < ke; k += 32) span(k, std::integral_constant<int, 1>{});
-    // the four waves' sums, in order; lane: row l16 of tile n, T's columns j0 + 16 j + 4 q ..+ 3
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int n = 0; n < NR; ++n) part[((j * NR + n) * 4 + wave) * 64 + lane] = acc[j][n];
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int n = 0; n < NR; ++n) {
-            if (((j * NR + n) & 3) != wave) continue;
-            const v4f* p = part + (j * NR + n) * 4 * 64 + lane;
-            const v4f s = p[0] + p[64] + p[128] + p[192];
-            const int col = j0 + 16 * j + 4 * q;
-            if (live[n] && col < PR) *reinterpret_cast<v4f*>(T + row[n] * PR + col) = s;
-        }
-}
-
-template <bool F32, int J>
+// ---------------------------------------------------------------------------------------------- T = X A^T, few rows
+// A workgroup: one adapter's rows of a window, 16 rows of A, one of the ks ranges of K, cut again over its four waves.
+template <bool F32>
 __global__ void __launch_bounds__(256) lora_shrink_kernel(LoraArgs a, int slots, int groups, int ks)
 {
-    extern __shared__ __align__(16) char smem[];
+    __shared__ v4f part[4 * 64];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // (slot, group of A's rows, range of K) of a window side by side
     uint32_t id = blockIdx.x;
     const int kr = id % ks;
     id /= ks;
-    const int g = id % groups;
+    const int j0 = id % groups * 16;
     id /= groups;
     const int slot = id % slots;
     const int64_t m0 = (int64_t)(id / slots) * WINDOW;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t steps = a.K / 32;
     const int kb = (int)(steps * (kr * 4 + wave) / (ks * 4)) * 32, ke = (int)(steps * (kr * 4 + wave + 1) / (ks * 4)) * 32;
-    float* const T = a.T + (int64_t)kr * a.M * a.n_parts * a.R;
-    const uint32_t turn = (uint32_t)(m0 / WINDOW) * 3 + (uint32_t)(g * 5 + slot * 7 + wave);
-    const int j0 = g * J * 16;
+    const int PR = a.n_parts * a.R;
+    float* const T = a.T + (int64_t)kr * a.M * PR;
     for_tiles(a, m0, slot, slots, false, [&](const Tile& t) {
         // (nothing to do where every one of these rows of A is past the adapter's rank)
         const int rank = rank_of(a, t.adapter);
+        if (j0 % a.R >= rank && (j0 + 8 >= PR || (j0 + 8) % a.R >= rank)) return;
+        const uint16_t* const ap = a.A + t.adapter * a.a_stride + (int64_t)min(j0 + l16, PR - 1) * a.K + 8 * q;
+        for (int row0 = 0; row0 < t.count; row0 += 16) {
+            const bool live = row0 + l16 < t.count;
+            const int64_t row = m0 + __shfl(t.row, (row0 + l16) & 63);
+            const char* const xp = (const char*)a.X + (row * a.ldx + 8 * q) * (F32 ? 4 : 2);
+            v4f acc = {0.f, 0.f, 0.f, 0.f};
+            // U steps of 32: all loads first, then the products
+            auto span = [&](int k, auto uc) {
+                constexpr int U = decltype(uc)::value;
+                v4i av[U], xv[U * (F32 ? 2 : 1)];
+#pragma unroll
+                for (int u = 0; u < U; ++u) av[u] = *reinterpret_cast<const v4i*>(ap + k + 32 * u);
+#pragma unroll
+                for (int u = 0; u < U * (F32 ? 2 : 1); ++u) xv[u] = (v4i){0, 0, 0, 0};
+                if (live)                                    // (rows that are not there cost no memory traffic)
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if constexpr (F32) {
+                            xv[2 * u] = *reinterpret_cast<const v4i*>(xp + (int64_t)(k + 32 * u) * 4);
+                            xv[2 * u + 1] = *reinterpret_cast<const v4i*>(xp + (int64_t)(k + 32 * u) * 4 + 16);
+                        } else {
+                            xv[u] = *reinterpret_cast<const v4i*>(xp + (int64_t)(k + 32 * u) * 2);
+                        }
+                    }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if constexpr (F32) {
+                        v4i hi, lo;
+                        split_bf16(xv[2 * u], xv[2 * u + 1], hi, lo);
+                        acc = mfma(av[u], lo, mfma(av[u], hi, acc));
+                    } else {
+                        acc = mfma(av[u], xv[u], acc);
+                    }
+                }
+            };
+            int k = kb;
+            for (; k + 128 <= ke; k += 128) span(k, std::integral_constant<int, 4>{});
+            for (; k < ke; k += 32) span(k, std::integral_constant<int, 1>{});
+            // the four waves' sums, in order; lane: row l16 of the row tile, T's columns j0 + 4 q ..+ 3
+            __syncthreads();
+            part[wave * 64 + lane] = acc;
+            __syncthreads();
+            if (wave == 0 && live && j0 + 4 * q < PR)
+                *reinterpret_cast<v4f*>(T + row * PR + j0 + 4 * q) = part[lane] + part[64 + lane] + part[128 + lane] + part[192 + lane];
+        }
+    });
+}
+
+// ---------------------------------------------------------------------------------------------- T = X A^T, many rows
+// A workgroup: one adapter's rows of a window (up to 64), 32 rows of A, one of the ks ranges of K, in stages of 64 k through a
+// ring in local memory.  A wave multiplies 16 rows.  Whole 128-byte pieces of rows an instruction: rows of X and A often lie
+// a multiple of 8 KiB apart, in one set of the vector cache, and operands that are loaded from there directly, half a line
+// of 16 rows each, evict one another (4000 rows, K = 4096, 128 ranks: 90 us in one range of K).
+constexpr int STAGES = 3;
+template <bool F32> constexpr int shrink_stage() { return 64 * (F32 ? 256 : 128) + 32 * 128; }
+
+template <bool F32>
+__global__ void __launch_bounds__(256) lora_shrink_tile_kernel(LoraArgs a, int slots, int groups, int ks)
+{
+    constexpr int XB = F32 ? 256 : 128, XL = F32 ? 4 : 2;    // bytes of a row's stage; loads of X a wave and stage (A: 1)
+    constexpr int STAGE = shrink_stage<F32>(), A_AT = 64 * XB;
+    extern __shared__ __align__(16) char smem[];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t id = blockIdx.x;
+    const int kr = id % ks;
+    id /= ks;
+    const int j0 = id % groups * 32;
+    id /= groups;
+    // (the windows' first adapters one after the other: as a rule there are no others, and every die has its share of work)
+    const uint32_t windows = (uint32_t)((a.M + WINDOW - 1) / WINDOW);
+    const int slot = id / windows;
+    const int64_t m0 = (int64_t)(id % windows) * WINDOW;
+    const int kb = (int)(a.K / 64 * kr / ks), n_st = (int)(a.K / 64 * (kr + 1) / ks) - kb;
+    const int PR = a.n_parts * a.R;
+    float* const T = a.T + (int64_t)kr * a.M * PR;
+    // 16-byte pieces are stored XORed: 16 rows at one piece lie in 16 different places of the 256 bytes delivered at once
+    auto swz = [](int row) { return F32 ? row & 15 : (row >> 1) & 7; };
+    auto swz_a = [](int row) { return (row >> 1) & 7; };
+
+    for_tiles(a, m0, slot, slots, false, [&](const Tile& t) {
+        const int rank = rank_of(a, t.adapter);
         bool any = false;
-        for (int j = j0; j < min(j0 + J * 16, a.n_parts * a.R); j += 8) any |= j % a.R < rank;
+        for (int j = j0; j < min(j0 + 32, PR); j += 8) any |= j % a.R < rank;
         if (!any) return;
-        // few rows an adapter: one row tile at a time, in few registers; else up to four together
-        if constexpr (J == 1)
-            for (int row0 = 0; row0 < t.count; row0 += 16) shrink<F32, J, 1>(a, t, m0, j0, row0, kb, ke, turn, (v4f*)smem, T);
-        else if (t.count <= 16) shrink<F32, J, 1>(a, t, m0, j0, 0, kb, ke, turn, (v4f*)smem, T);
-        else shrink<F32, J, 4>(a, t, m0, j0, 0, kb, ke, turn, (v4f*)smem, T);
+        const char* xsrc[XL];
+#pragma unroll
+        for (int j = 0; j < XL; ++j) {
+            const int at = (wave * XL + j) * 64 + lane, row = at / (XB / 16), piece = at % (XB / 16) ^ swz(row);
+            const int64_t from = m0 + __shfl(t.row, row < t.count ? row : 0);        // (rows that are not there: the first one again)
+            xsrc[j] = (const char*)a.X + from * a.ldx * (F32 ? 4 : 2) + (int64_t)kb * XB + piece * 16;
+        }
+        const int arow = wave * 8 + lane / 8;
+        const char* const asrc = (const char*)(a.A + t.adapter * a.a_stride + (int64_t)min(j0 + arow, PR - 1) * a.K) + (int64_t)kb * 128 +
+                                 (lane % 8 ^ swz_a(arow)) * 16;
+        auto fetch = [&](int st) {
+            char* const dst = smem + st % STAGES * STAGE;
+#pragma unroll
+            for (int j = 0; j < XL; ++j) load_lds16(xsrc[j] + (int64_t)st * XB, dst + (wave * XL + j) * 1024);
+            load_lds16(asrc + (int64_t)st * 128, dst + A_AT + wave * 1024);
+        };
+        __syncthreads();                                     // (the tile before is done with local memory)
+#pragma unroll
+        for (int st = 0; st < STAGES - 1; ++st)
+            if (st < n_st) fetch(st);
+        v4f acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        const int xrow = wave * 16 + l16;
+        for (int st = 0; st < n_st; ++st) {
+            // this stage is there; up to STAGES - 2 behind it are under way (at the end: none)
+            if (st + STAGES - 2 < n_st) wait_loads<(STAGES - 2) * (XL + 1)>();
+            else wait_loads<0>();
+            bare_barrier();                                  // every wave's part of it, and no wave reads the stage before any more
+            if (st + STAGES - 1 < n_st) fetch(st + STAGES - 1);
+            const char* const xb = smem + st % STAGES * STAGE + xrow * XB;
+            const char* const ab = smem + st % STAGES * STAGE + A_AT;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int p = 4 * s + q;
+                v4i av[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) av[j] = *reinterpret_cast<const v4i*>(ab + (16 * j + l16) * 128 + ((p ^ swz_a(16 * j + l16)) << 4));
+                if constexpr (F32) {
+                    const v4i x0 = *reinterpret_cast<const v4i*>(xb + ((2 * p ^ swz(xrow)) << 4));
+                    const v4i x1 = *reinterpret_cast<const v4i*>(xb + (((2 * p + 1) ^ swz(xrow)) << 4));
+                    v4i hi, lo;
+                    split_bf16(x0, x1, hi, lo);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[j] = mfma(av[j], lo, mfma(av[j], hi, acc[j]));
+                } else {
+                    const v4i xv = *reinterpret_cast<const v4i*>(xb + ((p ^ swz(xrow)) << 4));
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[j] = mfma(av[j], xv, acc[j]);
+                }
+            }
+        }
+        if (xrow < t.count) {
+            const int64_t row = m0 + __shfl(t.row, xrow);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (j0 + 16 * j + 4 * q < PR) *reinterpret_cast<v4f*>(T + row * PR + j0 + 16 * j + 4 * q) = acc[j];
+        }
     });
 }
 
@@ -251,7 +294,7 @@ __device__ __forceinline__ float silu(float z) { return z * __builtin_amdgcn_rcp
 // columns in an order that leaves 16 (with the gated activation: 8 gate and the 8 up) columns of one row in a lane.
 // S: steps of 32 ranks.
 template <int S, bool PAIRED>
-__global__ void __launch_bounds__(256, OC) lora_expand_kernel(LoraArgs a, int slots, int groups, int steps, int ks, int row_tiles)
+__global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraArgs a, int slots, int groups, int steps, int ks, int row_tiles)
 {
     extern __shared__ __align__(16) char smem[];             // T: [part][row tile][step][hi, lo][64 lanes] 16 bytes
     v4i* const ts = reinterpret_cast<v4i*>(smem);
@@ -300,58 +343,85 @@ __global__ void __launch_bounds__(256, OC) lora_expand_kernel(LoraArgs a, int sl
         }
         const char* const base = (const char*)(a.base + m0 * a.ldb);
         char* const Y = (char*)(a.Y + m0 * a.ldy);
-        v4i b0, b1;
-        auto load_base = [&](int64_t n0, uint32_t off, int n) {
-            b0 = b1 = (v4i){0, 0, 0, 0};
-            if (16 * n + l16 < t.count && a.base) {
-                const char* src = base + n0 * 2 + off;
-                if (n0 + c0 < a.N) b0 = *reinterpret_cast<const v4i*>(src);
-                if (n0 + c1 < a.N) b1 = *reinterpret_cast<const v4i*>(src + (c1 - c0) * 2);
+        v4i b0[4], b1[4];
+        auto load_base = [&](int64_t n0) {
+            const char* const src = base + n0 * 2;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                b0[n] = b1[n] = (v4i){0, 0, 0, 0};
+                if (16 * n + l16 < t.count && a.base) {
+                    if (n0 + c0 < a.N) b0[n] = *reinterpret_cast<const v4i*>(src + from[n]);
+                    if (n0 + c1 < a.N) b1[n] = *reinterpret_cast<const v4i*>(src + from[n] + (c1 - c0) * 2);
+                }
             }
         };
         // everything that the first columns need is asked for at once
         load_b(n_first);
-        load_base(n_first, from[0], 0);
+        load_base(n_first);
         const int rank = rank_of(a, t.adapter);
         const float scale = t.adapter < 0 || !a.scale ? 1.0f : a.scale[t.adapter];
         if (rank == 0 && a.act == ACT_NONE && a.base == a.Y) return;         // rows that stay where they are
         __syncthreads();                                     // (the tile before is done with local memory)
-        for (int e = threadIdx.x; e < a.n_parts * tiles * S * 64; e += blockDim.x) {
-            const int s = e / 64 % S, n = e / 64 / S % tiles, p = e / 64 / S / tiles;
+        // T of the tile's rows, scaled, as operands.  Items of 64 lanes: (part, row tile, step of ranks).
+        const int items = a.n_parts * tiles * S;
+        auto place = [&](int e, int& p, int& n, int& s) { s = e % S; n = e / S % tiles; p = e / S / tiles; };
+        auto source = [&](int e) {                           // nullptr: zeros
+            int p, n, s;
+            place(e, p, n, s);
             const int pos = 16 * n + l16, r = 32 * s + 8 * q;
-            const int64_t row = m0 + __shfl(t.row, pos);
-            float f[8];
+            const int64_t row = m0 + __shfl(t.row, pos & 63);
+            return e < items && pos < t.count && r < rank ? a.T + row * PR + p * a.R + r : nullptr;
+        };
+        auto put = [&](int e, float (&f)[8]) {
+            int p, n, s;
+            place(e, p, n, s);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = 0.0f;
-            if (pos < t.count && r < rank) {
-                const float* src = a.T + row * PR + p * a.R + r;
-                int c = 0;
-                for (; c + 4 <= ks; c += 4) {
-                    float4 x[4], y[4];
-#pragma unroll
-                    for (int g = 0; g < 4; ++g, src += a.M * PR) {
-                        x[g] = *reinterpret_cast<const float4*>(src);
-                        y[g] = *reinterpret_cast<const float4*>(src + 4);
-                    }
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        f[0] += x[g].x; f[1] += x[g].y; f[2] += x[g].z; f[3] += x[g].w;
-                        f[4] += y[g].x; f[5] += y[g].y; f[6] += y[g].z; f[7] += y[g].w;
-                    }
-                }
-                for (; c < ks; ++c, src += a.M * PR) {
-                    const float4 x = *reinterpret_cast<const float4*>(src), y = *reinterpret_cast<const float4*>(src + 4);
-                    f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
-                    f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = r + i < rank ? f[i] * scale : 0.0f;
+            for (int i = 0; i < 8; ++i) f[i] = 32 * s + 8 * q + i < rank ? f[i] * scale : 0.0f;
             v4i hi, lo;
             split_bf16(f, hi, lo);
             v4i* dst = ts + ((p * row_tiles + n) * S + s) * 128 + lane;
             dst[0] = hi;
             dst[64] = lo;
+        };
+        if (ks == 1) {                                       // four items' loads together
+            for (int e0 = wave; e0 < items; e0 += 4 * waves) {
+                float f[4][8];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float* src = source(e0 + g * waves);
+                    const v4f x = src ? *reinterpret_cast<const v4f*>(src) : (v4f){0.f, 0.f, 0.f, 0.f};
+                    const v4f y = src ? *reinterpret_cast<const v4f*>(src + 4) : (v4f){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[g][i] = i < 4 ? x[i & 3] : y[i & 3];
+                }
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    if (e0 + g * waves < items) put(e0 + g * waves, f[g]);
+            }
+        } else {                                             // eight parts' loads together
+            for (int e = wave; e < items; e += waves) {
+                const float* src = source(e);
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = 0.0f;
+                if (src)
+                    for (int c = 0; c < ks; c += 8, src += 8 * a.M * PR) {
+                        v4f x[8], y[8];
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) {
+                            x[g] = y[g] = (v4f){0.f, 0.f, 0.f, 0.f};
+                            if (c + g < ks) {
+                                x[g] = *reinterpret_cast<const v4f*>(src + g * a.M * PR);
+                                y[g] = *reinterpret_cast<const v4f*>(src + g * a.M * PR + 4);
+                            }
+                        }
+#pragma unroll
+                        for (int g = 0; g < 8; ++g)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) f[i] += i < 4 ? x[g][i & 3] : y[g][i & 3];
+                    }
+                put(e, f);
+            }
         }
         __syncthreads();
         for (int step = 0; step < steps; ++step) {
@@ -359,7 +429,7 @@ __global__ void __launch_bounds__(256, OC) lora_expand_kernel(LoraArgs a, int sl
             if (n0 >= a.N) break;
             if (step) {
                 load_b(n0);
-                load_base(n0, from[0], 0);
+                load_base(n0);
             }
             // the parts of the wave's columns: as a rule the same for every column of a matrix tile
             int part[2], first[2];
@@ -387,11 +457,10 @@ __global__ void __launch_bounds__(256, OC) lora_expand_kernel(LoraArgs a, int sl
                 v4f acc[4];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const uint32_t x = (uint32_t)b0[e / 2], y = (uint32_t)b1[e / 2];
+                    const uint32_t x = (uint32_t)b0[n][e / 2], y = (uint32_t)b1[n][e / 2];
                     acc[e / 4][e % 4] = __uint_as_float(e & 1 ? x & 0xffff0000u : x << 16);
                     acc[2 + e / 4][e % 4] = __uint_as_float(e & 1 ? y & 0xffff0000u : y << 16);
                 }
-                if (n + 1 < 4 && n + 1 < tiles) load_base(n0, from[(n + 1) & 3], n + 1);
                 if (rank > 0 && plain) {
                     v4i tv[2][S][2];
 #pragma unroll
@@ -453,15 +522,16 @@ __global__ void __launch_bounds__(256, OC) lora_expand_kernel(LoraArgs a, int sl
 
 struct Plan {
     int64_t windows;
-    int J, groups, ks, slots;            // shrink: 16-row tiles of A a workgroup, how many such, ranges of K; workgroups that share a window's adapters
+    int many, groups, ks, slots;         // shrink: the kernel for many rows; groups of A's rows, ranges of K; workgroups that share a window's adapters
     int steps, columns, eslots;          // expand: steps of 256 columns a workgroup, how many such; as above
 };
 
-// Slots: as many as a window has rows while that is a small grid (no search, see for_tiles), else enough to fill the machine.
+// Slots: a window's workgroups for its adapters.  Few windows: one for each row where adapters are about as many (no search, see
+// for_tiles), else one for each adapter; many: as fill the machine.
 int slots_for(int64_t M, int64_t windows, int64_t others, int64_t adapters)
 {
     const int64_t rows = std::min<int64_t>(M, WINDOW);
-    if (windows <= 4) return (int)rows;
+    if (windows <= 4) return (int)(2 * adapters >= rows ? rows : adapters);
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rows - 1, adapters), 1024 / (windows * others)));
 }
 
@@ -469,28 +539,30 @@ Plan make_plan(int n_parts, int R, int n_adapters, int64_t M, int64_t K, int64_t
 {
     Plan p;
     p.windows = (M + WINDOW - 1) / WINDOW;
-    const int tiles = (n_parts * R + 15) / 16;
-    p.J = p.windows > 4 ? JJ : 1;
-    p.groups = (tiles + p.J - 1) / p.J;
-    // K cut until there are eight workgroups on every CU, which wait for memory; one where there are many rows: every part of T
-    // is written and read again.  A wave's share is 64 numbers or more.
-    const int64_t busy = std::min<int64_t>(M, p.windows - 1 + n_adapters) * p.groups, want = p.windows > 4 ? LW : 2048;
-    p.ks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want / std::max<int64_t>(busy, 1), 16), K / 256));
+    p.many = p.windows > 4;
+    p.groups = (n_parts * R + (p.many ? 31 : 15)) / (p.many ? 32 : 16);
+    // K cut until there are eight workgroups on every CU, which wait for memory; one where there are many rows.  Every part of T
+    // is written, and read again by every group of columns: four where an adapter has several row tiles.  A wave's share is 64
+    // numbers or more.
+    const int64_t busy = std::min<int64_t>(M, p.windows - 1 + n_adapters) * p.groups, want = p.many ? 256 : 2048;
+    const int64_t most = M > 16 * (int64_t)n_adapters ? 4 : 16;
+    p.ks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want / std::max<int64_t>(busy, 1), most), K / 256));
     p.slots = slots_for(M, p.windows, p.groups * p.ks, n_adapters);
     const int64_t blocks = (N + 255) / 256;
-    p.steps = (int)std::max<int64_t>(1, std::min<int64_t>(blocks, blocks * p.windows / ST));
+    p.steps = (int)std::max<int64_t>(1, std::min<int64_t>(blocks, blocks * p.windows / 2048));
     p.columns = (int)((blocks + p.steps - 1) / p.steps);
     p.eslots = slots_for(M, p.windows, p.columns, (int64_t)n_adapters + 1);
     return p;
 }
 
-template <bool F32, int J>
+template <bool F32>
 int launch_shrink(const LoraArgs& a, const Plan& p, hipStream_t stream)
 {
-    const int row_tiles = J == 1 || a.M <= 16 ? 1 : 4, lds = J * row_tiles * 4096;
-    if (int rc = ensure_dynamic_lds((const void*)lora_shrink_kernel<F32, J>, lds, "w2_lora_add")) return rc;
+    const int lds = p.many ? STAGES * shrink_stage<F32>() : 0;
+    if (int rc = ensure_dynamic_lds((const void*)lora_shrink_tile_kernel<F32>, lds, "w2_lora_add")) return rc;
     const int64_t blocks = p.windows * p.slots * p.groups * p.ks;
-    hipLaunchKernelGGL((lora_shrink_kernel<F32, J>), dim3((unsigned)blocks), dim3(256), lds, stream, a, p.slots, p.groups, p.ks);
+    hipLaunchKernelGGL(p.many ? lora_shrink_tile_kernel<F32> : lora_shrink_kernel<F32>, dim3((unsigned)blocks), dim3(256), lds, stream, a, p.slots,
+                       p.groups, p.ks);
     return check_launch("w2_lora_add");
 }
 
@@ -515,10 +587,7 @@ size_t lora_workspace_bytes(int n_parts, int R, int n_adapters, int64_t M, int64
 int launch_lora(const LoraArgs& a, hipStream_t stream)
 {
     const Plan p = make_plan(a.n_parts, a.R, a.n_adapters, a.M, a.K, a.N);
-    int rc;
-    if (a.x_f32) rc = p.J == 1 ? launch_shrink<true, 1>(a, p, stream) : launch_shrink<true, JJ>(a, p, stream);
-    else rc = p.J == 1 ? launch_shrink<false, 1>(a, p, stream) : launch_shrink<false, JJ>(a, p, stream);
-    if (rc) return rc;
+    if (const int rc = a.x_f32 ? launch_shrink<true>(a, p, stream) : launch_shrink<false>(a, p, stream)) return rc;
     const int S = (a.R + 31) / 32;
     if (a.act == ACT_SILU_MUL)
         return S == 1 ? launch_expand<1, true>(a, p, stream) : S == 2 ? launch_expand<2, true>(a, p, stream) : launch_expand<4, true>(a, p, stream);
