@@ -539,13 +539,14 @@ Plan make_plan(int n_parts, int R, int n_adapters, int64_t M, int64_t K, int64_t
 {
     Plan p;
     p.windows = (M + WINDOW - 1) / WINDOW;
-    p.many = p.windows > 4;
+    p.many = p.windows > 4 || (M > 32 && M > 32 * (int64_t)n_adapters);
     p.groups = (n_parts * R + (p.many ? 31 : 15)) / (p.many ? 32 : 16);
     // K cut until there are eight workgroups on every CU, which wait for memory; one where there are many rows.  Every part of T
-    // is written, and read again by every group of columns: four where an adapter has several row tiles.  A wave's share is 64
+    // is written, and read again by every group of columns: eight (which are read
+    // together) where an adapter has several row tiles.  A wave's share is 64
     // numbers or more.
     const int64_t busy = std::min<int64_t>(M, p.windows - 1 + n_adapters) * p.groups, want = p.many ? 256 : 2048;
-    const int64_t most = M > 16 * (int64_t)n_adapters ? 4 : 16;
+    const int64_t most = M > 16 * (int64_t)n_adapters ? 8 : 16;
     p.ks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want / std::max<int64_t>(busy, 1), most), K / 256));
     p.slots = slots_for(M, p.windows, p.groups * p.ks, n_adapters);
     const int64_t blocks = (N + 255) / 256;
