@@ -405,6 +405,25 @@ def test_tree_long(w2):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,D", [(4, 1, 128), (8, 2, 64), (8, 4, 256), (5, 1, 128), (16, 2, 128), (12, 2, 96)])
+def test_tree_many_rows_over_long_contexts(w2, hq, hkv, D):
+    # two and four waves, chunks with a middle that nothing is checked in, and the same with pages that are not there
+    for t in (12, 40):
+        for absent in (False, True):
+            tree_case(w2, [(1500, t), (333, 3)], hq, hkv, D, page=32, absent=absent, seed=t + D)
+            tree_case(w2, [(1100, t)], hq, hkv, D, page=16, absent=absent, masked=False, split=False, seed=t + D + 1)
+        tree_case(w2, [(900, t)], hq, hkv, D, page=40, seed=t + D + 2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [640, 700, 768, 769, 1000, 1024, 1025])
+def test_tree_short_requests_in_one_launch(w2, n):
+    tree_case(w2, [(n, 1)], 8, 2, 128, masked=False, seed=n)
+    tree_case(w2, [(n, 3), (n - 600, 1)], 8, 4, 64, seed=n + 1)
+    tree_case(w2, [(n - i, 1) for i in range(16)], 8, 8, 64, masked=False, seed=n + 2)
+
+
+@pytest.mark.gpu
 def test_tree_one_token_is_row_of_a_chunk(w2):
     # the last row of a causal chunk is the single token of the same request
     out, lse = tree_case(w2, [(500, 50)], 8, 2, 128, masked=False, seed=3)
@@ -599,3 +618,88 @@ def test_refusals_of_the_binding_on_device_tensors(w2):
                  lambda: w2.tree_attention(q, cache, table, start, one, 3, 16, lse=q[:, :, 0])]:
         with pytest.raises(ValueError):
             call()
+
+
+# ------------------------------------------------------------------ the operators together
+def block_and_cache(w2, adapters=True):
+    from paper_2508_06753_amd import attention_block as ab, synth
+    hidden, n_q, n_kv, D, G = 512, 4, 2, 64, 64
+    width = (n_q + 2 * n_kv) * D
+
+    def packed(K, N, seed):
+        codes, scales = synth.make_weights(K, N, G, 0, seed=seed)
+        return w2.prepack(torch.from_numpy(codes).cuda(), torch.from_numpy(scales.view(np.int16)).cuda(), G)
+
+    qkv = w2.Lora(normal(11, 2, 3 * 8, hidden, std=0.04), normal(12, 2, width, 8), parts=[n_q * D, n_kv * D, n_kv * D])
+    o = w2.Lora(normal(13, 2, 8, n_q * D, std=0.06), normal(14, 2, hidden, 8))
+    w = [(1 + normal(15 + i, D, dtype=torch.float32, std=0.2)).bfloat16() for i in (0, 1)]
+    block = ab.AttentionBlock(packed(hidden, width, 1), packed(n_q * D, hidden, 2), hidden, n_q, n_kv, D, G, w2.Rope(D), *w,
+                              qkv_lora=qkv if adapters else None, o_lora=o if adapters else None)
+    k = normal(17, 24, 16, n_kv, D)
+    return ab, block, w2.KVCache(k, torch.zeros_like(k))
+
+
+@pytest.mark.gpu
+def test_block_runs_prompts_trees_and_tokens(w2):
+    """A step of the block against the operators' definitions on the projections that the library computes, and a drafted
+    branch against the same tokens as a plain sequence."""
+    ab, block, cache = block_and_cache(w2)
+    table = torch.arange(20, dtype=torch.int32).flip(0).view(2, 10).contiguous().cuda()
+    adapter, lens = [1, -1], [45, 70]
+    D, n_q, n_kv = block.head_dim, block.n_q, block.n_kv
+    history = [[], []]                                         # float64 keys and values of every committed token
+
+    def check(batch, X, y, commit):
+        M, starts = X.shape[0], batch.row_start.tolist()
+        qkv = w2.matmul_a8_fused(block.wqkv, block.hidden, block.width, block.G, X,
+                                 workspace=torch.empty(1 << 22, dtype=torch.uint8, device="cuda"))
+        ad = batch.adapter.cpu().numpy()
+        part = np.repeat([0, 1, 2], [n_q * D, n_kv * D, n_kv * D])
+        z, _ = want.lora(f64(X), f64(block.qkv_lora.A), f64(block.qkv_lora.B), ad, f64(qkv), part_of_column=part)
+        z = f64(torch.tensor(z).bfloat16()).reshape(M, -1, D)
+        pos, theta = batch.positions.tolist(), want.rope_frequencies(D, 10000.0)
+        q, _ = want.norm_rope(z[:, :n_q], f64(block.q_weight), block.eps, theta, False, 1.0, pos)
+        k, _ = want.norm_rope(z[:, n_q:n_q + n_kv], f64(block.k_weight), block.eps, theta, False, 1.0, pos)
+        out = np.zeros((M, n_q, D))
+        for r in range(2):
+            rows = slice(starts[r], starts[r + 1])
+            kk = np.stack([t[0] for t in history[r]] + list(k[rows]))
+            vv = np.stack([t[1] for t in history[r]] + list(z[rows, n_q + n_kv:]))
+            mask = None if batch.mask is None else batch.mask.cpu().numpy().view(np.uint64)[rows]
+            out[rows] = want.attention(q[rows], kk, vv, starts[r + 1] - starts[r], mask, D ** -0.5)[0]
+            if commit:
+                history[r] += [(k[i], z[i, n_q + n_kv:]) for i in range(starts[r], starts[r + 1])]
+        o = torch.tensor(out.reshape(M, -1)).bfloat16().cuda()
+        base = w2.matmul_a8_fused(block.wo, n_q * D, block.hidden, block.G, o,
+                                  workspace=torch.empty(1 << 22, dtype=torch.uint8, device="cuda"))
+        ref, _ = want.lora(f64(o), f64(block.o_lora.A), f64(block.o_lora.B), ad, f64(base))
+        # a bf16 number rounded the other way somewhere moves the int8 codes of its row: compare the rows' norms of the difference
+        off = np.linalg.norm(f64(y) - ref, axis=1) / np.linalg.norm(ref, axis=1)
+        assert off.max() < 0.02, off
+
+    def run(batch, seed, commit):
+        X = normal(seed, batch.positions.shape[0], block.hidden, dtype=torch.float32)
+        y = block.step(X, cache, batch)
+        check(batch, X, y, commit)
+        return X, y
+
+    run(ab.causal_batch([0, 0], lens, table, 16, "cuda", adapter), 21, True)
+    X, tree = run(ab.tree_batch(lens, [[-1, 0, 0, 1, 2], [-1, 0, 1]], table, 16, "cuda", adapter), 22, False)
+    # the branch 0, 2, 4 of request 0, alone, as a plain continuation (request 1: all of its tree is one branch)
+    pick = [0, 2, 4, 5, 6, 7]
+    batch = ab.causal_batch(lens, [3, 3], table, 16, "cuda", adapter)
+    line = block.step(X[pick].contiguous(), cache, batch)
+    off = (line.float() - tree[pick].float()).norm(dim=1) / tree[pick].float().norm(dim=1)
+    assert off.max().item() < 0.02, off
+
+
+@pytest.mark.gpu
+def test_block_without_adapters_and_main(w2, capsys):
+    ab, block, cache = block_and_cache(w2, adapters=False)
+    table = torch.arange(20, dtype=torch.int32).view(2, 10).contiguous().cuda()
+    batch = ab.causal_batch([0, 0], [5, 1], table, 16, "cuda")
+    y = block.step(normal(1, 6, block.hidden), cache, batch)
+    assert y.shape == (6, block.hidden) and torch.isfinite(y).all()
+    ab.main()
+    said = capsys.readouterr().out
+    assert said.count("finite True") == 3
