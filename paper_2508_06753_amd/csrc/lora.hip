@@ -293,8 +293,10 @@ __device__ __forceinline__ float silu(float z) { return z * __builtin_amdgcn_rcp
 // A workgroup: one adapter's rows of a window, `steps` times 64 columns a wave.  A wave's four matrix tiles take its 64
 // columns in an order that leaves 16 (with the gated activation: 8 gate and the 8 up) columns of one row in a lane.
 // S: steps of 32 ranks.
-template <int S, bool PAIRED>
-__global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraArgs a, int slots, int groups, int steps, int ks, int row_tiles)
+// NT: row tiles whose rows of base are asked for together: all four of a window, or one, in half the registers, where
+// adapters have few rows.
+template <int S, bool PAIRED, int NT>
+__global__ void __launch_bounds__(256, NT == 1 ? (S == 1 ? 4 : S == 2 ? 3 : 2) : S == 1 ? 3 : 2) lora_expand_kernel(LoraArgs a, int slots, int groups, int steps, int ks, int row_tiles)
 {
     extern __shared__ __align__(16) char smem[];             // T: [part][row tile][step][hi, lo][64 lanes] 16 bytes
     v4i* const ts = reinterpret_cast<v4i*>(smem);
@@ -334,30 +336,32 @@ __global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraAr
         // this lane's columns: 16 in a row, or 8 gate columns and the up columns 16 further; where they lie in the rows of row
         // tile n, from the window's first row on (strides are below 2^25: 32 bits)
         const int c0 = PAIRED ? 32 * (q >> 1) + 8 * (q & 1) : 16 * q, c1 = c0 + (PAIRED ? 16 : 8);
-        uint32_t from[4], to[4];
+        auto row_offset = [&](int n, int64_t ld) { return __shfl(t.row, (16 * n + l16) & 63) * (uint32_t)ld * 2; };
+        uint32_t from[NT], to[NT];
+        if constexpr (NT == 4)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const uint32_t row = __shfl(t.row, 16 * n + l16);
-            from[n] = (row * (uint32_t)a.ldb + c0) * 2;
-            to[n] = (row * (uint32_t)a.ldy + (PAIRED ? 8 * q : c0)) * 2;
-        }
+            for (int n = 0; n < NT; ++n) {
+                from[n] = row_offset(n, a.ldb) + 2 * c0;
+                to[n] = row_offset(n, a.ldy) + 2 * (PAIRED ? 8 * q : c0);
+            }
         const char* const base = (const char*)(a.base + m0 * a.ldb);
         char* const Y = (char*)(a.Y + m0 * a.ldy);
-        v4i b0[4], b1[4];
-        auto load_base = [&](int64_t n0) {
+        v4i b0[NT], b1[NT];
+        auto load_base = [&](int64_t n0, int first) {
             const char* const src = base + n0 * 2;
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
+            for (int n = 0; n < NT; ++n) {
+                const uint32_t off = NT == 4 ? from[n] : row_offset(first + n, a.ldb) + 2 * c0;
                 b0[n] = b1[n] = (v4i){0, 0, 0, 0};
-                if (16 * n + l16 < t.count && a.base) {
-                    if (n0 + c0 < a.N) b0[n] = *reinterpret_cast<const v4i*>(src + from[n]);
-                    if (n0 + c1 < a.N) b1[n] = *reinterpret_cast<const v4i*>(src + from[n] + (c1 - c0) * 2);
+                if (16 * (first + n) + l16 < t.count && a.base) {
+                    if (n0 + c0 < a.N) b0[n] = *reinterpret_cast<const v4i*>(src + off);
+                    if (n0 + c1 < a.N) b1[n] = *reinterpret_cast<const v4i*>(src + off + (c1 - c0) * 2);
                 }
             }
         };
         // everything that the first columns need is asked for at once
         load_b(n_first);
-        load_base(n_first);
+        load_base(n_first, 0);
         const int rank = rank_of(a, t.adapter);
         const float scale = t.adapter < 0 || !a.scale ? 1.0f : a.scale[t.adapter];
         if (rank == 0 && a.act == ACT_NONE && a.base == a.Y) return;         // rows that stay where they are
@@ -383,7 +387,7 @@ __global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraAr
             dst[0] = hi;
             dst[64] = lo;
         };
-        if (ks == 1) {                                       // four items' loads together
+        if (NT == 4 && ks == 1) {                            // four items' loads together
             for (int e0 = wave; e0 < items; e0 += 4 * waves) {
                 float f[4][8];
 #pragma unroll
@@ -398,17 +402,18 @@ __global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraAr
                 for (int g = 0; g < 4; ++g)
                     if (e0 + g * waves < items) put(e0 + g * waves, f[g]);
             }
-        } else {                                             // eight parts' loads together
+        } else {                                             // several parts' loads together
+            constexpr int PB = NT == 1 ? 4 : 8;
             for (int e = wave; e < items; e += waves) {
                 const float* src = source(e);
                 float f[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] = 0.0f;
                 if (src)
-                    for (int c = 0; c < ks; c += 8, src += 8 * a.M * PR) {
-                        v4f x[8], y[8];
+                    for (int c = 0; c < ks; c += PB, src += PB * a.M * PR) {
+                        v4f x[PB], y[PB];
 #pragma unroll
-                        for (int g = 0; g < 8; ++g) {
+                        for (int g = 0; g < PB; ++g) {
                             x[g] = y[g] = (v4f){0.f, 0.f, 0.f, 0.f};
                             if (c + g < ks) {
                                 x[g] = *reinterpret_cast<const v4f*>(src + g * a.M * PR);
@@ -416,7 +421,7 @@ __global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraAr
                             }
                         }
 #pragma unroll
-                        for (int g = 0; g < 8; ++g)
+                        for (int g = 0; g < PB; ++g)
 #pragma unroll
                             for (int i = 0; i < 8; ++i) f[i] += i < 4 ? x[g][i & 3] : y[g][i & 3];
                     }
@@ -429,7 +434,7 @@ __global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraAr
             if (n0 >= a.N) break;
             if (step) {
                 load_b(n0);
-                load_base(n0);
+                load_base(n0, 0);
             }
             // the parts of the wave's columns: as a rule the same for every column of a matrix tile
             int part[2], first[2];
@@ -450,14 +455,17 @@ __global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraAr
                             const int left = rank - 32 * s - 8 * q;
                             bv[i][s][e] &= (int)((left > 2 * e ? 0xffffu : 0u) | (left > 2 * e + 1 ? 0xffff0000u : 0u));
                         }
+            for (int group = 0; group < tiles; group += NT)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
+            for (int k = 0; k < NT; ++k) {
+                const int n = group + k;
                 if (n >= tiles) break;
+                if (NT == 1 && n) load_base(n0, n);
                 // the sums start from base
                 v4f acc[4];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const uint32_t x = (uint32_t)b0[n][e / 2], y = (uint32_t)b1[n][e / 2];
+                    const uint32_t x = (uint32_t)b0[k][e / 2], y = (uint32_t)b1[k][e / 2];
                     acc[e / 4][e % 4] = __uint_as_float(e & 1 ? x & 0xffff0000u : x << 16);
                     acc[2 + e / 4][e % 4] = __uint_as_float(e & 1 ? y & 0xffff0000u : y << 16);
                 }
@@ -490,8 +498,8 @@ __global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraAr
                             }
                         }
                 }
-                if (16 * n + l16 >= t.count) continue;
-                char* const dst = Y + (PAIRED ? n0 : 2 * n0) + to[n];
+                char* const dst = Y + (PAIRED ? n0 : 2 * n0) + (NT == 4 ? to[k] : row_offset(n, a.ldy) + 2 * (PAIRED ? 8 * q : c0));
+                const bool live = 16 * n + l16 < t.count;
                 v4i y0, y1;
                 if constexpr (PAIRED) {
 #pragma unroll
@@ -499,7 +507,7 @@ __global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraAr
                         const int i = e >> 1, c = (2 * e) & 3;
                         y0[e] = (int)pack_bf16(silu(acc[i][c]) * acc[2 + i][c], silu(acc[i][c + 1]) * acc[2 + i][c + 1]);
                     }
-                    if (n0 + c0 < a.N) *reinterpret_cast<v4i*>(dst) = y0;
+                    if (live && n0 + c0 < a.N) *reinterpret_cast<v4i*>(dst) = y0;
                 } else {
                     if (a.act == ACT_SILU)
 #pragma unroll
@@ -512,8 +520,8 @@ __global__ void __launch_bounds__(256, S == 1 ? 3 : 2) lora_expand_kernel(LoraAr
                         y0[e] = (int)pack_bf16(acc[i][c], acc[i][c + 1]);
                         y1[e] = (int)pack_bf16(acc[2 + i][c], acc[2 + i][c + 1]);
                     }
-                    if (n0 + c0 < a.N) *reinterpret_cast<v4i*>(dst) = y0;
-                    if (n0 + c1 < a.N) *reinterpret_cast<v4i*>(dst + 16) = y1;
+                    if (live && n0 + c0 < a.N) *reinterpret_cast<v4i*>(dst) = y0;
+                    if (live && n0 + c1 < a.N) *reinterpret_cast<v4i*>(dst + 16) = y1;
                 }
             }
         }
@@ -571,9 +579,10 @@ template <int S, bool PAIRED>
 int launch_expand(const LoraArgs& a, const Plan& p, hipStream_t stream)
 {
     const int row_tiles = (int)std::min<int64_t>(4, (a.M + 15) / 16), lds = a.n_parts * row_tiles * S * 2048;
-    if (int rc = ensure_dynamic_lds((const void*)lora_expand_kernel<S, PAIRED>, lds, "w2_lora_add")) return rc;
+    auto kern = a.M > 16 && p.many ? lora_expand_kernel<S, PAIRED, 4> : lora_expand_kernel<S, PAIRED, 1>;
+    if (int rc = ensure_dynamic_lds((const void*)kern, lds, "w2_lora_add")) return rc;
     const int64_t blocks = p.windows * p.eslots * ((p.columns + 7) / 8 * 8);
-    hipLaunchKernelGGL((lora_expand_kernel<S, PAIRED>), dim3((unsigned)blocks), dim3(256), lds, stream, a, p.eslots, p.columns, p.steps, p.ks, row_tiles);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), lds, stream, a, p.eslots, p.columns, p.steps, p.ks, row_tiles);
     return check_launch("w2_lora_add");
 }
 
