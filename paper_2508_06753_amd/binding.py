@@ -357,6 +357,36 @@ def matmul_a16(packed, K, N, G, X, out=None, variant=VARIANT_AUTO, workspace=Non
 
 # ---- the operators between the projections of an attention block
 
+_BF16, _F32, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
+
+
+def _vector(t, dtype, n, name, what):
+    """A dense one-dimensional device tensor of n elements (checks in the order of their cost: these calls are short)."""
+    if t.dtype is not dtype or t.numel() != n or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous device tensor {what} of {dtype}")
+    return t.data_ptr()
+
+
+def _rows(t, dtype, M, N, name):
+    """A device tensor [M, N] with unit inner stride -> (address, row stride)."""
+    if t.dtype is not dtype or t.shape != (M, N) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor [{M}, {N}] of {dtype}")
+    s = t.stride()
+    if s[1] != 1 and N > 1:
+        raise ValueError(f"{name} must have unit inner stride")
+    return t.data_ptr(), s[0] if M > 1 else N
+
+
+def _heads(t, M, n, D, name):
+    """A bf16 device tensor [M, n, D], dense within a row -> (address, row stride)."""
+    if t.dtype is not _BF16 or t.shape != (M, n, D) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor [{M}, {n}, {D}] of bfloat16")
+    s = t.stride()
+    if s[2] != 1 or (n > 1 and s[1] != D):
+        raise ValueError(f"{name} must be dense within a row")
+    return t.data_ptr(), s[0] if M > 1 else n * D
+
+
 class _LoraStruct(ctypes.Structure):
     _fields_ = [("A", _vp), ("B", _vp), ("rank", _vp), ("scale", _vp), ("a_stride", _i64), ("b_stride", _i64),
                 ("part_end", _i64 * 4), ("n_adapters", _int), ("max_rank", _int), ("n_parts", _int), ("gated", _int)]
@@ -406,34 +436,23 @@ def lora_add(lora, X, adapter, base, act=ACT_NONE, out=None, workspace=None):
     """Y bf16 = act(base + scale * (X A^T) B^T), each row of X (fp32 or bf16 [M,K]) with the adapter that `adapter` (int32
     [M], -1: none) names.  `base`: bf16 [M,N], the projection's result before its activation, or None for zero.
     `workspace`: a uint8 device tensor of lora_workspace_size(lora, M) bytes; allocated here if None."""
-    if X.dtype == torch.float32:
-        dt = DT_F32
-    elif X.dtype == torch.bfloat16:
-        dt = DT_BF16
-    else:
+    xdt = X.dtype
+    if xdt is not _F32 and xdt is not _BF16:
         raise ValueError("X must be float32 or bfloat16")
     M, K, N = X.shape[0], lora.K, lora.N
-    if not X.is_cuda or X.dim() != 2 or X.shape[1] != K or X.stride(1) != 1:
-        raise ValueError("X must be a device tensor [M,K] with unit inner stride")
-    _dev(adapter, torch.int32, "adapter")
-    if adapter.shape != (M,) or not adapter.is_contiguous():
-        raise ValueError("adapter must be contiguous [M]")
     n_out = N // 2 if act == ACT_SILU_MUL else N
-    if base is not None:
-        _dev(base, torch.bfloat16, "base")
-        if base.shape != (M, N) or base.stride(1) != 1:
-            raise ValueError("base must be [M,N] with unit inner stride")
-    Y = out if out is not None else torch.empty((M, n_out), dtype=torch.bfloat16, device=X.device)
-    if out is not None and (_dev(Y, torch.bfloat16, "out").shape != (M, n_out) or Y.stride(1) != 1):
-        raise ValueError("out must be [M, number of output columns] with unit inner stride")
+    xp, ldx = _rows(X, xdt, M, K, "X")
+    ap = _vector(adapter, _I32, M, "adapter", "[M]")
+    bp, ldb = (None, N) if base is None else _rows(base, _BF16, M, N, "base")
+    if out is None:
+        out = torch.empty((M, n_out), dtype=_BF16, device=X.device)
+    yp, ldy = _rows(out, _BF16, M, n_out, "out")
     if workspace is None:
         workspace = torch.empty(lora_workspace_size(lora, M), dtype=torch.uint8, device=X.device)
     wp, wb = _ws(workspace)
-    _check("w2_lora_add", _lib.w2_lora_add(
-        lora._ref, K, N, X.data_ptr(), dt, X.stride(0) if M > 1 else K, M, adapter.data_ptr(), _ptr(base),
-        base.stride(0) if base is not None and M > 1 else N, Y.data_ptr(), Y.stride(0) if M > 1 else n_out, act, wp, wb,
-        _stream()))
-    return Y
+    _check("w2_lora_add", _lib.w2_lora_add(lora._ref, K, N, xp, DT_F32 if xdt is _F32 else DT_BF16, ldx, M, ap, bp, ldb, yp, ldy,
+                                           act, wp, wb, _stream()))
+    return out
 
 
 ROPE_NONE, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS = 0, 1, 2, 3
@@ -495,24 +514,18 @@ def qk_norm_rope(x, n_q, rope, positions, cache, slots=None, q_weight=None, k_we
     """Norm and rotation of the heads of x (bf16 [M, (n_q + 2 * cache.n_heads) * head_dim], a fused QKV projection's rows):
     returns the queries, bf16 [M, n_q, head_dim]; keys and values go to the cache's `slots` (int64 [M], page * page_size +
     place; -1: not written; None: row m to slot m).  rope None: no rotation; a weight None: not normed."""
-    _dev(x, torch.bfloat16, "x")
     D, M = cache.head_dim, x.shape[0]
-    if x.dim() != 2 or x.shape[1] != (n_q + 2 * cache.n_heads) * D or x.stride(1) != 1:
-        raise ValueError("x must be [M, (n_q + 2 n_kv) * head_dim] with unit inner stride")
-    for t, dt, name in ((positions, torch.int32, "positions"), (slots, torch.int64, "slots")):
-        if t is not None and (_dev(t, dt, name).shape != (M,) or not t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous [M]")
-    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if t is not None and (_dev(t, torch.bfloat16, name).shape != (D,) or not t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous [head_dim]")
-    q = out if out is not None else torch.empty((M, n_q, D), dtype=torch.bfloat16, device=x.device)
-    if out is not None and (_dev(q, torch.bfloat16, "out").shape != (M, n_q, D) or q.stride(2) != 1 or q.stride(1) != D):
-        raise ValueError("out must be [M, n_q, head_dim], dense within a row")
-    _check("w2_qk_norm_rope", _lib.w2_qk_norm_rope(
-        x.data_ptr(), x.stride(0) if M > 1 else x.shape[1], M, n_q, _ptr(q_weight), _ptr(k_weight), eps,
-        rope._ref if rope is not None else None, _ptr(positions), q.data_ptr(), q.stride(0) if M > 1 else n_q * D,
-        cache._ref, _ptr(slots), _stream()))
-    return q
+    xp, ldx = _rows(x, _BF16, M, (n_q + 2 * cache.n_heads) * D, "x")
+    pp = None if positions is None else _vector(positions, _I32, M, "positions", "[M]")
+    sp = None if slots is None else _vector(slots, _I64, M, "slots", "[M]")
+    qw = None if q_weight is None else _vector(q_weight, _BF16, D, "q_weight", "[head_dim]")
+    kw = None if k_weight is None else _vector(k_weight, _BF16, D, "k_weight", "[head_dim]")
+    if out is None:
+        out = torch.empty((M, n_q, D), dtype=_BF16, device=x.device)
+    qp, ldq = _heads(out, M, n_q, D, "out")
+    _check("w2_qk_norm_rope", _lib.w2_qk_norm_rope(xp, ldx, M, n_q, qw, kw, eps, None if rope is None else rope._ref, pp, qp, ldq,
+                                                   cache._ref, sp, _stream()))
+    return out
 
 
 def tree_attention_workspace_size(n_requests, M, n_q, cache, max_rows, max_len, total_len=0):
@@ -530,35 +543,35 @@ def tree_attention(q, cache, page_table, row_start, kv_len, max_rows, max_len, m
     j: the row sees its request's drafted token j (None: causal); scale None: 1/sqrt(head_dim).  lse: fp32 [M, n_q], written
     if given.  `workspace`: a uint8 device tensor of tree_attention_workspace_size bytes; None: the keys of a request are
     not shared out over workgroups."""
-    _dev(q, torch.bfloat16, "q")
     M, n_q, D = q.shape
-    if D != cache.head_dim or q.stride(2) != 1 or (n_q > 1 and q.stride(1) != D):
-        raise ValueError("q must be [M, n_q, head_dim], dense within a row")
-    _dev(page_table, torch.int32, "page_table")
-    _dev(row_start, torch.int32, "row_start")
-    _dev(kv_len, torch.int32, "kv_len")
+    if D != cache.head_dim:
+        raise ValueError("q must be [M, n_q, head_dim] of the cache's head_dim")
+    qp, ldq = _heads(q, M, n_q, D, "q")
     R = kv_len.shape[0]
-    if page_table.dim() != 2 or page_table.shape[0] != R or page_table.stride(1) != 1 or row_start.shape != (R + 1,) or \
-            not row_start.is_contiguous() or not kv_len.is_contiguous():
-        raise ValueError("page_table must be [requests, pages], row_start [requests + 1], kv_len [requests]")
-    words = 0
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [requests, pages]")
+    cols = page_table.shape[1]
+    tp, ldt = _rows(page_table, _I32, R, cols, "page_table")
+    rp = _vector(row_start, _I32, R + 1, "row_start", "[requests + 1]")
+    lp = _vector(kv_len, _I32, R, "kv_len", "[requests]")
+    words, mp = 0, None
     if mask is not None:
-        _dev(mask, torch.int64, "mask")
-        if mask.dim() != 2 or mask.shape[0] != M or not mask.is_contiguous():
-            raise ValueError("mask must be contiguous [M, words]")
-        words = mask.shape[1]
-    o = out if out is not None else torch.empty((M, n_q, D), dtype=torch.bfloat16, device=q.device)
-    if out is not None and (_dev(o, torch.bfloat16, "out").shape != q.shape or o.stride(2) != 1 or (n_q > 1 and o.stride(1) != D)):
-        raise ValueError("out must be like q, dense within a row")
-    if lse is not None and (_dev(lse, torch.float32, "lse").shape != (M, n_q) or not lse.is_contiguous()):
-        raise ValueError("lse must be contiguous [M, n_q]")
+        if mask.dtype is not _I64 or mask.dim() != 2 or mask.shape[0] != M or not mask.is_contiguous() or not mask.is_cuda:
+            raise ValueError("mask must be a contiguous device tensor [M, words] of int64")
+        words, mp = mask.shape[1], mask.data_ptr()
+    if out is None:
+        out = torch.empty((M, n_q, D), dtype=_BF16, device=q.device)
+    op, ldo = _heads(out, M, n_q, D, "out")
+    ep = None
+    if lse is not None:
+        if lse.dtype is not _F32 or lse.shape != (M, n_q) or not lse.is_contiguous() or not lse.is_cuda:
+            raise ValueError("lse must be a contiguous device tensor [M, n_q] of float32")
+        ep = lse.data_ptr()
     wp, wb = _ws(workspace)
     _check("w2_tree_attention", _lib.w2_tree_attention(
-        q.data_ptr(), q.stride(0) if M > 1 else n_q * D, M, n_q, cache._ref, page_table.data_ptr(), page_table.shape[1],
-        page_table.stride(0) if R > 1 else page_table.shape[1], row_start.data_ptr(), kv_len.data_ptr(), R, max_rows, max_len,
-        total_len, _ptr(mask), words, D ** -0.5 if scale is None else scale, o.data_ptr(), o.stride(0) if M > 1 else n_q * D,
-        _ptr(lse), wp, wb, _stream()))
-    return o
+        qp, ldq, M, n_q, cache._ref, tp, cols, ldt, rp, lp, R, max_rows, max_len, total_len, mp, words,
+        D ** -0.5 if scale is None else scale, op, ldo, ep, wp, wb, _stream()))
+    return out
 
 
 def debug_group_acc_a8(packed, K, N, G, xq, variant=VARIANT_AUTO, tune=None):
