@@ -643,6 +643,8 @@ template <int DT, int W, bool P16> constexpr int tile_lds() { return RING * 2 * 
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 
+enum { CHECKED, WHOLE_HEADS, PADDED };                       // kinds of stages
+
 __device__ __forceinline__ float max16(const v16f& s)
 {
     float r;
@@ -729,11 +731,13 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
     int next[2] = {0, 0}, page = 0;
     const int half = wave * LOADS * 64 / PIECES >= 16;       // the run that a wave's 8 rows of a stage lie in
     uint32_t koffs[LOADS], voffs[LOADS];                     // where a lane's pieces lie in a run
+    bool real[LOADS];                                        // pieces of a head, not of what it is padded with
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
         const int at = (wave * LOADS + j) * 64 + lane, row = at / PIECES, d = (at % PIECES ^ swizzle32<DT>(row)) * 8;
         koffs[j] = (uint32_t)(row & 15) * 2 * (uint32_t)w.a.cache.k_slot_stride + 2 * d;
         voffs[j] = (uint32_t)(row & 15) * 2 * (uint32_t)w.a.cache.v_slot_stride + 2 * d;
+        real[j] = d < w.a.D;
     }
     auto fetch_pages = [&](int st) {
         if constexpr (P16) {
@@ -844,11 +848,11 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
         constexpr uint32_t far = near ? 0 : b * 2 * SB;
         read_vt32<near ? b * 2 * SB : 0, 16 * DT * 2>(vat[2 * g][0] + far, vat[2 * g][1] + far, vat[2 * g + 1][0] + far, vat[2 * g + 1][1] + far, vt);
     };
-    // INNER: a stage whose keys everybody sees, in the middle of a chunk whose pages are all there: nothing to check.
-    // cur: its scores, next: the next stage's.
-    auto stage = [&](int st, auto bc, auto inner, v16f& cur, v16f& nxt) {
+    // KIND: CHECKED, or a stage whose keys everybody sees, in the middle of a chunk whose pages are all there: nothing to check but
+    // (PADDED) where a head ends.  cur: its scores, next: the next stage's.
+    auto stage = [&](int st, auto bc, auto kind, v16f& cur, v16f& nxt) {
         constexpr int b = decltype(bc)::value, ahead = (b + RING - 1) % RING;
-        constexpr bool INNER = decltype(inner)::value;
+        constexpr bool INNER = decltype(kind)::value != CHECKED, WHOLE = decltype(kind)::value == WHOLE_HEADS;
         const uint32_t base = k0 + (uint32_t)st * 32;
         // the next stage is there; one behind it is under way
         if (INNER || st + 2 < stages) wait_loads<2 * LOADS>();
@@ -861,8 +865,13 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) {
                 char* const to = smem + ahead * 2 * SB + (wave * LOADS + j) * 1024;
-                load_lds_run<NT>((const char*)kh + x.k, koffs[j], to);
-                load_lds_run<NT>((const char*)vh + x.v, voffs[j], to + SB);
+                if constexpr (WHOLE) {
+                    load_lds_run<NT>((const char*)kh + x.k, koffs[j], to);
+                    load_lds_run<NT>((const char*)vh + x.v, voffs[j], to + SB);
+                } else {
+                    load_lds<NT>(real[j] ? (const void*)((const char*)kh + x.k + koffs[j]) : (const void*)g_zeros, to);
+                    load_lds<NT>(real[j] ? (const void*)((const char*)vh + x.v + voffs[j]) : (const void*)g_zeros, to + SB);
+                }
             }
         } else {
             if (st + RING - 1 < stages) {
@@ -881,6 +890,11 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
             }
         }
         if (idle) return;
+        // the next stage's keys: on their way while the maximum is taken, where there are registers for them
+        // (past the last stage: whatever the buffer holds, for scores that nobody uses)
+        v4i kf[KS];
+        if (DT < 256) read_k(smem + (b + 1) % RING * 2 * SB, kf);
+        __builtin_amdgcn_sched_barrier(0);
         float mx = max16(cur);
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         mx = max2(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
@@ -893,10 +907,8 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
 #pragma unroll
             for (int d = 0; d < DT / 32; ++d) o[d] *= shrink;
         }
-        // (past the last stage: scores of whatever the buffer holds, which nobody uses)
-        v4i kf[KS];
         __builtin_amdgcn_sched_barrier(0);
-        read_k(smem + (b + 1) % RING * 2 * SB, kf);
+        if (DT == 256) read_k(smem + (b + 1) % RING * 2 * SB, kf);
         v4i vt[2][2];
         read_v(bc, 0, vt);                                   // the first values' wait is the keys' too
         zero(nxt);
@@ -932,7 +944,7 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
     zero(sb);
     int inner = 0;                                           // stages of that kind, from the first on
     if (stages > 0) {
-        if (P16 && w.a.D == DT) {
+        if (P16) {
             inner = max(min((int)((k1 - k0) / 32) - RING, (int)((min(ctx, k1) - min(ctx, k0)) / 32)), 0) / RING * RING;
             const uint32_t p0 = divide(k0, w.a.page), p1 = divide(k1 - 1, w.a.page);
             bool all = inner > 0;
@@ -956,21 +968,26 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
     typedef std::integral_constant<int, 2> B2;
     typedef std::integral_constant<int, 3> B3;
     int st = 0;
-    for (; st < inner; st += RING) {
-        stage(st, B0{}, std::true_type{}, sa, sb);
-        stage(st + 1, B1{}, std::true_type{}, sb, sa);
-        stage(st + 2, B2{}, std::true_type{}, sa, sb);
-        stage(st + 3, B3{}, std::true_type{}, sb, sa);
-    }
+    auto ring = [&](auto kind) {
+        for (; st < inner; st += RING) {
+            stage(st, B0{}, kind, sa, sb);
+            stage(st + 1, B1{}, kind, sb, sa);
+            stage(st + 2, B2{}, kind, sa, sb);
+            stage(st + 3, B3{}, kind, sb, sa);
+        }
+    };
+    if (w.a.D == DT) ring(std::integral_constant<int, WHOLE_HEADS>{});
+    else ring(std::integral_constant<int, PADDED>{});
     // (the inner stages asked for three whole stages behind them)
     if (inner)
 #pragma unroll
         for (int b = 0; b < RING - 1; ++b) valid[b] = 0xffffffffu;
+    const std::integral_constant<int, CHECKED> checked;
     for (; st < stages; st += RING) {
-        stage(st, B0{}, std::false_type{}, sa, sb);
-        if (st + 1 < stages) stage(st + 1, B1{}, std::false_type{}, sb, sa);
-        if (st + 2 < stages) stage(st + 2, B2{}, std::false_type{}, sa, sb);
-        if (st + 3 < stages) stage(st + 3, B3{}, std::false_type{}, sb, sa);
+        stage(st, B0{}, checked, sa, sb);
+        if (st + 1 < stages) stage(st + 1, B1{}, checked, sb, sa);
+        if (st + 2 < stages) stage(st + 2, B2{}, checked, sa, sb);
+        if (st + 3 < stages) stage(st + 3, B3{}, checked, sb, sa);
     }
 
     const bool whole = sp.n_chunks == 1;
