@@ -416,6 +416,24 @@ def test_tree_many_rows_over_long_contexts(w2, hq, hkv, D):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,D", [(21, 3, 80), (5, 1, 40), (15, 5, 96), (6, 2, 72), (6, 2, 248)])
+def test_tree_padded_heads_over_long_contexts(w2, hq, hkv, D):
+    # heads shorter than the kernel's rows, in the middle of a chunk; what lies behind a head belongs to the next one
+    for t, split in ((13, True), (13, False), (50, True), (50, False)):
+        tree_case(w2, [(1200, t), (600, t - 5)], hq, hkv, D, page=48, split=split, seed=t + D)
+        tree_case(w2, [(1000, t)], hq, hkv, D, page=16, masked=False, split=split, heads_first=True, seed=t + D + 1)
+
+
+@pytest.mark.gpu
+def test_tree_many_units_and_chunks_of_one_length(w2):
+    # more units than run at once, and few over many keys: chunks by either rule
+    tree_case(w2, [(300 + 7 * i, 40) for i in range(20)], 16, 4, 128, page=32, seed=1)
+    tree_case(w2, [(260 + 9 * i, 70) for i in range(9)], 32, 16, 64, masked=False, seed=2)
+    tree_case(w2, [(7001, 20)], 8, 2, 128, page=16, seed=3)
+    tree_case(w2, [(7001, 20), (40, 20)], 8, 2, 128, page=16, total=False, slack=1, seed=4)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n", [640, 700, 768, 769, 1000, 1024, 1025])
 def test_tree_short_requests_in_one_launch(w2, n):
     tree_case(w2, [(n, 1)], 8, 2, 128, masked=False, seed=n)
