@@ -180,7 +180,8 @@ __global__ void __launch_bounds__(256) lora_shrink_kernel(LoraArgs a, int slots,
             };
             int k = kb;
             for (; k + 128 <= ke; k += 128) span(k, std::integral_constant<int, 4>{});
-            for (; k < ke; k += 32) span(k, std::integral_constant<int, 1>{});
+            for (; k + 64 <= ke; k += 64) span(k, std::integral_constant<int, 2>{});
+            if (k < ke) span(k, std::integral_constant<int, 1>{});
             // the four waves' sums, in order; lane: row l16 of the row tile, T's columns j0 + 4 q ..+ 3
             __syncthreads();
             part[wave * 64 + lane] = acc;
@@ -192,25 +193,27 @@ __global__ void __launch_bounds__(256) lora_shrink_kernel(LoraArgs a, int slots,
 }
 
 // ---------------------------------------------------------------------------------------------- T = X A^T, many rows
-// A workgroup: one adapter's rows of a window (up to 64), 32 rows of A, one of the ks ranges of K, in stages of 64 k through a
+// A workgroup: one adapter's rows of a window (up to 64), 16 J rows of A, one of the ks ranges of K, in stages of 64 k through a
 // ring in local memory.  A wave multiplies 16 rows.  Whole 128-byte pieces of rows an instruction: rows of X and A often lie
 // a multiple of 8 KiB apart, in one set of the vector cache, and operands that are loaded from there directly, half a line
-// of 16 rows each, evict one another (4000 rows, K = 4096, 128 ranks: 90 us in one range of K).
-constexpr int STAGES = 3;
-template <bool F32> constexpr int shrink_stage() { return 64 * (F32 ? 256 : 128) + 32 * 128; }
+// of 16 rows each, evict one another (4000 rows, K = 4096, 128 ranks: 90 us in one range of K against 30).
+// J = 4 where there are more than 32 rows of A: X is read half as often (2948 rows of 4096, fp32, 192 ranks: 64 -> 49 us; 3747,
+// bf16, 48 ranks: 26 -> 16).
+template <bool F32> constexpr int STAGES = F32 ? 3 : 4;       // (two workgroups on a CU, or more)
+template <bool F32, int J> constexpr int shrink_stage() { return 64 * (F32 ? 256 : 128) + 16 * J * 128; }
 
-template <bool F32>
+template <bool F32, int J>
 __global__ void __launch_bounds__(256) lora_shrink_tile_kernel(LoraArgs a, int slots, int groups, int ks)
 {
-    constexpr int XB = F32 ? 256 : 128, XL = F32 ? 4 : 2;    // bytes of a row's stage; loads of X a wave and stage (A: 1)
-    constexpr int STAGE = shrink_stage<F32>(), A_AT = 64 * XB;
+    constexpr int XB = F32 ? 256 : 128, XL = F32 ? 4 : 2, AL = J / 2;        // bytes of a row's stage; loads of X and of A a wave and stage
+    constexpr int STAGE = shrink_stage<F32, J>(), A_AT = 64 * XB, N = STAGES<F32>;
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t id = blockIdx.x;
     const int kr = id % ks;
     id /= ks;
-    const int j0 = id % groups * 32;
+    const int j0 = id % groups * 16 * J;
     id /= groups;
     // (the windows' first adapters one after the other: as a rule there are no others, and every die has its share of work)
     const uint32_t windows = (uint32_t)((a.M + WINDOW - 1) / WINDOW);
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__(256) lora_shrink_tile_kernel(LoraArgs a, int s
     for_tiles(a, m0, slot, slots, false, [&](const Tile& t) {
         const int rank = rank_of(a, t.adapter);
         bool any = false;
-        for (int j = j0; j < min(j0 + 32, PR); j += 8) any |= j % a.R < rank;
+        for (int j = j0; j < min(j0 + 16 * J, PR); j += 8) any |= j % a.R < rank;
         if (!any) return;
         const char* xsrc[XL];
 #pragma unroll
@@ -235,53 +238,59 @@ __global__ void __launch_bounds__(256) lora_shrink_tile_kernel(LoraArgs a, int s
             const int64_t from = m0 + __shfl(t.row, row < t.count ? row : 0);        // (rows that are not there: the first one again)
             xsrc[j] = (const char*)a.X + from * a.ldx * (F32 ? 4 : 2) + (int64_t)kb * XB + piece * 16;
         }
-        const int arow = wave * 8 + lane / 8;
-        const char* const asrc = (const char*)(a.A + t.adapter * a.a_stride + (int64_t)min(j0 + arow, PR - 1) * a.K) + (int64_t)kb * 128 +
-                                 (lane % 8 ^ swz_a(arow)) * 16;
+        const char* asrc[AL];
+#pragma unroll
+        for (int j = 0; j < AL; ++j) {
+            const int row = (wave * AL + j) * 8 + lane / 8;
+            asrc[j] = (const char*)(a.A + t.adapter * a.a_stride + (int64_t)min(j0 + row, PR - 1) * a.K) + (int64_t)kb * 128 + (lane % 8 ^ swz_a(row)) * 16;
+        }
         auto fetch = [&](int st) {
-            char* const dst = smem + st % STAGES * STAGE;
+            char* const dst = smem + st % N * STAGE;
 #pragma unroll
             for (int j = 0; j < XL; ++j) load_lds16(xsrc[j] + (int64_t)st * XB, dst + (wave * XL + j) * 1024);
-            load_lds16(asrc + (int64_t)st * 128, dst + A_AT + wave * 1024);
+#pragma unroll
+            for (int j = 0; j < AL; ++j) load_lds16(asrc[j] + (int64_t)st * 128, dst + A_AT + (wave * AL + j) * 1024);
         };
         __syncthreads();                                     // (the tile before is done with local memory)
 #pragma unroll
-        for (int st = 0; st < STAGES - 1; ++st)
+        for (int st = 0; st < N - 1; ++st)
             if (st < n_st) fetch(st);
-        v4f acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        v4f acc[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) acc[j] = (v4f){0.f, 0.f, 0.f, 0.f};
         const int xrow = wave * 16 + l16;
         for (int st = 0; st < n_st; ++st) {
-            // this stage is there; up to STAGES - 2 behind it are under way (at the end: none)
-            if (st + STAGES - 2 < n_st) wait_loads<(STAGES - 2) * (XL + 1)>();
+            // this stage is there; up to N - 2 behind it are under way (at the end: none)
+            if (st + N - 2 < n_st) wait_loads<(N - 2) * (XL + AL)>();
             else wait_loads<0>();
             bare_barrier();                                  // every wave's part of it, and no wave reads the stage before any more
-            if (st + STAGES - 1 < n_st) fetch(st + STAGES - 1);
-            const char* const xb = smem + st % STAGES * STAGE + xrow * XB;
-            const char* const ab = smem + st % STAGES * STAGE + A_AT;
+            if (st + N - 1 < n_st) fetch(st + N - 1);
+            const char* const xb = smem + st % N * STAGE + xrow * XB;
+            const char* const ab = smem + st % N * STAGE + A_AT;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const int p = 4 * s + q;
-                v4i av[2];
+                v4i av[J];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) av[j] = *reinterpret_cast<const v4i*>(ab + (16 * j + l16) * 128 + ((p ^ swz_a(16 * j + l16)) << 4));
+                for (int j = 0; j < J; ++j) av[j] = *reinterpret_cast<const v4i*>(ab + (16 * j + l16) * 128 + ((p ^ swz_a(16 * j + l16)) << 4));
                 if constexpr (F32) {
                     const v4i x0 = *reinterpret_cast<const v4i*>(xb + ((2 * p ^ swz(xrow)) << 4));
                     const v4i x1 = *reinterpret_cast<const v4i*>(xb + (((2 * p + 1) ^ swz(xrow)) << 4));
                     v4i hi, lo;
                     split_bf16(x0, x1, hi, lo);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[j] = mfma(av[j], lo, mfma(av[j], hi, acc[j]));
+                    for (int j = 0; j < J; ++j) acc[j] = mfma(av[j], lo, mfma(av[j], hi, acc[j]));
                 } else {
                     const v4i xv = *reinterpret_cast<const v4i*>(xb + ((p ^ swz(xrow)) << 4));
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[j] = mfma(av[j], xv, acc[j]);
+                    for (int j = 0; j < J; ++j) acc[j] = mfma(av[j], xv, acc[j]);
                 }
             }
         }
         if (xrow < t.count) {
             const int64_t row = m0 + __shfl(t.row, xrow);
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < J; ++j)
                 if (j0 + 16 * j + 4 * q < PR) *reinterpret_cast<v4f*>(T + row * PR + j0 + 16 * j + 4 * q) = acc[j];
         }
     });
@@ -307,8 +316,9 @@ __global__ void __launch_bounds__(256, NT == 1 ? (S == 1 ? 4 : S == 2 ? 3 : 2) :
     const uint32_t units = (uint32_t)((a.M + WINDOW - 1) / WINDOW) * slots, turn = blockIdx.x >> 3;
     const uint32_t g = (turn / units << 3) + (blockIdx.x & 7), unit = turn % units;
     if (g >= (uint32_t)groups) return;
-    const int slot = unit % slots;
-    const int64_t m0 = (int64_t)(unit / slots) * WINDOW;
+    const uint32_t windows = (uint32_t)((a.M + WINDOW - 1) / WINDOW);        // (their first adapters one after the other)
+    const int slot = unit / windows;
+    const int64_t m0 = (int64_t)(unit % windows) * WINDOW;
     const int PR = a.n_parts * a.R;
     const int64_t n_first = ((int64_t)g * steps * waves + wave) * 64;
     // the column (of the wave's 64) that row l16 of matrix tile t stands for
@@ -530,7 +540,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? (S == 1 ? 4 : S == 2 ? 3 : 2) :
 
 struct Plan {
     int64_t windows;
-    int many, groups, ks, slots;         // shrink: the kernel for many rows; groups of A's rows, ranges of K; workgroups that share a window's adapters
+    int many, j, groups, ks, slots;      // shrink: the kernel for many rows; groups of A's rows, ranges of K; workgroups that share a window's adapters
     int steps, columns, eslots;          // expand: steps of 256 columns a workgroup, how many such; as above
 };
 
@@ -548,30 +558,39 @@ Plan make_plan(int n_parts, int R, int n_adapters, int64_t M, int64_t K, int64_t
     Plan p;
     p.windows = (M + WINDOW - 1) / WINDOW;
     p.many = p.windows > 4 || (M > 32 && M > 32 * (int64_t)n_adapters);
-    p.groups = (n_parts * R + (p.many ? 31 : 15)) / (p.many ? 32 : 16);
-    // K cut until there are eight workgroups on every CU, which wait for memory; one where there are many rows.  Every part of T
-    // is written, and read again by every group of columns: eight (which are read
-    // together) where an adapter has several row tiles.  A wave's share is 64
-    // numbers or more.
-    const int64_t busy = std::min<int64_t>(M, p.windows - 1 + n_adapters) * p.groups, want = p.many ? 256 : 2048;
-    const int64_t most = M > 16 * (int64_t)n_adapters ? 8 : 16;
-    p.ks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want / std::max<int64_t>(busy, 1), most), K / 256));
+    p.j = !p.many ? 1 : n_parts * R > 32 ? 4 : 2;
+    p.groups = (n_parts * R + 16 * p.j - 1) / (16 * p.j);
+    // K cut until there are eight workgroups on every CU, which wait for memory, or of the larger ones for many rows one and a
+    // half, or one where they take 64 rows of A.  At most eight parts: every part of T is written, and read again by every group
+    // of columns, four parts together (us, both launches, one row, K = 4096, 64 ranks, 16 parts: 12.5, 8: 11.0; 9 rows of 5
+    // adapters of 128: 22 and 20; 574 rows, 128 ranks, 34816 columns, 2 parts: 83, 5: 98).  A wave's share is 128 numbers or
+    // more, which are one trip to memory.
+    const int64_t busy = std::min<int64_t>(M, p.windows - 1 + n_adapters) * p.groups, want = p.j == 4 ? 256 : p.many ? 384 : 2048;
+    p.ks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want / std::max<int64_t>(busy, 1), 8), K / 512));
     p.slots = slots_for(M, p.windows, p.groups * p.ks, n_adapters);
-    const int64_t blocks = (N + 255) / 256;
-    p.steps = (int)std::max<int64_t>(1, std::min<int64_t>(blocks, blocks * p.windows / 2048));
-    p.columns = (int)((blocks + p.steps - 1) / p.steps);
-    p.eslots = slots_for(M, p.windows, p.columns, (int64_t)n_adapters + 1);
+    // Columns of a workgroup: it reads T once for all of them, but the workgroups of a die (every eighth group of columns; room
+    // for so many at once) should fill whole rounds: the number of rounds times the steps of one, and what it does before its
+    // first step, about half a step and the reading of T (bytes against those of a step).  4000 rows, 28672 gated columns,
+    // us with 1, 3, 5, 7, 13 steps: 152, 123, 117, 110, 152; 933 rows, 34816, with 1, 2, 3: 66, 63, 51.
+    const int64_t blocks = (N + 255) / 256, most = p.many ? std::min<int64_t>(blocks, 16) : 1, room = 32 * (R <= 32 ? 3 : 2);
+    const double start = 0.5 + (double)(n_parts * R * p.ks) * 256 / (49152 + 512 * R);
+    double least = 1e30;
+    for (int64_t s = 1; s <= most; ++s) {
+        const int64_t columns = (blocks + s - 1) / s, slots = slots_for(M, p.windows, columns, (int64_t)n_adapters + 1);
+        const double cost = (double)(((columns + 7) / 8 * p.windows * slots + room - 1) / room) * (s + start);
+        if (cost < least) least = cost, p.steps = (int)s, p.columns = (int)columns, p.eslots = (int)slots;
+    }
     return p;
 }
 
 template <bool F32>
 int launch_shrink(const LoraArgs& a, const Plan& p, hipStream_t stream)
 {
-    const int lds = p.many ? STAGES * shrink_stage<F32>() : 0;
-    if (int rc = ensure_dynamic_lds((const void*)lora_shrink_tile_kernel<F32>, lds, "w2_lora_add")) return rc;
+    const int lds = p.j == 4 ? STAGES<F32> * shrink_stage<F32, 4>() : p.j == 2 ? STAGES<F32> * shrink_stage<F32, 2>() : 0;
+    const auto kern = p.j == 4 ? lora_shrink_tile_kernel<F32, 4> : p.j == 2 ? lora_shrink_tile_kernel<F32, 2> : lora_shrink_kernel<F32>;
+    if (int rc = ensure_dynamic_lds((const void*)kern, lds, "w2_lora_add")) return rc;
     const int64_t blocks = p.windows * p.slots * p.groups * p.ks;
-    hipLaunchKernelGGL(p.many ? lora_shrink_tile_kernel<F32> : lora_shrink_kernel<F32>, dim3((unsigned)blocks), dim3(256), lds, stream, a, p.slots,
-                       p.groups, p.ks);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), lds, stream, a, p.slots, p.groups, p.ks);
     return check_launch("w2_lora_add");
 }
 
