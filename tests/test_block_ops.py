@@ -110,6 +110,25 @@ def test_lora_activations_gated_strides(w2, act, gated, M):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("xdt", [torch.bfloat16, torch.float32])
+def test_lora_many_rows_of_wide_factors(w2, xdt):
+    # more rows of A than one workgroup takes, the last of them few; K in one to eight parts, of few and of many stages
+    lora_case(w2, 400, 512, [160, 80, 48], 24, 3, xdt=xdt, none=True, seed=1)
+    lora_case(w2, 330, 1280, [64, 32], 40, 2, xdt=xdt, ranks=[40, 9], seed=2)
+    lora_case(w2, 150, 4352, [48], 128, 2, xdt=xdt, seed=3)
+    lora_case(w2, 500, 768, [96], 128, 90, xdt=xdt, ranks=[128, 60, 0], none=True, seed=4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gated", [False, True])
+def test_lora_many_rows_and_columns(w2, gated):
+    # several steps of columns a workgroup, the last ones past the end, and windows of several adapters
+    lora_case(w2, 900, 256, [4096 + 264 - 8 * gated], 8, 40, gated=gated, act=2 * gated, none=True, seed=5)
+    lora_case(w2, 700, 256, [6016], 64, 2, gated=gated, act=2 * gated, pad=8, seed=6)
+    lora_case(w2, 1100, 512, [2496], 128, 3, gated=gated, act=1, ranks=[128, 8, 33], seed=7)
+
+
+@pytest.mark.gpu
 def test_lora_in_place_all_none_and_many_adapters(w2):
     lora_case(w2, 50, 512, [96], 16, 3, in_place=True)
     lora_case(w2, 40, 512, [96], 16, 64, none=True)
