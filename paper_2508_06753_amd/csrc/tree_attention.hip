@@ -711,12 +711,15 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
     const int chunk = unit / w.n_kv, r = blockIdx.y;
     const int hk = head_of(w, unit, chunk, r);
     const Span sp = make_span(w, r);
-    const int rho_wg = tile * 32 * W;
-    if (rho_wg >= sp.rows || chunk >= sp.n_chunks) return;
+    // the request's 32-row waves, spread evenly over its tiles: tiles that run alike stay close to each other in the keys, which
+    // then come from the L2 once
+    const int all_waves = (sp.rows + 31) / 32, tiles = (all_waves + W - 1) / W;
+    if (tile >= tiles || chunk >= sp.n_chunks) return;
+    const int wave0 = all_waves * tile / tiles, waves = all_waves * (tile + 1) / tiles - wave0, rho_wg = 32 * wave0;
     const uint32_t k0 = (uint32_t)chunk * w.chunk, ctx = max(sp.ctx, 0);
     uint32_t k1 = min((uint32_t)sp.len, k0 + w.chunk);
     if (!w.a.mask) {                                         // causal: nothing past the tile's last token
-        const int last = (int)divide((uint32_t)min(rho_wg + 32 * W, sp.rows) - 1, w.by_g);
+        const int last = (int)divide((uint32_t)min(rho_wg + 32 * waves, sp.rows) - 1, w.by_g);
         k1 = max(k0, min(k1, (uint32_t)max(sp.ctx + last + 1, 0)));
     }
     const int stages = (int)((k1 - k0 + 31) / 32);
@@ -800,7 +803,7 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
 
     // the lane's query row, its operands: numbers 16 ks + 8 h ..+ 7
     const int rho = rho_wg + wave * 32 + l32;
-    const bool live = rho < sp.rows, idle = rho_wg + wave * 32 >= sp.rows;       // (idle: a wave without rows, which only loads)
+    const bool idle = wave >= waves, live = !idle && rho < sp.rows;               // (idle: a wave without rows, which only loads)
     const int t = (int)divide((uint32_t)(live ? rho : 0), w.by_g), head = hk * w.a.G + (live ? rho : 0) - t * w.a.G;
     const int64_t row = sp.first + t;
     const uint64_t word = w.a.mask ? w.a.mask[row * w.a.mask_words] : 0;
