@@ -1,14 +1,22 @@
 // Attention of each request's drafted tokens over its pages of the cache.
 //
 // The query rows of a cache head are packed, row rho = (token i) * G + (query head g), so that a group's heads share what
-// is read of K and V.  Scores are held transposed: S^T = K Q^T by 16x16x32 matrix instructions puts 4 keys of one query row
-// in a lane, which is the operand layout of P^T in O^T = V^T P^T once the 32 keys of a step are numbered as (tile 0, 4q + i),
-// (tile 1, 4q + i), q = lane / 16: no weight crosses lanes.  V^T operands come from local memory by the transposing read.
-// Running maximum and sum per query row (m, l) in fp32; the outputs are rescaled only when a maximum has grown by more than
-// 8 powers of two, which fp32 sums and bf16 weights carry without loss; the sum is reduced over the lanes at the end.
+// is read of K and V.  Scores are held transposed: S^T = K Q^T puts keys of one query row in a lane, which is the operand
+// layout of P^T in O^T = V^T P^T once the 32 keys of a step are numbered to suit: no weight crosses lanes.  V^T operands come
+// from local memory by the transposing read.  Running maximum and sum per query row (m, l) in fp32; the outputs are rescaled
+// only when a maximum has grown by more than 8 powers of two, which fp32 sums and bf16 weights carry without loss; the sum is
+// reduced over the lanes at the end.
 //
-// tree_few_kernel: up to 32 packed rows (decoding, small trees).  Every wave of a workgroup takes other keys.
-// tree_tile_kernel: workgroups of 64 or 128 packed rows, 16 or 32 a wave, over shared stages of K and V.
+// tree_few_kernel: up to 32 packed rows (decoding, small trees), 16x16x32 instructions.  Every wave of a workgroup takes other
+// keys, which go to local memory past the registers, and nothing else waits for them.  Bound by memory: 48 requests of one
+// token, up to 8000 keys, 8 heads of 128: 967 MB in 155 us, 6.2 TB/s (a plain read of so much: 7.1).  One request of 700 keys:
+// 9.7 us, a launch and six trips to memory.
+// tree_tile_kernel: workgroups of 64 or 128 packed rows, 32 a wave, over a ring of shared stages of 32 keys, 32x32x16
+// instructions.  Up to 64 rows bound by memory and by how evenly the keys are dealt out (16 requests of 36 rows, 174 MB: 37 us,
+// 4.7 TB/s); above by what a wave does one after the other, with room in local memory and registers for two waves a SIMD:
+// 2 requests of 320 rows, up to 120000 keys: 212 GFLOP in 292 us, 0.73 PFLOP/s, the matrix pipe busy a third of the time, vector
+// instructions (16 exponentials a lane and stage) another; heads of 64, whose exponentials take longer than their products:
+// 4 requests of 1000 tokens, 81 GFLOP in 124 us, vector issue a half.
 // Keys of a request are cut into chunks for several workgroups where the batch alone does not fill the machine; partial
 // results meet in tree_join_kernel.
 #include <hip/hip_runtime.h>
@@ -171,11 +179,12 @@ Plan make_plan(int64_t n_requests, int64_t max_rows, int G, int n_kv, int D, int
         // As many workgroups as local memory has room for at once, however the keys are spread over the requests (each may have
         // a last chunk that is not full): a few more would take as long again (us: 16 requests of 36 rows and up to 4100 keys,
         // about 512 workgroups and up to 128 more: 47, at most 512: 36; 7 of 61 rows and up to 34226 keys, 16 heads: 278 and
-        // 220; of four waves two share a CU's SIMDs, and what is left of the last one runs faster: half that margin, 320 and 308
-        // for 2 requests of 320 rows and up to 120000 keys).  Where there are more units than that, parts pass through memory and little is gained, up to 48 keys a row
-        // (4 requests of 1000 tokens, 5000 keys, in a second chunk: 136 -> 148; 21 of 166 tokens, 7142 keys, 16 heads: 291 ->
-        // 282).  Else two keys a row are enough: workgroups without others beside them wait for memory most of the time
-        // (8 requests of 434 rows, 2434 keys, 3 heads: 76 in one chunk, 25 + 6 in ten).
+        // 220; of four waves two share a CU's SIMDs, and what is left of the last one runs faster: half that margin, 320 and
+        // 308 for 2 requests of 320 rows and up to 120000 keys).  Where there are more units than that, parts pass through
+        // memory and little is gained, up to 48 keys a row (4 requests of 1000 tokens, 5000 keys, in a second chunk: 136 ->
+        // 148; 21 of 166 tokens, 7142 keys, 16 heads: 291 -> 282).  Else two keys a row are enough: workgroups without others
+        // beside them wait for memory most of the time (8 requests of 434 rows, 2434 keys, 3 heads: 76 in one chunk, 25 + 6 in
+        // ten).
         const int64_t units = n_requests * n_kv * p.tiles, room = p.dt == 64 ? 1024 : p.dt == 128 ? 512 : 256;
         const int64_t rounds = std::max<int64_t>(1, (2 * units + room - 1) / room), free = rounds * room - (p.waves == 2 ? units : units / 2);
         chunk = std::max<int64_t>((all + free - 1) / free, (rounds > 1 ? 48 : 2) * tile_rows);
