@@ -11,8 +11,9 @@
 // Bound: few rows, by two launches and the trips to memory in each, one behind the other (whose adapter, its factors; T, the
 // stores): one row, K = 4096, 16 ranks, N = 6144: 4.0 + 5.3 us; 61 rows of 48 adapters, 37 MB: 12 + 10.3 us.  Many rows, by base
 // and Y: 4000 rows, K = 4096, 64 ranks, 28672 gated columns, 344 MB: 26 + 109 us, 3.2 TB/s in the second launch (a large copy: 4.75);
-// there two waves a SIMD (four row tiles of base and the factors in registers) load, multiply and store in turns.  Asking for
-// the next columns' base before this one's products (then with three steps a workgroup): 125 -> 142 us.
+// there two waves a SIMD (four row tiles of base and the factors in registers) load, multiply and store in turns.  Base by way
+// of local memory: 121 us; the next columns' base asked for before this one's products: no faster with all stores behind it,
+// slower among them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -567,12 +568,12 @@ Plan make_plan(int n_parts, int R, int n_adapters, int64_t M, int64_t K, int64_t
     p.j = !p.many ? 1 : n_parts * R > 32 ? 4 : 2;
     p.groups = (n_parts * R + 16 * p.j - 1) / (16 * p.j);
     // K cut until there are eight workgroups on every CU, which wait for memory, or of the larger ones for many rows one and a
-    // half, or one where they take 64 rows of A.  At most eight parts: every part of T is written, and read again by every group
-    // of columns, four parts together (us, both launches, one row, K = 4096, 64 ranks, 16 parts: 12.5, 8: 11.0; 9 rows of 5
-    // adapters of 128: 22 and 20; 574 rows, 128 ranks, 34816 columns, 2 parts: 83, 5: 98).  A wave's share is 128 numbers or
-    // more, which are one trip to memory.
+    // half, or one where they take 64 rows of A.  At most eight parts, four of a wide T: every part is written, and read again
+    // by every group of columns (us, both launches, one row, K = 4096, 64 ranks, 16 parts: 12.5, 8: 11.0; 9 rows of 5 adapters
+    // of 128: 22 and 20; 574 rows, 128 ranks, gated 34816 columns, 5 parts: 89, 4: 83; 218 fp32 rows of 384 ranks, 8 parts: 38,
+    // 4: 35).  A wave's share is 128 numbers or more, which are one trip to memory.
     const int64_t busy = std::min<int64_t>(M, p.windows - 1 + n_adapters) * p.groups, want = p.j == 4 ? 256 : p.many ? 384 : 2048;
-    p.ks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want / std::max<int64_t>(busy, 1), 8), K / 512));
+    p.ks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want / std::max<int64_t>(busy, 1), p.j == 4 ? 4 : 8), K / 512));
     p.slots = slots_for(M, p.windows, p.groups * p.ks, n_adapters);
     // Columns of a workgroup: it reads T once for all of them, but the workgroups of a die (every eighth group of columns; room
     // for so many at once) should fill whole rounds: the number of rounds times the steps of one, and what it does before its
