@@ -26,6 +26,7 @@
 #include <type_traits>
 
 #include "block_ops.h"
+#include "tree_plan.h"
 #include "w2_small_common.h"
 
 namespace w2 {
@@ -724,7 +725,8 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
     // then come from the L2 once
     const int all_waves = (sp.rows + 31) / 32, tiles = (all_waves + W - 1) / W;
     if (tile >= tiles || chunk >= sp.n_chunks) return;
-    const int wave0 = all_waves * tile / tiles, waves = all_waves * (tile + 1) / tiles - wave0, rho_wg = 32 * wave0;
+    const tree::Share own = tree::share(all_waves, tiles, tile);
+    const int waves = own.count, rho_wg = 32 * own.first;
     const uint32_t k0 = (uint32_t)chunk * w.chunk, ctx = max(sp.ctx, 0);
     uint32_t k1 = min((uint32_t)sp.len, k0 + w.chunk);
     if (!w.a.mask) {                                         // causal: nothing past the tile's last token

@@ -1,0 +1,50 @@
+"""How the attention of drafted tokens is cut up (csrc/tree_plan.h, compiled by itself), up to the largest sizes that its entry takes."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def compiled(tmp_path_factory, name, program):
+    if shutil.which("g++") is None:
+        pytest.skip("no g++")
+    d = tmp_path_factory.mktemp(name)
+    (d / "p.cpp").write_text(f'#include "{ROOT}/paper_2508_06753_amd/csrc/tree_plan.h"\n' + program)
+    subprocess.run(["g++", "-O2", "-fwrapv", "-std=c++17", "-o", str(d / "p"), str(d / "p.cpp")], check=True)
+    return subprocess.run([str(d / "p")], capture_output=True, text=True, check=True).stdout.splitlines()
+
+
+SHARES = r"""
+#include <stdio.h>
+#include <algorithm>
+using namespace w2;
+int main()
+{
+    // packed rows of a request: small ones all, then single cases up to what a grid of 2^24 - 1 workgroups of 128 rows counts
+    const auto walk = [](long long rows, int W) {
+        const int all = (int)((rows + 31) / 32), tiles = (all + W - 1) / W;
+        long long next = 0, bad = 0;
+        for (int t = 0; t < tiles; ++t) {
+            const tree::Share s = tree::share(all, tiles, t);
+            bad += s.first != next || s.count < 1 || s.count > W;
+            next = (long long)s.first + s.count;
+        }
+        printf("%lld %d %lld %lld\n", rows, W, bad, all - next);
+    };
+    for (int W : {2, 4}) {
+        for (long long rows = 1; rows <= 2000; rows += 13) walk(rows, W);
+        for (long long rows : {71ll * 42000, 128ll * 23200, 16ll * 186000, 8ll * 371000, 131072ll * 32, (1ll << 24) * 8, ((1ll << 24) - 1) * 32 * W, ((1ll << 24) - 1) * 32 * W - 100})
+            walk(rows, W);
+    }
+}
+"""
+
+
+def test_every_wave_of_rows_is_in_one_tile(tmp_path_factory):
+    lines = [tuple(map(int, l.split())) for l in compiled(tmp_path_factory, "share", SHARES)]
+    assert len(lines) > 300
+    for rows, waves, bad, left in lines:
+        assert bad == 0 and left == 0, f"{rows} packed rows, {waves} waves a tile: {bad} tiles are wrong, {left} waves are left over"
