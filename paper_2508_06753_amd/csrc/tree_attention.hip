@@ -40,7 +40,6 @@ typedef short v4s __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float SLACK = 8.0f;            // powers of two a maximum may grow by before the outputs are rescaled
-constexpr int MAX_CHUNKS = 128;
 
 __device__ __align__(16) const uint32_t g_zeros[4] = {0, 0, 0, 0};
 
@@ -149,69 +148,13 @@ __device__ __forceinline__ float max_over_q(float x)
     return max2(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-struct Plan {
-    int few;                             // tree_few_kernel, else tree_tile_kernel
-    int rt;                              // few: 16-row tiles a wave
-    int waves;                           // a workgroup
-    int dt;                              // head_dim padded to 64, 128 or 256
-    int tiles;                           // row tiles of a request
-    int chunk;                           // keys of a workgroup, a multiple of 32 * waves
-    int chunks;                          // of the longest request
-};
-
-Plan make_plan(int64_t n_requests, int64_t max_rows, int G, int n_kv, int D, int64_t max_len, int64_t total_len)
-{
-    Plan p;
-    const int64_t rows = max_rows * G;
-    p.dt = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-    p.few = rows <= (p.dt < 256 ? 32 : 16);
-    p.rt = p.few && rows <= 16 ? 1 : 2;
-    p.waves = !p.few && rows <= 64 ? 2 : 4;
-    const int rows_per_wg = p.few ? 16 * p.rt : 32 * p.waves;
-    p.tiles = (int)((rows + rows_per_wg - 1) / rows_per_wg);
-    if (total_len <= 0 || total_len > n_requests * max_len) total_len = n_requests * max_len;
-    const int64_t all = total_len * n_kv * p.tiles, tile_rows = std::min<int64_t>(rows, rows_per_wg);
-    int64_t chunk;
-    if (p.few) {
-        // workgroups for eight on every CU, each with so many keys that the parts of its rows, written and read again in 32 bits,
-        // stay a tenth of them
-        chunk = std::max<int64_t>((all + 2047) / 2048, std::max<int64_t>(128, 20 * tile_rows));
-    } else {
-        // As many workgroups as local memory has room for at once, however the keys are spread over the requests (each may have
-        // a last chunk that is not full): a few more would take as long again (us: 16 requests of 36 rows and up to 4100 keys,
-        // about 512 workgroups and up to 128 more: 47, at most 512: 36; 7 of 61 rows and up to 34226 keys, 16 heads: 278 and
-        // 220; of four waves two share a CU's SIMDs, and what is left of the last one runs faster: half that margin, 320 and
-        // 308 for 2 requests of 320 rows and up to 120000 keys).  Where there are more units than that, parts pass through
-        // memory and little is gained, up to 48 keys a row (4 requests of 1000 tokens, 5000 keys, in a second chunk: 136 ->
-        // 148; 21 of 166 tokens, 7142 keys, 16 heads: 291 -> 282).  Else two keys a row are enough: workgroups without others
-        // beside them wait for memory most of the time (8 requests of 434 rows, 2434 keys, 3 heads: 76 in one chunk, 25 + 6 in
-        // ten).
-        const int64_t units = n_requests * n_kv * p.tiles, room = p.dt == 64 ? 1024 : p.dt == 128 ? 512 : 256;
-        const int64_t rounds = std::max<int64_t>(1, (2 * units + room - 1) / room), free = rounds * room - (p.waves == 2 ? units : units / 2);
-        chunk = std::max<int64_t>((all + free - 1) / free, (rounds > 1 ? 48 : 2) * tile_rows);
-    }
-    chunk = std::max(chunk, (max_len + MAX_CHUNKS - 1) / MAX_CHUNKS);
-    if (!p.few) chunk = std::max<int64_t>(256, max_len / std::max<int64_t>(1, (max_len + chunk - 1) / chunk) + 1);    // (of one length)
-    if (max_rows * G * n_kv >= (int64_t)1 << 24) chunk = std::max(chunk, max_len);     // (more than a grid of the join counts)
-    chunk = (chunk + 127) / 128 * 128;
-    // a few short requests: eight waves share a request's keys and no second launch joins chunks (us, one request of 8 heads, 700
-    // keys: 9.6 against 6.1 + 3.3 and a launch, 1000 keys: 12.2 against 6.2 + 3.4; 16 requests of 1000: 13.6 against 14.3 + 3.6)
-    if (p.few && p.rt == 1 && p.dt < 256 && n_requests * n_kv <= 256 && max_len <= (n_requests * n_kv >= 64 ? 1024 : 768)) {
-        p.waves = 8;
-        chunk = 1024;
-    }
-    p.chunk = (int)std::min<int64_t>(chunk, (int64_t)1 << 31 >> 1);
-    p.chunks = (int)std::max<int64_t>(1, (max_len + p.chunk - 1) / p.chunk);
-    return p;
-}
-
 }  // namespace
 
 // partial results: O [chunk][row][head][D] fp32, then (maximum, sum) [chunk][row][head]
 size_t tree_workspace_bytes(int64_t n_requests, int64_t M, int n_q, int n_kv, int D, int64_t max_rows, int64_t max_len, int64_t total_len)
 {
     if (M == 0 || n_requests == 0 || max_rows == 0) return 0;
-    const Plan p = make_plan(n_requests, std::min(max_rows, M), n_q / n_kv, n_kv, D, max_len, total_len);
+    const tree::Plan p = tree::make_plan(n_requests, std::min(max_rows, M), n_q / n_kv, n_kv, D, max_len, total_len);
     return p.chunks < 2 ? 0 : (size_t)p.chunks * M * n_q * (D + 2) * sizeof(float);
 }
 
@@ -223,8 +166,8 @@ struct Work {
     float c;                             // |scale| * log2 e
     int flip;                            // scale < 0: queries change sign
     int same;                            // K and V have the same strides
-    uint32_t n_pages;
-    int tiles, chunk, chunks, n_kv;
+    uint32_t n_pages, chunk;
+    int tiles, chunks, n_kv;
     float* part_o;
     float2* part_ml;
 };
@@ -246,7 +189,7 @@ __device__ __forceinline__ Span make_span(const Work& w, int r)
     const int64_t len = min(min((int64_t)scalar_load(w.a.kv_len, r), w.a.max_len), w.a.table_cols * w.a.cache.page_size);
     s.len = (int)max(len, (int64_t)0);
     s.ctx = s.len - s.T;
-    s.n_chunks = max(1, (int)(((uint32_t)s.len + (uint32_t)w.chunk - 1) / (uint32_t)w.chunk));
+    s.n_chunks = max(1, (int)(((uint32_t)s.len + w.chunk - 1) / w.chunk));
     return s;
 }
 
@@ -1120,18 +1063,12 @@ int launch_tree_attention(const TreeArgs& a, hipStream_t stream)
 {
     const int n_kv = a.cache.n_heads;
     const int64_t max_len = std::min(a.max_len, a.table_cols * a.cache.page_size);
-    Plan p = make_plan(a.n_requests, a.max_rows, a.G, n_kv, a.D, max_len, a.total_len);
+    tree::Plan p = tree::make_plan(a.n_requests, a.max_rows, a.G, n_kv, a.D, max_len, a.total_len);
+    const size_t per = (size_t)a.M * a.n_q * (a.D + 2) * sizeof(float);
+    tree::fit(p, max_len, std::min<int64_t>((int64_t)(a.workspace_bytes / per), tree::MAX_CHUNKS));
     Work w = {};
     w.a = a;
     w.a.max_len = max_len;
-    const size_t per = (size_t)a.M * a.n_q * (a.D + 2) * sizeof(float);
-    const int64_t room = std::min<int64_t>((int64_t)(a.workspace_bytes / per), MAX_CHUNKS);
-    if (p.chunks > room) {                                   // no room for so many parts: longer chunks
-        p.chunks = (int)std::max<int64_t>(1, room);
-        p.chunk = (int)((max_len + p.chunks - 1) / p.chunks + 127) / 128 * 128;
-        p.chunk = std::max(p.chunk, 128);
-        p.chunks = (int)std::max<int64_t>(1, (max_len + p.chunk - 1) / p.chunk);
-    }
     w.by_g = make_divider((uint32_t)a.G);
     w.by_tiles = make_divider((uint32_t)p.tiles);
     // (a scale of zero as the smallest number: unseen keys stay at -infinity)

@@ -48,3 +48,36 @@ def test_every_wave_of_rows_is_in_one_tile(tmp_path_factory):
     assert len(lines) > 300
     for rows, waves, bad, left in lines:
         assert bad == 0 and left == 0, f"{rows} packed rows, {waves} waves a tile: {bad} tiles are wrong, {left} waves are left over"
+
+
+PLANS = r"""
+#include <stdio.h>
+using namespace w2;
+int main()
+{
+    const long long INT_MAX_ = (1ll << 31) - 1;
+    for (long long len : {0ll, 1ll, 127ll, 128ll, 129ll, 5000ll, 120000ll, 1ll << 20, 1ll << 30, INT_MAX_ - 128, INT_MAX_ - 127, INT_MAX_ - 126, INT_MAX_ - 1, INT_MAX_})
+        for (long long rows : {1ll, 2ll, 4ll, 9ll, 64ll, 1000ll, 1ll << 20})
+            for (int G : {1, 4, 16})
+                for (int D : {8, 64, 128, 256})
+                    for (long long requests : {1ll, 40ll, 65535ll})
+                        for (long long room : {0ll, 1ll, 2ll, 3ll, 7ll, 127ll, 128ll}) {
+                            tree::Plan p = tree::make_plan(requests, rows, G, 8, D, len, 0);
+                            const tree::Plan wish = p;
+                            tree::fit(p, len, room);
+                            const bool ok = p.chunks >= 1 && p.chunks <= std::max(1ll, room) && p.chunk >= 128 && p.chunk % 128 == 0 &&
+                                            p.chunk <= (1u << 31) && (long long)p.chunk * p.chunks >= len &&
+                                            (p.chunks == 1 || (long long)p.chunk * (p.chunks - 1) < len) &&
+                                            wish.chunks <= tree::MAX_CHUNKS && (room < wish.chunks || (p.chunk == wish.chunk && p.chunks == wish.chunks));
+                            if (!ok) printf("%lld keys, %lld rows of %d heads of %d, %lld requests, room for %lld: %d chunks of %u\n", len, rows, G, D, requests, room, p.chunks, p.chunk);
+                        }
+    printf("done\n");
+}
+"""
+
+
+def test_chunks_are_no_more_than_there_is_room_for(tmp_path_factory):
+    """Every key is in one chunk, whatever the longest request: parts of more chunks than the workspace holds would be written
+    behind it."""
+    lines = compiled(tmp_path_factory, "plans", PLANS)
+    assert lines == ["done"], lines[:5]
