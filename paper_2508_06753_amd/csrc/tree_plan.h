@@ -42,12 +42,14 @@ inline Plan make_plan(int64_t n_requests, int64_t max_rows, int G, int n_kv, int
     const int rows_per_wg = p.few ? 16 * p.rt : 32 * p.waves;
     p.tiles = (int)((rows + rows_per_wg - 1) / rows_per_wg);
     if (total_len <= 0 || total_len > n_requests * max_len) total_len = n_requests * max_len;
-    const int64_t all = total_len * n_kv * p.tiles, tile_rows = std::min<int64_t>(rows, rows_per_wg);
+    // (limits far above the batch's own are allowed, and their product is past 64 bits)
+    const __int128 all = (__int128)total_len * n_kv * p.tiles;
+    const int64_t tile_rows = std::min<int64_t>(rows, rows_per_wg);
     int64_t chunk;
     if (p.few) {
         // workgroups for eight on every CU, each with so many keys that the parts of its rows, written and read again in 32 bits,
         // stay a tenth of them
-        chunk = std::max<int64_t>((all + 2047) / 2048, std::max<int64_t>(128, 20 * tile_rows));
+        chunk = std::max<int64_t>((int64_t)((all + 2047) / 2048), std::max<int64_t>(128, 20 * tile_rows));
     } else {
         // As many workgroups as local memory has room for at once, however the keys are spread over the requests (each may have
         // a last chunk that is not full): a few more would take as long again (us: 16 requests of 36 rows and up to 4100 keys,
@@ -60,7 +62,7 @@ inline Plan make_plan(int64_t n_requests, int64_t max_rows, int G, int n_kv, int
         // ten).
         const int64_t units = n_requests * n_kv * p.tiles, room = p.dt == 64 ? 1024 : p.dt == 128 ? 512 : 256;
         const int64_t rounds = std::max<int64_t>(1, (2 * units + room - 1) / room), free = rounds * room - (p.waves == 2 ? units : units / 2);
-        chunk = std::max<int64_t>((all + free - 1) / free, (rounds > 1 ? 48 : 2) * tile_rows);
+        chunk = std::max<int64_t>((int64_t)((all + free - 1) / free), (rounds > 1 ? 48 : 2) * tile_rows);
     }
     chunk = std::max(chunk, (max_len + MAX_CHUNKS - 1) / MAX_CHUNKS);
     if (!p.few) chunk = std::max<int64_t>(256, max_len / std::max<int64_t>(1, (max_len + chunk - 1) / chunk) + 1);    // (of one length)

@@ -81,3 +81,26 @@ def test_chunks_are_no_more_than_there_is_room_for(tmp_path_factory):
     behind it."""
     lines = compiled(tmp_path_factory, "plans", PLANS)
     assert lines == ["done"], lines[:5]
+
+
+WIDE = r"""
+#include <stdio.h>
+using namespace w2;
+int main()
+{
+    // limits as wide as they go: more units than run at once by far
+    for (long long rows : {1ll << 17, 1ll << 20, (1ll << 20) + 77, (1ll << 21) - 16, (1ll << 24) - 128, 1ll << 24})
+        for (int G : {1, 16, 128})
+            for (int n_kv : {1, 8, 1024 / G}) {
+                const tree::Plan p = tree::make_plan(65535, rows, G, n_kv, 8, (1ll << 31) - 1, 0);
+                printf("%lld %d %d %d\n", rows, G, n_kv, p.chunks);
+            }
+}
+"""
+
+
+def test_plans_of_the_widest_limits(tmp_path_factory):
+    """Keys times heads times tiles pass 64 bits there.  Workgroups that are to hold them are at most two a unit and one round, so a
+    chunk has half of the longest request or more; a product that wrapped would cut the keys to pieces."""
+    for line in compiled(tmp_path_factory, "wide", WIDE):
+        assert int(line.split()[3]) <= 2, line
