@@ -3,8 +3,8 @@
     QKV projection (2-bit) [+ adapters] -> norm of q and k, rotation, K and V into the paged cache
       -> attention over the cache -> output projection (2-bit) [+ adapters]
 
-Every step is a call of ``binding``; this module holds the weights and the workspaces and allocates them when a larger batch
-than before comes.  ``python -m paper_2508_06753_amd.attention_block`` runs a prompt, a drafted tree and single tokens.
+Every step is a call of ``binding``; this module holds the weights and no memory of a step: steps may run on several streams,
+from several threads and in graphs.  ``python -m paper_2508_06753_amd.attention_block`` runs a prompt, a drafted tree and single tokens.
 """
 from dataclasses import dataclass
 from typing import Optional
@@ -39,16 +39,9 @@ class AttentionBlock:
         self.width = (n_q + 2 * n_kv) * head_dim
         self.rope, self.q_weight, self.k_weight, self.eps = rope, q_weight, k_weight, eps
         self.qkv_lora, self.o_lora = qkv_lora, o_lora
-        self._room = None
-
-    def _workspace(self, nbytes, device):
-        # one buffer for all steps: they run one after the other on one stream
-        if self._room is None or self._room.numel() < nbytes or self._room.device != device:
-            self._room = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        return self._room
 
     def workspace_size(self, M, batch, cache):
-        """Bytes that step() wants for M rows (a caller that captures a graph runs one step before, of the same size)."""
+        """Bytes of workspace of a step of M rows (a larger batch may need fewer)."""
         inner = self.n_q * self.head_dim
         sizes = [w2.workspace_size(M, self.hidden, self.width, self.G), w2.workspace_size(M, inner, self.hidden, self.G),
                  w2.tree_attention_workspace_size(batch.kv_len.shape[0], M, self.n_q, cache, batch.max_rows, batch.max_len,
@@ -56,10 +49,17 @@ class AttentionBlock:
         sizes += [w2.lora_workspace_size(a, M) for a in (self.qkv_lora, self.o_lora) if a is not None]
         return max(16, max(sizes))
 
-    def step(self, X, cache, batch):
-        """X (fp32 or bf16 [M, hidden]) -> bf16 [M, hidden]; the rows' keys and values go into `cache` (binding.KVCache)."""
+    def step(self, X, cache, batch, workspace=None):
+        """X (fp32 or bf16 [M, hidden]) -> bf16 [M, hidden]; the rows' keys and values go into `cache` (binding.KVCache).
+
+        `workspace`: a uint8 device tensor of workspace_size(M, batch, cache) bytes or more, which is the step's alone until it has
+        run; None: allocated for the step, like the tensors between its calls, from the current stream's memory (in a graph's
+        capture: from the graph's own)."""
         M = X.shape[0]
-        ws = self._workspace(self.workspace_size(M, batch, cache), X.device)
+        need = self.workspace_size(M, batch, cache)
+        ws = torch.empty(need, dtype=torch.uint8, device=X.device) if workspace is None else workspace
+        if ws.numel() < need:
+            raise ValueError(f"workspace has {ws.numel()} bytes, the step needs {need}")
         qkv = w2.matmul_a8_fused(self.wqkv, self.hidden, self.width, self.G, X, workspace=ws)
         if self.qkv_lora is not None and batch.adapter is not None:
             w2.lora_add(self.qkv_lora, X, batch.adapter, qkv, out=qkv, workspace=ws)

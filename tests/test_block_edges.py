@@ -1,0 +1,113 @@
+"""The operators between the projections where numbers are not finite, lengths disagree and buffers are shared.
+
+Bounds as in test_block_ops.py.  Where a number that is not finite reaches a result by the formula, the result's numbers that it
+reaches are compared by kind (NaN, +infinity, -infinity), all others as usual.
+"""
+import pytest
+
+from test_block_ops import block_and_cache, normal
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def w2():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2508_06753_amd import binding
+    return binding
+
+
+# ------------------------------------------------------------------ the block's workspace
+def test_a_step_keeps_no_memory(monkeypatch):
+    """Every call of a step gets the caller's workspace, or one that is the step's own; the block holds none behind it."""
+    from paper_2508_06753_amd import attention_block as ab
+    given = []
+
+    def call(shape):
+        def run(*args, workspace=None, out=None, **kw):
+            given.append(workspace)
+            return torch.zeros(shape(*args)) if out is None else out
+        return run
+
+    hidden, n_q, n_kv, D = 512, 4, 2, 64
+    width = (n_q + 2 * n_kv) * D
+    sizes = dict(matmul=0)
+    monkeypatch.setattr(ab.w2, "workspace_size", lambda *a: sizes["matmul"])
+    monkeypatch.setattr(ab.w2, "tree_attention_workspace_size", lambda *a: 1000)
+    monkeypatch.setattr(ab.w2, "lora_workspace_size", lambda *a: 300)
+    monkeypatch.setattr(ab.w2, "matmul_a8_fused", call(lambda w, K, N, G, X: (X.shape[0], N)))
+    monkeypatch.setattr(ab.w2, "lora_add", call(None))
+    monkeypatch.setattr(ab.w2, "qk_norm_rope", lambda x, n, *a, **kw: torch.zeros(x.shape[0], n, D))
+    monkeypatch.setattr(ab.w2, "tree_attention", call(lambda q, *a: q.shape))
+    lora = object()
+    block = ab.AttentionBlock(None, None, hidden, n_q, n_kv, D, 64, None, qkv_lora=lora, o_lora=lora)
+    state = dict(vars(block))
+    zeros = torch.zeros(2, dtype=torch.int32)
+    batch = ab.Batch(zeros, zeros.long(), zeros.view(2, 1), torch.zeros(3, dtype=torch.int32), zeros, 1, 1, adapter=zeros)
+    X = torch.zeros(2, hidden)
+    assert block.workspace_size(2, batch, None) == 1000
+    block.step(X, None, batch)
+    first = list(given)
+    assert len(first) == 5 and all(w is first[0] and w.numel() >= 1000 for w in first)
+    sizes["matmul"] = 5000
+    block.step(X, None, batch)
+    assert len(given) == 10 and all(w is given[5] and w.numel() >= 5000 for w in given[5:])
+    assert given[5].data_ptr() != first[0].data_ptr(), "two steps that have not run share memory"
+    assert vars(block) == state, "the block holds what a step used"
+    mine = torch.zeros(6000, dtype=torch.uint8)
+    block.step(X, None, batch, workspace=mine)
+    assert len(given) == 15 and all(w is mine for w in given[10:])
+    with pytest.raises(ValueError):
+        block.step(X, None, batch, workspace=mine[:4999])
+    assert len(given) == 15
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("own", [False, True])
+def test_a_captured_step_outlives_larger_ones(w2, own):
+    """A graph of a small step replayed behind a larger eager one: its result, and nothing of what was allocated since."""
+    ab, block, cache = block_and_cache(w2)
+    table = torch.arange(20, dtype=torch.int32).view(2, 10).contiguous().cuda()
+    block.step(normal(1, 90, block.hidden, dtype=torch.float32), cache, ab.causal_batch([0, 0], [50, 40], table, 16, "cuda", [0, 1]))
+    batch = ab.tree_batch([50, 40], [[-1, 0, 0], [-1, 0]], table, 16, "cuda", [1, 0])
+    X = normal(2, 5, block.hidden, dtype=torch.float32)
+    ws = torch.empty(block.workspace_size(5, batch, cache), dtype=torch.uint8, device="cuda") if own else None
+    block.step(X, cache, batch, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = block.step(X, cache, batch, workspace=ws)
+    other = w2.KVCache(torch.zeros(24, 16, block.n_kv, block.head_dim, dtype=torch.bfloat16, device="cuda"),
+                       torch.zeros(24, 16, block.n_kv, block.head_dim, dtype=torch.bfloat16, device="cuda"))
+    large = ab.causal_batch([0, 0], [150, 140], table, 16, "cuda", [0, 1])
+    for i in range(4):
+        block.step(normal(3 + i, 290, block.hidden, dtype=torch.float32), other, large)
+        marks = [torch.full((n,), 0x5a, dtype=torch.uint8, device="cuda") for n in (1 << 12, 1 << 16, 1 << 20, 1 << 22) for _ in range(3)]
+        X.copy_(normal(20 + i, 5, block.hidden, dtype=torch.float32))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        assert all((m == 0x5a).all() for m in marks), f"replay {i} wrote into memory of others"
+        assert torch.equal(got, block.step(X, cache, batch)), f"replay {i}"
+
+
+@pytest.mark.gpu
+def test_steps_on_two_streams(w2):
+    ab, block, _ = block_and_cache(w2)
+    table = torch.arange(20, dtype=torch.int32).view(2, 10).contiguous().cuda()
+    batches = [ab.causal_batch([0, 0], n, table, 16, "cuda", [0, 1]) for n in ([150, 140], [33, 71])]
+    rows = [normal(1 + i, b.positions.shape[0], block.hidden, dtype=torch.float32) for i, b in enumerate(batches)]
+    caches = [w2.KVCache(*(torch.zeros(24, 16, block.n_kv, block.head_dim, dtype=torch.bfloat16, device="cuda") for _ in range(2))) for _ in rows]
+    alone = [block.step(x, c, b) for x, c, b in zip(rows, caches, batches)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in rows]
+    results = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                results[i].append(block.step(rows[i], caches[i], batches[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(y, alone[i]) for y in results[i]), f"stream {i}"
