@@ -356,7 +356,9 @@ typedef struct {
     int n_adapters, max_rank, n_parts, gated;
 } w2_lora_t;
 
-/* Bytes of workspace (host out-pointer) that w2_lora_add needs for M rows. */
+/* Bytes of workspace (host out-pointer) that w2_lora_add wants for M rows: several parts of K where rows are few, so that fewer
+ * rows may want more.  With less it cuts K into fewer parts; one part is M * parts * max_rank floats (parts: n_parts, or 2 if
+ * gated), so that the size for the largest batch of a program serves all of them. */
 W2_API int w2_lora_workspace_size(const w2_lora_t* lora, int64_t M, int64_t K, int64_t N, size_t* bytes);
 
 /* X        dev, fp32 or bf16 [M][K], row stride ldx
@@ -367,7 +369,8 @@ W2_API int w2_lora_workspace_size(const w2_lora_t* lora, int64_t M, int64_t K, i
  * Y        dev, bf16 [M][N] ([M][N/2] for W2_ACT_SILU_MUL), row stride ldy; may be base itself except for
  *          W2_ACT_SILU_MUL
  * act      w2_act_t
- * workspace  dev, 16-byte aligned, w2_lora_workspace_size bytes, contents undefined before and after
+ * workspace  dev, 16-byte aligned, w2_lora_workspace_size bytes, or at least those of one part, contents undefined before and
+ *          after
  * K % 256 == 0, N % 8 == 0, as for the projections; ldb and ldy below 2^25. */
 W2_API int w2_lora_add(const w2_lora_t* lora, int64_t K, int64_t N, const void* X, w2_dtype_t x_dtype, int64_t ldx,
                        int64_t M, const int32_t* adapter, const uint16_t* base, int64_t ldb, uint16_t* Y, int64_t ldy,

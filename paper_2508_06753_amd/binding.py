@@ -435,7 +435,7 @@ def lora_workspace_size(lora, M):
 def lora_add(lora, X, adapter, base, act=ACT_NONE, out=None, workspace=None):
     """Y bf16 = act(base + scale * (X A^T) B^T), each row of X (fp32 or bf16 [M,K]) with the adapter that `adapter` (int32
     [M], -1: none) names.  `base`: bf16 [M,N], the projection's result before its activation, or None for zero.
-    `workspace`: a uint8 device tensor of lora_workspace_size(lora, M) bytes; allocated here if None."""
+    `workspace`: a uint8 device tensor of lora_workspace_size(lora, M) bytes, or of a larger batch's; allocated here if None."""
     xdt = X.dtype
     if xdt is not _F32 and xdt is not _BF16:
         raise ValueError("X must be float32 or bfloat16")

@@ -118,11 +118,11 @@ int w2_lora_add(const w2_lora_t* lora, int64_t K, int64_t N, const void* X, w2_d
     for (int p = 0; p < 4; ++p) a.end16[p] = a.gated || p >= a.n_parts ? 0x7fffffff : (int)((lora->part_end[p] + 15) / 16);
     a.X = X; a.x_f32 = x_dtype == W2_DT_F32; a.adapter = adapter; a.base = base; a.Y = Y;
     a.K = K; a.N = N; a.M = M; a.ldx = ldx; a.ldb = ldb; a.ldy = ldy; a.act = act;
-    const size_t need = lora_workspace_bytes(a.n_parts, a.R, a.n_adapters, M, K, N);
+    const size_t need = lora_part_bytes(a.n_parts, a.R, M);
     if (!workspace || workspace_bytes < need)
         return fail(W2_ERR_BUFFER_TOO_SMALL, "%s: workspace_bytes %zu < %zu", fn, workspace ? workspace_bytes : (size_t)0, need);
     a.T = (float*)workspace;
-    return launch_lora(a, (hipStream_t)stream);
+    return launch_lora(a, workspace_bytes, (hipStream_t)stream);
 }
 
 int w2_rope_phases(double base, int rotary_dim, w2_rope_scaling_t scaling, double factor, double original_len, double low,

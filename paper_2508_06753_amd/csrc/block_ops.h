@@ -47,7 +47,8 @@ struct LoraArgs {
     float* T;                           // the workspace: [K ranges][M][parts * R]
 };
 size_t lora_workspace_bytes(int n_parts, int R, int n_adapters, int64_t M, int64_t K, int64_t N);
-int launch_lora(const LoraArgs& a, hipStream_t stream);
+size_t lora_part_bytes(int n_parts, int R, int64_t M);      // of T for one part of K
+int launch_lora(const LoraArgs& a, size_t room, hipStream_t stream);       // room: bytes at a.T, at least one part's
 
 struct RopeArgs {
     const uint16_t* x;

@@ -614,15 +614,19 @@ int launch_expand(const LoraArgs& a, const Plan& p, hipStream_t stream)
 
 }  // namespace
 
+size_t lora_part_bytes(int n_parts, int R, int64_t M) { return (size_t)M * n_parts * R * sizeof(float); }
+
 size_t lora_workspace_bytes(int n_parts, int R, int n_adapters, int64_t M, int64_t K, int64_t N)
 {
     if (M == 0) return 0;
-    return ((size_t)make_plan(n_parts, R, n_adapters, M, K, N).ks * M * n_parts * R * sizeof(float) + 255) & ~(size_t)255;
+    return (make_plan(n_parts, R, n_adapters, M, K, N).ks * lora_part_bytes(n_parts, R, M) + 255) & ~(size_t)255;
 }
 
-int launch_lora(const LoraArgs& a, hipStream_t stream)
+int launch_lora(const LoraArgs& a, size_t room, hipStream_t stream)
 {
-    const Plan p = make_plan(a.n_parts, a.R, a.n_adapters, a.M, a.K, a.N);
+    Plan p = make_plan(a.n_parts, a.R, a.n_adapters, a.M, a.K, a.N);
+    // (as many parts of K as the workspace holds: fewer rows may want more room)
+    p.ks = (int)std::min<size_t>(p.ks, room / lora_part_bytes(a.n_parts, a.R, a.M));
     if (const int rc = a.x_f32 ? launch_shrink<true>(a, p, stream) : launch_shrink<false>(a, p, stream)) return rc;
     const int S = (a.R + 31) / 32;
     if (a.act == ACT_SILU_MUL)

@@ -3,9 +3,11 @@
 Bounds as in test_block_ops.py.  Where a number that is not finite reaches a result by the formula, the result's numbers that it
 reaches are compared by kind (NaN, +infinity, -infinity), all others as usual.
 """
+import numpy as np
 import pytest
 
-from test_block_ops import block_and_cache, normal
+from oracle import block_oracle as want
+from test_block_ops import U, block_and_cache, f64, near, normal
 
 torch = pytest.importorskip("torch")
 
@@ -16,6 +18,10 @@ def w2():
         pytest.skip("no GPU")
     from paper_2508_06753_amd import binding
     return binding
+
+
+def i32(x):
+    return torch.tensor(np.asarray(x, np.int32), device="cuda")
 
 
 # ------------------------------------------------------------------ the block's workspace
@@ -111,3 +117,26 @@ def test_steps_on_two_streams(w2):
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(y, alone[i]) for y in results[i]), f"stream {i}"
+
+
+# ------------------------------------------------------------------ adapters
+@pytest.mark.gpu
+@pytest.mark.parametrize("xdt", [torch.float32, torch.bfloat16])
+def test_a_workspace_for_many_rows_serves_fewer(w2, xdt):
+    """Parts of K are as many as the workspace holds: the size for a program's largest batch is enough for all of them."""
+    K, N, n, R = 4096, 256, 5, 64
+    lora = w2.Lora(normal(1, n, 2 * R, K, std=0.02), normal(2, n, N, R), gated=True)
+    sizes = {M: w2.lora_workspace_size(lora, M) for M in (1, 9, 40, 300, 1200, 4000)}
+    assert max(sizes.values()) > sizes[4000], "the case is about sizes that fall"
+    ws = torch.full((sizes[4000],), 0xff, dtype=torch.uint8, device="cuda")
+    for M in sizes:
+        rng = np.random.default_rng(M)
+        X, base, ad = normal(3, M, K, dtype=xdt), normal(4, M, N), rng.integers(-1, n, M).astype(np.int32)
+        for room in (ws, ws[:(M * 2 * R * 4 + 255) // 256 * 256]):  # (the least: one part)
+            Y = w2.lora_add(lora, X, i32(ad), base, workspace=room)
+            rows = rng.permutation(M)[:40]
+            ref, mag = want.lora(f64(X)[rows], f64(lora.A), f64(lora.B), ad[rows], f64(base)[rows], None, None, np.arange(N) // 16 % 2, 0)
+            near(f64(Y)[rows], ref, U * np.abs(ref) + 2.0 ** -13 * mag, f"{M} rows in {room.numel()} bytes")
+        if M * 2 * R * 4 > 256:
+            with pytest.raises(w2.W2Error):
+                w2.lora_add(lora, X, i32(ad), base, workspace=ws[:M * 2 * R * 4 - 256])
