@@ -438,8 +438,8 @@ W2_API int w2_qk_norm_rope(const uint16_t* x, int64_t ldx, int64_t M, int n_q, c
  * page_table dev, int32 [n_requests][table_cols], row stride ld_table; a number outside 0..n_pages-1: the keys of that
  *            page are not seen
  * row_start  dev, int32 [n_requests + 1], not decreasing, at most M;  kv_len  dev, int32 [n_requests]
- * max_rows, max_len  at least every T_r and kv_len[r] (the launch is planned by them; rows and keys past them are left
- *            out);  total_len  the sum of kv_len, or 0: not known
+ * max_rows, max_len  at least every T_r and kv_len[r] (the launch is planned by them; rows past max_rows are not written,
+ *            keys past max_len and past the page table's columns are not seen);  total_len  the sum of kv_len, or 0: not known
  * mask       dev, [M][mask_words] words of 64 bits, bit j in word j / 64; NULL: causal
  * workspace  optional (NULL / 0: none), 16-byte aligned: with w2_tree_attention_workspace_size bytes the keys of a
  *            request are shared out over several workgroups where the batch is small, and a second launch joins them

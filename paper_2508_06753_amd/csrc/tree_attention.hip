@@ -175,7 +175,7 @@ struct Work {
 // A request's rows and keys as one workgroup sees them.
 struct Span {
     int64_t first;                       // first row
-    int T, rows, len, ctx;               // drafted tokens, packed rows, keys, committed keys
+    int T, rows, len, ctx;               // drafted tokens, packed rows, keys that are not left out, committed keys (may be more)
     int n_chunks;
 };
 
@@ -186,9 +186,10 @@ __device__ __forceinline__ Span make_span(const Work& w, int r)
     s.first = lo;
     s.T = (int)max(min(hi - lo, w.a.M), (int64_t)0);
     s.rows = (int)min((int64_t)s.T, w.a.max_rows) * w.a.G;
-    const int64_t len = min(min((int64_t)scalar_load(w.a.kv_len, r), w.a.max_len), w.a.table_cols * w.a.cache.page_size);
-    s.len = (int)max(len, (int64_t)0);
-    s.ctx = s.len - s.T;
+    // (keys past max_len and the page table are left out; the drafted ones are the last of all)
+    const int keys = max(scalar_load(w.a.kv_len, r), 0);
+    s.len = (int)min(min((int64_t)keys, w.a.max_len), w.a.table_cols * w.a.cache.page_size);
+    s.ctx = keys - s.T;
     s.n_chunks = max(1, (int)(((uint32_t)s.len + w.chunk - 1) / w.chunk));
     return s;
 }

@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from oracle import block_oracle as want
-from test_block_ops import U, block_and_cache, f64, near, normal
+from test_block_ops import U, block_and_cache, f64, near, normal, tree_masks
 
 torch = pytest.importorskip("torch")
 
@@ -140,3 +140,89 @@ def test_a_workspace_for_many_rows_serves_fewer(w2, xdt):
         if M * 2 * R * 4 > 256:
             with pytest.raises(w2.W2Error):
                 w2.lora_add(lora, X, i32(ad), base, workspace=ws[:M * 2 * R * 4 - 256])
+
+
+# ------------------------------------------------------------------ attention
+class Requests:
+    """Requests of (keys, drafted tokens) over a cache whose pages are in some order; the oracle's view of them."""
+
+    def __init__(self, w2, requests, hq, hkv, D, page=16, seed=0, masks=None, scale=None):
+        self.w2, self.requests, self.hq, self.hkv, self.D, self.page = w2, requests, hq, hkv, D, page
+        self.scale = D ** -0.5 if scale is None else scale
+        rng = np.random.default_rng(seed)
+        need = [(n + page - 1) // page for n, _ in requests]
+        self.pages, self.M = sum(need) + 1, sum(t for _, t in requests)
+        order = rng.permutation(self.pages).astype(np.int32)
+        self.table = np.full((len(requests), max(need)), -1, np.int32)
+        self.starts = np.concatenate([[0], np.cumsum([t for _, t in requests])])
+        for r, c in enumerate(need):
+            self.table[r, :c] = order[sum(need[:r]):sum(need[:r + 1])]
+        self.k, self.v = normal(seed + 1, self.pages, page, hkv, D), normal(seed + 2, self.pages, page, hkv, D)
+        self.q = normal(seed + 3, self.M, hq, D, std=1.5)
+        self.mask = None
+        if masks is not None:
+            words = max(m.shape[1] for m in masks)
+            self.mask = np.zeros((self.M, words), np.uint64)
+            for r, m in enumerate(masks):
+                self.mask[self.starts[r]:self.starts[r + 1], :m.shape[1]] = m
+
+    def place(self, r, c):
+        return int(self.table[r, c // self.page]), c % self.page
+
+    def run(self, split=True, max_len=None, cols=None, lse=True, kv_len=None):
+        w2 = self.w2
+        cache = w2.KVCache(self.k, self.v)
+        most_t = max(t for _, t in self.requests)
+        most_n = max(n for n, _ in self.requests) if max_len is None else max_len
+        ws = None
+        if split:
+            size = w2.tree_attention_workspace_size(len(self.requests), self.M, self.hq, cache, most_t, most_n)
+            ws = torch.full((max(16, size),), 0xff, dtype=torch.uint8, device="cuda")
+        out = torch.full((self.M, self.hq, self.D), 7.0, dtype=torch.bfloat16, device="cuda")
+        L = torch.full((self.M, self.hq), 9.0, device="cuda")
+        table = i32(self.table if cols is None else self.table[:, :cols])
+        w2.tree_attention(self.q, cache, table, i32(self.starts), i32([n for n, _ in self.requests] if kv_len is None else kv_len), most_t, most_n,
+                          mask=None if self.mask is None else torch.tensor(self.mask.view(np.int64), device="cuda"),
+                          scale=self.scale, out=out, lse=L, workspace=ws)
+        return f64(out), f64(L)
+
+    def oracle(self, r, clip=None):
+        """One request's (out, lse, magnitude of the terms, largest score's terms); `clip`: keys from there on are left out."""
+        n, t = self.requests[r]
+        c = np.arange(n)
+        p = self.table[r, c // self.page]
+        k, v = f64(self.k)[p, c % self.page], f64(self.v)[p, c % self.page]
+        if clip is not None:
+            k[clip:] = np.nan
+        rows = slice(self.starts[r], self.starts[r + 1])
+        return want.attention(f64(self.q)[rows], k, v, t, None if self.mask is None else self.mask[rows], self.scale)
+
+    def check(self, got, what, clip=None):
+        out, lse = got
+        for r in range(len(self.requests)):
+            ref, ref_l, mag, big = self.oracle(r, clip)
+            rows = slice(self.starts[r], self.starts[r + 1])
+            near(out[rows], ref, U * np.abs(ref) + 2 * U * mag, f"{what}, request {r}")
+            empty = np.isinf(ref_l)
+            assert np.array_equal(np.isneginf(lse[rows]), empty), f"{what}, request {r}: rows that see nothing"
+            near(lse[rows][~empty], ref_l[~empty], (self.D + 8) * 2.0 ** -24 * big + 2.0 ** -18, f"{what}, request {r} lse")
+
+
+# heads, drafted tokens: the kernel for few rows (eight waves, four, two row tiles), the one for many
+FEW = [(8, 8, 64, 1), (8, 2, 128, 3), (8, 2, 128, 7), (4, 2, 256, 5)]
+MANY = [(8, 2, 128, 12), (8, 2, 64, 70), (8, 2, 256, 40), (6, 2, 96, 40)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,D,t", FEW + MANY)
+@pytest.mark.parametrize("masked", [False, True])
+def test_keys_past_the_limits_are_left_out(w2, hq, hkv, D, t, masked):
+    """kv_len above max_len, and above what the page table covers: the first keys, seen as if the others were there."""
+    rng = np.random.default_rng(t)
+    for n, page in ((300, 16), (1500, 16), (300, 24)):
+        for clip in (192, 288 if n == 300 else 1488, n - t):       # before the drafted tokens, among them, all of them away
+            clip = min(clip, n) // page * page
+            c = Requests(w2, [(n, t), (60, min(t, 60))], hq, hkv, D, page=page, seed=n + t, masks=[tree_masks(t, rng), tree_masks(min(t, 60), rng)] if masked else None)
+            c.check(c.run(max_len=clip), f"max_len {clip} of {n}, {t} tokens", clip)
+            c.check(c.run(cols=clip // page), f"{clip // page} pages of {page}, {n} keys, {t} tokens", clip)
+            c.check(c.run(cols=clip // page, split=False), f"{clip // page} pages of {page}, {n} keys, {t} tokens, one workgroup", clip)
