@@ -366,8 +366,8 @@ W2_API int w2_lora_workspace_size(const w2_lora_t* lora, int64_t M, int64_t K, i
  *          the row is act(base)
  * base     dev, bf16 [M][N], row stride ldb: the projection's result before its activation (a bias included), or
  *          NULL: zero
- * Y        dev, bf16 [M][N] ([M][N/2] for W2_ACT_SILU_MUL), row stride ldy; may be base itself except for
- *          W2_ACT_SILU_MUL
+ * Y        dev, bf16 [M][N] ([M][N/2] for W2_ACT_SILU_MUL), row stride ldy; may be base itself (ldy == ldb)
+ *          except for W2_ACT_SILU_MUL
  * act      w2_act_t
  * workspace  dev, 16-byte aligned, w2_lora_workspace_size bytes, or at least those of one part, contents undefined before and
  *          after

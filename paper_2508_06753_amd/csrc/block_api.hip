@@ -108,6 +108,7 @@ int w2_lora_add(const w2_lora_t* lora, int64_t K, int64_t N, const void* X, w2_d
     if (lora->a_stride < 0 || lora->a_stride % 8 || lora->b_stride < 0 || lora->b_stride % 8)
         return fail(W2_ERR_MISALIGNED, "%s: a_stride and b_stride must be multiples of 8, not negative", fn);
     if (act == ACT_SILU_MUL && base == Y) return fail(W2_ERR_INVALID_ARG, "%s: Y may not be base with the gated activation", fn);
+    if (base == Y && ldb != ldy) return fail(W2_ERR_INVALID_ARG, "%s: Y may be base only with the same row stride", fn);
     if ((base && ldb >= (int64_t)1 << 25) || ldy >= (int64_t)1 << 25)
         return fail(W2_ERR_UNSUPPORTED_SHAPE, "%s: ldb and ldy are limited to 2^25 - 8", fn);
     LoraArgs a = {};

@@ -3,6 +3,8 @@
 Bounds as in test_block_ops.py.  Where a number that is not finite reaches a result by the formula, the result's numbers that it
 reaches are compared by kind (NaN, +infinity, -infinity), all others as usual.
 """
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -120,6 +122,24 @@ def test_steps_on_two_streams(w2):
 
 
 # ------------------------------------------------------------------ adapters
+P = 4096                                                       # an aligned address that is never followed
+
+
+def add(w2, base=P, ldb=64, Y=2 * P, ldy=64, act=0, M=3, X=P, adapter=P, rank=None, scale=None):
+    lora = w2._LoraStruct(A=P, B=P, rank=rank, scale=scale, a_stride=256 * 16, b_stride=64 * 16, part_end=(ctypes.c_int64 * 4)(64, 0, 0, 0),
+                          n_adapters=2, max_rank=16, n_parts=1, gated=0)
+    return w2.raw().w2_lora_add(ctypes.byref(lora), 256, 64, X, w2.DT_BF16, 256, M, adapter, base, ldb, Y, ldy, act, P, 1 << 20, None)
+
+
+def test_adapters_in_place_need_one_stride():
+    # rows would be stored over rows that have not been read
+    from paper_2508_06753_amd import binding as w2
+    assert add(w2, base=P, Y=P, ldb=72, ldy=64) == w2.ERR_INVALID_ARG
+    assert add(w2, base=P, Y=P, ldb=64, ldy=128) == w2.ERR_INVALID_ARG
+    assert b"stride" in w2.raw().w2_last_error()
+    assert add(w2, base=P, Y=P, ldb=72, ldy=64, M=0) == 0
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("xdt", [torch.float32, torch.bfloat16])
 def test_a_workspace_for_many_rows_serves_fewer(w2, xdt):
