@@ -570,10 +570,11 @@ __global__ void __launch_bounds__(64 * W, DT == 256 ? 1 : 2) tree_few_kernel(Wor
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int v = 0; v < W; ++v) {
-                const float mv = ms[v * 16 + n], f = mv == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mv - top);
+                // (a wave whose keys the row does not see adds nothing; one without a maximum whose sum is NaN has seen NaN)
+                const float mv = ms[v * 16 + n], lv = ls[v * 16 + n], f = mv == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mv - top);
                 const float4 ov = *reinterpret_cast<const float4*>(os + (v * 16 + n) * LD + d);
-                if (mv != -INFINITY) {
-                    all = fmaf(ls[v * 16 + n], f, all);
+                if (mv != -INFINITY || lv != lv) {
+                    all = fmaf(lv, f, all);
                     acc.x = fmaf(ov.x, f, acc.x);
                     acc.y = fmaf(ov.y, f, acc.y);
                     acc.z = fmaf(ov.z, f, acc.z);

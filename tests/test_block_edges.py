@@ -246,3 +246,52 @@ def test_keys_past_the_limits_are_left_out(w2, hq, hkv, D, t, masked):
             c.check(c.run(max_len=clip), f"max_len {clip} of {n}, {t} tokens", clip)
             c.check(c.run(cols=clip // page), f"{clip // page} pages of {page}, {n} keys, {t} tokens", clip)
             c.check(c.run(cols=clip // page, split=False), f"{clip // page} pages of {page}, {n} keys, {t} tokens, one workgroup", clip)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,D,t", FEW + MANY)
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_queries_and_keys_that_are_not_finite_show(w2, hq, hkv, D, t, split, bad):
+    """A query with NaN or an infinity has no finite scores' softmax: its head's row is NaN, all others are as they were.  The same
+    of a key for the rows that see it."""
+    for n in (90, 1400):
+        c = Requests(w2, [(n, t), (50, 1)], hq, hkv, D, seed=n + t)
+        clean, clean_l = c.run(split)
+        c.check((clean, clean_l), f"{n} keys, {t} tokens")
+        row, head = t // 2, hq - 1
+        kept = c.q[row, head, 3].clone()
+        c.q[row, head, 3] = bad
+        out, lse = c.run(split)
+        assert np.isnan(out[row, head]).all() and np.isnan(lse[row, head]), f"{n} keys, {t} tokens: a row without a finite score"
+        out[row, head], lse[row, head] = clean[row, head], clean_l[row, head]
+        assert np.array_equal(out, clean) and np.array_equal(lse, clean_l), f"{n} keys, {t} tokens: the other rows"
+        c.q[row, head, 3] = kept
+        # the last drafted token's key: only the last row sees it
+        c.k[c.place(0, n - 1) + (hkv - 1, 5)] = float("nan")
+        out, lse = c.run(split)
+        hit = np.zeros(lse.shape, bool)
+        hit[t - 1, hq - hq // hkv:] = True
+        assert np.isnan(out[hit]).all() and np.isnan(lse[hit]).all(), f"{n} keys, {t} tokens: rows that see a key of NaN"
+        assert np.array_equal(out[~hit], clean[~hit]) and np.array_equal(lse[~hit], clean_l[~hit])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,D,t", FEW + MANY)
+@pytest.mark.parametrize("split", [False, True])
+def test_values_that_are_not_finite_show(w2, hq, hkv, D, t, split):
+    """A committed value that is NaN or infinite: that number of the outputs of its heads, and nothing else."""
+    for n in (90, 1400):
+        c = Requests(w2, [(n, t), (50, 1)], hq, hkv, D, seed=n + t)
+        clean, clean_l = c.run(split)
+        for at in (0, n - t - 1):
+            for bad in (float("nan"), float("inf")):
+                where = c.place(0, at) + (hkv - 1, D - 2)
+                kept = c.v[where].clone()
+                c.v[where] = bad
+                out, lse = c.run(split)
+                c.v[where] = kept
+                hit = np.zeros(out.shape, bool)
+                hit[:t, hq - hq // hkv:, D - 2] = True
+                assert not np.isfinite(out[hit]).any(), f"{n} keys, {t} tokens, value of key {at}"
+                assert np.array_equal(out[~hit], clean[~hit]) and np.array_equal(lse, clean_l)
