@@ -431,9 +431,9 @@ W2_API int w2_qk_norm_rope(const uint16_t* x, int64_t ldx, int64_t M, int n_q, c
  *   c < kv_len[r] - T_r, or bit j = c - (kv_len[r] - T_r) of the row's mask is set      (mask == NULL: j <= i)
  *   out = sum_c softmax_c(scale * q.k_c) v_c      lse = ln sum_c exp(scale * q.k_c)
  * over the keys seen, query heads in equal groups per cache head; a row that sees none: out 0, lse -infinity.  Keys
- * that no row of the request can see reach no result whatever their contents; a drafted token's own key and value are
- * multiplied by zero in the rows that do not see it, so they have to be finite.  T_r = 1 is plain decoding; no mask is
- * a causal chunk of a prompt.
+ * that no row of the request sees reach no result whatever their contents (a tree may be filled up with tokens that are
+ * not there); the value of a drafted token that some rows see is multiplied by zero in the others, so it has to be
+ * finite.  T_r = 1 is plain decoding; no mask is a causal chunk of a prompt.
  * q          dev, bf16 [M][n_q * head_dim], row stride ldq;  out  the same with ldo;  lse  dev, fp32 [M][n_q] or NULL
  * page_table dev, int32 [n_requests][table_cols], row stride ld_table; a number outside 0..n_pages-1: the keys of that
  *            page are not seen

@@ -202,10 +202,11 @@ __device__ __forceinline__ int head_of(const Work& w, uint32_t unit, int chunk, 
 }
 
 // Which of the keys base .. base + 3 (base a multiple of 4 from a tile's start on) the row sees, as 4 bits.
+template <bool MASK>
 __device__ __forceinline__ uint32_t seen4(const TreeArgs& a, const Span& sp, int64_t row, int t, uint64_t word0, uint32_t base)
 {
     const int j = (int)(base - (uint32_t)sp.ctx);            // drafted number of the first key
-    if (!a.mask) return j > t ? 0u : t - j >= 3 ? 15u : (2u << (t - j)) - 1u;
+    if (!MASK) return j > t ? 0u : t - j >= 3 ? 15u : (2u << (t - j)) - 1u;
     if (j <= -4) return 15u;
     if (j < 0) return (uint32_t)((word0 << -j) | ((1u << -j) - 1u)) & 15u;
     const uint64_t* const words = a.mask + row * a.mask_words;
@@ -329,6 +330,30 @@ __device__ __forceinline__ void scores(const char* kb, int l16, int q, const v4i
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) s[rt][t] = mfma(kf[t][ks], qf[rt][ks], s[rt][t]);
+}
+
+// A drafted key that no row sees (a tree filled up to its size) may hold anything: its weights are zeros, and its value has to be
+// made one.  Bits of keys, over the rows in 16 lanes (`halves`: 32)
+__device__ __forceinline__ uint32_t any_row(uint32_t x, bool halves)
+{
+    x |= (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xf, 0xf, true);       // quad_perm [1,0,3,2]
+    x |= (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xf, 0xf, true);       // quad_perm [2,3,0,1]
+    x |= (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xf, 0xf, true);      // row_half_mirror
+    x |= (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xf, 0xf, true);      // row_mirror
+    if (!halves) return x;
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return r[0] | r[1];
+}
+// masks of the eight values of a V^T operand, for the keys of eight bits
+__device__ __forceinline__ v4i value_masks(uint32_t seen)
+{
+    v4i m;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int lo = (int)(seen << (31 - 2 * e)) >> 31, hi = (int)(seen << (30 - 2 * e)) >> 31;
+        m[e] = (lo & 0xffff) | (hi & (int)0xffff0000);
+    }
+    return m;
 }
 
 // The running maximum (times c; -infinity: nothing seen yet), what is added to scores before the exponential, the lane's
@@ -492,16 +517,27 @@ __global__ void __launch_bounds__(64 * W, DT == 256 ? 1 : 2) tree_few_kernel(Wor
             wait_reads();
             fetch(false, kb);
         }
+        uint32_t seen = 0;                                   // by some row: the lane's keys, tile by tile
+        bool hidden = false;                                 // keys that are there and not seen
         if (valid != 0xffffffffu || base + 32 > ctx) {
+            uint32_t there = 0;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     uint32_t on = valid >> (16 * t + 4 * q) & 15u;
-                    if (base + 32 > ctx) on &= seen4(w.a, sp, x.row[rt], x.t[rt], x.word[rt], base + 16 * t + 4 * q);
+                    there |= on << 4 * t;
+                    const uint32_t key = base + 16 * t + 4 * q;
+                    if (base + 32 > ctx)
+                        on &= w.a.mask ? seen4<true>(w.a, sp, x.row[rt], x.t[rt], x.word[rt], key) : seen4<false>(w.a, sp, x.row[rt], x.t[rt], 0, key);
+                    seen |= on << 4 * t;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[rt][t][i] = on >> i & 1 ? s[rt][t][i] : -INFINITY;
                 }
+            if (w.a.mask && base + 32 > ctx) {               // (keys that are not there are zeros already)
+                seen = any_row(seen, false);
+                hidden = __builtin_amdgcn_ballot_w64((there & ~seen) != 0) != 0;
+            }
         }
         v4i hi[RT], lo[RT];
 #pragma unroll
@@ -525,6 +561,12 @@ __global__ void __launch_bounds__(64 * W, DT == 256 ? 1 : 2) tree_few_kernel(Wor
             const uint32_t at[4] = {vat[4 * g], vat[4 * g + 1], vat[4 * g + 2], vat[4 * g + 3]};
             v4i vt[4];
             read_vt<16 * DT * 2>(at, vt);
+            if (__builtin_expect(hidden, 0)) {
+                asm volatile("" : "+v"(seen));               // (masks are made here, not held in registers by the common path)
+                const v4i m = value_masks(seen);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vt[e] &= m;
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -647,7 +689,7 @@ __device__ __forceinline__ void read_vt32(uint32_t a0, uint32_t a1, uint32_t b0,
 // A wave holds 32 packed rows, one in lanes l and l + 32.  Scores: lane half h has keys 8 b + 4 h + i (b, i = 0..3) of a
 // stage, which are slots 4 b + i of the weights' operands.  The scores of the next stage are multiplied while this stage's
 // weights are made: matrix and vector instructions of one wave side by side.
-template <int DT, int W, bool P16>
+template <int DT, int W, bool P16, bool MASK>
 __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_kernel(Work w)
 {
     constexpr int KS = DT / 16, SB = stage_bytes<DT>();
@@ -674,7 +716,7 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
     const int waves = own.count, rho_wg = 32 * own.first;
     const uint32_t k0 = (uint32_t)chunk * w.chunk, ctx = max(sp.ctx, 0);
     uint32_t k1 = min((uint32_t)sp.len, k0 + w.chunk);
-    if (!w.a.mask) {                                         // causal: nothing past the tile's last token
+    if (!MASK) {                                             // causal: nothing past the tile's last token
         const int last = (int)divide((uint32_t)min(rho_wg + 32 * waves, sp.rows) - 1, w.by_g);
         k1 = max(k0, min(k1, (uint32_t)max(sp.ctx + last + 1, 0)));
     }
@@ -762,7 +804,7 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
     const bool idle = wave >= waves, live = !idle && rho < sp.rows;               // (idle: a wave without rows, which only loads)
     const int t = (int)divide((uint32_t)(live ? rho : 0), w.by_g), head = hk * w.a.G + (live ? rho : 0) - t * w.a.G;
     const int64_t row = sp.first + t;
-    const uint64_t word = w.a.mask ? w.a.mask[row * w.a.mask_words] : 0;
+    const uint64_t word = MASK ? w.a.mask[row * w.a.mask_words] : 0;
     v4i qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -813,6 +855,8 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
         constexpr int b = decltype(bc)::value, ahead = (b + RING - 1) % RING;
         constexpr bool INNER = decltype(kind)::value != CHECKED, WHOLE = decltype(kind)::value == WHOLE_HEADS;
         const uint32_t base = k0 + (uint32_t)st * 32;
+        uint32_t seen = 0;                                   // by some row: the lane's keys
+        bool hidden = false;                                 // keys that are there and not seen
         // the next stage is there; one behind it is under way
         if (INNER || st + 2 < stages) wait_loads<2 * LOADS>();
         else wait_loads<0>();
@@ -839,12 +883,19 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
                 valid[ahead] = fetch(st + RING - 1, ahead);
             }
             if (valid[b] != 0xffffffffu || base + 32 > ctx) {
+                uint32_t there = 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint32_t on = valid[b] >> (8 * e + 4 * h) & 15u;
-                    if (base + 32 > ctx) on &= seen4(w.a, sp, row, t, word, base + 8 * e + 4 * h);
+                    if (MASK) there |= on << 4 * e;
+                    if (base + 32 > ctx) on &= seen4<MASK>(w.a, sp, row, t, word, base + 8 * e + 4 * h);
+                    if (MASK) seen |= on << 4 * e;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) cur[4 * e + i] = on >> i & 1 ? cur[4 * e + i] : -INFINITY;
+                }
+                if (MASK && base + 32 > ctx) {               // (keys that are not there are zeros already)
+                    seen = any_row(seen, true);
+                    hidden = __builtin_amdgcn_ballot_w64((there & ~seen) != 0) != 0;
                 }
             }
         }
@@ -891,6 +942,15 @@ __global__ void __launch_bounds__(64 * W, W == 4 && DT < 256 ? 2 : 1) tree_tile_
 #pragma unroll
         for (int g = 0; g < DT / 64; ++g) {
             if (g) read_v(bc, g, vt);
+            if (MASK && !INNER && __builtin_expect(hidden, 0)) {
+                asm volatile("" : "+v"(seen));               // (masks are made here, not held in registers by the common path)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const v4i m = value_masks(seen >> 8 * k);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) vt[e][k] &= m;
+                }
+            }
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -1051,12 +1111,19 @@ int launch_few(const Work& w, bool p16, hipStream_t stream)
     return launch(p16 ? tree_few_kernel<DT, RT, W, true> : tree_few_kernel<DT, RT, W, false>, w, blocks, W, std::max(merge, tiles), stream);
 }
 
-template <int DT, int W>
+template <int DT, int W, bool MASK>
 int launch_tile(const Work& w, bool p16, hipStream_t stream)
 {
     const int64_t blocks = (int64_t)w.chunks * w.n_kv * w.tiles;
-    return p16 ? launch(tree_tile_kernel<DT, W, true>, w, blocks, W, tile_lds<DT, W, true>(), stream)
-               : launch(tree_tile_kernel<DT, W, false>, w, blocks, W, tile_lds<DT, W, false>(), stream);
+    return p16 ? launch(tree_tile_kernel<DT, W, true, MASK>, w, blocks, W, tile_lds<DT, W, true>(), stream)
+               : launch(tree_tile_kernel<DT, W, false, MASK>, w, blocks, W, tile_lds<DT, W, false>(), stream);
+}
+
+template <int DT>
+int launch_tile(const Work& w, int waves, bool p16, hipStream_t stream)
+{
+    if (w.a.mask) return waves == 2 ? launch_tile<DT, 2, true>(w, p16, stream) : launch_tile<DT, 4, true>(w, p16, stream);
+    return waves == 2 ? launch_tile<DT, 2, false>(w, p16, stream) : launch_tile<DT, 4, false>(w, p16, stream);
 }
 
 }  // namespace
@@ -1093,9 +1160,7 @@ int launch_tree_attention(const TreeArgs& a, hipStream_t stream)
         else if (p.waves == 8) rc = p.dt == 64 ? launch_few<64, 1, 8>(w, p16, stream) : launch_few<128, 1, 8>(w, p16, stream);
         else rc = p.dt == 64 ? launch_few<64, 1, 4>(w, p16, stream) : launch_few<128, 1, 4>(w, p16, stream);
     } else {
-        if (p.dt == 64) rc = p.waves == 2 ? launch_tile<64, 2>(w, p16, stream) : launch_tile<64, 4>(w, p16, stream);
-        else if (p.dt == 128) rc = p.waves == 2 ? launch_tile<128, 2>(w, p16, stream) : launch_tile<128, 4>(w, p16, stream);
-        else rc = p.waves == 2 ? launch_tile<256, 2>(w, p16, stream) : launch_tile<256, 4>(w, p16, stream);
+        rc = p.dt == 64 ? launch_tile<64>(w, p.waves, p16, stream) : p.dt == 128 ? launch_tile<128>(w, p.waves, p16, stream) : launch_tile<256>(w, p.waves, p16, stream);
     }
     if (rc || p.chunks < 2) return rc;
     int width = 1;

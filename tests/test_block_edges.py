@@ -295,3 +295,45 @@ def test_values_that_are_not_finite_show(w2, hq, hkv, D, t, split):
                 hit[:t, hq - hq // hkv:, D - 2] = True
                 assert not np.isfinite(out[hit]).any(), f"{n} keys, {t} tokens, value of key {at}"
                 assert np.array_equal(out[~hit], clean[~hit]) and np.array_equal(lse, clean_l)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,D,t", [h for h in FEW + MANY if h[3] > 1] + [(2, 2, 64, 100)])
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("page", [16, 24])
+def test_drafted_tokens_that_no_row_sees_may_hold_anything(w2, hq, hkv, D, t, split, page):
+    """A tree that is filled up to its size: tokens that are not there, whose keys and values were never written."""
+    rng = np.random.default_rng(t)
+    for n in (t, t + 77, 1400):
+        for hidden in ([0], [t - 1], list(range(t // 2, t)), list(range(0, t, 2)), list(range(t))):
+            own = tree_masks(t, rng)
+            for j in hidden:
+                own[:, j // 64] &= ~np.uint64(1 << (j % 64))
+            c = Requests(w2, [(n, t), (50, 1)], hq, hkv, D, page=page, seed=n + t, masks=[own, tree_masks(1, rng)])
+            ref = [c.oracle(r) for r in range(2)]
+            for j in hidden:
+                p, at = c.place(0, n - t + j)
+                c.k[p, at], c.v[p, at] = float("nan"), float("inf") if j % 2 else float("nan")
+            out, lse = c.run(split)
+            for r in range(2):
+                rows = slice(c.starts[r], c.starts[r + 1])
+                o, l, mag, big = ref[r]
+                what = f"{n} keys, {t} tokens, hidden {hidden[:3]}, request {r}"
+                near(out[rows], o, U * np.abs(o) + 2 * U * mag, what)
+                empty = np.isinf(l)
+                assert np.array_equal(np.isneginf(lse[rows]), empty), what
+                near(lse[rows][~empty], l[~empty], (D + 8) * 2.0 ** -24 * big + 2.0 ** -18, what + " lse")
+
+
+@pytest.mark.gpu
+def test_drafted_tokens_past_the_mask_may_hold_anything(w2):
+    # one word of mask, a hundred tokens: the last 36 are seen by nobody
+    own = tree_masks(100, np.random.default_rng(1))[:, :1].copy()
+    for hq, hkv, D in ((2, 2, 64), (4, 1, 128)):
+        c = Requests(w2, [(300, 100)], hq, hkv, D, masks=[own])
+        o, l, mag, _ = c.oracle(0)
+        for j in range(64, 100):
+            p, at = c.place(0, 200 + j)
+            c.k[p, at] = c.v[p, at] = float("nan")
+        out, _ = c.run()
+        near(out, o, U * np.abs(o) + 2 * U * mag, "mask of one word")
