@@ -159,14 +159,16 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(RopeArgs a, int per, 
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     const float e = 2 * i < VEC ? v0[(2 * i) % VEC] : v1[(2 * i) % VEC], o = 2 * i < VEC ? v0[(2 * i + 1) % VEC] : v1[(2 * i + 1) % VEC];
-                    y[2 * i] = e * c[i] - o * s[i];
-                    y[2 * i + 1] = o * c[i] + e * s[i];
+                    const bool turned = j * VEC + i < pairs;             // (the others meet nothing: they may be infinite)
+                    y[2 * i] = turned ? e * c[i] - o * s[i] : e;
+                    y[2 * i + 1] = turned ? o * c[i] + e * s[i] : o;
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    y[i] = v0[i] * c[i] - v1[i] * s[i];
-                    y[VEC + i] = v1[i] * c[i] + v0[i] * s[i];
+                    const bool turned = j * VEC + i < pairs;
+                    y[i] = v0[i] * c[i] - (turned ? v1[i] : 0.0f) * s[i];
+                    y[VEC + i] = v1[i] * c[i] + (turned ? v0[i] : 0.0f) * s[i];
                 }
             }
             Packed<VEC> y0 = u0[st], y1 = u1[st];            // (values stay)

@@ -337,3 +337,31 @@ def test_drafted_tokens_past_the_mask_may_hold_anything(w2):
             c.k[p, at] = c.v[p, at] = float("nan")
         out, _ = c.run()
         near(out, o, U * np.abs(o) + 2 * U * mag, "mask of one word")
+
+
+# ------------------------------------------------------------------ norm, rotation, cache
+@pytest.mark.gpu
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("D,rd", [(128, 96), (64, 0), (24, 12), (80, 60), (256, 4), (96, 72), (128, 64)])
+def test_numbers_that_are_not_rotated_meet_no_others(w2, D, rd, inter):
+    """Past the rotated part a number stays what it is, and so do its neighbours when it is NaN or infinite."""
+    M, hq, hkv = 5, 3, 2
+    x = normal(D + rd, M, (hq + 2 * hkv) * D)
+    y = x.view(M, -1, D)
+    for m in range(M):
+        for h in range(hq + hkv):
+            at = rd + (7 * m + 3 * h) % (D - rd)
+            y[m, h, at] = (float("inf"), float("nan"), -float("inf"))[(m + h) % 3]
+    clean = torch.where(torch.isfinite(y), y, torch.ones_like(y)).contiguous()
+    rope = w2.Rope(rd, interleaved=inter) if rd else None
+    pos = torch.arange(100, 100 + M, dtype=torch.int32, device="cuda")
+    results = []
+    for t in (x, clean.view(M, -1)):
+        k, v = (torch.zeros(1, 8, hkv, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        q = w2.qk_norm_rope(t, hq, rope, pos, w2.KVCache(k, v))
+        results.append(torch.cat((q, k[0, :M]), 1))
+    got, ref = results
+    bad = ~torch.isfinite(y[:, :hq + hkv])
+    assert torch.equal(got[~bad], ref[~bad]), "a neighbour changed"
+    assert torch.equal(torch.nan_to_num(got[bad]), torch.nan_to_num(y[:, :hq + hkv][bad])), "a number that is not finite changed"
+    assert torch.equal(torch.isnan(got[bad]), torch.isnan(y[:, :hq + hkv][bad]))
