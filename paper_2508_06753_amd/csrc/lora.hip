@@ -43,14 +43,30 @@ __device__ __forceinline__ void load_lds16(const void* src, char* dst)
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
-// eight floats as two bf16 parts whose sum has 16 bits of them
+constexpr float MOST_BF16 = 0x1.fep127f;
+
+// Eight floats as two bf16 parts whose sum has 16 bits of them.  FAR: numbers that are infinite, or round to infinity in bf16, are
+// among them: the first part stays finite, so that both have the number's sign, and the second is cut, so that the sum of a finite
+// number's is finite.
+template <bool FAR>
 __device__ __forceinline__ void split_bf16(const float (&f)[8], v4i& hi, v4i& lo)
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const uint32_t h = pack_bf16(f[2 * e], f[2 * e + 1]);
+        float a = f[2 * e], b = f[2 * e + 1];
+        if (FAR) {
+            a = __builtin_amdgcn_fmed3f(a, -MOST_BF16, MOST_BF16);
+            b = __builtin_amdgcn_fmed3f(b, -MOST_BF16, MOST_BF16);
+        }
+        const uint32_t h = pack_bf16(a, b);
+        a = f[2 * e] - __uint_as_float(h << 16);
+        b = f[2 * e + 1] - __uint_as_float(h & 0xffff0000u);
+        if (FAR) {
+            if (fabsf(f[2 * e]) > MOST_BF16) a = __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+            if (fabsf(f[2 * e + 1]) > MOST_BF16) b = __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+        }
         hi[e] = (int)h;
-        lo[e] = (int)pack_bf16(f[2 * e] - __uint_as_float(h << 16), f[2 * e + 1] - __uint_as_float(h & 0xffff0000u));
+        lo[e] = (int)pack_bf16(a, b);
     }
 }
 
@@ -60,13 +76,19 @@ __device__ __forceinline__ int part_of(const LoraArgs& a, int block)
     return (block >= a.end16[0]) + (block >= a.end16[1]) + (block >= a.end16[2]);
 }
 
-__device__ __forceinline__ void split_bf16(const v4i& x0, const v4i& x1, v4i& hi, v4i& lo)
+// of a row; top: the largest number that was split (not FAR)
+template <bool FAR>
+__device__ __forceinline__ void split_row(const v4i& x0, const v4i& x1, v4i& hi, v4i& lo, float& top)
 {
     float f[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = __int_as_float(e < 4 ? x0[e & 3] : x1[e & 3]);
-    split_bf16(f, hi, lo);
+    if (!FAR)
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) top = fmaxf(top, fmaxf(fabsf(f[e]), fabsf(f[e + 1])));
+    split_bf16<FAR>(f, hi, lo);
 }
+__device__ __forceinline__ bool is_far(float top) { return __builtin_expect(__builtin_amdgcn_ballot_w64(top > MOST_BF16) != 0, 0); }
 
 // One adapter's rows of a window.
 struct Tile {
@@ -155,9 +177,10 @@ __global__ void __launch_bounds__(256) lora_shrink_kernel(LoraArgs a, int slots,
             const bool live = row0 + l16 < t.count;
             const int64_t row = m0 + __shfl(t.row, (row0 + l16) & 63);
             const char* const xp = (const char*)a.X + (row * a.ldx + 8 * q) * (F32 ? 4 : 2);
-            v4f acc = {0.f, 0.f, 0.f, 0.f};
+            v4f acc;
+            float top = 0.0f;
             // U steps of 32: all loads first, then the products
-            auto span = [&](int k, auto uc) {
+            auto span = [&](int k, auto uc, auto far) {
                 constexpr int U = decltype(uc)::value;
                 v4i av[U], xv[U * (F32 ? 2 : 1)];
 #pragma unroll
@@ -178,17 +201,22 @@ __global__ void __launch_bounds__(256) lora_shrink_kernel(LoraArgs a, int slots,
                 for (int u = 0; u < U; ++u) {
                     if constexpr (F32) {
                         v4i hi, lo;
-                        split_bf16(xv[2 * u], xv[2 * u + 1], hi, lo);
+                        split_row<decltype(far)::value>(xv[2 * u], xv[2 * u + 1], hi, lo, top);
                         acc = mfma(av[u], lo, mfma(av[u], hi, acc));
                     } else {
                         acc = mfma(av[u], xv[u], acc);
                     }
                 }
             };
-            int k = kb;
-            for (; k + 128 <= ke; k += 128) span(k, std::integral_constant<int, 4>{});
-            for (; k + 64 <= ke; k += 64) span(k, std::integral_constant<int, 2>{});
-            if (k < ke) span(k, std::integral_constant<int, 1>{});
+            auto sum = [&](auto far) {
+                acc = (v4f){0.f, 0.f, 0.f, 0.f};
+                int k = kb;
+                for (; k + 128 <= ke; k += 128) span(k, std::integral_constant<int, 4>{}, far);
+                for (; k + 64 <= ke; k += 64) span(k, std::integral_constant<int, 2>{}, far);
+                if (k < ke) span(k, std::integral_constant<int, 1>{}, far);
+            };
+            sum(std::false_type{});
+            if (F32 && is_far(top)) sum(std::true_type{});
             // the four waves' sums, in order; lane: row l16 of the row tile, T's columns j0 + 4 q ..+ 3
             __syncthreads();
             part[wave * 64 + lane] = acc;
@@ -266,6 +294,7 @@ __global__ void __launch_bounds__(256) lora_shrink_tile_kernel(LoraArgs a, int s
 #pragma unroll
         for (int j = 0; j < J; ++j) acc[j] = (v4f){0.f, 0.f, 0.f, 0.f};
         const int xrow = wave * 16 + l16;
+        float top = 0.0f;
         for (int st = 0; st < n_st; ++st) {
             // this stage is there; up to N - 2 behind it are under way (at the end: none)
             if (st + N - 2 < n_st) wait_loads<(N - 2) * (XL + AL)>();
@@ -284,13 +313,28 @@ __global__ void __launch_bounds__(256) lora_shrink_tile_kernel(LoraArgs a, int s
                     const v4i x0 = *reinterpret_cast<const v4i*>(xb + ((2 * p ^ swz(xrow)) << 4));
                     const v4i x1 = *reinterpret_cast<const v4i*>(xb + (((2 * p + 1) ^ swz(xrow)) << 4));
                     v4i hi, lo;
-                    split_bf16(x0, x1, hi, lo);
+                    split_row<false>(x0, x1, hi, lo, top);
 #pragma unroll
                     for (int j = 0; j < J; ++j) acc[j] = mfma(av[j], lo, mfma(av[j], hi, acc[j]));
                 } else {
                     const v4i xv = *reinterpret_cast<const v4i*>(xb + ((p ^ swz(xrow)) << 4));
 #pragma unroll
                     for (int j = 0; j < J; ++j) acc[j] = mfma(av[j], xv, acc[j]);
+                }
+            }
+        }
+        if (F32 && is_far(top)) {                            // once more, straight from memory
+            const float* const x = (const float*)a.X + (m0 + __shfl(t.row, xrow < t.count ? xrow : 0)) * a.ldx + 8 * q;
+            const uint16_t* const A = a.A + t.adapter * a.a_stride + 8 * q;
+#pragma unroll
+            for (int j = 0; j < J; ++j) acc[j] = (v4f){0.f, 0.f, 0.f, 0.f};
+            for (int k = kb * 64; k < (kb + n_st) * 64; k += 32) {
+                v4i hi, lo;
+                split_row<true>(*reinterpret_cast<const v4i*>(x + k), *reinterpret_cast<const v4i*>(x + k + 4), hi, lo, top);
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const v4i av = *reinterpret_cast<const v4i*>(A + (int64_t)min(j0 + 16 * j + l16, PR - 1) * a.K + k);
+                    acc[j] = mfma(av, lo, mfma(av, hi, acc[j]));
                 }
             }
         }
@@ -399,7 +443,11 @@ __global__ void __launch_bounds__(256, NT == 1 ? (S == 1 ? 4 : S == 2 ? 3 : 2) :
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = 32 * s + 8 * q + i < rank ? f[i] * scale : 0.0f;
             v4i hi, lo;
-            split_bf16(f, hi, lo);
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
+            if (is_far(top)) split_bf16<true>(f, hi, lo);
+            else split_bf16<false>(f, hi, lo);
             v4i* dst = ts + ((p * row_tiles + n) * S + s) * 128 + lane;
             dst[0] = hi;
             dst[64] = lo;

@@ -162,6 +162,40 @@ def test_a_workspace_for_many_rows_serves_fewer(w2, xdt):
                 w2.lora_add(lora, X, i32(ad), base, workspace=ws[:M * 2 * R * 4 - 256])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 20, 150])
+@pytest.mark.parametrize("xdt", [torch.float32, torch.bfloat16])
+def test_infinite_rows_stay_infinite(w2, M, xdt):
+    """Row 0 has an infinity where all factors are positive: T is +infinity, and Y has the sign of B."""
+    K, N, R = 512, 96, 8
+    X, A, B, base = normal(1, M, K, dtype=xdt), normal(2, 1, R, K, std=0.05), normal(3, 1, N, R), normal(4, M, N)
+    A[:, :, 5] = A[:, :, 5].abs() + 0.01
+    B = (B.abs() + 0.01) * (1 - 2 * (torch.arange(N, device="cuda") % 2))[:, None]
+    B = B.bfloat16().contiguous()
+    lora, ad = w2.Lora(A, B), torch.zeros(M, dtype=torch.int32, device="cuda")
+    clean = w2.lora_add(lora, X, ad, base)
+    X[0, 5] = float("inf")
+    Y = w2.lora_add(lora, X, ad, base)
+    assert torch.equal(Y[1:], clean[1:]), "the other rows"
+    assert torch.equal(Y[0].float(), float("inf") * (1.0 - 2 * (torch.arange(N, device="cuda") % 2)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 20, 150])
+def test_largest_numbers_stay_finite(w2, M):
+    """Rows, and T, up to the largest fp32 number, which is past the largest of bf16."""
+    K, N, R = 512, 96, 8
+    X, A, B, base = normal(1, M, K, dtype=torch.float32), normal(2, 1, R, K, std=0.05), normal(3, 1, N, R, std=2.0 ** -100), normal(4, M, N)
+    A[:, :, 5] = 1.0
+    X[0, 5] = torch.finfo(torch.float32).max                    # T is that, too (the other terms are below its last bit)
+    X[M - 1, 5] = -torch.finfo(torch.float32).max
+    scale = torch.ones(1, device="cuda")
+    ad = np.zeros(M, np.int32)
+    ref, mag = want.lora(f64(X), f64(A), f64(B), ad, f64(base), None, [1.0], np.zeros(N, int), 0)
+    Y = w2.lora_add(w2.Lora(A, B, scale=scale), X, i32(ad), base)
+    near(Y, ref, U * np.abs(ref) + 2.0 ** -13 * mag, f"largest numbers, {M} rows")
+
+
 # ------------------------------------------------------------------ attention
 class Requests:
     """Requests of (keys, drafted tokens) over a cache whose pages are in some order; the oracle's view of them."""
