@@ -551,16 +551,18 @@ __global__ void __launch_bounds__(256, NT == 1 ? (S == 1 ? 4 : S == 2 ? 3 : 2) :
 #pragma unroll
                             for (int i = 0; i < 4; ++i) acc[i] = mfma(bv[i][s], tv[i >> 1][s][l], acc[i]);
                 } else if (rank > 0) {
+                    // (every part's sums for every column, and a lane keeps its columns' own: zeros in place of B would meet an infinite T)
+                    const int own[2] = {part_of(a, (int)((n0 + c0) >> 4)), part_of(a, (int)((n0 + c1) >> 4))};
                     for (int p = 0; p < a.n_parts; ++p)
 #pragma unroll
-                        for (int s = 0; s < S; ++s) {
-                            const v4i* src = ts + ((p * row_tiles + n) * S + s) * 128 + lane;
-                            const v4i hi = src[0], lo = src[64];
+                        for (int i = 0; i < 4; ++i) {
+                            v4f sum = acc[i];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const v4i b = part[i >> 1] == p ? bv[i][s] : (v4i){0, 0, 0, 0};
-                                acc[i] = mfma(b, lo, mfma(b, hi, acc[i]));
+                            for (int s = 0; s < S; ++s) {
+                                const v4i* src = ts + ((p * row_tiles + n) * S + s) * 128 + lane;
+                                sum = mfma(bv[i][s], src[64], mfma(bv[i][s], src[0], sum));
                             }
+                            acc[i] = own[i >> 1] == p ? sum : acc[i];
                         }
                 }
                 char* const dst = Y + (PAIRED ? n0 : 2 * n0) + (NT == 4 ? to[k] : row_offset(n, a.ldy) + 2 * (PAIRED ? 8 * q : c0));

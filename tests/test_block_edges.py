@@ -196,6 +196,31 @@ def test_largest_numbers_stay_finite(w2, M):
     near(Y, ref, U * np.abs(ref) + 2.0 ** -13 * mag, f"largest numbers, {M} rows")
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("act", [0, 2])
+@pytest.mark.parametrize("M", [1, 20, 150])
+def test_parts_do_not_meet_each_other(w2, gated, act, M):
+    """T of one part is past fp32's range: columns of the other parts are what they are."""
+    K, R, widths = 512, 16, [32, 16, 48]
+    N, P = sum(widths), 2 if gated else 3
+    X, A, B, base = normal(1, M, K), normal(2, 1, P * R, K, std=0.05), normal(3, 1, N, R), normal(4, M, N)
+    part = np.arange(N) // 16 % 2 if gated else np.repeat(np.arange(P), widths)
+    lora = lambda: w2.Lora(A, B, parts=None if gated else widths, gated=gated)  # noqa: E731
+    ad = np.zeros(M, np.int32)
+    A[:, :, 7] = 0
+    ref, mag = want.lora(f64(X), f64(A), f64(B), ad, f64(base), None, None, part, act)
+    X[:, 7] = 1e38
+    A[:, R:2 * R, 7] = 100.0                                     # part 1: infinite; the others: zero times 1e38
+    Y = f64(w2.lora_add(lora(), X, i32(ad), base, act=act))
+    out_part = part.reshape(-1, 2, 16)[:, 0].reshape(-1) if act == 2 else part
+    other = part.reshape(-1, 2, 16)[:, 1].reshape(-1) if act == 2 else part
+    keep = (out_part != 1) & (other != 1)
+    near(Y[:, keep], ref[:, keep], (U * np.abs(ref) + 2.0 ** -13 * mag)[:, keep], f"gated {gated}, act {act}, {M} rows")
+    if act == 0:
+        assert not np.isfinite(Y[:, ~keep]).any()
+
+
 # ------------------------------------------------------------------ attention
 class Requests:
     """Requests of (keys, drafted tokens) over a cache whose pages are in some order; the oracle's view of them."""
