@@ -101,6 +101,8 @@ int w2_lora_add(const w2_lora_t* lora, int64_t K, int64_t N, const void* X, w2_d
     if (!X || !adapter || !Y || !lora->A || !lora->B) return fail(W2_ERR_INVALID_ARG, "%s: NULL pointer", fn);
     if (!aligned16(X) || !aligned16(Y) || !aligned16(base) || !aligned16(lora->A) || !aligned16(lora->B) || !aligned16(workspace))
         return fail(W2_ERR_MISALIGNED, "%s: X, A, B, base, Y and workspace must be 16-byte aligned", fn);
+    if (((uintptr_t)adapter & 3) || ((uintptr_t)lora->rank & 3) || ((uintptr_t)lora->scale & 3))
+        return fail(W2_ERR_MISALIGNED, "%s: adapter, rank or scale is not aligned to its type", fn);
     const int64_t n_out = act == ACT_SILU_MUL ? N / 2 : N;
     if (ldx < K || ldx % 8) return fail(W2_ERR_MISALIGNED, "%s: ldx must be >= K and a multiple of 8", fn);
     if (base && (ldb < N || ldb % 8)) return fail(W2_ERR_MISALIGNED, "%s: ldb must be >= N and a multiple of 8", fn);
@@ -175,6 +177,8 @@ int w2_qk_norm_rope(const uint16_t* x, int64_t ldx, int64_t M, int n_q, const ui
     if (!x || !q) return fail(W2_ERR_INVALID_ARG, "%s: NULL pointer", fn);
     if (!aligned16(x) || !aligned16(q) || !aligned16(q_weight) || !aligned16(k_weight))
         return fail(W2_ERR_MISALIGNED, "%s: x, q and the weights must be 16-byte aligned", fn);
+    if (((uintptr_t)positions & 3) || ((uintptr_t)slots & 7))
+        return fail(W2_ERR_MISALIGNED, "%s: positions or slots is not aligned to its type", fn);
     if (ldx < (int64_t)(n_q + 2 * cache->n_heads) * D || ldx % 8)
         return fail(W2_ERR_MISALIGNED, "%s: ldx must be >= the heads' columns and a multiple of 8", fn);
     if (ldq < (int64_t)n_q * D || ldq % 8) return fail(W2_ERR_MISALIGNED, "%s: ldq must be >= n_q * head_dim and a multiple of 8", fn);

@@ -140,6 +140,18 @@ def test_adapters_in_place_need_one_stride():
     assert add(w2, base=P, Y=P, ldb=72, ldy=64, M=0) == 0
 
 
+def test_arrays_of_numbers_are_aligned_to_their_types():
+    # (the attention's are in test_block_ops.py)
+    from paper_2508_06753_amd import binding as w2
+    assert add(w2, adapter=P + 2) == add(w2, rank=P + 1) == add(w2, scale=P + 2) == w2.ERR_MISALIGNED
+    cache = w2._CacheStruct(k=P, v=P, n_pages=4, page_size=16, k_page_stride=2048, k_slot_stride=128, k_head_stride=64, v_page_stride=2048,
+                            v_slot_stride=128, v_head_stride=64, n_heads=2, head_dim=64)
+    rope = w2._RopeStruct(P, 64, 0, 1.0)
+    for positions, slots in ((P + 2, P), (P, P + 4)):
+        assert w2.raw().w2_qk_norm_rope(P, 512, 2, 4, None, None, 0.0, ctypes.byref(rope), positions, 2 * P, 256, ctypes.byref(cache), slots,
+                                        None) == w2.ERR_MISALIGNED
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("xdt", [torch.float32, torch.bfloat16])
 def test_a_workspace_for_many_rows_serves_fewer(w2, xdt):
