@@ -410,6 +410,94 @@ def test_drafted_tokens_past_the_mask_may_hold_anything(w2):
         near(out, o, U * np.abs(o) + 2 * U * mag, "mask of one word")
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,D", [(8, 2, 128), (8, 2, 64), (6, 2, 96), (4, 2, 256)])
+def test_single_tokens_agree_with_the_rows_of_a_chunk(w2, hq, hkv, D):
+    """The two kernels with each other: rows of a causal chunk, and each as the single token behind its predecessors."""
+    n, t = 500, 50
+    c = Requests(w2, [(n, t)], hq, hkv, D, seed=3)
+    out, lse = c.run()
+    c.check((out, lse), "chunk")
+    _, _, mag, big = c.oracle(0)
+    for i in (t - 1, 0, 17):
+        kept, c.requests, c.M, c.starts, q = c.requests, [(n - t + 1 + i, 1)], 1, [0, 1], c.q
+        c.q = q[i:i + 1]
+        one, one_l = c.run()
+        c.requests, c.M, c.starts, c.q = kept, t, [0, t], q
+        # both within the bounds of the oracle: twice them of each other
+        near(one[0], out[i], 2 * U * np.abs(out[i]) + 4 * U * mag[i], f"row {i}")
+        near(one_l[0], lse[i], 2 * ((D + 8) * 2.0 ** -24 * big + 2.0 ** -18), f"row {i} lse")
+
+
+def one_part(q, k, v, t, scale):
+    """Causal attention whose weights are rounded to bf16 once before they meet v: what the bound below has to notice."""
+    T, hq, D = q.shape
+    out = np.zeros((T, hq, D))
+    for i in range(T):
+        n = k.shape[0] - t + i + 1
+        for h in range(hq):
+            kv = h * k.shape[1] // hq
+            s = scale * (k[:n, kv] @ q[i, h])
+            p = np.exp(s - s.max())
+            out[i, h] = f64(torch.tensor(p).bfloat16()) @ v[:n, kv] / p.sum()
+    return out
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,D,t", FEW)
+@pytest.mark.parametrize("split", [False, True])
+def test_few_rows_hold_weights_in_sixteen_bits(w2, hq, hkv, D, t, split):
+    """The kernel for few rows multiplies weights in two bf16 parts: one rounding of the output, and of the terms 2^-16 for
+    the parts (2^-8 of 2^-8), 2^-18 of sums and exponentials, and twice the scores' own error, (D + 8) 2^-24 of their
+    terms.  Weights in one part leave that bound where keys are few."""
+    for n in (t + 2, t + 11, 70):
+        c = Requests(w2, [(n, t)] * 3, hq, hkv, D, seed=n + t)
+        out, _ = c.run(split)
+        noticed = 0
+        for r in range(3):
+            ref, _, mag, big = c.oracle(r)
+            rows = slice(c.starts[r], c.starts[r + 1])
+            bound = U * np.abs(ref) + (2.0 ** -16 + 2.0 ** -18 + 2 * (D + 8) * 2.0 ** -24 * big) * mag
+            near(out[rows], ref, bound, f"{n} keys, {t} tokens")
+            at = np.arange(n)
+            k, v = (f64(x)[c.table[r, at // c.page], at % c.page] for x in (c.k, c.v))
+            once = f64(torch.tensor(one_part(f64(c.q)[rows], k, v, t, c.scale)).bfloat16())
+            noticed += np.count_nonzero(np.abs(once - ref) > bound)
+        assert noticed > 0
+
+
+def plain_causal(q, k, v, n_drafted, scale):
+    """want.attention without a mask, for many rows at once: (out, lse, terms' magnitude, largest score's terms)."""
+    T, hq, D = q.shape
+    L, hkv, _ = k.shape
+    seen = np.arange(L)[None, :] <= np.arange(T)[:, None] + (L - n_drafted)
+    out, mag, lse, big = np.zeros((T, hq, D)), np.zeros((T, hq, D)), np.zeros((T, hq)), 0.0
+    for h in range(hq):
+        kk, vv = k[:, h * hkv // hq], v[:, h * hkv // hq]
+        s = np.where(seen, scale * (q[:, h] @ kk.T), -np.inf)
+        big = max(big, float(np.max(np.abs(scale) * (np.abs(q[:, h]) @ np.abs(kk).T))))
+        top = s.max(1, keepdims=True)
+        p = np.exp(s - top)
+        total = p.sum(1, keepdims=True)
+        lse[:, h] = (top + np.log(total))[:, 0]
+        out[:, h], mag[:, h] = p / total @ vv, p / total @ np.abs(vv)
+    return out, lse, mag, big
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,D,t,n", [(8, 1, 64, 1501, 1501), (16, 1, 128, 700, 1900), (32, 4, 128, 333, 333), (6, 2, 96, 901, 1203)])
+def test_prompts_of_many_row_tiles(w2, hq, hkv, D, t, n):
+    c = Requests(w2, [(n, t)], hq, hkv, D, seed=t)
+    at = np.arange(n)
+    k, v = (f64(x)[c.table[0, at // 16], at % 16] for x in (c.k, c.v))
+    ref, ref_l, mag, big = plain_causal(f64(c.q), k, v, t, c.scale)
+    few = want.attention(f64(c.q)[:1], k[:n - t + 1], v[:n - t + 1], 1, None, c.scale)[0]
+    assert np.abs(few - ref[:1]).max() < 1e-12
+    out, lse = c.run()
+    near(out, ref, U * np.abs(ref) + 2 * U * mag, f"{t} tokens")
+    near(lse, ref_l, (D + 8) * 2.0 ** -24 * big + 2.0 ** -18, f"{t} tokens, lse")
+
+
 # ------------------------------------------------------------------ norm, rotation, cache
 @pytest.mark.gpu
 @pytest.mark.parametrize("inter", [False, True])
