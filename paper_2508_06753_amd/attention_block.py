@@ -108,6 +108,7 @@ def tree_batch(starts, parents, page_table, page_size, device, adapter=None):
 
 
 def main():
+    """True: every row is finite, and none of zeros."""
     from . import synth
     hidden, n_q, n_kv, D, G, page, n_requests = 1024, 8, 2, 128, 128, 16, 3
     width = (n_q + 2 * n_kv) * D
@@ -130,13 +131,16 @@ def main():
     k = torch.zeros(64, page, n_kv, D, dtype=torch.bfloat16, device="cuda")
     cache = w2.KVCache(k, torch.zeros_like(k))
     table = torch.randperm(60, generator=torch.Generator().manual_seed(5))[:n_requests * 16].view(n_requests, 16).int().cuda()
-    adapter, lens = [0, 1, -1], [37, 120, 64]
+    adapter, lens, sound = [0, 1, -1], [37, 120, 64], True
     for what, batch in [("prompts", causal_batch([0, 0, 0], lens, table, page, "cuda", adapter)),
                         ("drafted trees", tree_batch(lens, [[-1, 0, 0, 1], [-1, 0, 1, 1, 0], [-1]], table, page, "cuda", adapter)),
                         ("single tokens", causal_batch(lens, [1, 1, 1], table, page, "cuda", adapter))]:
         X = torch.randn(batch.positions.shape[0], hidden, device="cuda", generator=torch.Generator(device="cuda").manual_seed(6))
         y = block.step(X, cache, batch)
-        print(f"{what}: {y.shape[0]} rows, rms {y.float().square().mean().sqrt().item():.3f}, finite {bool(torch.isfinite(y).all())}")
+        finite = bool(torch.isfinite(y).all())
+        sound &= finite and bool((y != 0).any(dim=1).all())
+        print(f"{what}: {y.shape[0]} rows, rms {y.float().square().mean().sqrt().item():.3f}, finite {finite}")
+    return sound
 
 
 if __name__ == "__main__":
