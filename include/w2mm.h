@@ -337,6 +337,7 @@ W2_API int w2_workspace_size(int64_t M, int64_t K, int64_t N, int G, int a16, si
  *   T[m,p,r] = sum_k X[m,k] A[a,p,r,k]                               (fp32)
  *   z[m,n]   = base[m,n] + scale[a] * sum_r T[m,p(n),r] B[a,n,r]      (fp32)
  *   Y        = bf16 of z, silu(z), or silu(z_gate) z_up               (one rounding)
+ * (T and fp32 X are multiplied with 16 bits of each number.)
  * A       dev, bf16, adapter a's row p*max_rank + r at A + a*a_stride + (p*max_rank + r)*K
  * B       dev, bf16, adapter a's column n at B + a*b_stride + n*max_rank
  * rank    dev, int32 [n_adapters], or NULL: every adapter has rank max_rank.  Entries of A and B at r >= rank[a]
@@ -434,12 +435,17 @@ W2_API int w2_qk_norm_rope(const uint16_t* x, int64_t ldx, int64_t M, int n_q, c
  * that no row of the request sees reach no result whatever their contents (a tree may be filled up with tokens that are
  * not there); the value of a drafted token that some rows see is multiplied by zero in the others, so it has to be
  * finite.  T_r = 1 is plain decoding; no mask is a causal chunk of a prompt.
+ * Scores, maxima, sums and outputs are held in fp32, and lse is of unrounded weights.  Before they meet V weights are
+ * rounded: to 16 bits where max_rows times the query heads of a cache head are up to 32 (16 for head_dim > 128), to bf16
+ * above, which changes an output by about as much as its own rounding does.  Where an infinity reaches an output, the
+ * output is infinite or NaN.
  * q          dev, bf16 [M][n_q * head_dim], row stride ldq;  out  the same with ldo;  lse  dev, fp32 [M][n_q] or NULL
  * page_table dev, int32 [n_requests][table_cols], row stride ld_table; a number outside 0..n_pages-1: the keys of that
  *            page are not seen
  * row_start  dev, int32 [n_requests + 1], not decreasing, at most M;  kv_len  dev, int32 [n_requests]
  * max_rows, max_len  at least every T_r and kv_len[r] (the launch is planned by them; rows past max_rows are not written,
- *            keys past max_len and past the page table's columns are not seen);  total_len  the sum of kv_len, or 0: not known
+ *            keys past max_len and past the page table's columns are not seen);  total_len  the sum of kv_len, or 0: not
+ *            known.  Rows of out and lse that no request owns are not written
  * mask       dev, [M][mask_words] words of 64 bits, bit j in word j / 64; NULL: causal
  * workspace  optional (NULL / 0: none), 16-byte aligned: with w2_tree_attention_workspace_size bytes the keys of a
  *            request are shared out over several workgroups where the batch is small, and a second launch joins them

@@ -75,7 +75,8 @@ class AttentionBlock:
 
 
 def causal_batch(starts, counts, page_table, page_size, device, adapter=None):
-    """The Batch of `counts` new tokens of each request behind `starts` committed ones: prompts, chunks, single tokens."""
+    """The Batch of `counts` new tokens of each request behind `starts` committed ones: prompts, chunks, single tokens.  Built row by
+    row on the host, from a copy of the page table that waits for the GPU: a program that serves keeps its own."""
     rows = [(r, starts[r] + i) for r in range(len(starts)) for i in range(counts[r])]
     i32 = dict(dtype=torch.int32, device=device)
     lens = [s + c for s, c in zip(starts, counts)]

@@ -541,8 +541,8 @@ def tree_attention(q, cache, page_table, row_start, kv_len, max_rows, max_len, m
 
     page_table int32 [requests, pages], row_start int32 [requests + 1], kv_len int32 [requests]; mask int64 [M, words], bit
     j: the row sees its request's drafted token j (None: causal); scale None: 1/sqrt(head_dim).  lse: fp32 [M, n_q], written
-    if given.  `workspace`: a uint8 device tensor of tree_attention_workspace_size bytes; None: the keys of a request are
-    not shared out over workgroups."""
+    if given.  Rows that no request owns are not written.  `workspace`: a uint8 device tensor of tree_attention_workspace_size
+    bytes; None: the keys of a request are not shared out over workgroups."""
     M, n_q, D = q.shape
     if D != cache.head_dim:
         raise ValueError("q must be [M, n_q, head_dim] of the cache's head_dim")

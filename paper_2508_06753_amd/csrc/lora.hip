@@ -6,14 +6,15 @@
 // the call.  An adapter's factors are read once a window.  Two launches: lora_shrink_kernel writes T, fp32, in `ks` parts
 // of K; lora_expand_kernel adds them in order and finishes Y.  Matrix instructions 16x16x32 with the factors' rows on one
 // side and the tile's rows on the other; numbers in 32 bits (T, and X if it is fp32) go in as two bf16 parts, 16 bits of
-// mantissa, in two instructions.
+// mantissa, in two instructions: the outputs' rounding to 8 hides it.
 //
-// Bound: few rows, by two launches and the trips to memory in each, one behind the other (whose adapter, its factors; T, the
-// stores): one row, K = 4096, 16 ranks, N = 6144: 4.0 + 5.3 us; 61 rows of 48 adapters, 37 MB: 12 + 10.3 us.  Many rows, by base
-// and Y: 4000 rows, K = 4096, 64 ranks, 28672 gated columns, 344 MB: 26 + 109 us, 3.2 TB/s in the second launch (a large copy: 4.75);
-// there two waves a SIMD (four row tiles of base and the factors in registers) load, multiply and store in turns.  Base by way
-// of local memory: 121 us; the next columns' base asked for before this one's products: no faster with all stores behind it,
-// slower among them.
+// Bound (kernels alone, in a trace): few rows, by two launches and the trips to memory in each, one behind the other (whose
+// adapter, its factors; T, the stores): one row, K = 4096, 16 ranks, N = 6144: 4.0 + 5.5 us; 61 rows of 48 adapters, 37 MB: 12.3 +
+// 10.9 us; 37 fp32 rows, K = 14336: 8.3 + 6.2, the first in 216 workgroups of four trips a wave.  Many rows, by base and Y: 4000
+// rows, K = 4096, 64 ranks, 28672 gated columns, 344 MB: 26 + 109 us, 3.2 TB/s in the second launch (a large copy: 4.75); there two
+// waves a SIMD (four row tiles of base and the factors in registers) load, multiply and store in turns.  Base by way of local
+// memory: 121 us; the next columns' base asked for before this one's products: no faster with all stores behind it, slower among
+// them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -621,13 +622,15 @@ Plan make_plan(int n_parts, int R, int n_adapters, int64_t M, int64_t K, int64_t
     // half, or one where they take 64 rows of A.  At most eight parts, four of a wide T: every part is written, and read again
     // by every group of columns (us, both launches, one row, K = 4096, 64 ranks, 16 parts: 12.5, 8: 11.0; 9 rows of 5 adapters
     // of 128: 22 and 20; 574 rows, 128 ranks, gated 34816 columns, 5 parts: 89, 4: 83; 218 fp32 rows of 384 ranks, 8 parts: 38,
-    // 4: 35).  A wave's share is 128 numbers or more, which are one trip to memory.
+    // 4: 35).  That is of K = 4096 and 5120; 37 rows of nine adapters and K = 14336 come to 216 workgroups, and eight parts have
+    // not been compared with more there.  A wave's share is 128 numbers or more, which are one trip to memory.
     const int64_t busy = std::min<int64_t>(M, p.windows - 1 + n_adapters) * p.groups, want = p.j == 4 ? 256 : p.many ? 384 : 2048;
     p.ks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want / std::max<int64_t>(busy, 1), p.j == 4 ? 4 : 8), K / 512));
     p.slots = slots_for(M, p.windows, p.groups * p.ks, n_adapters);
     // Columns of a workgroup: it reads T once for all of them, but the workgroups of a die (every eighth group of columns; room
     // for so many at once) should fill whole rounds: the number of rounds times the steps of one, and what it does before its
-    // first step, about half a step and the reading of T (bytes against those of a step).  4000 rows, 28672 gated columns,
+    // first step, about half a step and the reading of T (bytes against those of a step, 49152 of base and Y: gated columns with
+    // their activation; others have 65536, and are planned alike).  4000 rows, 28672 gated columns,
     // us with 1, 3, 5, 7, 13 steps: 152, 123, 117, 110, 152; 933 rows, 34816, with 1, 2, 3: 66, 63, 51.
     const int64_t blocks = (N + 255) / 256, most = p.many ? std::min<int64_t>(blocks, 16) : 1, room = 32 * (R <= 32 ? 3 : 2);
     const double start = 0.5 + (double)(n_parts * R * p.ks) * 256 / (49152 + 512 * R);

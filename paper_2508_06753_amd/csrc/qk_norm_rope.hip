@@ -10,8 +10,8 @@
 // whatever the position (fp32 positions times frequencies are off by 0.004 radians at 131072 already); the sine
 // instruction takes turns.
 //
-// Bound by memory: 8191 rows of 40 + 2 * 8 heads of 128, 235 MB, in 53 us, 4.4 TB/s (a large copy: 4.75); 96 rows in 4.6 us, one in
-// 3.7: a launch and two trips to memory.
+// Bound by memory: 8191 rows of 40 + 2 * 8 heads of 128, 235 MB, in 53 us, 4.4 TB/s (a large copy: 4.75); 96 rows in 4.5 us, one in
+// 4.0: a launch and two trips to memory.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -4,19 +4,23 @@
 // is read of K and V.  Scores are held transposed: S^T = K Q^T puts keys of one query row in a lane, which is the operand
 // layout of P^T in O^T = V^T P^T once the 32 keys of a step are numbered to suit: no weight crosses lanes.  V^T operands come
 // from local memory by the transposing read.  Running maximum and sum per query row (m, l) in fp32; the outputs are rescaled
-// only when a maximum has grown by more than 8 powers of two, which fp32 sums and bf16 weights carry without loss; the sum is
-// reduced over the lanes at the end.
+// only when a maximum has grown by more than 8 powers of two: weights up to 256, which neither fp32 sums nor bf16 weights overflow
+// by; the sum is reduced over the lanes at the end.
 //
+// Times by the caller's clock among other calls; kernels alone, in a trace, where one is named.
 // tree_few_kernel: up to 32 packed rows (decoding, small trees), 16x16x32 instructions.  Every wave of a workgroup takes other
-// keys, which go to local memory past the registers, and nothing else waits for them.  Bound by memory: 48 requests of one
-// token, up to 8000 keys, 8 heads of 128: 967 MB in 155 us, 6.2 TB/s (a plain read of so much: 7.1).  One request of 700 keys:
-// 9.7 us, a launch and six trips to memory.
+// keys, which go to local memory past the registers, and nothing else waits for them.  Weights meet V in two bf16 parts, 16 bits:
+// the matrix pipe has the room.  Bound by memory: 48 requests of one token, up to 8000 keys, 8 heads of 128: 967 MB in 155 us alone,
+// 6.2 TB/s (a plain read of so much: 7.1).  One request of 700 keys: 9.8 us alone, a launch and six trips to memory.
 // tree_tile_kernel: workgroups of 64 or 128 packed rows, 32 a wave, over a ring of shared stages of 32 keys, 32x32x16
-// instructions.  Up to 64 rows bound by memory and by how evenly the keys are dealt out (16 requests of 36 rows, 174 MB: 37 us,
-// 4.7 TB/s); above by what a wave does one after the other, with room in local memory and registers for two waves a SIMD:
-// 2 requests of 320 rows, up to 120000 keys: 212 GFLOP in 292 us, 0.73 PFLOP/s, the matrix pipe busy a third of the time, vector
-// instructions (16 exponentials a lane and stage) another; heads of 64, whose exponentials take longer than their products:
-// 4 requests of 1000 tokens, 81 GFLOP in 124 us, vector issue a half.
+// instructions.  Weights are rounded to bf16 once (against 64 bits the outputs are off by 0.0023 of their norm, 0.0017 of it
+// the outputs' own rounding): a second part would be half as many products again.  Up to 64 rows bound by memory and by how
+// evenly the keys are dealt out (16 requests of 36 rows, 174 MB: 38 us alone, 4.6 TB/s); above by what a wave does one after the
+// other, with room in local memory and registers for two waves a SIMD: 2 requests of 320 rows, up to 120000 keys: 212 GFLOP in
+// 299 us with the join's 9, 0.73 PFLOP/s, the matrix pipe busy a third of the time, vector instructions (16 exponentials a lane
+// and stage) another; heads of 64, whose exponentials take longer than their products: 4 requests of 1000 tokens, 81 GFLOP in
+// 123 us, vector issue a half.  With a mask it is a kernel of its own: what it does about keys that no row sees costs prompts 1 to
+// 3 % where it is a branch of theirs.
 // Keys of a request are cut into chunks for several workgroups where the batch alone does not fill the machine; partial
 // results meet in tree_join_kernel.
 #include <hip/hip_runtime.h>
