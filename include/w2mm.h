@@ -459,6 +459,99 @@ W2_API int w2_tree_attention(const uint16_t* q, int64_t ldq, int64_t M, int n_q,
                              int64_t ldo, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * The feed-forward half of a decoder layer, for serving: what stands between
+ * two blocks, the router, and 2-bit experts.  The conventions at the top of
+ * this file hold, and as above no number inside a device array (expert ids)
+ * makes a kernel leave the buffers that the host-side arguments describe.
+ * ------------------------------------------------------------------------ */
+
+/* Between two blocks: norm of a block's output y, gate, residual scale, the sum, norm before the next block.  Over a row's N
+ * numbers, in fp32:
+ *   b  = y, or with post_norm  y / sqrt(mean(y^2) + eps) * (post_weight + weight_offset)
+ *   r' = residual_scale * residual + block_scale * gate * b
+ *   x  = r' / sqrt(mean(r'^2) + eps) * (weight + weight_offset)
+ * r' and x are rounded once each, x from the unrounded r'.
+ * weight, post_weight  dev, bf16 [N], or NULL: the factor (weight + weight_offset) is 1
+ * gate  dev, bf16, or NULL: 1; row m at gate + m*ld_gate (ld_gate = 0: one row for all; else at least N, a multiple of 8) */
+typedef struct {
+    const uint16_t *weight, *post_weight, *gate;
+    int64_t ld_gate;
+    float weight_offset, eps, residual_scale, block_scale;
+    int post_norm;
+} w2_norm_t;
+
+/* residual      dev, fp32 or bf16 (r_dtype) [M][N], row stride ldr, or NULL: zero
+ * y             dev, bf16 [M][N], row stride ldy, or NULL: zero (the first block of a stack)
+ * residual_out  dev, r_dtype, row stride ldro: r'; may be residual itself (ldro == ldr), or NULL: not wanted
+ * x             dev, bf16, row stride ldx; may be y itself (ldx == ldy), or NULL: not wanted (behind the last block)
+ * xq, sx        dev, int8 [M][N] dense and fp32 [M], both or neither (NULL): x's rows as w2_quantize_rows makes them of the
+ *               bf16 x, bit for bit, for w2_matmul_a8 (x itself need not be wanted then)
+ * N % 8 == 0 (16 for xq), N <= 65536, M < 2^31; all 16-byte aligned (sx: 4), row strides multiples of 8. */
+W2_API int w2_residual_norm(const w2_norm_t* norm, const void* residual, w2_dtype_t r_dtype, int64_t ldr, const uint16_t* y,
+                            int64_t ldy, int64_t M, int64_t N, void* residual_out, int64_t ldro, uint16_t* x, int64_t ldx,
+                            int8_t* xq, float* sx, void* stream);
+
+/* Which experts each row goes to.
+ *   l[m,e] = sum_k x[m,k] W[e,k]        p = softmax_e(l) (W2_SCORE_SOFTMAX) or sigmoid(l) (W2_SCORE_SIGMOID)
+ *   c      = p + choice_bias             (choice_bias NULL: p)
+ * With n_groups > 1 the experts are n_groups equal ranges, and only those of the top_groups ranges with the largest sum of
+ * their group_top (1 or 2) largest c can be chosen.  Chosen are the top_k largest c, ties to the lower index (of groups too), in
+ * falling order; their weights are scale * p, with renormalise != 0 divided by the sum of the chosen p.
+ * Scores and choices are computed in 64 bits: two experts change places only where exact arithmetic would be in doubt too.  A
+ * score that is NaN counts as lower than any number.
+ * weight       dev, bf16 [n_experts][K], row stride ldw;  choice_bias  dev, fp32 [n_experts]
+ * n_experts up to 1024, n_groups a divisor of it up to 64, top_k <= 64 and <= the experts of top_groups groups. */
+typedef enum { W2_SCORE_SOFTMAX = 0, W2_SCORE_SIGMOID = 1 } w2_score_t;
+typedef struct {
+    const uint16_t* weight;
+    const float* choice_bias;
+    int64_t ldw;
+    int n_experts, top_k, score, renormalise, n_groups, top_groups, group_top;
+    float scale;
+} w2_router_t;
+
+/* Bytes of workspace (host out-pointer) of w2_moe_route for M rows; the size for the largest batch of a program serves all. */
+W2_API int w2_moe_route_workspace_size(const w2_router_t* router, int64_t M, int64_t K, size_t* bytes);
+
+/* x        dev, bf16 [M][K], row stride ldx;  K % 8 == 0, K <= 2^20, M <= 2^24; x, weight and workspace 16-byte aligned, ldx and
+ *          ldw multiples of 8
+ * ids      dev, int32 [M][top_k];  weights  dev, fp32 [M][top_k]
+ * logits   dev, fp32 [M][n_experts] or NULL: l, rounded
+ * workspace  dev, contents undefined before and after */
+W2_API int w2_moe_route(const w2_router_t* router, const uint16_t* x, int64_t ldx, int64_t M, int64_t K, int32_t* ids,
+                        float* weights, float* logits, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The 2-bit experts of a layer.  Expert e's matrices are blobs of w2_prepack: gate_up + e*gate_up_stride holds [hidden ->
+ * 2 inter], gate and up columns alternating by 16 as for W2_ACT_SILU_MUL, down + e*down_stride holds [inter -> hidden].  Strides
+ * in bytes, multiples of 16 and at least the blob's size.  hidden and inter multiples of 256, G in {64, 128}. */
+typedef struct {
+    const void *gate_up, *down;
+    int64_t gate_up_stride, down_stride;
+    int64_t hidden, inter;
+    int n_experts, G;
+} w2_experts_t;
+
+W2_API int w2_moe_experts_workspace_size(const w2_experts_t* experts, int64_t M, int top_k, size_t* bytes);
+
+/* Every row through its experts:
+ *   h[m,j] = silu(g) * u,  (g, u) = x[m] W_gate_up[ids[m,j]]           Y[m] = base[m] + sum_j weights[m,j] h[m,j] W_down[ids[m,j]]
+ * Sums in fp32, one rounding of Y; h is rounded to the bits of two eight-bit numbers (below).  The matrix instructions multiply
+ * a weight's exact value with each number of x (or h) as the sum of two e4m3 numbers, scaled by a power of two for 128
+ * numbers in a row: a bf16 number is exactly such a sum down to 2^-14 of the largest of its 128, and off by at most 2^-22 of
+ * that below.
+ * x        dev, bf16 [M][hidden], row stride ldx;  a row with an infinity or NaN gives a row of NaN
+ * ids      dev, int32 [M][top_k], any order, repetitions allowed; a number outside 0..n_experts-1 (-1): no expert, the slot adds
+ *          nothing (its weight is not read)
+ * weights  dev, fp32 [M][top_k]
+ * base     dev, bf16 [M][hidden], row stride ldb (a shared expert's result), or NULL: zero
+ * Y        dev, bf16 [M][hidden], row stride ldy; may be base itself (ldy == ldb), not x
+ * workspace  dev, 16-byte aligned, w2_moe_experts_workspace_size bytes (or a larger batch's), contents undefined before and after
+ * x, base, Y 16-byte aligned, strides multiples of 8; M * top_k <= 2^24, top_k <= 64, n_experts <= 1024, hidden and inter <= 2^17. */
+W2_API int w2_moe_experts(const w2_experts_t* experts, const uint16_t* x, int64_t ldx, int64_t M, const int32_t* ids,
+                          const float* weights, int top_k, const uint16_t* base, int64_t ldb, uint16_t* Y, int64_t ldy,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Test-only exports.
  * w2_debug_group_acc_a8: the int32 group accumulators acc[M][K/G][N] (dense)
  *   exactly as the chosen kernel family holds them before the dequant step.

@@ -57,6 +57,11 @@ _SIGS = {
     "w2_tree_attention_workspace_size": [_i64, _i64, _int, _int, _int, _i64, _i64, _i64, ctypes.POINTER(_sz)],
     "w2_tree_attention": [_vp, _i64, _i64, _int, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _vp, _int,
                           ctypes.c_float, _vp, _i64, _vp, _vp, _sz, _vp],
+    "w2_residual_norm": [_vp, _vp, _int, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp],
+    "w2_moe_route_workspace_size": [_vp, _i64, _i64, ctypes.POINTER(_sz)],
+    "w2_moe_route": [_vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _sz, _vp],
+    "w2_moe_experts_workspace_size": [_vp, _i64, _int, ctypes.POINTER(_sz)],
+    "w2_moe_experts": [_vp, _vp, _i64, _i64, _vp, _vp, _int, _vp, _i64, _vp, _i64, _vp, _sz, _vp],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -571,6 +576,181 @@ def tree_attention(q, cache, page_table, row_start, kv_len, max_rows, max_len, m
     _check("w2_tree_attention", _lib.w2_tree_attention(
         qp, ldq, M, n_q, cache._ref, tp, cols, ldt, rp, lp, R, max_rows, max_len, total_len, mp, words,
         D ** -0.5 if scale is None else scale, op, ldo, ep, wp, wb, _stream()))
+    return out
+
+
+# ---- the feed-forward half of a decoder layer
+
+class _NormStruct(ctypes.Structure):
+    _fields_ = [("weight", _vp), ("post_weight", _vp), ("gate", _vp), ("ld_gate", _i64), ("weight_offset", ctypes.c_float),
+                ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float), ("block_scale", ctypes.c_float), ("post_norm", _int)]
+
+
+class Norm:
+    """What stands between two blocks (w2_norm_t): the weights (bf16 [N] on the device, or None: factors of 1) of the norm before
+    the next block and of the one after the last (`post_norm`: there is one; default: if it has a weight), scales of the residual
+    and of the block's output."""
+
+    def __init__(self, weight=None, post_weight=None, weight_offset=0.0, eps=1e-6, residual_scale=1.0, block_scale=1.0,
+                 post_norm=None):
+        for t, name in ((weight, "weight"), (post_weight, "post_weight")):
+            if t is not None and (_dev(t, _BF16, name).dim() != 1 or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous [N]")
+        if weight is not None and post_weight is not None and weight.shape != post_weight.shape:
+            raise ValueError("weight and post_weight must have one length")
+        self.weight, self.post_weight = weight, post_weight
+        self.N = None if weight is None and post_weight is None else (post_weight if weight is None else weight).shape[0]
+        post = post_weight is not None if post_norm is None else bool(post_norm)
+        if post_weight is not None and not post:
+            raise ValueError("post_weight without a norm to use it")
+        self._c = _NormStruct(_ptr(weight), _ptr(post_weight), None, 0, weight_offset, eps, residual_scale, block_scale, int(post))
+        self._ref = ctypes.byref(self._c)
+
+
+def residual_norm(norm, residual, y, gate=None, out=None, residual_out=None, quantize=False):
+    """(x, r') of a block's output y (bf16 [M,N]) and the residual (fp32 or bf16 [M,N]); either may be None: zero.
+
+    r' = residual_scale * residual + block_scale * gate * (y, normed if norm.post_norm), x = r' normed, bf16.  `gate`: bf16 [N] or
+    [M,N].  out: x's place (may be y); residual_out: r''s (may be residual; of residual's type, fp32 without one).  quantize=True
+    returns (x, r', xq, sx), xq int8 [M,N] and sx fp32 [M] as quantize_rows makes them of x."""
+    some = residual if residual is not None else y
+    if some is None:
+        raise ValueError("neither residual nor y")
+    if some.dim() != 2:
+        raise ValueError("residual and y must be [M, N]")
+    M, N = some.shape
+    if norm.N is not None and norm.N != N:
+        raise ValueError(f"the norm's weights have {norm.N} numbers, the rows {N}")
+    rdt = residual.dtype if residual is not None else residual_out.dtype if residual_out is not None else _F32
+    if rdt is not _F32 and rdt is not _BF16:
+        raise ValueError("residual must be float32 or bfloat16")
+    rp, ldr = (None, N) if residual is None else _rows(residual, rdt, M, N, "residual")
+    yp, ldy = (None, N) if y is None else _rows(y, _BF16, M, N, "y")
+    c, ref = norm._c, norm._ref
+    if gate is not None:
+        c = _NormStruct.from_buffer_copy(norm._c)            # a call's own: the norm may be in use by another thread
+        if gate.dim() == 1:
+            c.gate, c.ld_gate = _vector(gate, _BF16, N, "gate", "[N] or [M, N]"), 0
+        else:
+            c.gate, c.ld_gate = _rows(gate, _BF16, M, N, "gate")
+        ref = ctypes.byref(c)
+    if out is None:
+        out = torch.empty((M, N), dtype=_BF16, device=some.device)
+    if residual_out is None:
+        residual_out = torch.empty((M, N), dtype=rdt, device=some.device)
+    xp, ldx = _rows(out, _BF16, M, N, "out")
+    op, ldro = _rows(residual_out, rdt, M, N, "residual_out")
+    xq = sx = None
+    if quantize:
+        xq = torch.empty((M, N), dtype=torch.int8, device=some.device)
+        sx = torch.empty(M, dtype=_F32, device=some.device)
+    _check("w2_residual_norm", _lib.w2_residual_norm(ref, rp, DT_F32 if rdt is _F32 else DT_BF16, ldr, yp, ldy, M, N, op, ldro, xp,
+                                                     ldx, _ptr(xq), _ptr(sx), _stream()))
+    return (out, residual_out, xq, sx) if quantize else (out, residual_out)
+
+
+class _RouterStruct(ctypes.Structure):
+    _fields_ = [("weight", _vp), ("choice_bias", _vp), ("ldw", _i64), ("n_experts", _int), ("top_k", _int), ("score", _int),
+                ("renormalise", _int), ("n_groups", _int), ("top_groups", _int), ("group_top", _int), ("scale", ctypes.c_float)]
+
+
+class Router:
+    """A router (w2_router_t): weight bf16 [n_experts, K], score "softmax" or "sigmoid", choice_bias fp32 [n_experts] or None."""
+
+    def __init__(self, weight, top_k, score="softmax", renormalise=True, scale=1.0, choice_bias=None, n_groups=1, top_groups=1,
+                 group_top=1):
+        if _dev(weight, _BF16, "weight").dim() != 2 or weight.stride(1) != 1:
+            raise ValueError("weight must be [n_experts, K] with unit inner stride")
+        if score not in ("softmax", "sigmoid"):
+            raise ValueError("score must be 'softmax' or 'sigmoid'")
+        self.n_experts, self.K = weight.shape
+        if choice_bias is not None:
+            _vector(choice_bias, _F32, self.n_experts, "choice_bias", "[n_experts]")
+        self.weight, self.choice_bias, self.top_k = weight, choice_bias, top_k
+        self._c = _RouterStruct(_ptr(weight), _ptr(choice_bias), weight.stride(0) if self.n_experts > 1 else self.K, self.n_experts,
+                                top_k, ("softmax", "sigmoid").index(score), int(renormalise), n_groups, top_groups, group_top, scale)
+        self._ref = ctypes.byref(self._c)
+
+
+def moe_route_workspace_size(router, M):
+    out = _sz(0)
+    _check("w2_moe_route_workspace_size", _lib.w2_moe_route_workspace_size(router._ref, M, router.K, ctypes.byref(out)))
+    return out.value
+
+
+def _table(t, dtype, M, n, name):
+    """A dense device tensor [M, n] -> its address."""
+    if t.dtype is not dtype or t.shape != (M, n) or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous device tensor [{M}, {n}] of {dtype}")
+    return t.data_ptr()
+
+
+def moe_route(router, x, ids=None, weights=None, logits=None, workspace=None):
+    """(ids int32, weights fp32) [M, top_k] of the rows x (bf16 [M,K]); logits: fp32 [M, n_experts], written if given.
+    `workspace`: a uint8 device tensor of moe_route_workspace_size(router, M) bytes, or of a larger batch's; allocated here if
+    None."""
+    M, k = x.shape[0], router.top_k
+    xp, ldx = _rows(x, _BF16, M, router.K, "x")
+    if ids is None:
+        ids = torch.empty((M, k), dtype=_I32, device=x.device)
+    if weights is None:
+        weights = torch.empty((M, k), dtype=_F32, device=x.device)
+    ip, wp = _table(ids, _I32, M, k, "ids"), _table(weights, _F32, M, k, "weights")
+    lp = None if logits is None else _table(logits, _F32, M, router.n_experts, "logits")
+    if workspace is None:
+        workspace = torch.empty(moe_route_workspace_size(router, M), dtype=torch.uint8, device=x.device)
+    sp, sb = _ws(workspace)
+    _check("w2_moe_route", _lib.w2_moe_route(router._ref, xp, ldx, M, router.K, ip, wp, lp, sp, sb, _stream()))
+    return ids, weights
+
+
+class _ExpertsStruct(ctypes.Structure):
+    _fields_ = [("gate_up", _vp), ("down", _vp), ("gate_up_stride", _i64), ("down_stride", _i64), ("hidden", _i64), ("inter", _i64),
+                ("n_experts", _int), ("G", _int)]
+
+
+class Experts:
+    """The 2-bit experts of a layer (w2_experts_t): gate_up and down uint8 [n_experts, bytes], each row a blob of prepack:
+    [hidden -> 2 inter] with gate and up columns alternating by 16, and [inter -> hidden]."""
+
+    def __init__(self, gate_up, down, hidden, inter, G):
+        sizes = packed_size(hidden, 2 * inter, G), packed_size(inter, hidden, G)
+        for t, name, size in ((gate_up, "gate_up", sizes[0]), (down, "down", sizes[1])):
+            if _dev(t, torch.uint8, name).dim() != 2 or t.stride(1) != 1 or t.shape[1] < size:
+                raise ValueError(f"{name} must be [n_experts, bytes] with unit inner stride and at least {size} bytes a row")
+        if gate_up.shape[0] != down.shape[0] or gate_up.shape[0] < 1:
+            raise ValueError("gate_up and down must have a row for every expert")
+        self.gate_up, self.down, self.hidden, self.inter, self.G = gate_up, down, hidden, inter, G
+        self.n_experts = gate_up.shape[0]
+        self._c = _ExpertsStruct(_ptr(gate_up), _ptr(down), gate_up.stride(0), down.stride(0), hidden, inter, self.n_experts, G)
+        self._ref = ctypes.byref(self._c)
+
+
+def moe_experts_workspace_size(experts, M, top_k):
+    out = _sz(0)
+    _check("w2_moe_experts_workspace_size", _lib.w2_moe_experts_workspace_size(experts._ref, M, top_k, ctypes.byref(out)))
+    return out.value
+
+
+def moe_experts(experts, x, ids, weights, base=None, out=None, workspace=None):
+    """Y bf16 [M, hidden] = base + the weighted sum of the rows' experts.  x bf16 [M, hidden]; ids int32 and weights fp32
+    [M, top_k] as moe_route gives them (an id outside the experts, -1: the slot adds nothing); base bf16 [M, hidden] or None.
+    out may be base.  `workspace`: a uint8 device tensor of moe_experts_workspace_size(experts, M, top_k) bytes, or of a larger
+    batch's; allocated here if None."""
+    M, N = x.shape[0], experts.hidden
+    if ids.dim() != 2:
+        raise ValueError("ids must be [M, top_k]")
+    k = ids.shape[1]
+    xp, ldx = _rows(x, _BF16, M, N, "x")
+    ip, wp = _table(ids, _I32, M, k, "ids"), _table(weights, _F32, M, k, "weights")
+    bp, ldb = (None, N) if base is None else _rows(base, _BF16, M, N, "base")
+    if out is None:
+        out = torch.empty((M, N), dtype=_BF16, device=x.device)
+    yp, ldy = _rows(out, _BF16, M, N, "out")
+    if workspace is None:
+        workspace = torch.empty(moe_experts_workspace_size(experts, M, k), dtype=torch.uint8, device=x.device)
+    sp, sb = _ws(workspace)
+    _check("w2_moe_experts", _lib.w2_moe_experts(experts._ref, xp, ldx, M, ip, wp, k, bp, ldb, yp, ldy, sp, sb, _stream()))
     return out
 
 
