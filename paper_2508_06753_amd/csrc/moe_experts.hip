@@ -14,6 +14,7 @@
 // them, g = the units g and g + 4 of a half, which is one lane group's 32 k of the instruction.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "block_ops.h"
@@ -60,11 +61,11 @@ __device__ __forceinline__ float scale_down(int e) { return __int_as_float((254 
 
 // Workgroup 0 sorts the choices by expert (stable: which rows share a tile is the same every time); the others convert x, a
 // thread 32 numbers.
-__global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, Tile* tiles, int64_t max_tiles, int rows, int* sorted, int* place,
-                                                           char* xs, char* xe)
+__global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* total_tiles, Tile* tiles, int64_t max_tiles, int rows, int* tile_rows,
+                                                           int* place, char* xs, char* xe)
 {
     __shared__ int s_count[16][1024];   // of each wave's share, then where its rows of each expert begin
-    __shared__ int s_sum[2][16];
+    __shared__ int s_sum[2][16], s_first[1024], s_tile[1024];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int E = a.e.n_experts;
     if (blockIdx.x > 0) {
@@ -104,13 +105,21 @@ __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, Tile* 
         xe[m * moe::exp_bytes(a.e.hidden) + kt * 8 + g * 2 + half] = (char)e;
         return;
     }
+    constexpr int AT_ONCE = 8;          // loads of 64 choices under way together
     const int A = (int)(a.M * a.top_k);
     for (int i = tid; i < 16 * 1024; i += 1024) (&s_count[0][0])[i] = 0;
     __syncthreads();
     const int share = (A + 1023) / 1024 * 64, begin = min(A, wave * share), end = min(A, begin + share);
-    for (int i = begin + lane; i < end; i += 64) {
-        const int id = a.ids[i];
-        if ((unsigned)id < (unsigned)E) atomicAdd(&s_count[wave][id], 1);
+    for (int i0 = begin; i0 < end; i0 += 64 * AT_ONCE) {
+        int id[AT_ONCE];
+#pragma unroll
+        for (int b = 0; b < AT_ONCE; ++b) {
+            const int i = i0 + b * 64 + lane;
+            id[b] = i < end ? a.ids[i] : -1;
+        }
+#pragma unroll
+        for (int b = 0; b < AT_ONCE; ++b)
+            if ((unsigned)id[b] < (unsigned)E) atomicAdd(&s_count[wave][id[b]], 1);
     }
     __syncthreads();
     // thread e: expert e's rows, and where they and its tiles begin
@@ -131,6 +140,9 @@ __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, Tile* 
     }
     first -= count;
     tile -= n_tiles;
+    if (tid == 0) *total_tiles = all_tiles;
+    s_first[tid] = first;
+    s_tile[tid] = tile;
     for (int t = 0; t < n_tiles; ++t) tiles[tile + t] = Tile{tid, first + t * rows, min(rows, count - t * rows), 0};
     for (int64_t t = all_tiles + tid; t < max_tiles; t += 1024) tiles[t] = Tile{0, 0, 0, 0};
     for (int w = 0; w < 16; ++w) {
@@ -139,22 +151,32 @@ __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, Tile* 
         first += n;
     }
     __syncthreads();
-    for (int i0 = begin; i0 < end; i0 += 64) {
-        const int i = i0 + lane;
-        const int id = i < end ? a.ids[i] : -1;
-        const bool live = (unsigned)id < (unsigned)E;
-        uint64_t same = __ballot(live);
-        for (int b = 0; b < 10; ++b) {
-            const uint64_t set = __ballot(live && id >> b & 1);
-            same &= id >> b & 1 ? set : ~set;
+    for (int i0 = begin; i0 < end; i0 += 64 * AT_ONCE) {
+        int ids[AT_ONCE];
+#pragma unroll
+        for (int b = 0; b < AT_ONCE; ++b) {
+            const int i = i0 + b * 64 + lane;
+            ids[b] = i < end ? a.ids[i] : -1;
         }
-        const int before = __popcll(same & (((uint64_t)1 << lane) - 1));
-        const int at = live ? s_count[wave][id] : 0;
-        if (live) {
-            sorted[at + before] = i;
-            if (before == 0) s_count[wave][id] = at + __popcll(same);
+#pragma unroll
+        for (int b = 0; b < AT_ONCE; ++b) {
+            if (i0 + b * 64 >= end) break;
+            const int i = i0 + b * 64 + lane, id = ids[b];
+            const bool live = (unsigned)id < (unsigned)E;
+            uint64_t same = __ballot(live);                  // the lanes of the same expert
+            for (int bit = 0; E >> bit; ++bit) {
+                const uint64_t set = __ballot(live && id >> bit & 1);
+                same &= id >> bit & 1 ? set : ~set;
+            }
+            const int before = __popcll(same & (((uint64_t)1 << lane) - 1));
+            const int at = live ? s_count[wave][id] : 0;
+            if (live) {
+                const int n = at + before - s_first[id], t = n / rows;
+                tile_rows[(s_tile[id] + t) * rows + n - t * rows] = i / a.top_k;
+                if (before == 0) s_count[wave][id] = at + __popcll(same);
+            }
+            if (i < end) place[i] = live ? at + before : -1;
         }
-        if (i < end) place[i] = live ? at + before : -1;
     }
 }
 
@@ -164,277 +186,469 @@ __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, Tile* 
 // (b1 b0): sign b1, magnitude b0 | (b1 & ~b0) << 1.
 __device__ __forceinline__ void to_fp4(uint32_t w, int& lo, int& hi)
 {
-    const uint32_t t = w << 1;
-    const uint32_t mag = w & ~(t & 0xaaaaaaaau);             // magnitudes in place
+    const uint32_t mag = __builtin_amdgcn_bitop3_b32(w, w << 1, 0xaaaaaaaau, 0x70);       // w & ~(w << 1 & 0xaa..): magnitudes in place
     const uint32_t sign = w & 0xaaaaaaaau;
-    lo = (int)((mag & 0x33333333u) | (sign << 2 & 0xccccccccu));
-    hi = (int)((mag >> 2 & 0x33333333u) | (sign & 0xccccccccu));
+    lo = (int)__builtin_amdgcn_bitop3_b32(mag, sign << 2, 0x33333333u, 0xe4);             // bits of the mask from the first, the others from the second
+    hi = (int)__builtin_amdgcn_bitop3_b32(mag >> 2, sign, 0x33333333u, 0xe4);
 }
-
-constexpr int STRIDE = 528;             // bytes of a row's 256 k in local memory: 512, its exponents, and 4 banks on to the next row
 
 struct ProductArgs {
     const char* blob;
     int64_t blob_stride, codes_bytes;
     int n_kt;
     const Tile* tiles;
-    const int* sorted;                  // up: whose rows; down: nullptr, rows lie in sorted order
-    int top_k;
+    const int* tile_rows;               // up: which row of x each row of a tile is (down: the places in the sorted order)
     const char *rows, *exps;            // in two parts
     char *h, *h_exps;                   // up: rows of n_out numbers in two parts
     float* z;                           // down: rows of n_out numbers
     int n_out;
 };
 
-// A workgroup: eight waves = 8 / KS pairs of column blocks times KS ranges of K, up to 16 * RT rows of one expert.  UP: a pair
-// is a block of gate columns and one of up columns; silu(gate) * up leaves in two parts.  Not UP: two blocks; sums leave in fp32.
-template <bool UP, int RT, int KS, int GPT>
-__global__ void __launch_bounds__(512) moe_product_kernel(ProductArgs a)
+// Scale of group g of the 256 k that a lane's scales belong to
+template <int GPT>
+struct Scales;
+template <> struct Scales<2> { typedef uint32_t type; };
+template <> struct Scales<4> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+__device__ __forceinline__ float scale_at(uint32_t d, int g) { return __uint_as_float(g ? d & 0xffff0000u : d << 16); }
+__device__ __forceinline__ float scale_at(Scales<4>::type d, int g) { return __uint_as_float(g & 1 ? d[g >> 1] & 0xffff0000u : d[g >> 1] << 16); }
+
+// x (eight-bit) times b (four-bit) into acc; ex's byte BYTE: the rows' power of two; the column's, 2^1, makes q of q / 2
+template <int BYTE>
+__device__ __forceinline__ v4f product(v8i x, const int (&b)[4], v4f acc, int ex)
 {
-    constexpr int R = 16 * RT, P = 8 / KS, NP = RT * KS;
-    extern __shared__ char s_mem[];                          // [2 buffers][KS][R][STRIDE]
-    __shared__ int s_src[R];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, q = lane >> 4;
-    const Tile tile = a.tiles[blockIdx.y];
-    if (tile.rows == 0) return;
-    // pairs of a workgroup lie so that the units g and g + 4 of 128 numbers of h are both its own
-    const int p = wave % P, kr = wave / P;
-    int pair;
-    if (UP) pair = blockIdx.x / KS * 8 + blockIdx.x % KS * (P / 2) + p % (P / 2) + p / (P / 2) * 4;
-    else pair = blockIdx.x * P + p;
-    const int steps = (a.n_kt + KS - 1) / KS;
-    const char* const blob = a.blob + tile.expert * a.blob_stride;
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, (v8i){b[0], b[1], b[2], b[3], 0, 0, 0, 0}, acc, 0, 4, BYTE, ex, 0, 128);
+}
 
-    // weights of the wave's column blocks, from its first k tile on
-    const int kt0 = kr * steps, my_steps = max(0, min(steps, a.n_kt - kt0));
-    const char* codes[2];
-    const char* scales[2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const int64_t t = (int64_t)(2 * pair + c) * a.n_kt + kt0;
-        codes[c] = blob + t * 1024 + lane * 16;
-        scales[c] = blob + a.codes_bytes + (t * 16 + col) * GPT * 2;
-    }
-    typedef typename std::conditional<GPT == 2, uint32_t, uint2>::type Scales;
-    uint4 w[2];
-    Scales sc[2];
-    auto load_weights = [&](int s) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            w[c] = *reinterpret_cast<const uint4*>(codes[c] + (int64_t)s * 1024);
-            sc[c] = *reinterpret_cast<const Scales*>(scales[c] + (int64_t)s * 32 * GPT);
-        }
-    };
-    if (my_steps > 0) load_weights(0);
+__device__ __forceinline__ v8i join(v4i a, v4i b) { return (v8i){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
 
-    if (tid < R) {
-        const int r = min(tid, tile.rows - 1);
-        s_src[tid] = UP ? a.sorted[tile.first + r] / a.top_k : tile.first + r;
-    }
-    __syncthreads();
-    const char *src[NP], *src_e = nullptr;
-    int kt_of[NP], to[NP];
-    const int row_b = a.n_kt * 512;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int piece = tid + i * 512, r = piece / 32 % R, k = piece / (32 * R);
-        src[i] = a.rows + (int64_t)s_src[r] * row_b + (int64_t)k * steps * 512 + piece % 32 * 16;
-        kt_of[i] = k * steps;
-        to[i] = (k * R + r) * STRIDE + piece % 32 * 16;
-    }
-    int kt_e = 0, to_e = 0;
-    if (tid < R * KS) {
-        src_e = a.exps + (int64_t)s_src[tid % R] * a.n_kt * 8 + (int64_t)(tid / R) * steps * 8;
-        kt_e = tid / R * steps;
-        to_e = tid * STRIDE + 512;
-    }
-    uint4 staged[NP];
-    uint2 staged_e = make_uint2(0, 0);
-    auto fetch = [&](int s) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            staged[i] = make_uint4(0, 0, 0, 0);
-            if (kt_of[i] + s < a.n_kt) staged[i] = *reinterpret_cast<const uint4*>(src[i] + s * 512);
-        }
-        if (src_e && kt_e + s < a.n_kt) staged_e = *reinterpret_cast<const uint2*>(src_e + s * 8);
-    };
-    auto put = [&](int buffer) {
-        char* const at = s_mem + buffer * (KS * R * STRIDE);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) *reinterpret_cast<uint4*>(at + to[i]) = staged[i];
-        if (src_e) *reinterpret_cast<uint2*>(at + to_e) = staged_e;
-    };
-    fetch(0);
-    put(0);
-    __syncthreads();
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void* p, int64_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(uint32_t)min(bytes, (int64_t)0xffffffff), 0x00020000);
+}
 
-    v4f y[RT][2] = {};
-    const bool packed = RT == 1 && tile.rows <= 8;           // hi in rows 0 to 7 of the instruction, lo in 8 to 15
-    const int row = packed ? col & 7 : col;
-    const int unit = 4 * (q & 1) + (q >> 1);
-    for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) fetch(s + 1);
-        if (s < my_steps) {
-            uint4 now[2] = {w[0], w[1]};
-            Scales f[2] = {sc[0], sc[1]};
-            if (s + 1 < my_steps) load_weights(s + 1);
-            const char* const at = s_mem + (s & 1) * (KS * R * STRIDE) + kr * R * STRIDE;
-            int e[RT];
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource32(const void* p, int bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+
+__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+
+__device__ __forceinline__ float finite_or_inf(float h)      // |h|, a NaN as the largest
+{
+    h = fabsf(h);
+    return h < INFINITY ? h : INFINITY;
+}
+
+// exponent field of the largest of 16 lanes' numbers
+__device__ __forceinline__ int largest_field(float m)
+{
+    m = fmaxf(m, dpp_move_f32<0xB1>(m));
+    m = fmaxf(m, dpp_move_f32<0x4E>(m));
+    m = fmaxf(m, dpp_move_f32<0x141>(m));
+    m = fmaxf(m, dpp_move_f32<0x140>(m));
+    return (int)(__float_as_uint(m) >> 23);
+}
+
+// What the wave of a pair of blocks leaves: h in two parts (UP; every wave of the workgroup calls it), or rows of z.  The
+// workgroup's P pairs are the units c0 .. c0 + P/2 - 1 and those four further on of the 128 numbers u of h.  s_mem: P * R * 36 bytes.
+template <int RT, int P>
+__device__ __forceinline__ void store_h(const ProductArgs& a, const Tile& tile, char* s_mem, v4f (&y)[RT][2], int p, bool mine, int u, int c0, int threads)
+{
+    constexpr int R = 16 * RT;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
+    int* const s_top = reinterpret_cast<int*>(s_mem);        // [P][R]: exponent field of the largest |h| of a row's unit
+    char* const s_out = s_mem + P * R * 4;                   // [R][2 parts][P units][16]
+    float h[RT][4];
+    if (mine) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r) e[r] = *reinterpret_cast<const uint16_t*>(at + (r * 16 + row) * STRIDE + 512 + q * 2);
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                int b[2][4];
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    to_fp4(j ? now[c].z : now[c].x, b[c][0], b[c][1]);
-                    to_fp4(j ? now[c].w : now[c].y, b[c][2], b[c][3]);
-                }
-                auto group = [&](int c, int g) -> float {   // scale of group g of this column's 256 k
-                    uint32_t d;
-                    if constexpr (GPT == 2) d = f[c];
-                    else d = g < 2 ? f[c].x : f[c].y;
-                    return __uint_as_float(g & 1 ? d & 0xffff0000u : d << 16);
-                };
-                auto part = [&](int r, int lo) -> v8i {
-                    const char* t = at + (r * 16 + row) * STRIDE + j * 256 + lo * 128 + unit * 16;
-                    const v4i x = *reinterpret_cast<const v4i*>(t), z = *reinterpret_cast<const v4i*>(t + 32);
-                    return (v8i){x[0], x[1], x[2], x[3], z[0], z[1], z[2], z[3]};
-                };
-                auto mul = [&](v8i x, v8i b8, v4f acc, int ex) -> v4f {
-                    // format 0: E4M3 rows, 4: E2M1 columns; the column's power of two, 2^1, makes q of q / 2
-                    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, b8, acc, 0, 4, 0, ex, 0, 128);
-                };
-                if (packed) {
-                    const int ex = ((e[0] >> (8 * j)) & 255) - (col >> 3) * 5;
-                    const v8i x = part(0, col >> 3);
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        if constexpr (GPT == 2) {
-                            const v4f acc = mul(x, (v8i){b[c][0], b[c][1], b[c][2], b[c][3], 0, 0, 0, 0}, (v4f){0, 0, 0, 0}, ex);
-                            y[0][c] += acc * group(c, j);
-                        } else {
-                            const v4f a0 = mul(x, (v8i){b[c][0], b[c][1], 0, 0, 0, 0, 0, 0}, (v4f){0, 0, 0, 0}, ex);
-                            const v4f a1 = mul(x, (v8i){0, 0, b[c][2], b[c][3], 0, 0, 0, 0}, (v4f){0, 0, 0, 0}, ex);
-                            y[0][c] += a0 * group(c, 2 * j);
-                            y[0][c] += a1 * group(c, 2 * j + 1);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        const int ex = (e[r] >> (8 * j)) & 255;
-                        const v8i hi = part(r, 0), lo = part(r, 1);
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            if constexpr (GPT == 2) {
-                                const v8i b8 = {b[c][0], b[c][1], b[c][2], b[c][3], 0, 0, 0, 0};
-                                v4f acc = mul(lo, b8, (v4f){0, 0, 0, 0}, ex - 5);
-                                acc = mul(hi, b8, acc, ex);
-                                y[r][c] += acc * group(c, j);
-                            } else {
-                                const v8i b0 = {b[c][0], b[c][1], 0, 0, 0, 0, 0, 0}, b1 = {0, 0, b[c][2], b[c][3], 0, 0, 0, 0};
-                                v4f a0 = mul(lo, b0, (v4f){0, 0, 0, 0}, ex - 5), a1 = mul(lo, b1, (v4f){0, 0, 0, 0}, ex - 5);
-                                a0 = mul(hi, b0, a0, ex);
-                                a1 = mul(hi, b1, a1, ex);
-                                y[r][c] += a0 * group(c, 2 * j);
-                                y[r][c] += a1 * group(c, 2 * j + 1);
-                            }
-                        }
-                    }
-                }
+            for (int i = 0; i < 4; ++i) {
+                h[r][i] = silu_mul(y[r][0][i], y[r][1][i]);
+                const int top = largest_field(finite_or_inf(h[r][i]));
+                if (col == 0) s_top[p * R + r * 16 + q * 4 + i] = top;
             }
-        }
-        if (s + 1 < steps) put((s + 1) & 1);
-        __syncthreads();
     }
-    if (packed) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[0][c][i] += __shfl_xor(y[0][c][i], 32);
-    }
-    // ranges of K meet in local memory, in their order
-    if constexpr (KS > 1) {
-        v4f* const part = reinterpret_cast<v4f*>(s_mem);     // [KS - 1][P][RT * 2][64]
-        if (kr > 0) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) part[(((kr - 1) * P + p) * RT * 2 + r * 2 + c) * 64 + lane] = y[r][c];
-        }
-        __syncthreads();
-        if (kr == 0) {
-            for (int k = 0; k < KS - 1; ++k)
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) y[r][c] += part[((k * P + p) * RT * 2 + r * 2 + c) * 64 + lane];
-        }
-        __syncthreads();
-    }
-    if constexpr (!UP) {
-        if (kr > 0) return;
+    __syncthreads();
+    if (mine) {
+        const int byte = 2 * (col & 7) + (col >> 3);
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int m = r * 16 + q * 4 + i;
+                const int ex = shared_exponent(max(s_top[p % (P / 2) * R + m], s_top[(p % (P / 2) + P / 2) * R + m]));
+                uint32_t hi, lo;
+                split2(h[r][i], 0.0f, scale_down(ex), hi, lo);
+                s_out[((m * 2 + 0) * P + p) * 16 + byte] = (char)hi;
+                s_out[((m * 2 + 1) * P + p) * 16 + byte] = (char)lo;
+                if (p < P / 2 && col == 0 && m < tile.rows)
+                    a.h_exps[(int64_t)(tile.first + m) * (a.n_out / 32) + u / 2 * 8 + (c0 + p) * 2 + (u & 1)] = (char)ex;
+            }
+    }
+    __syncthreads();
+    for (int i = tid; i < tile.rows * 2 * P; i += threads) { // 16 bytes: a unit of a part of a row
+        const int m = i / (2 * P), part = i / P % 2, pp = i % P;
+        const int to_unit = c0 + pp % (P / 2) + pp / (P / 2) * 4;
+        *reinterpret_cast<uint4*>(a.h + (int64_t)(tile.first + m) * a.n_out * 2 + u * 256 + part * 128 + to_unit * 16) =
+            *reinterpret_cast<const uint4*>(s_out + i * 16);
+    }
+}
+
+// Few rows: bound by the weights' way from memory.  A workgroup: four waves = 4 / KS pairs of column blocks times KS ranges of K, up to
+// eight rows of one expert, hi in rows 0 to 7 of the instruction, lo in 8 to 15.  UP: a pair is a block of gate columns and one of up columns;
+// silu(gate) * up leaves in two parts.  Not UP: two blocks; sums leave in fp32.  The next four tiles of weights of each column block are
+// under way while one is multiplied; rows come through local memory, four tiles of K (over all ranges) at a time.  Every load
+// is unconditional, what lies past a wave's range is out of its resource and reads as zeros, so that the waits count exactly.
+constexpr int FEW_W = 4, FEW_WAVES = 4, FEW_ROWS = 8;
+constexpr int NT = 2;                   // weights pass through the caches once
+
+template <int KS>
+struct FewShape {
+    static constexpr int P = FEW_WAVES / KS, CK = 4 / KS, R = FEW_ROWS, STRIDE = CK * 512 + 16, BUFFER = KS * R * STRIDE, EXPS = KS * R * CK * 8;
+    static constexpr int THREADS = FEW_WAVES * 64, PIECES = KS * CK;
+    static_assert(THREADS == R * 32, "a thread fetches 16 bytes of its row's 512 of each tile");
+    // what leaves: the ranges' sums, the largest numbers and two parts of h
+    static constexpr int LEAVE = std::max((KS - 1) * P * 2048, P * 16 * 36), LDS = 2 * BUFFER + 2 * EXPS + 512 + LEAVE;
+};
+
+// units: groups of P pairs that a workgroup takes one behind the other, the next one's weights under way before the last one's sums leave
+template <bool UP, int KS, int GPT>
+__global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kernel(ProductArgs a, int64_t row_bytes_all, int units)
+{
+    typedef FewShape<KS> S;
+    constexpr int P = S::P, CK = S::CK, R = S::R, STRIDE = S::STRIDE, BUFFER = S::BUFFER, EXPS = S::EXPS, THREADS = S::THREADS;
+    extern __shared__ char s_mem[];                          // [2][KS][R][STRIDE], exponents [2][KS][R][CK * 8], 512 bytes for no one; what leaves
+    char* const s_leave = s_mem + 2 * BUFFER + 2 * EXPS + 512;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Tile tile = a.tiles[blockIdx.y];
+    // which rows (of what may be there: how many are is not known yet)
+    const int* const tile_rows = a.tile_rows + (int64_t)blockIdx.y * R;
+    const int r_in = tid / 32, r_e = tid % R, t_e = tid / R; // KS * CK * R threads: the exponents of a row's tile each
+    const bool has_e = tid < KS * CK * R;
+    uint32_t row = UP ? tile_rows[r_in] : r_in, row_e = UP ? tile_rows[r_e] : r_e;
+    if (tile.rows == 0) return;
+    const int p = wave % P, kr = wave / P;
+    const int steps = (a.n_kt + KS - 1) / KS, steps4 = (steps + FEW_W - 1) / FEW_W * FEW_W;
+    const int kt0 = kr * steps, my_steps = max(0, min(steps, a.n_kt - kt0));
+    const char* const blob = a.blob + tile.expert * a.blob_stride;
+    // pairs of a workgroup lie so that the units g and g + 4 of 128 numbers of h are both its own
+    constexpr int GROUPS = 8 / P;
+    auto pair_of = [&](int group) { return UP ? group / GROUPS * 8 + group % GROUPS * (P / 2) + p % (P / 2) + p / (P / 2) * 4 : group * P + p; };
+    struct Weights {                    // of the wave's first column block, its range of K; the second one follows
+        const char *codes, *scales;
+        int tiles;
+    };
+    auto weights_of = [&](int group, bool there) {
+        const int64_t t = (int64_t)(2 * pair_of(group)) * a.n_kt + kt0;
+        return Weights{blob + t * 1024, blob + a.codes_bytes + t * 32 * GPT, there ? my_steps : 0};
+    };
+    v4i w[FEW_W][2];
+    typename Scales<GPT>::type sc[FEW_W][2];
+    auto load_weights = [&](const Weights& r, int s, int slot) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const __amdgpu_buffer_rsrc_t wr = resource32(r.codes + (int64_t)c * a.n_kt * 1024, r.tiles * 1024);
+            const __amdgpu_buffer_rsrc_t sr = resource32(r.scales + (int64_t)c * a.n_kt * 32 * GPT, r.tiles * 32 * GPT);
+            w[slot][c] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(wr, s * 1024 + lane * 16, 0, NT));
+            if constexpr (GPT == 2) sc[slot][c] = __builtin_amdgcn_raw_buffer_load_b32(sr, s * 64 + col * 4, 0, 0);
+            else sc[slot][c] = __builtin_bit_cast(Scales<4>::type, __builtin_amdgcn_raw_buffer_load_b64(sr, s * 128 + col * 8, 0, 0));
+        }
+    };
+
+    // a row that is not there is out of range
+    const __amdgpu_buffer_rsrc_t rr = resource(a.rows, row_bytes_all), er = resource(a.exps, row_bytes_all / 64);
+    const int n_in = r_in < tile.rows ? a.n_kt : 0, n_in_e = has_e && r_e < tile.rows ? a.n_kt : 0;     // tiles of K that the row has
+    if (!UP) {
+        row += tile.first;
+        row_e += tile.first;
+    }
+    const uint32_t src = row * (uint32_t)(a.n_kt * 512) + tid % 32 * 16, src_e = row_e * (uint32_t)(a.n_kt * 8);
+    char* const to = s_mem + r_in * STRIDE + tid % 32 * 16;
+    // (the other threads write beside them: without a branch, past which the compiler would carry the products and all their operands)
+    char* const to_e = s_mem + 2 * BUFFER + (has_e ? ((t_e / CK * R + r_e) * CK + t_e % CK) * 8 : 2 * EXPS + (tid & 63) * 8);
+    const int next_e = has_e ? EXPS : 0;
+    v4i staged[S::PIECES];
+    uint2 staged_e;
+    auto fetch = [&](int s) {           // s: first of the CK steps
+#pragma unroll
+        for (int i = 0; i < S::PIECES; ++i) {
+            const int kt = i / CK * steps + i % CK + s;
+            staged[i] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rr, kt < n_in ? src + kt * 512 : 0xffffffffu, 0, 0));
+        }
+        const int kt = t_e / CK * steps + t_e % CK + s;
+        staged_e = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(er, kt < n_in_e ? src_e + kt * 8 : 0xffffffffu, 0, 0));
+    };
+    auto put = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < S::PIECES; ++i) *reinterpret_cast<v4i*>(to + buffer * BUFFER + i / CK * R * STRIDE + i % CK * 512) = staged[i];
+        *reinterpret_cast<uint2*>(to_e + buffer * next_e) = staged_e;
+    };
+    const int group0 = blockIdx.x * units;
+    Weights now = weights_of(group0, true);
+    fetch(0);
+#pragma unroll
+    for (int i = 0; i < FEW_W; ++i) load_weights(now, i, i);
+    put(0);
+    __syncthreads();
+
+    const int unit = 4 * (q & 1) + (q >> 1);
+    const char* const at = s_mem + (kr * R + (col & 7)) * STRIDE + unit * 16 + (col >> 3) * 128;
+    const char* const at_e = s_mem + 2 * BUFFER + (kr * R + (col & 7)) * CK * 8 + q * 2;
+    const int lo_exp = (col >> 3) * 0x0505;
+    int turn = 0;                       // the buffer that a chunk of four steps begins in
+    for (int g = 0; g < units; ++g) {
+        const Weights then = weights_of(group0 + g + 1, g + 1 < units);
+        v4f y[1][2] = {};
+        for (int s = 0; s < steps4; s += FEW_W) {
+            const bool last = s + FEW_W >= steps4;
+            const Weights ahead = last ? then : now;
+            const int s_ahead = last ? 0 : s + FEW_W;
+#pragma unroll
+            for (int i = 0; i < FEW_W; ++i) {
+                if (i % CK == 0) fetch(s + i + CK < steps4 ? s + i + CK : 0);
+                const int buffer = (i / CK + turn) & 1;
+                // (up-converted only now: a turn early, as they come, the weights would take twice the registers)
+                asm volatile("" : "+v"(w[i][0]), "+v"(w[i][1]), "+v"(sc[i][0]), "+v"(sc[i][1]));
+                const char* const x0 = at + buffer * BUFFER + i % CK * 512;
+                const int e = *reinterpret_cast<const uint16_t*>(at_e + buffer * EXPS + i % CK * 8) - lo_exp;
+                auto half = [&](auto jc) {
+                    constexpr int j = decltype(jc)::value;
+                    const v8i x = join(*reinterpret_cast<const v4i*>(x0 + j * 256), *reinterpret_cast<const v4i*>(x0 + j * 256 + 32));
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        int b[4];
+                        to_fp4((uint32_t)w[i][n][2 * j], b[0], b[1]);
+                        to_fp4((uint32_t)w[i][n][2 * j + 1], b[2], b[3]);
+                        const v4f zero = {0, 0, 0, 0};
+                        if constexpr (GPT == 2) y[0][n] += product<j>(x, b, zero, e) * scale_at(sc[i][n], j);
+                        else {
+                            y[0][n] += product<j>(x, {b[0], b[1], 0, 0}, zero, e) * scale_at(sc[i][n], 2 * j);
+                            y[0][n] += product<j>(x, {0, 0, b[2], b[3]}, zero, e) * scale_at(sc[i][n], 2 * j + 1);
+                        }
+                    }
+                };
+                half(std::integral_constant<int, 0>{});
+                half(std::integral_constant<int, 1>{});
+                // here, and not where they are read: carried on, the products' operands would take every register
+                asm volatile("" : "+v"(y[0][0]), "+v"(y[0][1]));
+                __builtin_amdgcn_sched_barrier(0);
+                load_weights(ahead, s_ahead + i, i);
+                if (i % CK == CK - 1) {
+                    put((i / CK + 1 + turn) & 1);
+                    __syncthreads();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (CK == 4) turn ^= 1;
+        }
+        // hi's sums and lo's
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[0][n][i] += __shfl_xor(y[0][n][i], 32);
+        if constexpr (KS > 1) {                              // ranges of K meet in local memory, in their order
+            v4f* const part = reinterpret_cast<v4f*>(s_leave);         // [KS - 1][P][2][64]
+            if (kr > 0) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n) part[(((kr - 1) * P + p) * 2 + n) * 64 + lane] = y[0][n];
+            }
+            __syncthreads();
+            if (kr == 0) {
+#pragma unroll
+                for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) y[0][n] += part[((k * P + p) * 2 + n) * 64 + lane];
+            }
+            __syncthreads();
+        }
+        const int group = group0 + g;
+        if constexpr (UP) {
+            store_h<1, P>(a, tile, s_leave, y, p, kr == 0, group / GROUPS, group % GROUPS * (P / 2), THREADS);
+        } else if (kr == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int m = q * 4 + i;
                 if (m < tile.rows) {
-                    float* const out = a.z + (int64_t)(tile.first + m) * a.n_out + pair * 32 + col;
-                    out[0] = y[r][0][i];
-                    out[16] = y[r][1][i];
+                    float* const out = a.z + (int64_t)(tile.first + m) * a.n_out + pair_of(group) * 32 + col;
+                    out[0] = y[0][0][i];
+                    out[16] = y[0][1][i];
                 }
             }
-    } else {
-        float* const s_top = reinterpret_cast<float*>(s_mem);          // [P][R]: the largest |h| of a row's unit
-        char* const s_out = s_mem + P * R * 4;                         // [R][2 parts][P units][16]
-        float h[RT][4];
-        if (kr == 0) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float g = y[r][0][i];
-                    h[r][i] = g / (1.0f + __expf(-g)) * y[r][1][i];
-                    float m = fabsf(h[r][i]);
-                    if (!(m < INFINITY)) m = INFINITY;       // a NaN counts as the largest exponent
-                    m = fmaxf(m, dpp_move_f32<0xB1>(m));
-                    m = fmaxf(m, dpp_move_f32<0x4E>(m));
-                    m = fmaxf(m, dpp_move_f32<0x141>(m));
-                    m = fmaxf(m, dpp_move_f32<0x140>(m));
-                    if (col == 0) s_top[p * R + r * 16 + q * 4 + i] = m;
-                }
         }
+        now = then;
+    }
+}
+
+// Many rows: bound by the matrix pipe.  A workgroup: four waves of 64 columns each (two pairs of blocks), up to 64 rows of
+// one expert, half a tile of K (128) at a time through local memory.  As wide a wave as that because each wave reads every
+// row's operands: with 32 columns a wave the local memory is asked for as long as the matrix pipe is.
+constexpr int TILE_ROWS = 64;
+constexpr int TILE_STRIDE = 256 + 16;
+
+template <bool UP, int GPT>
+__global__ void __launch_bounds__(256, 2) moe_tile_kernel(ProductArgs a, const int* n_tiles, int col_groups)
+{
+    __shared__ __align__(16) char s_mem[2 * TILE_ROWS * TILE_STRIDE];
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // the workgroups of an XCD take tiles in a row: row tiles of an expert meet its weights in that die's L2
+    const int total = *n_tiles * col_groups, per = (total + 7) / 8, idx = blockIdx.x >> 3, lin = (blockIdx.x & 7) * per + idx;
+    if (idx >= per || lin >= total) return;
+    const int cg = lin % col_groups;
+    const int* const tile_rows = a.tile_rows + (int64_t)(lin / col_groups) * TILE_ROWS;
+    const Tile tile = a.tiles[lin / col_groups];
+    int pair[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) pair[n] = cg * 8 + (UP ? wave + 4 * n : wave * 2 + n);
+    const char* const blob = a.blob + tile.expert * a.blob_stride;
+    const char *codes[4], *scales[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const int64_t t = (int64_t)(2 * pair[c / 2] + c % 2) * a.n_kt;
+        codes[c] = blob + t * 1024;
+        scales[c] = blob + a.codes_bytes + t * 32 * GPT;
+    }
+    v4i w[4];
+    typename Scales<GPT>::type sc[4];
+    auto load_weights = [&](int kt) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            w[c] = *reinterpret_cast<const v4i*>(codes[c] + (int64_t)kt * 1024 + lane * 16);
+            sc[c] = *reinterpret_cast<const typename Scales<GPT>::type*>(scales[c] + (int64_t)kt * 32 * GPT + col * 2 * GPT);
+        }
+    };
+    auto row_of = [&](int r) -> int64_t {
+        r = min(r, tile.rows - 1);
+        return UP ? tile_rows[r] : tile.first + r;
+    };
+    auto body = [&](auto rt_c) {
+        constexpr int RT = decltype(rt_c)::value;
+        const char* src[RT];            // 16 pieces of a row's 128 k, RT rows (16 apart) to a thread
+        const char* exps[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            src[r] = a.rows + row_of(r * 16 + tid / 16) * (a.n_kt * 512) + tid % 16 * 16;
+            exps[r] = a.exps + row_of(r * 16 + col) * (a.n_kt * 8) + q * 2;
+        }
+        const int to = tid / 16 * TILE_STRIDE + tid % 16 * 16;
+        v4i staged[RT];
+        int e[RT], e_next[RT];
+        auto fetch = [&](int h) {       // half tile h
+#pragma unroll
+            for (int r = 0; r < RT; ++r) staged[r] = *reinterpret_cast<const v4i*>(src[r] + (int64_t)h * 256);
+        };
+        auto put = [&](int buffer) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) *reinterpret_cast<v4i*>(s_mem + (buffer * TILE_ROWS + r * 16) * TILE_STRIDE + to) = staged[r];
+        };
+        auto load_exps = [&](int kt) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) e_next[r] = *reinterpret_cast<const uint16_t*>(exps[r] + (int64_t)kt * 8);
+        };
+        v4f y[RT][4] = {};
+        const int unit = 4 * (q & 1) + (q >> 1);
+        const char* const at = s_mem + col * TILE_STRIDE + unit * 16;
+        auto half = [&](auto jc, const v4i (&wn)[4], const typename Scales<GPT>::type (&f)[4]) {
+            constexpr int j = decltype(jc)::value;
+            int b[4][4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                to_fp4((uint32_t)wn[c][2 * j], b[c][0], b[c][1]);
+                to_fp4((uint32_t)wn[c][2 * j + 1], b[c][2], b[c][3]);
+            }
+            const v4f zero = {0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const char* const x = at + (j * TILE_ROWS + r * 16) * TILE_STRIDE;
+                const v8i hi = join(*reinterpret_cast<const v4i*>(x), *reinterpret_cast<const v4i*>(x + 32));
+                const v8i lo = join(*reinterpret_cast<const v4i*>(x + 128), *reinterpret_cast<const v4i*>(x + 160));
+                const int el = e[r] - 0x0505;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if constexpr (GPT == 2) y[r][c] += product<j>(hi, b[c], product<j>(lo, b[c], zero, el), e[r]) * scale_at(f[c], j);
+                    else {
+                        const int b0[4] = {b[c][0], b[c][1], 0, 0}, b1[4] = {0, 0, b[c][2], b[c][3]};
+                        y[r][c] += product<j>(hi, b0, product<j>(lo, b0, zero, el), e[r]) * scale_at(f[c], 2 * j);
+                        y[r][c] += product<j>(hi, b1, product<j>(lo, b1, zero, el), e[r]) * scale_at(f[c], 2 * j + 1);
+                    }
+                }
+            }
+        };
+        fetch(0);
+        load_weights(0);
+        load_exps(0);
+        put(0);
         __syncthreads();
-        const int u = blockIdx.x / KS, c0 = blockIdx.x % KS * (P / 2);     // 128 numbers of h, the first of the units here
-        if (kr == 0) {
-            const int slot = col & 7, byte = 2 * slot + (col >> 3);
+        for (int kt = 0; kt < a.n_kt; ++kt) {
+            const int next = min(kt + 1, a.n_kt - 1);
+            v4i wn[4];
+            typename Scales<GPT>::type f[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                wn[c] = w[c];
+                f[c] = sc[c];
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) e[r] = e_next[r];
+            fetch(2 * kt + 1);
+            load_weights(next);
+            load_exps(next);
+            half(std::integral_constant<int, 0>{}, wn, f);
+            put(1);
+            __syncthreads();
+            fetch(2 * next);
+            half(std::integral_constant<int, 1>{}, wn, f);
+            put(0);
+            __syncthreads();
+        }
+        if constexpr (UP) {
+            // the wave's two pairs are the units g = wave and g + 4 of 128 numbers of h: they share a power of two
+            char* const s_out = s_mem;                       // [rows][2 parts][8 units][16]
+            const int byte = 2 * (col & 7) + (col >> 3);
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int m = r * 16 + q * 4 + i;
-                    const float top = fmaxf(s_top[p % (P / 2) * R + m], s_top[(p % (P / 2) + P / 2) * R + m]);
-                    const int ex = shared_exponent((int)(__float_as_uint(top) >> 23));
+                    const float h0 = silu_mul(y[r][0][i], y[r][1][i]), h1 = silu_mul(y[r][2][i], y[r][3][i]);
+                    const int ex = shared_exponent(largest_field(fmaxf(finite_or_inf(h0), finite_or_inf(h1))));
                     uint32_t hi, lo;
-                    split2(h[r][i], 0.0f, scale_down(ex), hi, lo);
-                    s_out[((m * 2 + 0) * P + p) * 16 + byte] = (char)hi;
-                    s_out[((m * 2 + 1) * P + p) * 16 + byte] = (char)lo;
-                    if (p < P / 2 && col == 0 && m < tile.rows)
-                        a.h_exps[(int64_t)(tile.first + m) * (a.n_out / 32) + u / 2 * 8 + (c0 + p) * 2 + (u & 1)] = (char)ex;
+                    split2(h0, h1, scale_down(ex), hi, lo);
+                    char* const to16 = s_out + m * 256 + wave * 16 + byte;
+                    to16[0] = (char)hi;
+                    to16[64] = (char)(hi >> 8);
+                    to16[128] = (char)lo;
+                    to16[192] = (char)(lo >> 8);
+                    if (col == 0 && m < tile.rows) a.h_exps[(int64_t)(tile.first + m) * (a.n_out / 32) + cg / 2 * 8 + wave * 2 + (cg & 1)] = (char)ex;
+                }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const int m = r * 16 + tid / 16;
+                if (m < tile.rows)
+                    *reinterpret_cast<uint4*>(a.h + (int64_t)(tile.first + m) * a.n_out * 2 + cg * 256 + tid % 16 * 16) =
+                        *reinterpret_cast<const uint4*>(s_out + m * 256 + tid % 16 * 16);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int m = r * 16 + q * 4 + i;
+                    if (m < tile.rows) {
+                        float* const out = a.z + (int64_t)(tile.first + m) * a.n_out + pair[0] * 32 + col;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) out[16 * c] = y[r][c][i];
+                    }
                 }
         }
-        __syncthreads();
-        for (int i = tid; i < R * 2 * P; i += 512) {         // 16 bytes: a unit of a part of a row
-            const int m = i / (2 * P), part = i / P % 2, pp = i % P;
-            if (m < tile.rows) {
-                const int to_unit = c0 + pp % (P / 2) + pp / (P / 2) * 4;
-                *reinterpret_cast<uint4*>(a.h + (int64_t)(tile.first + m) * a.n_out * 2 + u * 256 + part * 128 + to_unit * 16) =
-                    *reinterpret_cast<const uint4*>(s_out + i * 16);
-            }
-        }
-    }
+    };
+    if (tile.rows <= 16) body(std::integral_constant<int, 1>{});
+    else if (tile.rows <= 32) body(std::integral_constant<int, 2>{});
+    else if (tile.rows <= 48) body(std::integral_constant<int, 3>{});
+    else body(std::integral_constant<int, 4>{});
 }
 
 // Y = base + the weighted rows of z, in the order of the slots
@@ -465,30 +679,28 @@ __global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const i
     *reinterpret_cast<uint4*>(a.Y + m * a.ldy + n) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
 }
 
-template <bool UP, int RT, int KS, int GPT>
-int launch_product(const ProductArgs& a, int64_t tiles, hipStream_t stream)
+template <bool UP, int KS, int GPT>
+int launch_few(const ProductArgs& a, int64_t tiles, int64_t row_bytes_all, int units, hipStream_t stream)
 {
-    constexpr int P = 8 / KS;
-    const size_t lds = (size_t)2 * KS * 16 * RT * STRIDE;
-    auto* const kern = moe_product_kernel<UP, RT, KS, GPT>;
-    const int rc = ensure_dynamic_lds((const void*)kern, lds, "w2_moe_experts");
+    typedef FewShape<KS> S;
+    auto* const kern = moe_few_kernel<UP, KS, GPT>;
+    const int rc = ensure_dynamic_lds((const void*)kern, S::LDS, "w2_moe_experts");
     if (rc) return rc;
     const int pairs = UP ? a.n_out / 16 : a.n_out / 32;
-    ProductArgs b = a;
-    for (int64_t t = 0; t < tiles; t += 65535) {             // what a grid's y takes
-        b.tiles = a.tiles + t;
-        hipLaunchKernelGGL(kern, dim3((unsigned)(pairs / P), (unsigned)std::min<int64_t>(tiles - t, 65535)), dim3(512), lds, stream, b);
-    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)(pairs / S::P / units), (unsigned)tiles), dim3(S::THREADS), S::LDS, stream, a, row_bytes_all, units);
     return 0;
 }
 
 template <bool UP, int GPT>
-int launch_shape(const ProductArgs& a, int rt, int ks, int64_t tiles, hipStream_t stream)
+int launch_product(const ProductArgs& a, const moe::Plan& p, int64_t row_bytes_all, const int* n_tiles, hipStream_t stream)
 {
-    if (rt == 1) return ks == 1 ? launch_product<UP, 1, 1, GPT>(a, tiles, stream) : ks == 2 ? launch_product<UP, 1, 2, GPT>(a, tiles, stream)
-                                                                                            : launch_product<UP, 1, 4, GPT>(a, tiles, stream);
-    if (rt == 2) return ks == 1 ? launch_product<UP, 2, 1, GPT>(a, tiles, stream) : launch_product<UP, 2, 2, GPT>(a, tiles, stream);
-    return launch_product<UP, 4, 1, GPT>(a, tiles, stream);
+    if (!p.few) {
+        const int groups = UP ? a.n_out / 128 : a.n_out / 256;
+        hipLaunchKernelGGL((moe_tile_kernel<UP, GPT>), dim3((unsigned)((p.tiles * groups + 7) / 8 * 8)), dim3(256), 0, stream, a, n_tiles, groups);
+        return 0;
+    }
+    const moe::Cut& c = UP ? p.up : p.down;
+    return c.ks == 1 ? launch_few<UP, 1, GPT>(a, p.tiles, row_bytes_all, c.units, stream) : launch_few<UP, 2, GPT>(a, p.tiles, row_bytes_all, c.units, stream);
 }
 
 }  // namespace
@@ -503,29 +715,29 @@ int launch_moe_experts(const ExpertsArgs& a, hipStream_t stream)
     const int64_t A = a.M * a.top_k, hidden = a.e.hidden, inter = a.e.inter;
     const moe::Workspace ws = moe::workspace(hidden, inter, a.e.n_experts, a.M, a.top_k);
     char* const w = (char*)a.workspace;
-    const int rt = moe::pick_rt(A, a.e.n_experts);
-    const int64_t tiles = moe::most_tiles(A, a.e.n_experts, 16 * rt);
-    Tile* const tile = (Tile*)(w + ws.tiles);
-    int* const sorted = (int*)(w + ws.sorted);
+    const moe::Plan plan = moe::plan(hidden, inter, a.e.n_experts, A);
+    int* const n_tiles = (int*)(w + ws.tiles);
+    Tile* const tile = (Tile*)(w + ws.tiles + 256);
+    int* const tile_rows = (int*)(w + ws.tile_rows);
     int* const place = (int*)(w + ws.place);
     const int64_t convert = (a.M * (hidden / 32) + 1023) / 1024;
-    hipLaunchKernelGGL(moe_prepare_kernel, dim3((unsigned)(1 + convert)), dim3(1024), 0, stream, a, tile, tiles, 16 * rt, sorted, place,
-                       w + ws.xs, w + ws.xe);
+    hipLaunchKernelGGL(moe_prepare_kernel, dim3((unsigned)(1 + convert)), dim3(1024), 0, stream, a, n_tiles, tile, plan.tiles, plan.rows, tile_rows,
+                       place, w + ws.xs, w + ws.xe);
     ProductArgs u = {};
     u.blob = (const char*)a.e.gate_up; u.blob_stride = a.e.gate_up_stride; u.codes_bytes = (int64_t)a.up.codes_bytes;
-    u.n_kt = (int)(hidden / 256); u.tiles = tile; u.sorted = sorted; u.top_k = a.top_k;
+    u.n_kt = (int)(hidden / 256); u.tiles = tile; u.tile_rows = tile_rows;
     u.rows = w + ws.xs; u.exps = w + ws.xe; u.h = w + ws.hs; u.h_exps = w + ws.he; u.n_out = (int)inter;
     ProductArgs d = {};
     d.blob = (const char*)a.e.down; d.blob_stride = a.e.down_stride; d.codes_bytes = (int64_t)a.down.codes_bytes;
     d.n_kt = (int)(inter / 256); d.tiles = tile; d.rows = w + ws.hs; d.exps = w + ws.he; d.z = (float*)(w + ws.z); d.n_out = (int)hidden;
-    const int ks_u = moe::pick_ks(rt, tiles * (inter / 128), u.n_kt), ks_d = moe::pick_ks(rt, tiles * (hidden / 256), d.n_kt);
+    const int64_t x_bytes = a.M * (int64_t)moe::row_bytes(hidden), h_bytes = A * (int64_t)moe::row_bytes(inter);
     int rc;
     if (a.e.G == 128) {
-        if ((rc = launch_shape<true, 2>(u, rt, ks_u, tiles, stream))) return rc;
-        if ((rc = launch_shape<false, 2>(d, rt, ks_d, tiles, stream))) return rc;
+        if ((rc = launch_product<true, 2>(u, plan, x_bytes, n_tiles, stream))) return rc;
+        if ((rc = launch_product<false, 2>(d, plan, h_bytes, n_tiles, stream))) return rc;
     } else {
-        if ((rc = launch_shape<true, 4>(u, rt, ks_u, tiles, stream))) return rc;
-        if ((rc = launch_shape<false, 4>(d, rt, ks_d, tiles, stream))) return rc;
+        if ((rc = launch_product<true, 4>(u, plan, x_bytes, n_tiles, stream))) return rc;
+        if ((rc = launch_product<false, 4>(d, plan, h_bytes, n_tiles, stream))) return rc;
     }
     hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)a.M, (unsigned)((hidden + 2047) / 2048)), dim3(256), 0, stream, a, (const int*)place,
                        (const float*)(w + ws.z));

@@ -14,11 +14,45 @@ namespace moe {
 constexpr size_t row_bytes(int64_t K) { return (size_t)K * 2; }
 constexpr size_t exp_bytes(int64_t K) { return (size_t)K / 32; }
 
-struct Workspace {                      // offsets in bytes, each a multiple of 256; none shrinks when M grows
-    size_t tiles, sorted, place, xs, xe, hs, he, z, total;
+inline int64_t most_tiles(int64_t A, int E, int rows) { return std::min<int64_t>(A, E + A / rows); }
+
+struct Cut {                            // of a product's columns and K, few rows
+    int ks;                             // ranges (1, 2) that the four waves of a workgroup cut K into
+    int units;                          // groups of 4 / ks pairs of column blocks that a workgroup takes one behind the other
 };
 
-inline int64_t most_tiles(int64_t A, int E, int rows) { return std::min<int64_t>(A, E + A / rows); }
+struct Plan {
+    bool few;                           // the kernel for few rows, or the one for many
+    int rows;                           // of a tile, at most
+    int64_t tiles;                      // at most
+    Cut up, down;
+};
+
+// pairs: of column blocks; used: tiles that are likely there
+inline Cut cut(int64_t used, int64_t pairs, int64_t n_kt)
+{
+    Cut c;
+    c.ks = used * (pairs / 4) < 768 && n_kt >= 4 ? 2 : 1;
+    c.units = 1;
+    while (c.units < 8 && pairs / 4 * c.ks % (2 * c.units) == 0 && used * (pairs / 4 * c.ks / (2 * c.units)) >= 1536) c.units *= 2;
+    return c;
+}
+
+inline Plan plan(int64_t hidden, int64_t inter, int E, int64_t A)
+{
+    Plan p;
+    const int64_t used = std::min<int64_t>(A, E);
+    p.few = A <= 4 * used;
+    p.rows = p.few ? 8 : 64;
+    p.tiles = most_tiles(A, E, p.rows);
+    p.up = cut(used, inter / 16, hidden / 256);
+    p.down = cut(used, hidden / 32, inter / 256);
+    return p;
+}
+
+struct Workspace {                      // offsets in bytes, each a multiple of 256; none shrinks when M grows
+    size_t tiles, tile_rows, place, xs, xe, hs, he, z, total;
+};
 
 inline Workspace workspace(int64_t hidden, int64_t inter, int E, int64_t M, int top_k)
 {
@@ -26,8 +60,9 @@ inline Workspace workspace(int64_t hidden, int64_t inter, int E, int64_t M, int 
     Workspace w;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
-    w.tiles = take((size_t)most_tiles(A, E, 16) * 16);       // the shortest tiles are the most
-    w.sorted = take((size_t)A * 4);
+    w.tiles = take(256 + (size_t)most_tiles(A, E, 8) * 16); // their number, and the tiles; the shortest ones are the most
+    const Plan p = plan(hidden, inter, E, A);
+    w.tile_rows = take((size_t)p.tiles * p.rows * 4);
     w.place = take((size_t)A * 4);
     w.xs = take((size_t)M * row_bytes(hidden));
     w.xe = take((size_t)M * exp_bytes(hidden));
@@ -36,25 +71,6 @@ inline Workspace workspace(int64_t hidden, int64_t inter, int E, int64_t M, int 
     w.z = take((size_t)A * hidden * 4);
     w.total = at;
     return w;
-}
-
-// Row tiles of 16 a workgroup's wave holds (rt) and the ranges that its waves cut K into (ks).
-struct Shape {
-    int rt, ks;
-};
-
-inline int pick_rt(int64_t A, int E)
-{
-    const int64_t used = std::min<int64_t>(A, E), per = A / used;
-    return per <= 8 ? 1 : per <= 24 ? 2 : 4;
-}
-
-// blocks: workgroups of eight waves without ranges
-inline int pick_ks(int rt, int64_t blocks, int64_t n_kt)
-{
-    int ks = 1;
-    while (ks < 4 && rt * ks < 4 && blocks * ks < 512 && n_kt >= 4 * ks) ks *= 2;
-    return ks;
 }
 
 }  // namespace moe
