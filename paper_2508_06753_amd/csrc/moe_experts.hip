@@ -57,6 +57,51 @@ __device__ __forceinline__ void split2(float a, float b, float f, uint32_t& hi, 
 // 2^(127 - e) for a biased exponent e of 5 .. 248
 __device__ __forceinline__ float scale_down(int e) { return __int_as_float((254 - e) << 23); }
 
+// 32 numbers that share an exponent, the b-th ones of a row x: numbers 16 g .. and 64 + 16 g .. of 128
+__device__ __forceinline__ void split_block(const uint16_t* x, int b, char* row, char* exps)
+{
+    const int kt = b / 8, half = (b & 7) >> 2, g = b & 3;
+    const uint16_t* const src = x + kt * 256 + half * 128 + g * 16;
+    uint32_t d[2][8], top = 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint4 p = *reinterpret_cast<const uint4*>(src + u * 64), q = *reinterpret_cast<const uint4*>(src + u * 64 + 8);
+        const uint32_t w[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            d[u][j] = w[j];
+            top = max(top, max(w[j] & 0x7fffu, w[j] >> 16 & 0x7fffu));
+        }
+    }
+    const int e = shared_exponent((int)(top >> 7));
+    const float f = scale_down(e);
+    char* const dst = row + kt * 512 + half * 256 + g * 16;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        uint32_t hi[8], lo[8];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {                        // numbers n and n + 8 of the unit are neighbours
+            const uint32_t lw = d[u][n / 2], hw = d[u][4 + n / 2];
+            const float p = __uint_as_float(n & 1 ? lw & 0xffff0000u : lw << 16), q = __uint_as_float(n & 1 ? hw & 0xffff0000u : hw << 16);
+            split2(p, q, f, hi[n], lo[n]);
+        }
+        *reinterpret_cast<uint4*>(dst + u * 64) = make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16);
+        *reinterpret_cast<uint4*>(dst + u * 64 + 128) = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
+    }
+    exps[kt * 8 + g * 2 + half] = (char)e;
+}
+
+// The lanes of a wave that hold the same number below 2^bits, of those that are live
+__device__ __forceinline__ uint64_t same_lanes(int id, bool live, int bits)
+{
+    uint64_t same = __ballot(live);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot(live && id >> b & 1);
+        same &= id >> b & 1 ? set : ~set;
+    }
+    return same;
+}
+
 // ---------------------------------------------------------------- before the products: who goes where, and x in two parts
 
 // Workgroup 0 sorts the choices by expert (stable: which rows share a tile is the same every time); the others convert x, a
@@ -72,42 +117,12 @@ __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* t
         const int64_t blocks = a.e.hidden / 32, i = (int64_t)(blockIdx.x - 1) * 1024 + tid;
         if (i >= a.M * blocks) return;
         const int64_t m = i / blocks, b = i - m * blocks;
-        const int64_t kt = b / 8;
-        const int half = (int)(b & 7) >> 2, g = (int)(b & 3);
-        const uint16_t* src = a.x + m * a.ldx + kt * 256 + half * 128 + g * 16;
-        uint32_t d[2][8], top = 0;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const uint4 p = *reinterpret_cast<const uint4*>(src + u * 64), q = *reinterpret_cast<const uint4*>(src + u * 64 + 8);
-            const uint32_t w[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                d[u][j] = w[j];
-                top = max(top, max(w[j] & 0x7fffu, w[j] >> 16 & 0x7fffu));
-            }
-        }
-        const int e = shared_exponent((int)(top >> 7));
-        const float f = scale_down(e);
-        char* dst = xs + m * moe::row_bytes(a.e.hidden) + kt * 512 + half * 256 + g * 16;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            uint32_t hi[8], lo[8];
-            // numbers n and n + 8 of the unit are neighbours
-#pragma unroll
-            for (int n = 0; n < 8; ++n) {
-                const uint32_t lw = d[u][n / 2], hw = d[u][4 + n / 2];
-                const float p = __uint_as_float(n & 1 ? lw & 0xffff0000u : lw << 16), q = __uint_as_float(n & 1 ? hw & 0xffff0000u : hw << 16);
-                split2(p, q, f, hi[n], lo[n]);
-            }
-            *reinterpret_cast<uint4*>(dst + u * 64) = make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16);
-            *reinterpret_cast<uint4*>(dst + u * 64 + 128) = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
-        }
-        xe[m * moe::exp_bytes(a.e.hidden) + kt * 8 + g * 2 + half] = (char)e;
+        split_block(a.x + m * a.ldx, (int)b, xs + m * moe::row_bytes(a.e.hidden), xe + m * moe::exp_bytes(a.e.hidden));
         return;
     }
     constexpr int AT_ONCE = 8;          // loads of 64 choices under way together
-    const int A = (int)(a.M * a.top_k);
-    for (int i = tid; i < 16 * 1024; i += 1024) (&s_count[0][0])[i] = 0;
+    const int A = (int)(a.M * a.top_k), bits = 32 - __clz(E);
+    for (int w = 0; w < 16; ++w) s_count[w][tid] = 0;
     __syncthreads();
     const int share = (A + 1023) / 1024 * 64, begin = min(A, wave * share), end = min(A, begin + share);
     for (int i0 = begin; i0 < end; i0 += 64 * AT_ONCE) {
@@ -163,11 +178,7 @@ __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* t
             if (i0 + b * 64 >= end) break;
             const int i = i0 + b * 64 + lane, id = ids[b];
             const bool live = (unsigned)id < (unsigned)E;
-            uint64_t same = __ballot(live);                  // the lanes of the same expert
-            for (int bit = 0; E >> bit; ++bit) {
-                const uint64_t set = __ballot(live && id >> bit & 1);
-                same &= id >> bit & 1 ? set : ~set;
-            }
+            const uint64_t same = same_lanes(id, live, bits);          // the lanes of the same expert
             const int before = __popcll(same & (((uint64_t)1 << lane) - 1));
             const int at = live ? s_count[wave][id] : 0;
             if (live) {
@@ -221,6 +232,21 @@ __device__ __forceinline__ v4f product(v8i x, const int (&b)[4], v4f acc, int ex
 
 __device__ __forceinline__ v8i join(v4i a, v4i b) { return (v8i){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
 
+// Half j of a lane's 256 k of one column block, rows x in one part each, onto y
+template <int GPT, int J>
+__device__ __forceinline__ void multiply(v8i x, int e, v4i w, typename Scales<GPT>::type sc, v4f& y)
+{
+    int b[4];
+    to_fp4((uint32_t)w[2 * J], b[0], b[1]);
+    to_fp4((uint32_t)w[2 * J + 1], b[2], b[3]);
+    const v4f zero = {0, 0, 0, 0};
+    if constexpr (GPT == 2) y += product<J>(x, b, zero, e) * scale_at(sc, J);
+    else {
+        y += product<J>(x, {b[0], b[1], 0, 0}, zero, e) * scale_at(sc, 2 * J);
+        y += product<J>(x, {0, 0, b[2], b[3]}, zero, e) * scale_at(sc, 2 * J + 1);
+    }
+}
+
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void* p, int64_t bytes)
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(uint32_t)min(bytes, (int64_t)0xffffffff), 0x00020000);
@@ -251,8 +277,8 @@ __device__ __forceinline__ int largest_field(float m)
 
 // What the wave of a pair of blocks leaves: h in two parts (UP; every wave of the workgroup calls it), or rows of z.  The
 // workgroup's P pairs are the units c0 .. c0 + P/2 - 1 and those four further on of the 128 numbers u of h.  s_mem: P * R * 36 bytes.
-template <int RT, int P>
-__device__ __forceinline__ void store_h(const ProductArgs& a, const Tile& tile, char* s_mem, v4f (&y)[RT][2], int p, bool mine, int u, int c0, int threads)
+template <int RT, int P, typename F>
+__device__ __forceinline__ void store_h(char* hs, char* he, int inter, int rows, F place, char* s_mem, v4f (&y)[RT][2], int p, bool mine, int u, int c0, int threads)
 {
     constexpr int R = 16 * RT;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
@@ -282,15 +308,14 @@ __device__ __forceinline__ void store_h(const ProductArgs& a, const Tile& tile, 
                 split2(h[r][i], 0.0f, scale_down(ex), hi, lo);
                 s_out[((m * 2 + 0) * P + p) * 16 + byte] = (char)hi;
                 s_out[((m * 2 + 1) * P + p) * 16 + byte] = (char)lo;
-                if (p < P / 2 && col == 0 && m < tile.rows)
-                    a.h_exps[(int64_t)(tile.first + m) * (a.n_out / 32) + u / 2 * 8 + (c0 + p) * 2 + (u & 1)] = (char)ex;
+                if (p < P / 2 && col == 0 && m < rows) he[(int64_t)place(m) * moe::exp_bytes(inter) + u / 2 * 8 + (c0 + p) * 2 + (u & 1)] = (char)ex;
             }
     }
     __syncthreads();
-    for (int i = tid; i < tile.rows * 2 * P; i += threads) { // 16 bytes: a unit of a part of a row
+    for (int i = tid; i < rows * 2 * P; i += threads) {      // 16 bytes: a unit of a part of a row
         const int m = i / (2 * P), part = i / P % 2, pp = i % P;
         const int to_unit = c0 + pp % (P / 2) + pp / (P / 2) * 4;
-        *reinterpret_cast<uint4*>(a.h + (int64_t)(tile.first + m) * a.n_out * 2 + u * 256 + part * 128 + to_unit * 16) =
+        *reinterpret_cast<uint4*>(hs + (int64_t)place(m) * moe::row_bytes(inter) + u * 256 + part * 128 + to_unit * 16) =
             *reinterpret_cast<const uint4*>(s_out + i * 16);
     }
 }
@@ -312,9 +337,8 @@ struct FewShape {
     static constexpr int LEAVE = std::max((KS - 1) * P * 2048, P * 16 * 36), LDS = 2 * BUFFER + 2 * EXPS + 512 + LEAVE;
 };
 
-// units: groups of P pairs that a workgroup takes one behind the other, the next one's weights under way before the last one's sums leave
 template <bool UP, int KS, int GPT>
-__global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kernel(ProductArgs a, int64_t row_bytes_all, int units)
+__global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kernel(ProductArgs a, int64_t row_bytes_all)
 {
     typedef FewShape<KS> S;
     constexpr int P = S::P, CK = S::CK, R = S::R, STRIDE = S::STRIDE, BUFFER = S::BUFFER, EXPS = S::EXPS, THREADS = S::THREADS;
@@ -335,25 +359,22 @@ __global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kern
     const char* const blob = a.blob + tile.expert * a.blob_stride;
     // pairs of a workgroup lie so that the units g and g + 4 of 128 numbers of h are both its own
     constexpr int GROUPS = 8 / P;
-    auto pair_of = [&](int group) { return UP ? group / GROUPS * 8 + group % GROUPS * (P / 2) + p % (P / 2) + p / (P / 2) * 4 : group * P + p; };
-    struct Weights {                    // of the wave's first column block, its range of K; the second one follows
-        const char *codes, *scales;
-        int tiles;
-    };
-    auto weights_of = [&](int group, bool there) {
-        const int64_t t = (int64_t)(2 * pair_of(group)) * a.n_kt + kt0;
-        return Weights{blob + t * 1024, blob + a.codes_bytes + t * 32 * GPT, there ? my_steps : 0};
-    };
+    const int group = blockIdx.x, pair = UP ? group / GROUPS * 8 + group % GROUPS * (P / 2) + p % (P / 2) + p / (P / 2) * 4 : group * P + p;
+    __amdgpu_buffer_rsrc_t wr[2], sr[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const int64_t t = (int64_t)(2 * pair + c) * a.n_kt + kt0;
+        wr[c] = resource32(blob + t * 1024, my_steps * 1024);
+        sr[c] = resource32(blob + a.codes_bytes + t * 32 * GPT, my_steps * 32 * GPT);
+    }
     v4i w[FEW_W][2];
     typename Scales<GPT>::type sc[FEW_W][2];
-    auto load_weights = [&](const Weights& r, int s, int slot) {
+    auto load_weights = [&](int s, int slot) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            const __amdgpu_buffer_rsrc_t wr = resource32(r.codes + (int64_t)c * a.n_kt * 1024, r.tiles * 1024);
-            const __amdgpu_buffer_rsrc_t sr = resource32(r.scales + (int64_t)c * a.n_kt * 32 * GPT, r.tiles * 32 * GPT);
-            w[slot][c] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(wr, s * 1024 + lane * 16, 0, NT));
-            if constexpr (GPT == 2) sc[slot][c] = __builtin_amdgcn_raw_buffer_load_b32(sr, s * 64 + col * 4, 0, 0);
-            else sc[slot][c] = __builtin_bit_cast(Scales<4>::type, __builtin_amdgcn_raw_buffer_load_b64(sr, s * 128 + col * 8, 0, 0));
+            w[slot][c] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(wr[c], s * 1024 + lane * 16, 0, NT));
+            if constexpr (GPT == 2) sc[slot][c] = __builtin_amdgcn_raw_buffer_load_b32(sr[c], s * 64 + col * 4, 0, 0);
+            else sc[slot][c] = __builtin_bit_cast(Scales<4>::type, __builtin_amdgcn_raw_buffer_load_b64(sr[c], s * 128 + col * 8, 0, 0));
         }
     };
 
@@ -385,11 +406,9 @@ __global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kern
         for (int i = 0; i < S::PIECES; ++i) *reinterpret_cast<v4i*>(to + buffer * BUFFER + i / CK * R * STRIDE + i % CK * 512) = staged[i];
         *reinterpret_cast<uint2*>(to_e + buffer * next_e) = staged_e;
     };
-    const int group0 = blockIdx.x * units;
-    Weights now = weights_of(group0, true);
     fetch(0);
 #pragma unroll
-    for (int i = 0; i < FEW_W; ++i) load_weights(now, i, i);
+    for (int i = 0; i < FEW_W; ++i) load_weights(i, i);
     put(0);
     __syncthreads();
 
@@ -398,86 +417,68 @@ __global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kern
     const char* const at_e = s_mem + 2 * BUFFER + (kr * R + (col & 7)) * CK * 8 + q * 2;
     const int lo_exp = (col >> 3) * 0x0505;
     int turn = 0;                       // the buffer that a chunk of four steps begins in
-    for (int g = 0; g < units; ++g) {
-        const Weights then = weights_of(group0 + g + 1, g + 1 < units);
-        v4f y[1][2] = {};
-        for (int s = 0; s < steps4; s += FEW_W) {
-            const bool last = s + FEW_W >= steps4;
-            const Weights ahead = last ? then : now;
-            const int s_ahead = last ? 0 : s + FEW_W;
+    v4f y[1][2] = {};
+    for (int s = 0; s < steps4; s += FEW_W) {
 #pragma unroll
-            for (int i = 0; i < FEW_W; ++i) {
-                if (i % CK == 0) fetch(s + i + CK < steps4 ? s + i + CK : 0);
-                const int buffer = (i / CK + turn) & 1;
-                // (up-converted only now: a turn early, as they come, the weights would take twice the registers)
-                asm volatile("" : "+v"(w[i][0]), "+v"(w[i][1]), "+v"(sc[i][0]), "+v"(sc[i][1]));
-                const char* const x0 = at + buffer * BUFFER + i % CK * 512;
-                const int e = *reinterpret_cast<const uint16_t*>(at_e + buffer * EXPS + i % CK * 8) - lo_exp;
-                auto half = [&](auto jc) {
-                    constexpr int j = decltype(jc)::value;
-                    const v8i x = join(*reinterpret_cast<const v4i*>(x0 + j * 256), *reinterpret_cast<const v4i*>(x0 + j * 256 + 32));
+        for (int i = 0; i < FEW_W; ++i) {
+            if (i % CK == 0) fetch(s + i + CK);
+            const int buffer = (i / CK + turn) & 1;
+            // (up-converted only now: a turn early, as they come, the weights would take twice the registers)
+            asm volatile("" : "+v"(w[i][0]), "+v"(w[i][1]), "+v"(sc[i][0]), "+v"(sc[i][1]));
+            const char* const x0 = at + buffer * BUFFER + i % CK * 512;
+            const int e = *reinterpret_cast<const uint16_t*>(at_e + buffer * EXPS + i % CK * 8) - lo_exp;
+            auto half = [&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                const v8i x = join(*reinterpret_cast<const v4i*>(x0 + j * 256), *reinterpret_cast<const v4i*>(x0 + j * 256 + 32));
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        int b[4];
-                        to_fp4((uint32_t)w[i][n][2 * j], b[0], b[1]);
-                        to_fp4((uint32_t)w[i][n][2 * j + 1], b[2], b[3]);
-                        const v4f zero = {0, 0, 0, 0};
-                        if constexpr (GPT == 2) y[0][n] += product<j>(x, b, zero, e) * scale_at(sc[i][n], j);
-                        else {
-                            y[0][n] += product<j>(x, {b[0], b[1], 0, 0}, zero, e) * scale_at(sc[i][n], 2 * j);
-                            y[0][n] += product<j>(x, {0, 0, b[2], b[3]}, zero, e) * scale_at(sc[i][n], 2 * j + 1);
-                        }
-                    }
-                };
-                half(std::integral_constant<int, 0>{});
-                half(std::integral_constant<int, 1>{});
-                // here, and not where they are read: carried on, the products' operands would take every register
-                asm volatile("" : "+v"(y[0][0]), "+v"(y[0][1]));
-                __builtin_amdgcn_sched_barrier(0);
-                load_weights(ahead, s_ahead + i, i);
-                if (i % CK == CK - 1) {
-                    put((i / CK + 1 + turn) & 1);
-                    __syncthreads();
-                }
-                __builtin_amdgcn_sched_barrier(0);
+                for (int n = 0; n < 2; ++n) multiply<GPT, j>(x, e, w[i][n], sc[i][n], y[0][n]);
+            };
+            half(std::integral_constant<int, 0>{});
+            half(std::integral_constant<int, 1>{});
+            // here, and not where they are read: carried on, the products' operands would take every register
+            asm volatile("" : "+v"(y[0][0]), "+v"(y[0][1]));
+            __builtin_amdgcn_sched_barrier(0);
+            load_weights(s + i + FEW_W, i);
+            if (i % CK == CK - 1) {
+                put((i / CK + 1 + turn) & 1);
+                __syncthreads();
             }
-            if (CK == 4) turn ^= 1;
+            __builtin_amdgcn_sched_barrier(0);
         }
-        // hi's sums and lo's
+        if (CK == 4) turn ^= 1;
+    }
+    // hi's sums and lo's
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[0][n][i] += __shfl_xor(y[0][n][i], 32);
-        if constexpr (KS > 1) {                              // ranges of K meet in local memory, in their order
-            v4f* const part = reinterpret_cast<v4f*>(s_leave);         // [KS - 1][P][2][64]
-            if (kr > 0) {
+        for (int i = 0; i < 4; ++i) y[0][n][i] += __shfl_xor(y[0][n][i], 32);
+    if constexpr (KS > 1) {                              // ranges of K meet in local memory, in their order
+        v4f* const part = reinterpret_cast<v4f*>(s_leave);         // [KS - 1][P][2][64]
+        if (kr > 0) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n) part[(((kr - 1) * P + p) * 2 + n) * 64 + lane] = y[0][n];
-            }
-            __syncthreads();
-            if (kr == 0) {
-#pragma unroll
-                for (int k = 0; k < KS - 1; ++k)
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) y[0][n] += part[((k * P + p) * 2 + n) * 64 + lane];
-            }
-            __syncthreads();
+            for (int n = 0; n < 2; ++n) part[(((kr - 1) * P + p) * 2 + n) * 64 + lane] = y[0][n];
         }
-        const int group = group0 + g;
-        if constexpr (UP) {
-            store_h<1, P>(a, tile, s_leave, y, p, kr == 0, group / GROUPS, group % GROUPS * (P / 2), THREADS);
-        } else if (kr == 0) {
+        __syncthreads();
+        if (kr == 0) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int m = q * 4 + i;
-                if (m < tile.rows) {
-                    float* const out = a.z + (int64_t)(tile.first + m) * a.n_out + pair_of(group) * 32 + col;
-                    out[0] = y[0][0][i];
-                    out[16] = y[0][1][i];
-                }
+            for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) y[0][n] += part[((k * P + p) * 2 + n) * 64 + lane];
+        }
+        __syncthreads();
+    }
+    if constexpr (UP) {
+        store_h<1, P>(a.h, a.h_exps, a.n_out, tile.rows, [&](int m) { return tile.first + m; }, s_leave, y, p, kr == 0, group / GROUPS, group % GROUPS * (P / 2), THREADS);
+    } else if (kr == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int m = q * 4 + i;
+            if (m < tile.rows) {
+                float* const out = a.z + (int64_t)(tile.first + m) * a.n_out + pair * 32 + col;
+                out[0] = y[0][0][i];
+                out[16] = y[0][1][i];
             }
         }
-        now = then;
     }
 }
 
@@ -651,6 +652,267 @@ __global__ void __launch_bounds__(256, 2) moe_tile_kernel(ProductArgs a, const i
     else body(std::integral_constant<int, 4>{});
 }
 
+// ---------------------------------------------------------------- up to 64 choices in two launches
+
+// Every workgroup finds out for itself which rows share an expert: lane i of a wave holds choice i.  Tiles of up to eight
+// choices of one expert, in the order of their first ones.
+struct Choice {
+    int id, tile, row;                  // of lane i's choice: its expert (-1: none), its tile, its row there
+    int tiles;                          // all of them
+};
+
+__device__ __forceinline__ Choice choose(const int32_t* ids, int A, int E)
+{
+    const int lane = threadIdx.x & 63;
+    Choice c;
+    const int id = lane < A ? ids[lane] : -1;
+    const bool live = (unsigned)id < (unsigned)E;
+    const uint64_t before = ((uint64_t)1 << lane) - 1;
+    uint64_t same = same_lanes(id, live, 32 - __clz(E));
+    const int nth = __popcll(same & before);
+    const uint64_t firsts = __ballot(live && nth % 8 == 0);
+    // the first choice of the lane's tile: eight choices of the expert further on for each tile before it
+    for (int n = nth / 8; __any(live && n > 0); --n)
+        if (n > 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) same &= same - 1;
+        }
+    c.id = live ? id : -1;
+    c.row = nth % 8;
+    c.tile = live ? __popcll(firsts & (((uint64_t)1 << (__ffsll((unsigned long long)same) - 1)) - 1)) : -1;
+    c.tiles = __popcll(firsts);
+    return c;
+}
+
+constexpr int TINY_EARLY = 2;
+constexpr int TINY_W = 4, TINY_KS = 4, TINY_P = 2;           // of the gate and up projection: 8 waves = 2 pairs of blocks times 4 ranges of K
+
+// A workgroup: a tile and `units` groups of two pairs of blocks.  It brings its rows into two parts in local memory itself, all of K,
+// and then streams weights past them; h leaves by the number of its choice.
+template <int GPT>
+__global__ void __launch_bounds__(512, 2) moe_tiny_up_kernel(ExpertsArgs a, char* hs, char* he, int units, int lds_rows)
+{
+    constexpr int P = TINY_P, KS = TINY_KS;
+    extern __shared__ char s_mem[];                          // rows [lds_rows][2 K + 16], exponents [lds_rows][K / 32]
+    __shared__ __align__(16) char s_leave[(KS - 1) * P * 2048];
+    __shared__ int s_row[8];
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int A = (int)(a.M * a.top_k), n_kt = (int)(a.e.hidden / 256);
+    const int stride = n_kt * 512 + 16, blocks = n_kt * 8;
+    char* const s_exp = s_mem + lds_rows * stride;
+    auto bring = [&](int rows, auto source) {                // 32 numbers at a time
+        for (int r = 0, b = tid; r < rows; b += 512) {
+            while (r < rows && b >= blocks) {
+                b -= blocks;
+                ++r;
+            }
+            if (r < rows) split_block(a.x + source(r) * a.ldx, b, s_mem + r * stride, s_exp + r * blocks);
+        }
+    };
+    // one or two rows of x are brought in before it is known which choices they are
+    const bool early = a.M <= TINY_EARLY;
+    const Choice c = choose(a.ids, A, a.e.n_experts);
+    if (early) bring((int)a.M, [](int r) { return (int64_t)r; });
+    if ((int)blockIdx.y >= c.tiles) return;
+    const uint64_t mine = __ballot(c.tile == (int)blockIdx.y);
+    const int rows = __popcll(mine), expert = __builtin_amdgcn_readlane(c.id, __ffsll((unsigned long long)mine) - 1);
+    const int p = wave % P, kr = wave / P;
+    const int steps = (n_kt + KS - 1) / KS, steps4 = (steps + TINY_W - 1) / TINY_W * TINY_W;
+    const int kt0 = kr * steps, my_steps = max(0, min(steps, n_kt - kt0));
+    const char* const blob = (const char*)a.e.gate_up + expert * a.e.gate_up_stride;
+    constexpr int GROUPS = 8 / P;       // pairs of a workgroup lie so that the units g and g + 4 of 128 numbers of h are both its own
+    struct Weights {                    // of the wave's first column block, its range of K; the second one follows
+        const char *codes, *scales;
+        int tiles;
+    };
+    auto weights_of = [&](int unit) {
+        const int group = blockIdx.x * units + unit;
+        const int pair = group / GROUPS * 8 + group % GROUPS * (P / 2) + p % (P / 2) + p / (P / 2) * 4;
+        const int64_t t = (int64_t)(2 * pair) * n_kt + kt0;
+        return Weights{blob + t * 1024, blob + a.up.codes_bytes + t * 32 * GPT, unit < units ? my_steps : 0};
+    };
+    v4i w[TINY_W][2];
+    typename Scales<GPT>::type sc[TINY_W][2];
+    auto load_weights = [&](const Weights& r, int s, int slot) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const __amdgpu_buffer_rsrc_t wr = resource32(r.codes + (int64_t)n * n_kt * 1024, r.tiles * 1024);
+            const __amdgpu_buffer_rsrc_t sr = resource32(r.scales + (int64_t)n * n_kt * 32 * GPT, r.tiles * 32 * GPT);
+            w[slot][n] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(wr, s * 1024 + lane * 16, 0, NT));
+            if constexpr (GPT == 2) sc[slot][n] = __builtin_amdgcn_raw_buffer_load_b32(sr, s * 64 + col * 4, 0, 0);
+            else sc[slot][n] = __builtin_bit_cast(Scales<4>::type, __builtin_amdgcn_raw_buffer_load_b64(sr, s * 128 + col * 8, 0, 0));
+        }
+    };
+    Weights now = weights_of(0);
+#pragma unroll
+    for (int i = 0; i < TINY_W; ++i) load_weights(now, i, i);
+
+    if (wave == 0 && c.tile == (int)blockIdx.y) s_row[c.row] = lane;
+    __syncthreads();
+    if (!early) {
+        bring(rows, [&](int r) { return (int64_t)(s_row[r] / a.top_k); });
+        __syncthreads();
+    }
+
+    const int nth = min(col & 7, rows - 1), row = early ? s_row[nth] / a.top_k : nth;         // (rows that are not there: the last one again)
+    const char* const at = s_mem + row * stride + (4 * (q & 1) + (q >> 1)) * 16 + (col >> 3) * 128;
+    const char* const at_e = s_exp + row * blocks + q * 2;
+    const int lo_exp = (col >> 3) * 0x0505;
+    for (int unit = 0; unit < units; ++unit) {
+        const Weights then = weights_of(unit + 1);
+        v4f y[1][2] = {};
+        for (int s = 0; s < steps4; s += TINY_W) {
+            const bool last = s + TINY_W >= steps4;
+            const Weights ahead = last ? then : now;
+            const int s_ahead = last ? 0 : s + TINY_W;
+#pragma unroll
+            for (int i = 0; i < TINY_W; ++i) {
+                asm volatile("" : "+v"(w[i][0]), "+v"(w[i][1]), "+v"(sc[i][0]), "+v"(sc[i][1]));
+                const int kt = min(kt0 + s + i, n_kt - 1);   // (past the range: weights of zero, and numbers that are there)
+                const char* const x0 = at + kt * 512;
+                const int e = *reinterpret_cast<const uint16_t*>(at_e + kt * 8) - lo_exp;
+                auto half = [&](auto jc) {
+                    constexpr int j = decltype(jc)::value;
+                    const v8i x = join(*reinterpret_cast<const v4i*>(x0 + j * 256), *reinterpret_cast<const v4i*>(x0 + j * 256 + 32));
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) multiply<GPT, j>(x, e, w[i][n], sc[i][n], y[0][n]);
+                };
+                half(std::integral_constant<int, 0>{});
+                half(std::integral_constant<int, 1>{});
+                asm volatile("" : "+v"(y[0][0]), "+v"(y[0][1]));
+                __builtin_amdgcn_sched_barrier(0);
+                load_weights(ahead, s_ahead + i, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[0][n][i] += __shfl_xor(y[0][n][i], 32);
+        v4f* const part = reinterpret_cast<v4f*>(s_leave);   // [KS - 1][P][2][64]
+        if (kr > 0) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) part[(((kr - 1) * P + p) * 2 + n) * 64 + lane] = y[0][n];
+        }
+        __syncthreads();
+        if (kr == 0) {
+#pragma unroll
+            for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) y[0][n] += part[((k * P + p) * 2 + n) * 64 + lane];
+        }
+        __syncthreads();
+        const int group = blockIdx.x * units + unit;
+        store_h<1, P>(hs, he, (int)a.e.inter, rows, [&](int m) { return s_row[m]; }, s_leave, y, p, kr == 0, group / GROUPS, group % GROUPS * (P / 2), 512);
+        __syncthreads();
+        now = then;
+    }
+}
+
+// A workgroup: one block of columns, eight waves.  All tiles one behind the other are a run of K that the waves share out; a wave adds
+// a tile's rows, weighted, to its sums of every row of Y, and the waves' sums meet in their order.
+template <int GPT>
+__global__ void __launch_bounds__(512, 2) moe_tiny_down_kernel(ExpertsArgs a, const char* hs, const char* he)
+{
+    extern __shared__ char s_mem[];                          // sums [8][M][16]
+    __shared__ int s_row[64][8], s_expert[64], s_rows[64];
+    __shared__ float s_weight[64];
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int A = (int)(a.M * a.top_k), M = (int)a.M, n_kt = (int)(a.e.inter / 256);
+    const Choice c = choose(a.ids, A, a.e.n_experts);
+    if (wave == 0) {
+        s_rows[lane] = 0;
+        if (c.id >= 0) {
+            s_row[c.tile][c.row] = lane;
+            s_expert[c.tile] = c.id;
+            atomicMax(&s_rows[c.tile], c.row + 1);
+            s_weight[lane] = a.weights[lane];
+        }
+    }
+    float* const sums = reinterpret_cast<float*>(s_mem) + wave * M * 16;
+    for (int i = lane; i < M * 16; i += 64) sums[i] = 0.0f;
+    __syncthreads();
+
+    const int all = c.tiles * n_kt, begin = all * wave / 8, end = all * (wave + 1) / 8;
+    const int64_t cb = blockIdx.x;
+    const char* const codes = (const char*)a.e.down + cb * n_kt * 1024 + lane * 16;
+    const char* const scales = (const char*)a.e.down + a.down.codes_bytes + cb * n_kt * 32 * GPT + col * 2 * GPT;
+    const int in_row = (4 * (q & 1) + (q >> 1)) * 16 + (col >> 3) * 128;
+    const int lo_exp = (col >> 3) * 0x0505;
+    struct Slot {
+        v4i w, x[4];
+        typename Scales<GPT>::type sc;
+        int e;
+    } slot[TINY_W];
+    // the next step to load, its tile and what is its own
+    int next = begin, tile_l = begin / n_kt, kt_l = begin - tile_l * n_kt;
+    const char *codes_l = codes, *scales_l = scales, *x_l = hs, *e_l = he;
+    auto enter = [&]() {                // tile_l's weights and rows
+        const int expert = __builtin_amdgcn_readfirstlane(s_expert[tile_l]), row = s_row[tile_l][min(col & 7, s_rows[tile_l] - 1)];
+        codes_l = codes + expert * a.e.down_stride;
+        scales_l = scales + expert * a.e.down_stride;
+        x_l = hs + row * moe::row_bytes(a.e.inter) + in_row;
+        e_l = he + row * moe::exp_bytes(a.e.inter) + q * 2;
+    };
+    auto load = [&](Slot& t) {
+        if (next < end) {
+            t.w = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(codes_l + (int64_t)kt_l * 1024));
+            t.sc = *reinterpret_cast<const typename Scales<GPT>::type*>(scales_l + kt_l * 32 * GPT);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t.x[j] = *reinterpret_cast<const v4i*>(x_l + kt_l * 512 + j / 2 * 256 + j % 2 * 32);
+            t.e = *reinterpret_cast<const uint16_t*>(e_l + kt_l * 8);
+            if (++next < end && ++kt_l == n_kt) {
+                kt_l = 0;
+                ++tile_l;
+                enter();
+            }
+        }
+    };
+    if (begin < end) enter();
+#pragma unroll
+    for (int i = 0; i < TINY_W; ++i) load(slot[i]);
+    v4f y = {};
+    int tile = begin / n_kt, left = n_kt - (begin - tile * n_kt);
+    for (int s = begin; s < end; s += TINY_W) {
+#pragma unroll
+        for (int i = 0; i < TINY_W; ++i) {
+            if (s + i < end) {
+                const int e = slot[i].e - lo_exp;
+                multiply<GPT, 0>(join(slot[i].x[0], slot[i].x[1]), e, slot[i].w, slot[i].sc, y);
+                multiply<GPT, 1>(join(slot[i].x[2], slot[i].x[3]), e, slot[i].w, slot[i].sc, y);
+                load(slot[i]);
+                if (--left == 0 || s + i + 1 == end) {       // the tile's rows, or the wave's share of them
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[r] += __shfl_xor(y[r], 32);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)              // four rows of the instruction and then the next: two may be one row of Y
+                        if (q == h) {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (4 * h + r < s_rows[tile]) {
+                                    const int at = s_row[tile][4 * h + r];
+                                    sums[at / a.top_k * 16 + col] += s_weight[at] * y[r];
+                                }
+                        }
+                    y = (v4f){0, 0, 0, 0};
+                    ++tile;
+                    left = n_kt;
+                }
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < M * 16; i += 512) {
+        const int64_t m = i / 16, n = cb * 16 + i % 16;
+        float t = a.base ? __uint_as_float((uint32_t)a.base[m * a.ldb + n] << 16) : 0.0f;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) t += reinterpret_cast<const float*>(s_mem)[v * M * 16 + i];
+        a.Y[m * a.ldy + n] = (uint16_t)pack_bf16(t, t);
+    }
+}
+
 // Y = base + the weighted rows of z, in the order of the slots
 __global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const int* place, const float* z)
 {
@@ -680,14 +942,14 @@ __global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const i
 }
 
 template <bool UP, int KS, int GPT>
-int launch_few(const ProductArgs& a, int64_t tiles, int64_t row_bytes_all, int units, hipStream_t stream)
+int launch_few(const ProductArgs& a, int64_t tiles, int64_t row_bytes_all, hipStream_t stream)
 {
     typedef FewShape<KS> S;
     auto* const kern = moe_few_kernel<UP, KS, GPT>;
     const int rc = ensure_dynamic_lds((const void*)kern, S::LDS, "w2_moe_experts");
     if (rc) return rc;
     const int pairs = UP ? a.n_out / 16 : a.n_out / 32;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(pairs / S::P / units), (unsigned)tiles), dim3(S::THREADS), S::LDS, stream, a, row_bytes_all, units);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(pairs / S::P), (unsigned)tiles), dim3(S::THREADS), S::LDS, stream, a, row_bytes_all);
     return 0;
 }
 
@@ -699,8 +961,7 @@ int launch_product(const ProductArgs& a, const moe::Plan& p, int64_t row_bytes_a
         hipLaunchKernelGGL((moe_tile_kernel<UP, GPT>), dim3((unsigned)((p.tiles * groups + 7) / 8 * 8)), dim3(256), 0, stream, a, n_tiles, groups);
         return 0;
     }
-    const moe::Cut& c = UP ? p.up : p.down;
-    return c.ks == 1 ? launch_few<UP, 1, GPT>(a, p.tiles, row_bytes_all, c.units, stream) : launch_few<UP, 2, GPT>(a, p.tiles, row_bytes_all, c.units, stream);
+    return (UP ? p.ks_up : p.ks_down) == 1 ? launch_few<UP, 1, GPT>(a, p.tiles, row_bytes_all, stream) : launch_few<UP, 2, GPT>(a, p.tiles, row_bytes_all, stream);
 }
 
 }  // namespace
@@ -710,11 +971,29 @@ size_t experts_workspace_bytes(const w2_experts_t& e, int64_t M, int top_k)
     return moe::workspace(e.hidden, e.inter, e.n_experts, M, top_k).total;
 }
 
+namespace {
+
+template <int GPT>
+int launch_tiny(const ExpertsArgs& a, const moe::Tiny& t, char* hs, char* he, hipStream_t stream)
+{
+    const int rc = ensure_dynamic_lds((const void*)moe_tiny_up_kernel<GPT>, t.lds, "w2_moe_experts");
+    if (rc) return rc;
+    hipLaunchKernelGGL((moe_tiny_up_kernel<GPT>), dim3((unsigned)(a.e.inter / 16 / TINY_P / t.units), (unsigned)t.tiles), dim3(512), t.lds, stream, a, hs,
+                       he, t.units, t.rows);
+    hipLaunchKernelGGL((moe_tiny_down_kernel<GPT>), dim3((unsigned)(a.e.hidden / 16)), dim3(512), (size_t)a.M * 512, stream, a, (const char*)hs,
+                       (const char*)he);
+    return check_launch("w2_moe_experts");
+}
+
+}  // namespace
+
 int launch_moe_experts(const ExpertsArgs& a, hipStream_t stream)
 {
     const int64_t A = a.M * a.top_k, hidden = a.e.hidden, inter = a.e.inter;
     const moe::Workspace ws = moe::workspace(hidden, inter, a.e.n_experts, a.M, a.top_k);
     char* const w = (char*)a.workspace;
+    const moe::Tiny tiny = moe::tiny(hidden, inter, a.e.n_experts, A);
+    if (tiny.fits) return a.e.G == 128 ? launch_tiny<2>(a, tiny, w + ws.hs, w + ws.he, stream) : launch_tiny<4>(a, tiny, w + ws.hs, w + ws.he, stream);
     const moe::Plan plan = moe::plan(hidden, inter, a.e.n_experts, A);
     int* const n_tiles = (int*)(w + ws.tiles);
     Tile* const tile = (Tile*)(w + ws.tiles + 256);

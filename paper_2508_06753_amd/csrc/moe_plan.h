@@ -16,27 +16,15 @@ constexpr size_t exp_bytes(int64_t K) { return (size_t)K / 32; }
 
 inline int64_t most_tiles(int64_t A, int E, int rows) { return std::min<int64_t>(A, E + A / rows); }
 
-struct Cut {                            // of a product's columns and K, few rows
-    int ks;                             // ranges (1, 2) that the four waves of a workgroup cut K into
-    int units;                          // groups of 4 / ks pairs of column blocks that a workgroup takes one behind the other
-};
-
 struct Plan {
     bool few;                           // the kernel for few rows, or the one for many
     int rows;                           // of a tile, at most
     int64_t tiles;                      // at most
-    Cut up, down;
+    int ks_up, ks_down;                 // few: ranges (1, 2) that the four waves of a workgroup cut K into
 };
 
 // pairs: of column blocks; used: tiles that are likely there
-inline Cut cut(int64_t used, int64_t pairs, int64_t n_kt)
-{
-    Cut c;
-    c.ks = used * (pairs / 4) < 768 && n_kt >= 4 ? 2 : 1;
-    c.units = 1;
-    while (c.units < 8 && pairs / 4 * c.ks % (2 * c.units) == 0 && used * (pairs / 4 * c.ks / (2 * c.units)) >= 1536) c.units *= 2;
-    return c;
-}
+inline int ranges(int64_t used, int64_t pairs, int64_t n_kt) { return used * (pairs / 4) < 768 && n_kt >= 8 ? 2 : 1; }
 
 inline Plan plan(int64_t hidden, int64_t inter, int E, int64_t A)
 {
@@ -45,9 +33,30 @@ inline Plan plan(int64_t hidden, int64_t inter, int E, int64_t A)
     p.few = A <= 4 * used;
     p.rows = p.few ? 8 : 64;
     p.tiles = most_tiles(A, E, p.rows);
-    p.up = cut(used, inter / 16, hidden / 256);
-    p.down = cut(used, hidden / 32, inter / 256);
+    p.ks_up = ranges(used, inter / 16, hidden / 256);
+    p.ks_down = ranges(used, hidden / 32, inter / 256);
     return p;
+}
+
+// Up to 64 choices (a lane of a wave each): two launches that need nothing prepared.
+struct Tiny {
+    bool fits;
+    int tiles, rows;                    // at most, and rows of a tile
+    int units;                          // groups of two pairs of blocks that a workgroup takes one behind the other
+    size_t lds;                         // rows and their exponents
+};
+
+inline Tiny tiny(int64_t hidden, int64_t inter, int E, int64_t A)
+{
+    Tiny t;
+    t.tiles = (int)most_tiles(A, E, 8);
+    t.rows = (int)std::min<int64_t>(A, 8);                    // (or of x, where two of those are all)
+    t.lds = (size_t)t.rows * (row_bytes(hidden) + 16 + exp_bytes(hidden));
+    t.fits = A <= 64 && t.lds <= (size_t)128 << 10 && t.tiles * hidden * inter <= (int64_t)1 << 27;
+    const int64_t groups = inter / 32;
+    t.units = 1;
+    while (t.units < 8 && groups % (2 * t.units) == 0 && t.tiles * (groups / (2 * t.units)) >= 512) t.units *= 2;
+    return t;
 }
 
 struct Workspace {                      // offsets in bytes, each a multiple of 256; none shrinks when M grows
