@@ -20,6 +20,7 @@
 #include "block_ops.h"
 #include "ffn_ops.h"
 #include "moe_plan.h"
+#include "w2_small_common.h"
 
 namespace w2 {
 
@@ -230,6 +231,15 @@ __device__ __forceinline__ v4f product(v8i x, const int (&b)[4], v4f acc, int ex
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, (v8i){b[0], b[1], b[2], b[3], 0, 0, 0, 0}, acc, 0, 4, BYTE, ex, 0, 128);
 }
 
+// A lane group's two exponents, in the lower bytes of a dword (what lies behind them, of the next group or the next buffer of the
+// workspace, is not used; a load of 16 bits is widened where the compiler likes, and the wait for it stands there)
+__device__ __forceinline__ int load_exponents(const char* p)
+{
+    int e;
+    __builtin_memcpy(&e, p, 4);
+    return e;
+}
+
 __device__ __forceinline__ v8i join(v4i a, v4i b) { return (v8i){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
 
 // Half j of a lane's 256 k of one column block, rows x in one part each, onto y
@@ -257,7 +267,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource32(const void* p, int 
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
 }
 
-__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+// (the reciprocal is good to one step of fp32; an infinite exponential gives 0)
+__device__ __forceinline__ float silu_mul(float g, float u) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u; }
 
 __device__ __forceinline__ float finite_or_inf(float h)      // |h|, a NaN as the largest
 {
@@ -482,16 +493,20 @@ __global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kern
     }
 }
 
-// Many rows: bound by the matrix pipe.  A workgroup: four waves of 64 columns each (two pairs of blocks), up to 64 rows of
-// one expert, half a tile of K (128) at a time through local memory.  As wide a wave as that because each wave reads every
-// row's operands: with 32 columns a wave the local memory is asked for as long as the matrix pipe is.
-constexpr int TILE_ROWS = 64;
-constexpr int TILE_STRIDE = 256 + 16;
+// Many rows: bound by the matrix pipe.  A workgroup: four waves of 64 columns each (two pairs of blocks), up to 32 rows of
+// one expert.  As wide a wave as that because each wave reads every row's operands: with 32 columns a wave the local memory is
+// asked for as long as the matrix pipe is.  A stage is 128 of K: its rows go from global to local memory directly, three stages
+// ahead in a ring of four, a KiB (256 bytes of four rows) per instruction; the 16-byte piece p of row r stands at p ^ (r mod 16),
+// so that reads of 16 rows touch every bank once.  Weights and exponents of 256 of K are asked for two tiles ahead.
+//
+// Waits (vector memory operations complete in order): behind stage s its successor's rows have landed, which were asked for in
+// stage s - 2.  Asked for since: rows of two more stages, and one tile's weights (4), scales (4) and exponents (RT).
+constexpr int TILE_ROWS = 32, RING = 4;
 
 template <bool UP, int GPT>
-__global__ void __launch_bounds__(256, 2) moe_tile_kernel(ProductArgs a, const int* n_tiles, int col_groups)
+__global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(ProductArgs a, int64_t row_bytes_all, const int* n_tiles, int col_groups)
 {
-    __shared__ __align__(16) char s_mem[2 * TILE_ROWS * TILE_STRIDE];
+    __shared__ __align__(16) char s_mem[RING * TILE_ROWS * 256];
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // the workgroups of an XCD take tiles in a row: row tiles of an expert meet its weights in that die's L2
@@ -511,102 +526,111 @@ __global__ void __launch_bounds__(256, 2) moe_tile_kernel(ProductArgs a, const i
         codes[c] = blob + t * 1024;
         scales[c] = blob + a.codes_bytes + t * 32 * GPT;
     }
-    v4i w[4];
-    typename Scales<GPT>::type sc[4];
-    auto load_weights = [&](int kt) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            w[c] = *reinterpret_cast<const v4i*>(codes[c] + (int64_t)kt * 1024 + lane * 16);
-            sc[c] = *reinterpret_cast<const typename Scales<GPT>::type*>(scales[c] + (int64_t)kt * 32 * GPT + col * 2 * GPT);
-        }
-    };
-    auto row_of = [&](int r) -> int64_t {
+    auto row_of = [&](int r) -> int64_t {                    // (rows that are not there: the last one again)
         r = min(r, tile.rows - 1);
         return UP ? tile_rows[r] : tile.first + r;
     };
     auto body = [&](auto rt_c) {
-        constexpr int RT = decltype(rt_c)::value;
-        const char* src[RT];            // 16 pieces of a row's 128 k, RT rows (16 apart) to a thread
+        constexpr int RT = decltype(rt_c)::value, BUFFER = RT * 16 * 256;
+        const __amdgpu_buffer_rsrc_t rows = resource(a.rows, row_bytes_all);
+        uint32_t src[RT];
         const char* exps[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            src[r] = a.rows + row_of(r * 16 + tid / 16) * (a.n_kt * 512) + tid % 16 * 16;
+            const int row = (wave * RT + r) * 4 + q;         // of the KiB that this wave brings
+            src[r] = (uint32_t)row_of(row) * (uint32_t)(a.n_kt * 512) + (col ^ (row & 15)) * 16;
             exps[r] = a.exps + row_of(r * 16 + col) * (a.n_kt * 8) + q * 2;
         }
-        const int to = tid / 16 * TILE_STRIDE + tid % 16 * 16;
-        v4i staged[RT];
-        int e[RT], e_next[RT];
-        auto fetch = [&](int h) {       // half tile h
+        struct Weights {
+            v4i w[4];
+            typename Scales<GPT>::type sc[4];
+            int e[RT];
+        } wa, wb;
+        auto load_weights = [&](int kt, Weights& r) {        // (past the last tile: that one again, the loads are counted)
+            kt = min(kt, a.n_kt - 1);
 #pragma unroll
-            for (int r = 0; r < RT; ++r) staged[r] = *reinterpret_cast<const v4i*>(src[r] + (int64_t)h * 256);
-        };
-        auto put = [&](int buffer) {
+            for (int c = 0; c < 4; ++c) {
+                r.w[c] = *reinterpret_cast<const v4i*>(codes[c] + (int64_t)kt * 1024 + lane * 16);
+                r.sc[c] = *reinterpret_cast<const typename Scales<GPT>::type*>(scales[c] + (int64_t)kt * 32 * GPT + col * 2 * GPT);
+            }
 #pragma unroll
-            for (int r = 0; r < RT; ++r) *reinterpret_cast<v4i*>(s_mem + (buffer * TILE_ROWS + r * 16) * TILE_STRIDE + to) = staged[r];
+            for (int i = 0; i < RT; ++i) r.e[i] = load_exponents(exps[i] + (int64_t)kt * 8);
         };
-        auto load_exps = [&](int kt) {
+        auto load_rows = [&](int stage) {
+            char* const to = s_mem + (stage & (RING - 1)) * BUFFER + wave * RT * 1024;
+            const uint32_t off = (uint32_t)min(stage, 2 * a.n_kt - 1) * 256;
 #pragma unroll
-            for (int r = 0; r < RT; ++r) e_next[r] = *reinterpret_cast<const uint16_t*>(exps[r] + (int64_t)kt * 8);
+            for (int r = 0; r < RT; ++r) load_to_lds(rows, (int8_t*)to + r * 1024, src[r], off);
         };
-        v4f y[RT][4] = {};
+        int at[4];                      // hi and lo, lower and upper 16 bytes of a lane's operand
         const int unit = 4 * (q & 1) + (q >> 1);
-        const char* const at = s_mem + col * TILE_STRIDE + unit * 16;
-        auto half = [&](auto jc, const v4i (&wn)[4], const typename Scales<GPT>::type (&f)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i] = col * 256 + (((i >> 1) * 8 + unit + (i & 1) * 2) ^ col) * 16;
+        v4f y[RT][4] = {};
+        auto stage = [&](int s, auto jc, Weights& wt) {
             constexpr int j = decltype(jc)::value;
+            const char* const x = s_mem + (s & (RING - 1)) * BUFFER;
             int b[4][4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                to_fp4((uint32_t)wn[c][2 * j], b[c][0], b[c][1]);
-                to_fp4((uint32_t)wn[c][2 * j + 1], b[c][2], b[c][3]);
+                to_fp4((uint32_t)wt.w[c][2 * j], b[c][0], b[c][1]);
+                to_fp4((uint32_t)wt.w[c][2 * j + 1], b[c][2], b[c][3]);
             }
             const v4f zero = {0, 0, 0, 0};
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const char* const x = at + (j * TILE_ROWS + r * 16) * TILE_STRIDE;
-                const v8i hi = join(*reinterpret_cast<const v4i*>(x), *reinterpret_cast<const v4i*>(x + 32));
-                const v8i lo = join(*reinterpret_cast<const v4i*>(x + 128), *reinterpret_cast<const v4i*>(x + 160));
-                const int el = e[r] - 0x0505;
+                auto piece = [&](int i) { return *reinterpret_cast<const v4i*>(x + r * 4096 + at[i]); };
+                const v8i hi = join(piece(0), piece(1)), lo = join(piece(2), piece(3));
+                const int eh = wt.e[r], el = wt.e[r] - 0x0505;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    if constexpr (GPT == 2) y[r][c] += product<j>(hi, b[c], product<j>(lo, b[c], zero, el), e[r]) * scale_at(f[c], j);
+                    if constexpr (GPT == 2) y[r][c] += product<j>(hi, b[c], product<j>(lo, b[c], zero, el), eh) * scale_at(wt.sc[c], j);
                     else {
                         const int b0[4] = {b[c][0], b[c][1], 0, 0}, b1[4] = {0, 0, b[c][2], b[c][3]};
-                        y[r][c] += product<j>(hi, b0, product<j>(lo, b0, zero, el), e[r]) * scale_at(f[c], 2 * j);
-                        y[r][c] += product<j>(hi, b1, product<j>(lo, b1, zero, el), e[r]) * scale_at(f[c], 2 * j + 1);
+                        y[r][c] += product<j>(hi, b0, product<j>(lo, b0, zero, el), eh) * scale_at(wt.sc[c], 2 * j);
+                        y[r][c] += product<j>(hi, b1, product<j>(lo, b1, zero, el), eh) * scale_at(wt.sc[c], 2 * j + 1);
                     }
                 }
             }
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) asm volatile("" : "+v"(y[r][c]));          // here, not behind the barrier
+            wait_loads<3 * RT + 8>();
+            bare_barrier();
         };
-        fetch(0);
-        load_weights(0);
-        load_exps(0);
-        put(0);
-        __syncthreads();
-        for (int kt = 0; kt < a.n_kt; ++kt) {
-            const int next = min(kt + 1, a.n_kt - 1);
-            v4i wn[4];
-            typename Scales<GPT>::type f[4];
+        // in the order of the loop: stage 0's wait counts what the others do
+        load_weights(0, wa);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                wn[c] = w[c];
-                f[c] = sc[c];
-            }
-#pragma unroll
-            for (int r = 0; r < RT; ++r) e[r] = e_next[r];
-            fetch(2 * kt + 1);
-            load_weights(next);
-            load_exps(next);
-            half(std::integral_constant<int, 0>{}, wn, f);
-            put(1);
-            __syncthreads();
-            fetch(2 * next);
-            half(std::integral_constant<int, 1>{}, wn, f);
-            put(0);
-            __syncthreads();
+        for (int s = 0; s < RING - 1; ++s) load_rows(s);
+        __builtin_amdgcn_sched_barrier(0);
+        load_weights(1, wb);
+        wait_loads<3 * RT + 8>();
+        bare_barrier();
+        auto tile_of_k = [&](int kt, Weights& wt) {
+            load_rows(2 * kt + 3);
+            __builtin_amdgcn_sched_barrier(0);
+            stage(2 * kt, std::integral_constant<int, 0>{}, wt);
+            load_rows(2 * kt + 4);
+            __builtin_amdgcn_sched_barrier(0);
+            // the second half of the tile needs its weights still: the next but one's follow it
+            stage(2 * kt + 1, std::integral_constant<int, 1>{}, wt);
+            load_weights(kt + 2, wt);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        int kt = 0;                     // (two at a time without a branch between them, past which the compiler would count fewer loads)
+        for (; kt + 1 < a.n_kt; kt += 2) {
+            tile_of_k(kt, wa);
+            tile_of_k(kt + 1, wb);
         }
+        if (kt < a.n_kt) tile_of_k(kt, wa);
+        wait_loads<0>();                // what was asked for past the end has landed
+        __syncthreads();
         if constexpr (UP) {
             // the wave's two pairs are the units g = wave and g + 4 of 128 numbers of h: they share a power of two
-            char* const s_out = s_mem;                       // [rows][2 parts][8 units][16]
+            char* const s_out = s_mem;                       // [rows][2 parts][8 units][16], then exponents [rows][4]
+            char* const s_exp = s_mem + TILE_ROWS * 256;
             const int byte = 2 * (col & 7) + (col >> 3);
 #pragma unroll
             for (int r = 0; r < RT; ++r)
@@ -622,14 +646,16 @@ __global__ void __launch_bounds__(256, 2) moe_tile_kernel(ProductArgs a, const i
                     to16[64] = (char)(hi >> 8);
                     to16[128] = (char)lo;
                     to16[192] = (char)(lo >> 8);
-                    if (col == 0 && m < tile.rows) a.h_exps[(int64_t)(tile.first + m) * (a.n_out / 32) + cg / 2 * 8 + wave * 2 + (cg & 1)] = (char)ex;
+                    s_exp[m * 4 + wave] = (char)ex;          // (the same from 16 lanes)
                 }
             __syncthreads();
+            if (tid < tile.rows * 4)
+                a.h_exps[(int64_t)(tile.first + tid / 4) * moe::exp_bytes(a.n_out) + cg / 2 * 8 + tid % 4 * 2 + (cg & 1)] = s_exp[tid];
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 const int m = r * 16 + tid / 16;
                 if (m < tile.rows)
-                    *reinterpret_cast<uint4*>(a.h + (int64_t)(tile.first + m) * a.n_out * 2 + cg * 256 + tid % 16 * 16) =
+                    *reinterpret_cast<uint4*>(a.h + (int64_t)(tile.first + m) * moe::row_bytes(a.n_out) + cg * 256 + tid % 16 * 16) =
                         *reinterpret_cast<const uint4*>(s_out + m * 256 + tid % 16 * 16);
             }
         } else {
@@ -647,9 +673,7 @@ __global__ void __launch_bounds__(256, 2) moe_tile_kernel(ProductArgs a, const i
         }
     };
     if (tile.rows <= 16) body(std::integral_constant<int, 1>{});
-    else if (tile.rows <= 32) body(std::integral_constant<int, 2>{});
-    else if (tile.rows <= 48) body(std::integral_constant<int, 3>{});
-    else body(std::integral_constant<int, 4>{});
+    else body(std::integral_constant<int, 2>{});
 }
 
 // ---------------------------------------------------------------- up to 64 choices in two launches
@@ -862,7 +886,7 @@ __global__ void __launch_bounds__(512, 2) moe_tiny_down_kernel(ExpertsArgs a, co
             t.sc = *reinterpret_cast<const typename Scales<GPT>::type*>(scales_l + kt_l * 32 * GPT);
 #pragma unroll
             for (int j = 0; j < 4; ++j) t.x[j] = *reinterpret_cast<const v4i*>(x_l + kt_l * 512 + j / 2 * 256 + j % 2 * 32);
-            t.e = *reinterpret_cast<const uint16_t*>(e_l + kt_l * 8);
+            t.e = load_exponents(e_l + kt_l * 8);
             if (++next < end && ++kt_l == n_kt) {
                 kt_l = 0;
                 ++tile_l;
@@ -958,7 +982,7 @@ int launch_product(const ProductArgs& a, const moe::Plan& p, int64_t row_bytes_a
 {
     if (!p.few) {
         const int groups = UP ? a.n_out / 128 : a.n_out / 256;
-        hipLaunchKernelGGL((moe_tile_kernel<UP, GPT>), dim3((unsigned)((p.tiles * groups + 7) / 8 * 8)), dim3(256), 0, stream, a, n_tiles, groups);
+        hipLaunchKernelGGL((moe_tile_kernel<UP, GPT>), dim3((unsigned)((p.tiles * groups + 7) / 8 * 8)), dim3(256), 0, stream, a, row_bytes_all, n_tiles, groups);
         return 0;
     }
     return (UP ? p.ks_up : p.ks_down) == 1 ? launch_few<UP, 1, GPT>(a, p.tiles, row_bytes_all, stream) : launch_few<UP, 2, GPT>(a, p.tiles, row_bytes_all, stream);
@@ -987,8 +1011,24 @@ int launch_tiny(const ExpertsArgs& a, const moe::Tiny& t, char* hs, char* he, hi
 
 }  // namespace
 
-int launch_moe_experts(const ExpertsArgs& a, hipStream_t stream)
+int launch_moe_experts(const ExpertsArgs& all, hipStream_t stream)
 {
+    const int64_t most = moe::most_rows(all.e.hidden, all.e.inter, all.top_k);
+    if (all.M > most) {                 // rows by rows
+        ExpertsArgs part = all;
+        for (int64_t m = 0; m < all.M; m += most) {
+            part.M = std::min(most, all.M - m);
+            part.x = all.x + m * all.ldx;
+            part.ids = all.ids + m * all.top_k;
+            part.weights = all.weights + m * all.top_k;
+            if (all.base) part.base = all.base + m * all.ldb;
+            part.Y = all.Y + m * all.ldy;
+            const int rc = launch_moe_experts(part, stream);
+            if (rc) return rc;
+        }
+        return 0;
+    }
+    const ExpertsArgs& a = all;
     const int64_t A = a.M * a.top_k, hidden = a.e.hidden, inter = a.e.inter;
     const moe::Workspace ws = moe::workspace(hidden, inter, a.e.n_experts, a.M, a.top_k);
     char* const w = (char*)a.workspace;

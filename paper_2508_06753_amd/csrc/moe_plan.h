@@ -31,7 +31,7 @@ inline Plan plan(int64_t hidden, int64_t inter, int E, int64_t A)
     Plan p;
     const int64_t used = std::min<int64_t>(A, E);
     p.few = A <= 4 * used;
-    p.rows = p.few ? 8 : 64;
+    p.rows = p.few ? 8 : 32;
     p.tiles = most_tiles(A, E, p.rows);
     p.ks_up = ranges(used, inter / 16, hidden / 256);
     p.ks_down = ranges(used, hidden / 32, inter / 256);
@@ -63,8 +63,17 @@ struct Workspace {                      // offsets in bytes, each a multiple of 
     size_t tiles, tile_rows, place, xs, xe, hs, he, z, total;
 };
 
+// Rows that go together: their two parts lie within 2 GiB, offsets in 32 bits reach them, and their sums within 4 GiB
+inline int64_t most_rows(int64_t hidden, int64_t inter, int top_k)
+{
+    const int64_t rows = std::min(((int64_t)1 << 31) / (int64_t)row_bytes(hidden),
+                                  ((int64_t)1 << 31) / (top_k * std::max<int64_t>((int64_t)row_bytes(inter), hidden * 2)));
+    return std::max<int64_t>(rows, 1);
+}
+
 inline Workspace workspace(int64_t hidden, int64_t inter, int E, int64_t M, int top_k)
 {
+    M = std::min(M, most_rows(hidden, inter, top_k));
     const int64_t A = M * top_k;
     Workspace w;
     size_t at = 0;
