@@ -105,13 +105,12 @@ __device__ __forceinline__ uint64_t same_lanes(int id, bool live, int bits)
 
 // ---------------------------------------------------------------- before the products: who goes where, and x in two parts
 
-// Workgroup 0 sorts the choices by expert (stable: which rows share a tile is the same every time); the others convert x, a
-// thread 32 numbers.
-__global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* total_tiles, Tile* tiles, int64_t max_tiles, int rows, int* tile_rows,
-                                                           int* place, char* xs, char* xe)
+// Workgroup 0 sorts the choices by expert; the others convert x, a thread 32 numbers.  A choice's place among its expert's is
+// whichever it gets: what a row gives does not depend on the rows beside it, nor on where it stands.
+__global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* total_tiles, Tile* tiles, int64_t max_tiles, int rows_log2, Divider by_top_k,
+                                                           int* tile_rows, int* place, char* xs, char* xe)
 {
-    __shared__ int s_count[16][1024];   // of each wave's share, then where its rows of each expert begin
-    __shared__ int s_sum[2][16], s_first[1024], s_tile[1024];
+    __shared__ int s_next[1024], s_first[1024], s_tile[1024], s_sum[2][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int E = a.e.n_experts;
     if (blockIdx.x > 0) {
@@ -121,27 +120,21 @@ __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* t
         split_block(a.x + m * a.ldx, (int)b, xs + m * moe::row_bytes(a.e.hidden), xe + m * moe::exp_bytes(a.e.hidden));
         return;
     }
-    constexpr int AT_ONCE = 8;          // loads of 64 choices under way together
-    const int A = (int)(a.M * a.top_k), bits = 32 - __clz(E);
-    for (int w = 0; w < 16; ++w) s_count[w][tid] = 0;
+    constexpr int AT_ONCE = 4;          // loads of 1024 choices under way together
+    const int A = (int)(a.M * a.top_k), rows = 1 << rows_log2;
+    s_next[tid] = 0;
     __syncthreads();
-    const int share = (A + 1023) / 1024 * 64, begin = min(A, wave * share), end = min(A, begin + share);
-    for (int i0 = begin; i0 < end; i0 += 64 * AT_ONCE) {
+    for (int i0 = tid; i0 < A; i0 += 1024 * AT_ONCE) {
         int id[AT_ONCE];
 #pragma unroll
-        for (int b = 0; b < AT_ONCE; ++b) {
-            const int i = i0 + b * 64 + lane;
-            id[b] = i < end ? a.ids[i] : -1;
-        }
+        for (int b = 0; b < AT_ONCE; ++b) id[b] = i0 + b * 1024 < A ? a.ids[i0 + b * 1024] : -1;
 #pragma unroll
         for (int b = 0; b < AT_ONCE; ++b)
-            if ((unsigned)id[b] < (unsigned)E) atomicAdd(&s_count[wave][id[b]], 1);
+            if ((unsigned)id[b] < (unsigned)E) atomicAdd(&s_next[id[b]], 1);
     }
     __syncthreads();
     // thread e: expert e's rows, and where they and its tiles begin
-    int count = 0;
-    for (int w = 0; w < 16; ++w) count += s_count[w][tid];
-    const int n_tiles = (count + rows - 1) / rows;
+    const int count = s_next[tid], n_tiles = (count + rows - 1) >> rows_log2;
     int first = count, tile = n_tiles;                       // inclusive sums over the experts
     for (int off = 1; off < 64; off <<= 1) {
         const int p = __shfl_up(first, off), q = __shfl_up(tile, off);
@@ -157,37 +150,26 @@ __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* t
     first -= count;
     tile -= n_tiles;
     if (tid == 0) *total_tiles = all_tiles;
-    s_first[tid] = first;
-    s_tile[tid] = tile;
     for (int t = 0; t < n_tiles; ++t) tiles[tile + t] = Tile{tid, first + t * rows, min(rows, count - t * rows), 0};
     for (int64_t t = all_tiles + tid; t < max_tiles; t += 1024) tiles[t] = Tile{0, 0, 0, 0};
-    for (int w = 0; w < 16; ++w) {
-        const int n = s_count[w][tid];
-        s_count[w][tid] = first;
-        first += n;
-    }
+    s_first[tid] = first;
+    s_tile[tid] = tile;
+    s_next[tid] = 0;
     __syncthreads();
-    for (int i0 = begin; i0 < end; i0 += 64 * AT_ONCE) {
-        int ids[AT_ONCE];
+    for (int i0 = tid; i0 < A; i0 += 1024 * AT_ONCE) {
+        int id[AT_ONCE];
+#pragma unroll
+        for (int b = 0; b < AT_ONCE; ++b) id[b] = i0 + b * 1024 < A ? a.ids[i0 + b * 1024] : -1;
 #pragma unroll
         for (int b = 0; b < AT_ONCE; ++b) {
-            const int i = i0 + b * 64 + lane;
-            ids[b] = i < end ? a.ids[i] : -1;
-        }
-#pragma unroll
-        for (int b = 0; b < AT_ONCE; ++b) {
-            if (i0 + b * 64 >= end) break;
-            const int i = i0 + b * 64 + lane, id = ids[b];
-            const bool live = (unsigned)id < (unsigned)E;
-            const uint64_t same = same_lanes(id, live, bits);          // the lanes of the same expert
-            const int before = __popcll(same & (((uint64_t)1 << lane) - 1));
-            const int at = live ? s_count[wave][id] : 0;
+            const int i = i0 + b * 1024;
+            const bool live = (unsigned)id[b] < (unsigned)E;
+            int n = 0;
             if (live) {
-                const int n = at + before - s_first[id], t = n / rows;
-                tile_rows[(s_tile[id] + t) * rows + n - t * rows] = i / a.top_k;
-                if (before == 0) s_count[wave][id] = at + __popcll(same);
+                n = atomicAdd(&s_next[id[b]], 1);
+                tile_rows[(s_tile[id[b]] << rows_log2) + n] = (int)divide((uint32_t)i, by_top_k);
             }
-            if (i < end) place[i] = live ? at + before : -1;
+            if (i < A) place[i] = live ? s_first[id[b]] + n : -1;
         }
     }
 }
@@ -212,7 +194,8 @@ struct ProductArgs {
     const int* tile_rows;               // up: which row of x each row of a tile is (down: the places in the sorted order)
     const char *rows, *exps;            // in two parts
     char *h, *h_exps;                   // up: rows of n_out numbers in two parts
-    float* z;                           // down: rows of n_out numbers
+    float* z;                           // down: rows of n_out numbers (few rows in fp32, many in fp16 with exponents of 32 columns)
+    char* z_exps;
     int n_out;
 };
 
@@ -285,6 +268,11 @@ __device__ __forceinline__ int largest_field(float m)
     m = fmaxf(m, dpp_move_f32<0x140>(m));
     return (int)(__float_as_uint(m) >> 23);
 }
+
+// A number as fp16 beside a power of two: the largest of 32 lands in 2^14 .. 2^15.  ex: that power's exponent field
+__device__ __forceinline__ int half_exponent(int field) { return max(field - 14, 1); }
+__device__ __forceinline__ float half_scale(int ex) { return __int_as_float((254 - ex) << 23); }
+__device__ __forceinline__ uint16_t to_half(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 
 // What the wave of a pair of blocks leaves: h in two parts (UP; every wave of the workgroup calls it), or rows of z.  The
 // workgroup's P pairs are the units c0 .. c0 + P/2 - 1 and those four further on of the 128 numbers u of h.  s_mem: P * R * 36 bytes.
@@ -659,17 +647,29 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
                         *reinterpret_cast<const uint4*>(s_out + m * 256 + tid % 16 * 16);
             }
         } else {
+            // 16 bits a number and a power of two for 32 columns: 2^-12 of the number, half the bytes of fp32 twice
+            uint16_t* const s_out = reinterpret_cast<uint16_t*>(s_mem);          // [rows][256 columns], then exponents [rows][8]
+            char* const s_exp = s_mem + TILE_ROWS * 512;
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int m = r * 16 + q * 4 + i;
-                    if (m < tile.rows) {
-                        float* const out = a.z + (int64_t)(tile.first + m) * a.n_out + pair[0] * 32 + col;
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) out[16 * c] = y[r][c][i];
+                    for (int n = 0; n < 2; ++n) {
+                        const float u = y[r][2 * n][i], v = y[r][2 * n + 1][i];
+                        const int ex = half_exponent(largest_field(fmaxf(finite_or_inf(u), finite_or_inf(v))));
+                        const float f = half_scale(ex);
+                        s_out[m * 256 + wave * 64 + n * 32 + col] = to_half(u * f);
+                        s_out[m * 256 + wave * 64 + n * 32 + 16 + col] = to_half(v * f);
+                        s_exp[m * 8 + wave * 2 + n] = (char)ex;        // (the same from 16 lanes)
                     }
                 }
+            __syncthreads();
+            if (tid < tile.rows * 8) a.z_exps[(int64_t)(tile.first + tid / 8) * (a.n_out / 32) + cg * 8 + tid % 8] = s_exp[tid];
+            for (int i = tid; i < tile.rows * 32; i += 256)
+                *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.z) + (int64_t)(tile.first + i / 32) * a.n_out + cg * 256 + i % 32 * 8) =
+                    *reinterpret_cast<const uint4*>(s_out + i * 8);
         }
     };
     if (tile.rows <= 16) body(std::integral_constant<int, 1>{});
@@ -937,8 +937,9 @@ __global__ void __launch_bounds__(512, 2) moe_tiny_down_kernel(ExpertsArgs a, co
     }
 }
 
-// Y = base + the weighted rows of z, in the order of the slots
-__global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const int* place, const float* z)
+// Y = base + the weighted rows of z, in the order of the slots; four rows of z under way together
+template <bool HALF>
+__global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const int* place, const float* z, const char* z_exps)
 {
     const int64_t m = blockIdx.x;
     const int n = (blockIdx.y * 256 + threadIdx.x) * 8;
@@ -953,14 +954,39 @@ __global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const i
             y[2 * i + 1] = __uint_as_float(d[i] & 0xffff0000u);
         }
     }
-    for (int j = 0; j < a.top_k; ++j) {
-        const int at = place[m * a.top_k + j];
-        if (at < 0) continue;
-        const float w = a.weights[m * a.top_k + j];
-        const float4* t = reinterpret_cast<const float4*>(z + (int64_t)at * a.e.hidden + n);
-        const float4 p = t[0], q = t[1];
-        y[0] = fmaf(w, p.x, y[0]); y[1] = fmaf(w, p.y, y[1]); y[2] = fmaf(w, p.z, y[2]); y[3] = fmaf(w, p.w, y[3]);
-        y[4] = fmaf(w, q.x, y[4]); y[5] = fmaf(w, q.y, y[5]); y[6] = fmaf(w, q.z, y[6]); y[7] = fmaf(w, q.w, y[7]);
+    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+    for (int j = 0; j < a.top_k; j += 4) {
+        int at[4], ex[4];
+        float w[4];
+        float4 p[4], q[4];
+        v8h h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i] = j + i < a.top_k ? place[m * a.top_k + j + i] : -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (at[i] >= 0) {
+                w[i] = a.weights[m * a.top_k + j + i];
+                if constexpr (HALF) {
+                    h[i] = *reinterpret_cast<const v8h*>(reinterpret_cast<const uint16_t*>(z) + (int64_t)at[i] * a.e.hidden + n);
+                    ex[i] = (uint8_t)z_exps[(int64_t)at[i] * (a.e.hidden / 32) + n / 32];
+                } else {
+                    const float4* const t = reinterpret_cast<const float4*>(z + (int64_t)at[i] * a.e.hidden + n);
+                    p[i] = t[0];
+                    q[i] = t[1];
+                }
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (at[i] < 0) continue;
+            if constexpr (HALF) {
+                const float f = __int_as_float(ex[i] << 23);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = fmaf(w[i], (float)h[i][e] * f, y[e]);
+            } else {
+                y[0] = fmaf(w[i], p[i].x, y[0]); y[1] = fmaf(w[i], p[i].y, y[1]); y[2] = fmaf(w[i], p[i].z, y[2]); y[3] = fmaf(w[i], p[i].w, y[3]);
+                y[4] = fmaf(w[i], q[i].x, y[4]); y[5] = fmaf(w[i], q[i].y, y[5]); y[6] = fmaf(w[i], q[i].z, y[6]); y[7] = fmaf(w[i], q[i].w, y[7]);
+            }
+        }
     }
     *reinterpret_cast<uint4*>(a.Y + m * a.ldy + n) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
 }
@@ -1040,15 +1066,15 @@ int launch_moe_experts(const ExpertsArgs& all, hipStream_t stream)
     int* const tile_rows = (int*)(w + ws.tile_rows);
     int* const place = (int*)(w + ws.place);
     const int64_t convert = (a.M * (hidden / 32) + 1023) / 1024;
-    hipLaunchKernelGGL(moe_prepare_kernel, dim3((unsigned)(1 + convert)), dim3(1024), 0, stream, a, n_tiles, tile, plan.tiles, plan.rows, tile_rows,
-                       place, w + ws.xs, w + ws.xe);
+    hipLaunchKernelGGL(moe_prepare_kernel, dim3((unsigned)(1 + convert)), dim3(1024), 0, stream, a, n_tiles, tile, plan.tiles, plan.few ? 3 : 5,
+                       make_divider((uint32_t)a.top_k), tile_rows, place, w + ws.xs, w + ws.xe);
     ProductArgs u = {};
     u.blob = (const char*)a.e.gate_up; u.blob_stride = a.e.gate_up_stride; u.codes_bytes = (int64_t)a.up.codes_bytes;
     u.n_kt = (int)(hidden / 256); u.tiles = tile; u.tile_rows = tile_rows;
     u.rows = w + ws.xs; u.exps = w + ws.xe; u.h = w + ws.hs; u.h_exps = w + ws.he; u.n_out = (int)inter;
     ProductArgs d = {};
     d.blob = (const char*)a.e.down; d.blob_stride = a.e.down_stride; d.codes_bytes = (int64_t)a.down.codes_bytes;
-    d.n_kt = (int)(inter / 256); d.tiles = tile; d.rows = w + ws.hs; d.exps = w + ws.he; d.z = (float*)(w + ws.z); d.n_out = (int)hidden;
+    d.n_kt = (int)(inter / 256); d.tiles = tile; d.rows = w + ws.hs; d.exps = w + ws.he; d.z = (float*)(w + ws.z); d.z_exps = w + ws.ze; d.n_out = (int)hidden;
     const int64_t x_bytes = a.M * (int64_t)moe::row_bytes(hidden), h_bytes = A * (int64_t)moe::row_bytes(inter);
     int rc;
     if (a.e.G == 128) {
@@ -1058,8 +1084,9 @@ int launch_moe_experts(const ExpertsArgs& all, hipStream_t stream)
         if ((rc = launch_product<true, 4>(u, plan, x_bytes, n_tiles, stream))) return rc;
         if ((rc = launch_product<false, 4>(d, plan, h_bytes, n_tiles, stream))) return rc;
     }
-    hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)a.M, (unsigned)((hidden + 2047) / 2048)), dim3(256), 0, stream, a, (const int*)place,
-                       (const float*)(w + ws.z));
+    const dim3 combine((unsigned)a.M, (unsigned)((hidden + 2047) / 2048));
+    if (plan.few) hipLaunchKernelGGL((moe_combine_kernel<false>), combine, dim3(256), 0, stream, a, (const int*)place, (const float*)d.z, (const char*)d.z_exps);
+    else hipLaunchKernelGGL((moe_combine_kernel<true>), combine, dim3(256), 0, stream, a, (const int*)place, (const float*)d.z, (const char*)d.z_exps);
     return check_launch("w2_moe_experts");
 }
 
