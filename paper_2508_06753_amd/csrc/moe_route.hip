@@ -1,7 +1,8 @@
 // Which experts each row goes to: scores of the router's product, then the choice.
 //
 // The order of two scores decides which weights a row meets, so scores are computed in 64 bits: with sums in 32 bits about one row in
-// ten thousand would pick another expert than exact arithmetic does.
+// ten thousand would pick another expert than exact arithmetic does.  A product of two bf16 numbers has 16 bits, so sums of
+// 2^20 of them in 64 are as good as exact.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -12,34 +13,76 @@ namespace w2 {
 
 namespace {
 
-constexpr int ROWS = 8;
+typedef double v4d __attribute__((ext_vector_type(4)));
 
-// One wave: one expert, ROWS rows.
-__global__ void __launch_bounds__(256) route_logits_kernel(RouteArgs a, double* logits)
+constexpr int WAVES = 8;
+
+// A workgroup: 16 T rows by 16 T experts, one of the parts of K, eight waves that share it out.  The matrix instruction is the one for
+// 64-bit numbers (16 x 16 x 4); a lane asks for 8 numbers of a row in a row of memory, and step i multiplies the i-th of
+// them: which of K's numbers those are is the same on both sides.  Sums of the waves meet in their order.
+template <int T>
+__global__ void __launch_bounds__(WAVES * 64) route_logits_kernel(RouteArgs a, double* part, int parts)
 {
-    const int lane = threadIdx.x & 63, e = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t m0 = (int64_t)blockIdx.y * ROWS;
-    if (e >= a.r.n_experts) return;
-    double acc[ROWS] = {};
-    for (int64_t k = lane * 8; k < a.K; k += 512) {
-        const uint4 w4 = *reinterpret_cast<const uint4*>(a.r.weight + e * a.r.ldw + k);
-        const uint32_t wd[4] = {w4.x, w4.y, w4.z, w4.w};
+    __shared__ double s_sum[WAVES][T * T][256];
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4, wave = tid >> 6;
+    const int E = a.r.n_experts;
+    const int64_t m0 = (int64_t)blockIdx.x * (16 * T);
+    const int e0 = blockIdx.y * (16 * T);
+    const int blocks = (int)((a.K + 31) / 32), ranges = parts * WAVES, range = blockIdx.z * WAVES + wave;
+    const int begin = (int)((int64_t)blocks * range / ranges), end = (int)((int64_t)blocks * (range + 1) / ranges);
+    const uint16_t *x[T], *w[T];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            if (m0 + r >= a.M) break;
-            const uint4 x4 = *reinterpret_cast<const uint4*>(a.x + (m0 + r) * a.ldx + k);
-            const uint32_t xd[4] = {x4.x, x4.y, x4.z, x4.w};
+    for (int t = 0; t < T; ++t) {       // (rows and experts that are not there: the last one again)
+        x[t] = a.x + min(m0 + t * 16 + col, a.M - 1) * a.ldx + q * 8;
+        w[t] = a.r.weight + (int64_t)min(e0 + t * 16 + col, E - 1) * a.r.ldw + q * 8;
+    }
+    v4d acc[T][T] = {};
+    uint4 xs[T], ws[T], xn[T], wn[T];
+    auto load = [&](int b, uint4 (&to_x)[T], uint4 (&to_w)[T]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                acc[r] = fma((double)__uint_as_float(xd[i] << 16), (double)__uint_as_float(wd[i] << 16), acc[r]);
-                acc[r] = fma((double)__uint_as_float(xd[i] & 0xffff0000u), (double)__uint_as_float(wd[i] & 0xffff0000u), acc[r]);
+        for (int t = 0; t < T; ++t) {
+            to_x[t] = to_w[t] = make_uint4(0, 0, 0, 0);
+            if (b * 32 + q * 8 < a.K) {                      // K % 8 == 0: eight numbers or none
+                to_x[t] = *reinterpret_cast<const uint4*>(x[t] + (int64_t)b * 32);
+                to_w[t] = *reinterpret_cast<const uint4*>(w[t] + (int64_t)b * 32);
             }
         }
-    }
+    };
+    auto at = [](const uint4& v, int i) -> double {
+        const uint32_t d = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
+        return (double)__uint_as_float(i & 1 ? d & 0xffff0000u : d << 16);
+    };
+    if (begin < end) load(begin, xn, wn);
+    for (int b = begin; b < end; ++b) {
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        for (int off = 32; off; off >>= 1) acc[r] += __shfl_xor(acc[r], off);
-        if (lane == 0 && m0 + r < a.M) logits[(m0 + r) * a.r.n_experts + e] = acc[r];
+        for (int t = 0; t < T; ++t) {
+            xs[t] = xn[t];
+            ws[t] = wn[t];
+        }
+        if (b + 1 < end) load(b + 1, xn, wn);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int r = 0; r < T; ++r)
+#pragma unroll
+                for (int c = 0; c < T; ++c) acc[r][c] = __builtin_amdgcn_mfma_f64_16x16x4f64(at(xs[r], i), at(ws[c], i), acc[r][c], 0, 0, 0);
+    }
+    // number i of a lane: row 4 i + q, column col
+#pragma unroll
+    for (int r = 0; r < T; ++r)
+#pragma unroll
+        for (int c = 0; c < T; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s_sum[wave][r * T + c][(4 * i + q) * 16 + col] = acc[r][c][i];
+    __syncthreads();
+    for (int o = tid; o < T * T * 256; o += WAVES * 64) {
+        const int t = o / 256, in = o % 256;
+        const int64_t m = m0 + t / T * 16 + in / 16;
+        const int e = e0 + t % T * 16 + in % 16;
+        double s = s_sum[0][t][in];
+#pragma unroll
+        for (int v = 1; v < WAVES; ++v) s += s_sum[v][t][in];
+        if (m < a.M && e < E) part[((int64_t)blockIdx.z * a.M + m) * E + e] = s;
     }
 }
 
@@ -52,125 +95,202 @@ __device__ __forceinline__ uint64_t sortable(double c)
     return (uint64_t)(b < 0 ? ~b : b | (int64_t)1 << 63);
 }
 
-// One wave: one row.  Expert e in lane e / PER.
-template <int PER>
-__global__ void __launch_bounds__(64) route_select_kernel(RouteArgs a, const double* logits)
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)           // the same in every lane
 {
-    __shared__ uint64_t s_key[1024];
-    __shared__ double s_val[1024];
-    const int lane = threadIdx.x, E = a.r.n_experts;
-    const int64_t m = blockIdx.x;
+    auto move = [](uint32_t x, auto ctrl) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xf, 0xf, true); };
+    v = max(v, move(v, std::integral_constant<int, 0xB1>{}));
+    v = max(v, move(v, std::integral_constant<int, 0x4E>{}));
+    v = max(v, move(v, std::integral_constant<int, 0x141>{}));
+    v = max(v, move(v, std::integral_constant<int, 0x140>{}));
+    const uint32_t r0 = __builtin_amdgcn_readlane(v, 0), r1 = __builtin_amdgcn_readlane(v, 16);
+    const uint32_t r2 = __builtin_amdgcn_readlane(v, 32), r3 = __builtin_amdgcn_readlane(v, 48);
+    return max(max(r0, r1), max(r2, r3));
+}
+
+__device__ __forceinline__ double wave_max(double v)
+{
+    for (int off = 32; off; off >>= 1) v = fmax(v, __shfl_xor(v, off));
+    return v;
+}
+
+__device__ __forceinline__ double wave_total(double v)
+{
+    for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off);
+    return v;
+}
+
+// One wave: one row, expert e in lane e / PER; four rows a workgroup.  The largest key of the wave is found by its upper
+// 32 bits, moves that ride on the comparison, and by the lower ones where two lanes share those: a round of the choice is 150 cycles.
+template <int PER, bool GROUPS>
+__global__ void __launch_bounds__(256) route_select_kernel(RouteArgs a, const double* part, int parts)
+{
+    extern __shared__ double s_all[];                        // GROUPS: [4][64 * PER]
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, E = a.r.n_experts;
+    const int64_t m = (int64_t)blockIdx.x * 4 + wave;
+    if (m >= a.M) return;
     double l[PER], p[PER];
     uint64_t key[PER];
     double top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const int e = lane * PER + j;
-        l[j] = e < E ? logits[m * E + e] : 0.0;
-        if (e < E) top = fmax(top, l[j]);
-        if (a.logits && e < E) a.logits[m * E + e] = (float)l[j];
-    }
-    for (int off = 32; off; off >>= 1) top = fmax(top, __shfl_xor(top, off));
-    double sum = 0.0;
+    for (int j = 0; j < PER; ++j) l[j] = 0.0;
+    constexpr int AT_ONCE = PER <= 4 ? 8 : 16 / PER;         // parts whose sums are under way together
+    for (int s0 = 0; s0 < parts; s0 += AT_ONCE) {
+        double v[AT_ONCE][PER];
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const bool is = lane * PER + j < E;
-        p[j] = a.r.score == W2_SCORE_SOFTMAX ? exp(l[j] - top) : 1.0 / (1.0 + exp(-l[j]));
-        if (is) sum += p[j];
+        for (int s = 0; s < AT_ONCE; ++s)
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                v[s][j] = s0 + s < parts && lane * PER + j < E ? part[((int64_t)(s0 + s) * a.M + m) * E + lane * PER + j] : 0.0;
+#pragma unroll
+        for (int s = 0; s < AT_ONCE; ++s)
+#pragma unroll
+            for (int j = 0; j < PER; ++j) l[j] += v[s][j];
     }
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+        if (lane * PER + j < E) {
+            top = fmax(top, l[j]);
+            if (a.logits) a.logits[m * E + lane * PER + j] = (float)l[j];
+        }
     if (a.r.score == W2_SCORE_SOFTMAX) {
-        for (int off = 32; off; off >>= 1) sum += __shfl_xor(sum, off);
+        top = wave_max(top);
+        double sum = 0.0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            p[j] = lane * PER + j < E ? exp(l[j] - top) : 0.0;
+            sum += p[j];
+        }
+        sum = wave_total(sum);
 #pragma unroll
         for (int j = 0; j < PER; ++j) p[j] /= sum;
+    } else {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) p[j] = 1.0 / (1.0 + exp(-l[j]));
     }
     // without a bias and without sums over groups the scores' own order decides: it does not run out of digits
-    const bool by_logit = !a.r.choice_bias && (a.r.n_groups == 1 || a.r.group_top == 1);
+    const bool by_logit = !a.r.choice_bias && (!GROUPS || a.r.group_top == 1);
+    double* const s_val = s_all + wave * (64 * PER);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
         const int e = lane * PER + j;
-        const double c = by_logit ? l[j] : a.r.choice_bias && e < E ? p[j] + (double)a.r.choice_bias[e] : p[j];
+        double c = by_logit ? l[j] : p[j];
+        if (a.r.choice_bias && e < E) c += (double)a.r.choice_bias[e];
         key[j] = e < E ? sortable(c) : 0;
-        s_key[e] = key[j];
-        s_val[e] = c;
+        if constexpr (GROUPS) s_val[e] = c == c ? c : -INFINITY;
     }
-    if (a.r.n_groups > 1) {
-        __syncthreads();
+    if constexpr (GROUPS) {
+        // (a wave's own part of local memory, in order: no barrier)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const int size = E / a.r.n_groups;
-        // lane g: the score of group g
-        uint64_t score = 0;
-        if (lane < a.r.n_groups) {
-            double first = -INFINITY, second = -INFINITY;
-            for (int i = 0; i < size; ++i) {
-                const double c = s_val[lane * size + i];
-                if (c > first) { second = first; first = c; }
-                else if (c > second) second = c;
+        int lanes = 1;                                       // of a group, a power of two
+        while (2 * lanes * a.r.n_groups <= 64) lanes *= 2;
+        const int g = lane / lanes;
+        double first = -INFINITY, second = -INFINITY;
+        if (g < a.r.n_groups)
+            for (int i = lane % lanes; i < size; i += lanes) {
+                const double c = s_val[g * size + i];
+                second = fmax(second, fmin(first, c));
+                first = fmax(first, c);
             }
-            score = sortable(a.r.group_top == 2 && size > 1 ? first + second : first);
+        for (int off = 1; off < lanes; off <<= 1) {
+            const double f = __shfl_xor(first, off), s = __shfl_xor(second, off);
+            second = fmax(fmin(first, f), fmax(second, s));
+            first = fmax(first, f);
         }
+        const uint64_t score = sortable(a.r.group_top == 2 && size > 1 ? first + second : first);
         int better = 0;
-        for (int g = 0; g < a.r.n_groups; ++g) {
-            const uint64_t other = __shfl(score, g);
-            better += other > score || (other == score && g < lane);
+        for (int o = 0; o < a.r.n_groups; ++o) {
+            const uint64_t other = __shfl((unsigned long long)score, o * lanes);
+            better += other > score || (other == score && o < g);
         }
-        const uint64_t open = __ballot(lane < a.r.n_groups && better < a.r.top_groups);
+        const uint64_t open = __ballot(lane % lanes == 0 && g < a.r.n_groups && better < a.r.top_groups);
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int e = lane * PER + j;
-            if (e < E && !(open >> (e / size) & 1)) key[j] = 0;
+            if (e < E && !(open >> (e / size * lanes) & 1)) key[j] = 0;
         }
     }
     int my_id = 0;
     double my_p = 0.0;
     for (int i = 0; i < a.r.top_k; ++i) {
         uint64_t best = 0;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) best = max(best, key[j]);
-        uint64_t all = best;
-        for (int off = 32; off; off >>= 1) all = max(all, (uint64_t)__shfl_xor((unsigned long long)all, off));
-        const int winner = __ffsll(__ballot(best == all)) - 1;
         int id = 0;
         double pv = 0.0;
 #pragma unroll
-        for (int j = PER - 1; j >= 0; --j)
-            if (key[j] == all) { id = lane * PER + j; pv = p[j]; }
-        id = __shfl(id, winner);
-        pv = __shfl(pv, winner);
+        for (int j = 0; j < PER; ++j)
+            if (key[j] > best || j == 0) {
+                best = key[j];
+                id = lane * PER + j;
+                pv = p[j];
+            }
+        uint64_t winners = __ballot((uint32_t)(best >> 32) == wave_max_u32((uint32_t)(best >> 32)));
+        if (winners & (winners - 1)) {                       // (the lane's own upper half again where it lost: 0 below all keys)
+            const uint32_t low = winners >> lane & 1 ? (uint32_t)best : 0;
+            winners &= __ballot(low == wave_max_u32(low));
+        }
+        const int winner = __ffsll((unsigned long long)winners) - 1;
+        id = __builtin_amdgcn_readlane(id, winner);
+        const int64_t pb = __double_as_longlong(pv);
+        const uint32_t p0 = __builtin_amdgcn_readlane((int)pb, winner), p1 = __builtin_amdgcn_readlane((int)(pb >> 32), winner);
 #pragma unroll
         for (int j = 0; j < PER; ++j)
             if (lane * PER + j == id) key[j] = 0;
-        if (lane == i) { my_id = id; my_p = pv; }
+        if (lane == i) {
+            my_id = id;
+            my_p = __longlong_as_double((int64_t)((uint64_t)p1 << 32 | p0));
+        }
     }
-    double total = lane < a.r.top_k ? my_p : 0.0;
-    for (int off = 32; off; off >>= 1) total += __shfl_xor(total, off);
+    const double total = a.r.renormalise ? wave_total(lane < a.r.top_k ? my_p : 0.0) : 1.0;
     if (lane < a.r.top_k) {
         a.ids[m * a.r.top_k + lane] = my_id;
-        a.weights[m * a.r.top_k + lane] = (float)((a.r.renormalise ? my_p / total : my_p) * (double)a.r.scale);
+        a.weights[m * a.r.top_k + lane] = (float)(my_p / total * (double)a.r.scale);
     }
+}
+
+struct Shape {
+    int t, parts;
+};
+
+// Parts of K across workgroups until there are two to a CU
+Shape shape(int E, int64_t M, int64_t K)
+{
+    Shape s;
+    const int64_t wide = ((M + 31) / 32) * ((E + 31) / 32), narrow = ((M + 15) / 16) * ((E + 15) / 16);
+    s.t = wide >= 192 ? 2 : 1;
+    s.parts = s.t == 2 ? 1 : (int)std::min<int64_t>(std::min<int64_t>(8, std::max<int64_t>(1, 512 / narrow)), std::max<int64_t>(1, K / 256));
+    return s;
 }
 
 }  // namespace
 
+// (no less for more rows: parts * M * n_experts is at most 512 * 256 sums where there are parts)
 size_t route_workspace_bytes(int n_experts, int64_t M, int64_t)
 {
-    return (size_t)M * n_experts * sizeof(double);
+    return (size_t)std::min<int64_t>(8 * M, M + (512 * 256 + n_experts - 1) / n_experts) * n_experts * sizeof(double);
 }
 
 int launch_moe_route(const RouteArgs& a, hipStream_t stream)
 {
-    double* const logits = (double*)a.workspace;
+    double* const part = (double*)a.workspace;
     const int E = a.r.n_experts;
-    RouteArgs b = a;
-    for (int64_t m0 = 0; m0 < a.M; m0 += (int64_t)ROWS * 65535) {          // grid y is limited to 65535
-        b.M = std::min(a.M - m0, (int64_t)ROWS * 65535);
-        b.x = a.x + m0 * a.ldx;
-        hipLaunchKernelGGL(route_logits_kernel, dim3((E + 3) / 4, (unsigned)((b.M + ROWS - 1) / ROWS)), dim3(256), 0, stream, b, logits + m0 * E);
-    }
-    auto select = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)a.M), dim3(64), 0, stream, a, (const double*)logits); };
-    if (E <= 64) select(route_select_kernel<1>);
-    else if (E <= 128) select(route_select_kernel<2>);
-    else if (E <= 256) select(route_select_kernel<4>);
-    else if (E <= 512) select(route_select_kernel<8>);
-    else select(route_select_kernel<16>);
+    const Shape s = shape(E, a.M, a.K);
+    auto logits = [&](auto kern, int t) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)((a.M + 16 * t - 1) / (16 * t)), (unsigned)((E + 16 * t - 1) / (16 * t)), (unsigned)s.parts), dim3(WAVES * 64), 0,
+                           stream, a, part, s.parts);
+    };
+    if (s.t == 2) logits(route_logits_kernel<2>, 2);
+    else logits(route_logits_kernel<1>, 1);
+    auto select = [&](auto per) {
+        constexpr int PER = decltype(per)::value;
+        const dim3 grid((unsigned)((a.M + 3) / 4));
+        if (a.r.n_groups > 1) hipLaunchKernelGGL((route_select_kernel<PER, true>), grid, dim3(256), 4 * 64 * PER * sizeof(double), stream, a, (const double*)part, s.parts);
+        else hipLaunchKernelGGL((route_select_kernel<PER, false>), grid, dim3(256), 0, stream, a, (const double*)part, s.parts);
+    };
+    if (E <= 64) select(std::integral_constant<int, 1>{});
+    else if (E <= 128) select(std::integral_constant<int, 2>{});
+    else if (E <= 256) select(std::integral_constant<int, 4>{});
+    else if (E <= 512) select(std::integral_constant<int, 8>{});
+    else select(std::integral_constant<int, 16>{});
     return check_launch("w2_moe_route");
 }
 
