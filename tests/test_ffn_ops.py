@@ -396,6 +396,92 @@ def test_norm_and_route_in_a_graph(w2):
             assert torch.equal(a, b)
 
 
+# ------------------------------------------------------------------ the operators together
+def layer_and_cache(w2, shared=True, seed=0):
+    from paper_2508_06753_amd import attention_block as ab, decoder_layer as dl, synth
+    hidden, n_q, n_kv, D, G = 512, 4, 2, 64, 64
+    width = (n_q + 2 * n_kv) * D
+
+    def packed(K, N, s):
+        codes, scales = synth.make_weights(K, N, G, 0, seed=s)
+        return codes, scales, w2.prepack(torch.from_numpy(codes).cuda(), torch.from_numpy(scales.view(np.int16)).cuda(), G)
+
+    bank = Bank(w2, hidden, 256, 12, G, seed=seed + 3)
+    one = [packed(hidden, 512, seed + 4), packed(256, hidden, seed + 5)] if shared else None
+    attention = ab.AttentionBlock(packed(hidden, width, seed + 1)[2], packed(n_q * D, hidden, seed + 2)[2], hidden, n_q, n_kv, D, G, w2.Rope(D))
+    router = w2.Router(normal(seed + 6, 12, hidden, std=0.1), 3, scale=1.5)
+    weight = lambda s: (1 + normal(s, hidden, dtype=torch.float32, std=0.2)).bfloat16()  # noqa: E731
+    norms = w2.Norm(weight(seed + 7)), w2.Norm(weight(seed + 8), post_weight=weight(seed + 9), block_scale=0.5)
+    layer = dl.DecoderLayer(attention, dl.MoeBlock(router, bank.experts, None if one is None else (one[0][2], one[1][2], 256)), *norms)
+    k = normal(seed + 10, 24, 16, n_kv, D)
+    return ab, layer, bank, one, w2.KVCache(k, torch.zeros_like(k))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shared", [False, True])
+def test_layer_runs_prompts_and_tokens(w2, shared):
+    """A step of a layer against the operators' definitions, around the attention that the library computes."""
+    ab, layer, bank, one, cache = layer_and_cache(w2, shared)
+    table = torch.arange(20, dtype=torch.int32).flip(0).view(2, 10).contiguous().cuda()
+    lens = [45, 70]
+    for batch in (ab.causal_batch([0, 0], lens, table, 16, "cuda"), ab.causal_batch(lens, [1, 1], table, 16, "cuda")):
+        M = batch.positions.shape[0]
+        r, y = normal(M, M, 512, dtype=torch.float32), normal(M + 1, M, 512)
+        keep = cache.k.clone(), cache.v.clone()
+        r2, y2 = layer.step(r.clone(), y, cache, batch)
+        cache.k.copy_(keep[0])
+        cache.v.copy_(keep[1])
+        n1, n2 = layer.attention_norm, layer.moe_norm
+        x64, r64, _, _ = want.residual_norm(f64(r), f64(y), f64(n1.weight))
+        x = torch.tensor(x64).bfloat16().cuda()
+        a = f64(layer.attention.step(x, cache, batch))
+        x64, r64, _, _ = want.residual_norm(r64, a, f64(n2.weight), f64(n2.post_weight), True, block_scale=0.5)
+        x = f64(torch.tensor(x64).bfloat16())
+        router = layer.moe.router
+        ids, weights, _, gaps = want.route(x, f64(router.weight), 3, scale=1.5)
+        base = None
+        if shared:
+            (c1, s1, _), (c2, s2, _) = one
+            from paper_2508_06753_amd.synth import bf16_bits_to_f32
+            w1 = want.dequantise(c1, bf16_bits_to_f32(s1).astype(np.float64), 64, 2)
+            wd = want.dequantise(c2, bf16_bits_to_f32(s2).astype(np.float64), 64, 2)
+            base, _, _ = want.experts(x, np.zeros((M, 1), int), np.ones((M, 1)), lambda e: w1, lambda e: wd)
+        ref, _, _ = want.experts(x, ids, weights, bank.weights(0), bank.weights(1), base)
+        assert np.abs(f64(r2) - r64).max() < 0.02 * np.abs(r64).max()
+        # a bf16 number rounded the other way somewhere moves what follows, now and then the choice: rows whose choice was clear
+        off = np.linalg.norm(f64(y2) - ref, axis=1) / np.linalg.norm(ref, axis=1)
+        assert (gaps > 0.01).sum() >= 1 and off[gaps > 0.01].max() < 0.03, off
+
+
+@pytest.mark.gpu
+def test_layer_in_a_graph_and_main(w2, capsys):
+    """A captured step of a layer gives the eager one's bits at every replay; the steps of the command are sound."""
+    ab, layer, _, _, cache = layer_and_cache(w2)
+    table = torch.arange(20, dtype=torch.int32).view(2, 10).contiguous().cuda()
+    layer.step(normal(1, 25, 512, dtype=torch.float32), None, cache, ab.causal_batch([0, 0], [20, 5], table, 16, "cuda"))
+    batch = ab.causal_batch([20, 5], [1, 3], table, 16, "cuda")
+    r, y = normal(2, 4, 512), normal(3, 4, 512)                # a residual of 16 bits
+    want_r, want_y = (t.clone() for t in layer.step(r, y, cache, batch))
+    space = torch.empty(layer.workspace_size(4, batch, cache), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got_r, got_y = layer.step(r, y, cache, batch, workspace=space)
+    for _ in range(3):
+        got_r.zero_()
+        got_y.zero_()
+        space.fill_(0xff)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got_r, want_r) and torch.equal(got_y, want_y)
+        (y.float() @ y.float().t()).sum().item()
+    with pytest.raises(ValueError):
+        layer.moe.step(y, workspace=space[:64])
+    from paper_2508_06753_amd import decoder_layer
+    assert decoder_layer.main()
+    assert capsys.readouterr().out.count("finite True") == 2
+
+
 # ------------------------------------------------------------------ refusals
 def test_c_entries_refuse_bad_arguments_before_any_launch():
     from paper_2508_06753_amd import binding as w2
