@@ -535,10 +535,13 @@ W2_API int w2_moe_experts_workspace_size(const w2_experts_t* experts, int64_t M,
 
 /* Every row through its experts:
  *   h[m,j] = silu(g) * u,  (g, u) = x[m] W_gate_up[ids[m,j]]           Y[m] = base[m] + sum_j weights[m,j] h[m,j] W_down[ids[m,j]]
- * Sums in fp32, one rounding of Y; h is rounded to the bits of two eight-bit numbers (below).  The matrix instructions multiply
- * a weight's exact value with each number of x (or h) as the sum of two e4m3 numbers, scaled by a power of two for 128
- * numbers in a row: a bf16 number is exactly such a sum down to 2^-14 of the largest of its 128, and off by at most 2^-22 of
- * that below.
+ * Sums in fp32, one rounding of Y.  The matrix instructions multiply a weight's exact value with each number of x (or h) as the
+ * sum of two e4m3 numbers, scaled by a power of two that 32 numbers share (k = 16 g .. 16 g + 15 and 64 + 16 g .. of each 128): a
+ * bf16 number of x is exactly such a sum down to 2^-14 of the largest of its 32 and off by at most 2^-22 of that below, h is
+ * rounded to one, by at most 2^-9 of itself or 2^-22 of that.  Of 8 neighbouring products the bits 13 places below the largest are cut off.  Where experts have
+ * many rows each, the sums of a row's experts wait for each other rounded to 11 bits (2^-11 of
+ * each).
+ * What a row gives does not depend on which rows stand beside it, apart from their number.
  * x        dev, bf16 [M][hidden], row stride ldx;  a row with an infinity or NaN gives a row of NaN
  * ids      dev, int32 [M][top_k], any order, repetitions allowed; a number outside 0..n_experts-1 (-1): no expert, the slot adds
  *          nothing (its weight is not read)

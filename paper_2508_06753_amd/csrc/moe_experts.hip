@@ -647,7 +647,7 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
                         *reinterpret_cast<const uint4*>(s_out + m * 256 + tid % 16 * 16);
             }
         } else {
-            // 16 bits a number and a power of two for 32 columns: 2^-12 of the number, half the bytes of fp32 twice
+            // fp16 and a power of two for 32 columns: off by at most 2^-11 of the number, half the bytes that fp32 would have written and read
             uint16_t* const s_out = reinterpret_cast<uint16_t*>(s_mem);          // [rows][256 columns], then exponents [rows][8]
             char* const s_exp = s_mem + TILE_ROWS * 512;
 #pragma unroll
@@ -1018,7 +1018,7 @@ int launch_product(const ProductArgs& a, const moe::Plan& p, int64_t row_bytes_a
 
 size_t experts_workspace_bytes(const w2_experts_t& e, int64_t M, int top_k)
 {
-    return moe::workspace(e.hidden, e.inter, e.n_experts, M, top_k).total;
+    return moe::workspace(e.hidden, e.inter, e.n_experts, e.G, M, top_k).total;
 }
 
 namespace {
@@ -1056,11 +1056,11 @@ int launch_moe_experts(const ExpertsArgs& all, hipStream_t stream)
     }
     const ExpertsArgs& a = all;
     const int64_t A = a.M * a.top_k, hidden = a.e.hidden, inter = a.e.inter;
-    const moe::Workspace ws = moe::workspace(hidden, inter, a.e.n_experts, a.M, a.top_k);
+    const moe::Workspace ws = moe::workspace(hidden, inter, a.e.n_experts, a.e.G, a.M, a.top_k);
     char* const w = (char*)a.workspace;
-    const moe::Tiny tiny = moe::tiny(hidden, inter, a.e.n_experts, A);
+    const moe::Tiny tiny = moe::tiny(hidden, inter, a.e.n_experts, a.e.G, A);
     if (tiny.fits) return a.e.G == 128 ? launch_tiny<2>(a, tiny, w + ws.hs, w + ws.he, stream) : launch_tiny<4>(a, tiny, w + ws.hs, w + ws.he, stream);
-    const moe::Plan plan = moe::plan(hidden, inter, a.e.n_experts, A);
+    const moe::Plan plan = moe::plan(hidden, inter, a.e.n_experts, a.e.G, A);
     int* const n_tiles = (int*)(w + ws.tiles);
     Tile* const tile = (Tile*)(w + ws.tiles + 256);
     int* const tile_rows = (int*)(w + ws.tile_rows);

@@ -26,11 +26,16 @@ struct Plan {
 // pairs: of column blocks; used: tiles that are likely there
 inline int ranges(int64_t used, int64_t pairs, int64_t n_kt) { return used * (pairs / 4) < 768 && n_kt >= 8 ? 2 : 1; }
 
-inline Plan plan(int64_t hidden, int64_t inter, int E, int64_t A)
+// Choices per expert up to which the kernel for few rows takes them.  It reads an expert's weights once for every eight rows,
+// the other one once for 32 and is bound by issue.  us a call at 6, 8 choices an expert (128 of 4096 x 1024, groups of 128): few 107, 122, many 112, 114; at 8, 16
+// with groups of 64, whose products the matrix pipe does in halves (32 of 5120 x 2048): 87, 131 and 102, 140.
+constexpr int few_per_expert(int G) { return G == 128 ? 6 : 16; }
+
+inline Plan plan(int64_t hidden, int64_t inter, int E, int G, int64_t A)
 {
     Plan p;
     const int64_t used = std::min<int64_t>(A, E);
-    p.few = A <= 4 * used;
+    p.few = A <= few_per_expert(G) * used;
     p.rows = p.few ? 8 : 32;
     p.tiles = most_tiles(A, E, p.rows);
     p.ks_up = ranges(used, inter / 16, hidden / 256);
@@ -38,7 +43,9 @@ inline Plan plan(int64_t hidden, int64_t inter, int E, int64_t A)
     return p;
 }
 
-// Up to 64 choices (a lane of a wave each): two launches that need nothing prepared.
+// Up to 64 choices (a lane of a wave each) and not too many weights: two launches that need nothing prepared, where the others are four.
+// Their workgroups bring in all of their rows before the first product, which long streams of weights do not make up for.  us a call, two launches and four:
+// 4096 x 1024, top 8, 1 to 4 tokens 15, 21, 31 and 22, 25, 34, 8 tokens 48 and 44; 5120 x 2048 with groups of 64, top 4, 1 and 2 tokens 23, 39 and 26, 31.
 struct Tiny {
     bool fits;
     int tiles, rows;                    // at most, and rows of a tile
@@ -46,13 +53,13 @@ struct Tiny {
     size_t lds;                         // rows and their exponents
 };
 
-inline Tiny tiny(int64_t hidden, int64_t inter, int E, int64_t A)
+inline Tiny tiny(int64_t hidden, int64_t inter, int E, int G, int64_t A)
 {
     Tiny t;
     t.tiles = (int)most_tiles(A, E, 8);
     t.rows = (int)std::min<int64_t>(A, 8);                    // (or of x, where two of those are all)
     t.lds = (size_t)t.rows * (row_bytes(hidden) + 16 + exp_bytes(hidden));
-    t.fits = A <= 64 && t.lds <= (size_t)128 << 10 && t.tiles * hidden * inter <= (int64_t)1 << 27;
+    t.fits = A <= 64 && t.lds <= (size_t)128 << 10 && t.tiles * hidden * inter <= (int64_t)1 << (G == 128 ? 27 : 26);
     const int64_t groups = inter / 32;
     t.units = 1;
     while (t.units < 8 && groups % (2 * t.units) == 0 && t.tiles * (groups / (2 * t.units)) >= 512) t.units *= 2;
@@ -71,7 +78,7 @@ inline int64_t most_rows(int64_t hidden, int64_t inter, int top_k)
     return std::max<int64_t>(rows, 1);
 }
 
-inline Workspace workspace(int64_t hidden, int64_t inter, int E, int64_t M, int top_k)
+inline Workspace workspace(int64_t hidden, int64_t inter, int E, int G, int64_t M, int top_k)
 {
     M = std::min(M, most_rows(hidden, inter, top_k));
     const int64_t A = M * top_k;
@@ -79,7 +86,7 @@ inline Workspace workspace(int64_t hidden, int64_t inter, int E, int64_t M, int 
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
     w.tiles = take(256 + (size_t)most_tiles(A, E, 8) * 16); // their number, and the tiles; the shortest ones are the most
-    const Plan p = plan(hidden, inter, E, A);
+    const Plan p = plan(hidden, inter, E, G, A);
     w.tile_rows = take((size_t)p.tiles * p.rows * 4);
     w.place = take((size_t)A * 4);
     w.xs = take((size_t)M * row_bytes(hidden));
@@ -87,7 +94,7 @@ inline Workspace workspace(int64_t hidden, int64_t inter, int E, int64_t M, int 
     w.hs = take((size_t)A * row_bytes(inter));
     w.he = take((size_t)A * exp_bytes(inter));
     // sums: fp32 of few rows, fp16 of many
-    w.z = take(std::max((size_t)std::min<int64_t>(A, 4 * (int64_t)E) * hidden * 4, (size_t)A * hidden * 2));
+    w.z = take(std::max((size_t)std::min<int64_t>(A, few_per_expert(G) * (int64_t)E) * hidden * 4, (size_t)A * hidden * 2));
     w.ze = take((size_t)A * hidden / 32);
     w.total = at;
     return w;

@@ -6,6 +6,7 @@
 // where it is quantised.  A sum is reduced by moves inside the waves and one trip through local memory.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "block_ops.h"
@@ -42,10 +43,10 @@ __device__ __forceinline__ uint32_t quant_bits(float x, float inv)
 }
 
 template <int NV, bool RBF>
-__global__ void __launch_bounds__(1024) residual_norm_kernel(NormArgs a, float inv_n)
+__global__ void __launch_bounds__(1024) residual_norm_kernel(NormArgs a, int64_t m0, float inv_n)
 {
     __shared__ float s_red[3][16];
-    const int64_t m = blockIdx.x;
+    const int64_t m = m0 + blockIdx.x;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n_waves = blockDim.x >> 6;
     const int step = blockDim.x * 8;
     const int N = (int)a.N;
@@ -156,6 +157,9 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(NormArgs a, float i
     if (tid == 0) a.sx[m] = amax > 0.0f ? __fdiv_rn(amax, 127.0f) : 0.0f;
 }
 
+// a launch has fewer than 2^32 threads
+constexpr int64_t ROWS_A_LAUNCH = (int64_t)1 << 20;
+
 }  // namespace
 
 int launch_residual_norm(const NormArgs& a, hipStream_t stream)
@@ -168,8 +172,11 @@ int launch_residual_norm(const NormArgs& a, hipStream_t stream)
     const float inv_n = (float)(1.0 / (double)a.N);
     auto go = [&](auto nv_c) {
         constexpr int NV = decltype(nv_c)::value;
-        if (a.r_bf16) hipLaunchKernelGGL((residual_norm_kernel<NV, true>), dim3((unsigned)a.M), dim3(threads), 0, stream, a, inv_n);
-        else hipLaunchKernelGGL((residual_norm_kernel<NV, false>), dim3((unsigned)a.M), dim3(threads), 0, stream, a, inv_n);
+        for (int64_t m0 = 0; m0 < a.M; m0 += ROWS_A_LAUNCH) {
+            const dim3 grid((unsigned)std::min(ROWS_A_LAUNCH, a.M - m0));
+            if (a.r_bf16) hipLaunchKernelGGL((residual_norm_kernel<NV, true>), grid, dim3(threads), 0, stream, a, m0, inv_n);
+            else hipLaunchKernelGGL((residual_norm_kernel<NV, false>), grid, dim3(threads), 0, stream, a, m0, inv_n);
+        }
         return check_launch("w2_residual_norm");
     };
     if (nv <= 1) return go(std::integral_constant<int, 1>{});

@@ -96,6 +96,11 @@ def test_norm_forms(w2, gate, post, rdt):
 
 
 @pytest.mark.gpu
+def test_norm_more_rows_than_a_launch_takes(w2):
+    norm_case(w2, 2 ** 20 + 5, 8, gate="rows", post=True, seed=5)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M,N", [(1, 256), (3, 4096), (90, 5120), (2, 65536), (2, 16)])
 def test_norm_quantised_rows_are_those_of_quantize_rows(w2, M, N):
     if N % 256 == 0:                                          # what quantize_rows takes
@@ -328,6 +333,21 @@ def test_experts_numbers_of_every_size(w2, M):
             w2.moe_experts(bank.experts, (x * f).bfloat16(), ids, w)
     y = w2.moe_experts(bank.experts, torch.zeros_like(x).bfloat16(), ids, w)
     assert not y.any()
+
+
+@pytest.mark.gpu
+def test_experts_more_rows_than_go_together(w2):
+    """Rows whose parts pass 2 GiB go in turns; offsets of x and Y pass 32 bits.  A row's bits are those of a small batch."""
+    M, most = 2 ** 22 + 90, 2 ** 22                          # 512 bytes of a row's two parts in 2 GiB
+    bank = Bank(w2, 256, 256, 5, 128, seed=8)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(M, 264, generator=g, device="cuda", dtype=torch.bfloat16)[:, :256]
+    ids = torch.randint(-1, 5, (M, 1), generator=g, device="cuda", dtype=torch.int32)
+    w = torch.rand(M, 1, generator=g, device="cuda")
+    y = w2.moe_experts(bank.experts, x, ids, w)
+    for part in (slice(0, 400), slice(most - 400, most), slice(most, M)):
+        small = experts_check(w2, bank, x[part].contiguous(), ids[part].contiguous(), w[part].contiguous(), what=str(part))
+        assert torch.equal(y[part], small)
 
 
 @pytest.mark.gpu
