@@ -225,19 +225,46 @@ __device__ __forceinline__ int load_exponents(const char* p)
 
 __device__ __forceinline__ v8i join(v4i a, v4i b) { return (v8i){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
 
+// Up to 8 rows, each of them in the instruction twice, hi and lo.  Its row 4 q + i leaves in number i of lane group q, so with 2 L rows (L = 1, 2, 4)
+// row r's parts stand at 4 (r / L) + r % L and 8 further on: a lane then has L numbers to scale and add, not four.
+template <int L>
+__device__ __forceinline__ int row_of_lane(int col) { return (col >> 2 & 1) * L + (col & (L - 1)); }
+
 // Half j of a lane's 256 k of one column block, rows x in one part each, onto y
-template <int GPT, int J>
-__device__ __forceinline__ void multiply(v8i x, int e, v4i w, typename Scales<GPT>::type sc, v4f& y)
+template <int GPT, int J, int L>
+__device__ __forceinline__ void multiply(v8i x, int e, v4i w, typename Scales<GPT>::type sc, float (&y)[L])
 {
     int b[4];
     to_fp4((uint32_t)w[2 * J], b[0], b[1]);
     to_fp4((uint32_t)w[2 * J + 1], b[2], b[3]);
     const v4f zero = {0, 0, 0, 0};
-    if constexpr (GPT == 2) y += product<J>(x, b, zero, e) * scale_at(sc, J);
+    auto add = [&](v4f p, float scale) {
+#pragma unroll
+        for (int i = 0; i < L; ++i) y[i] = fmaf(p[i], scale, y[i]);
+    };
+    if constexpr (GPT == 2) add(product<J>(x, b, zero, e), scale_at(sc, J));
     else {
-        y += product<J>(x, {b[0], b[1], 0, 0}, zero, e) * scale_at(sc, 2 * J);
-        y += product<J>(x, {0, 0, b[2], b[3]}, zero, e) * scale_at(sc, 2 * J + 1);
+        add(product<J>(x, {b[0], b[1], 0, 0}, zero, e), scale_at(sc, 2 * J));
+        add(product<J>(x, {0, 0, b[2], b[3]}, zero, e), scale_at(sc, 2 * J + 1));
     }
+}
+
+template <int L>
+__device__ __forceinline__ void hold(float (&y)[2][L])       // the sums are here now, the products not carried on
+{
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < L; ++i) asm volatile("" : "+v"(y[n][i]));
+}
+
+// f with the L that up to 8 rows need
+template <typename F>
+__device__ __forceinline__ void with_rows(int rows, F f)
+{
+    if (rows <= 2) f(std::integral_constant<int, 1>{});
+    else if (rows <= 4) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 4>{});
 }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void* p, int64_t bytes)
@@ -274,41 +301,37 @@ __device__ __forceinline__ int half_exponent(int field) { return max(field - 14,
 __device__ __forceinline__ float half_scale(int ex) { return __int_as_float((254 - ex) << 23); }
 __device__ __forceinline__ uint16_t to_half(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 
-// What the wave of a pair of blocks leaves: h in two parts (UP; every wave of the workgroup calls it), or rows of z.  The
-// workgroup's P pairs are the units c0 .. c0 + P/2 - 1 and those four further on of the 128 numbers u of h.  s_mem: P * R * 36 bytes.
-template <int RT, int P, typename F>
-__device__ __forceinline__ void store_h(char* hs, char* he, int inter, int rows, F place, char* s_mem, v4f (&y)[RT][2], int p, bool mine, int u, int c0, int threads)
+// What the wave of a pair of blocks leaves of h, in two parts (every wave of the workgroup calls it).  The workgroup's P pairs are the
+// units c0 .. c0 + P/2 - 1 and those four further on of the 128 numbers u of h.  s_mem: P * 16 * 36 bytes.
+template <int P, int L, typename F>
+__device__ __forceinline__ void store_h(char* hs, char* he, int inter, int rows, F place, char* s_mem, float (&y)[2][L], int p, bool mine, int u, int c0, int threads)
 {
-    constexpr int R = 16 * RT;
+    constexpr int R = 4 * L;            // (half of them: hi's and lo's sums have met, lanes 32 apart hold the same)
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
     int* const s_top = reinterpret_cast<int*>(s_mem);        // [P][R]: exponent field of the largest |h| of a row's unit
     char* const s_out = s_mem + P * R * 4;                   // [R][2 parts][P units][16]
-    float h[RT][4];
+    float h[L];
     if (mine) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                h[r][i] = silu_mul(y[r][0][i], y[r][1][i]);
-                const int top = largest_field(finite_or_inf(h[r][i]));
-                if (col == 0) s_top[p * R + r * 16 + q * 4 + i] = top;
-            }
+        for (int i = 0; i < L; ++i) {
+            h[i] = silu_mul(y[0][i], y[1][i]);
+            const int top = largest_field(finite_or_inf(h[i]));
+            if (col == 0) s_top[p * R + q * L + i] = top;
+        }
     }
     __syncthreads();
     if (mine) {
         const int byte = 2 * (col & 7) + (col >> 3);
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int m = r * 16 + q * 4 + i;
-                const int ex = shared_exponent(max(s_top[p % (P / 2) * R + m], s_top[(p % (P / 2) + P / 2) * R + m]));
-                uint32_t hi, lo;
-                split2(h[r][i], 0.0f, scale_down(ex), hi, lo);
-                s_out[((m * 2 + 0) * P + p) * 16 + byte] = (char)hi;
-                s_out[((m * 2 + 1) * P + p) * 16 + byte] = (char)lo;
-                if (p < P / 2 && col == 0 && m < rows) he[(int64_t)place(m) * moe::exp_bytes(inter) + u / 2 * 8 + (c0 + p) * 2 + (u & 1)] = (char)ex;
-            }
+        for (int i = 0; i < L; ++i) {
+            const int m = q * L + i;
+            const int ex = shared_exponent(max(s_top[p % (P / 2) * R + m], s_top[(p % (P / 2) + P / 2) * R + m]));
+            uint32_t hi, lo;
+            split2(h[i], 0.0f, scale_down(ex), hi, lo);
+            s_out[((m * 2 + 0) * P + p) * 16 + byte] = (char)hi;
+            s_out[((m * 2 + 1) * P + p) * 16 + byte] = (char)lo;
+            if (p < P / 2 && col == 0 && m < rows) he[(int64_t)place(m) * moe::exp_bytes(inter) + u / 2 * 8 + (c0 + p) * 2 + (u & 1)] = (char)ex;
+        }
     }
     __syncthreads();
     for (int i = tid; i < rows * 2 * P; i += threads) {      // 16 bytes: a unit of a part of a row
@@ -316,6 +339,34 @@ __device__ __forceinline__ void store_h(char* hs, char* he, int inter, int rows,
         const int to_unit = c0 + pp % (P / 2) + pp / (P / 2) * 4;
         *reinterpret_cast<uint4*>(hs + (int64_t)place(m) * moe::row_bytes(inter) + u * 256 + part * 128 + to_unit * 16) =
             *reinterpret_cast<const uint4*>(s_out + i * 16);
+    }
+}
+
+// Sums of a pair of blocks: hi's and lo's, then the ranges of K, in their order, in local memory ([KS - 1][P][2 L][64])
+template <int KS, int P, int L>
+__device__ __forceinline__ void join_sums(float (&y)[2][L], float* part, int p, int kr, int lane)
+{
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < L; ++i) y[n][i] += __shfl_xor(y[n][i], 32);
+    if constexpr (KS > 1) {
+        if (kr > 0) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < L; ++i) part[(((kr - 1) * P + p) * 2 * L + n * L + i) * 64 + lane] = y[n][i];
+        }
+        __syncthreads();
+        if (kr == 0) {
+#pragma unroll
+            for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < L; ++i) y[n][i] += part[((k * P + p) * 2 * L + n * L + i) * 64 + lane];
+        }
+        __syncthreads();
     }
 }
 
@@ -352,75 +403,84 @@ __global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kern
     const bool has_e = tid < KS * CK * R;
     uint32_t row = UP ? tile_rows[r_in] : r_in, row_e = UP ? tile_rows[r_e] : r_e;
     if (tile.rows == 0) return;
-    const int p = wave % P, kr = wave / P;
-    const int steps = (a.n_kt + KS - 1) / KS, steps4 = (steps + FEW_W - 1) / FEW_W * FEW_W;
-    const int kt0 = kr * steps, my_steps = max(0, min(steps, a.n_kt - kt0));
-    const char* const blob = a.blob + tile.expert * a.blob_stride;
-    // pairs of a workgroup lie so that the units g and g + 4 of 128 numbers of h are both its own
-    constexpr int GROUPS = 8 / P;
-    const int group = blockIdx.x, pair = UP ? group / GROUPS * 8 + group % GROUPS * (P / 2) + p % (P / 2) + p / (P / 2) * 4 : group * P + p;
-    __amdgpu_buffer_rsrc_t wr[2], sr[2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const int64_t t = (int64_t)(2 * pair + c) * a.n_kt + kt0;
-        wr[c] = resource32(blob + t * 1024, my_steps * 1024);
-        sr[c] = resource32(blob + a.codes_bytes + t * 32 * GPT, my_steps * 32 * GPT);
-    }
-    v4i w[FEW_W][2];
-    typename Scales<GPT>::type sc[FEW_W][2];
-    auto load_weights = [&](int s, int slot) {
+    with_rows(tile.rows, [&](auto l_c) {
+        constexpr int L = decltype(l_c)::value;
+        const int p = wave % P, kr = wave / P;
+        const int steps = (a.n_kt + KS - 1) / KS;
+        const int kt0 = kr * steps, my_steps = max(0, min(steps, a.n_kt - kt0));
+        const char* const blob = a.blob + tile.expert * a.blob_stride;
+        // pairs of a workgroup lie so that the units g and g + 4 of 128 numbers of h are both its own
+        constexpr int GROUPS = 8 / P;
+        const int group = blockIdx.x, pair = UP ? group / GROUPS * 8 + group % GROUPS * (P / 2) + p % (P / 2) + p / (P / 2) * 4 : group * P + p;
+        __amdgpu_buffer_rsrc_t wr[2], sr[2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            w[slot][c] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(wr[c], s * 1024 + lane * 16, 0, NT));
-            if constexpr (GPT == 2) sc[slot][c] = __builtin_amdgcn_raw_buffer_load_b32(sr[c], s * 64 + col * 4, 0, 0);
-            else sc[slot][c] = __builtin_bit_cast(Scales<4>::type, __builtin_amdgcn_raw_buffer_load_b64(sr[c], s * 128 + col * 8, 0, 0));
+            const int64_t t = (int64_t)(2 * pair + c) * a.n_kt + kt0;
+            wr[c] = resource32(blob + t * 1024, my_steps * 1024);
+            sr[c] = resource32(blob + a.codes_bytes + t * 32 * GPT, my_steps * 32 * GPT);
         }
-    };
-
-    // a row that is not there is out of range
-    const __amdgpu_buffer_rsrc_t rr = resource(a.rows, row_bytes_all), er = resource(a.exps, row_bytes_all / 64);
-    const int n_in = r_in < tile.rows ? a.n_kt : 0, n_in_e = has_e && r_e < tile.rows ? a.n_kt : 0;     // tiles of K that the row has
-    if (!UP) {
-        row += tile.first;
-        row_e += tile.first;
-    }
-    const uint32_t src = row * (uint32_t)(a.n_kt * 512) + tid % 32 * 16, src_e = row_e * (uint32_t)(a.n_kt * 8);
-    char* const to = s_mem + r_in * STRIDE + tid % 32 * 16;
-    // (the other threads write beside them: without a branch, past which the compiler would carry the products and all their operands)
-    char* const to_e = s_mem + 2 * BUFFER + (has_e ? ((t_e / CK * R + r_e) * CK + t_e % CK) * 8 : 2 * EXPS + (tid & 63) * 8);
-    const int next_e = has_e ? EXPS : 0;
-    v4i staged[S::PIECES];
-    uint2 staged_e;
-    auto fetch = [&](int s) {           // s: first of the CK steps
+        v4i w[FEW_W][2];
+        typename Scales<GPT>::type sc[FEW_W][2];
+        auto load_weights = [&](int s, int slot) {
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i) {
-            const int kt = i / CK * steps + i % CK + s;
-            staged[i] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rr, kt < n_in ? src + kt * 512 : 0xffffffffu, 0, 0));
+            for (int c = 0; c < 2; ++c) {
+                w[slot][c] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(wr[c], s * 1024 + lane * 16, 0, NT));
+                if constexpr (GPT == 2) sc[slot][c] = __builtin_amdgcn_raw_buffer_load_b32(sr[c], s * 64 + col * 4, 0, 0);
+                else sc[slot][c] = __builtin_bit_cast(Scales<4>::type, __builtin_amdgcn_raw_buffer_load_b64(sr[c], s * 128 + col * 8, 0, 0));
+            }
+        };
+
+        // a row that is not there is out of range
+        const __amdgpu_buffer_rsrc_t rr = resource(a.rows, row_bytes_all), er = resource(a.exps, row_bytes_all / 64);
+        const int n_in = r_in < tile.rows ? a.n_kt : 0, n_in_e = has_e && r_e < tile.rows ? a.n_kt : 0;     // tiles of K that the row has
+        if (!UP) {
+            row += tile.first;
+            row_e += tile.first;
         }
-        const int kt = t_e / CK * steps + t_e % CK + s;
-        staged_e = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(er, kt < n_in_e ? src_e + kt * 8 : 0xffffffffu, 0, 0));
-    };
-    auto put = [&](int buffer) {
+        const uint32_t src = row * (uint32_t)(a.n_kt * 512) + tid % 32 * 16, src_e = row_e * (uint32_t)(a.n_kt * 8);
+        char* const to = s_mem + r_in * STRIDE + tid % 32 * 16;
+        // (the other threads write beside them: without a branch, past which the compiler would carry the products and all their operands)
+        char* const to_e = s_mem + 2 * BUFFER + (has_e ? ((t_e / CK * R + r_e) * CK + t_e % CK) * 8 : 2 * EXPS + (tid & 63) * 8);
+        const int next_e = has_e ? EXPS : 0;
+        v4i staged[S::PIECES];
+        uint2 staged_e;
+        auto fetch = [&](int s) {           // s: first of the CK steps
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i) *reinterpret_cast<v4i*>(to + buffer * BUFFER + i / CK * R * STRIDE + i % CK * 512) = staged[i];
-        *reinterpret_cast<uint2*>(to_e + buffer * next_e) = staged_e;
-    };
-    fetch(0);
+            for (int i = 0; i < S::PIECES; ++i) {
+                const int kt = i / CK * steps + i % CK + s;
+                staged[i] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rr, kt < n_in ? src + kt * 512 : 0xffffffffu, 0, 0));
+            }
+            const int kt = t_e / CK * steps + t_e % CK + s;
+            staged_e = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(er, kt < n_in_e ? src_e + kt * 8 : 0xffffffffu, 0, 0));
+        };
+        auto put = [&](int buffer) {
 #pragma unroll
-    for (int i = 0; i < FEW_W; ++i) load_weights(i, i);
-    put(0);
-    __syncthreads();
-
-    const int unit = 4 * (q & 1) + (q >> 1);
-    const char* const at = s_mem + (kr * R + (col & 7)) * STRIDE + unit * 16 + (col >> 3) * 128;
-    const char* const at_e = s_mem + 2 * BUFFER + (kr * R + (col & 7)) * CK * 8 + q * 2;
-    const int lo_exp = (col >> 3) * 0x0505;
-    int turn = 0;                       // the buffer that a chunk of four steps begins in
-    v4f y[1][2] = {};
-    for (int s = 0; s < steps4; s += FEW_W) {
+            for (int i = 0; i < S::PIECES; ++i) *reinterpret_cast<v4i*>(to + buffer * BUFFER + i / CK * R * STRIDE + i % CK * 512) = staged[i];
+            *reinterpret_cast<uint2*>(to_e + buffer * next_e) = staged_e;
+        };
+        // in the order of the loop, whose waits count what is under way from either side
+        fetch(0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < FEW_W; ++i) {
-            if (i % CK == 0) fetch(s + i + CK);
+            load_weights(i, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        put(0);
+        __syncthreads();
+
+        const int unit = 4 * (q & 1) + (q >> 1);
+        const int lo_exp = (col >> 3) * 0x0505;
+        const int row_in = kr * R + row_of_lane<L>(col);
+        const char* const at = s_mem + row_in * STRIDE + unit * 16 + (col >> 3) * 128;
+        const char* const at_e = s_mem + 2 * BUFFER + row_in * CK * 8 + q * 2;
+        int turn = 0;                   // the buffer that a chunk of four steps begins in
+        float y[2][L] = {};
+        // step s, with the weights in slot i, or what is left behind the last four
+        auto step = [&](int s, auto i_c, auto rest_c) {
+            constexpr int i = decltype(i_c)::value;
+            constexpr bool REST = decltype(rest_c)::value;
+            if (i % CK == 0 && !(REST && i + CK >= FEW_W)) fetch(s + CK);
             const int buffer = (i / CK + turn) & 1;
             // (up-converted only now: a turn early, as they come, the weights would take twice the registers)
             asm volatile("" : "+v"(w[i][0]), "+v"(w[i][1]), "+v"(sc[i][0]), "+v"(sc[i][1]));
@@ -430,55 +490,48 @@ __global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kern
                 constexpr int j = decltype(jc)::value;
                 const v8i x = join(*reinterpret_cast<const v4i*>(x0 + j * 256), *reinterpret_cast<const v4i*>(x0 + j * 256 + 32));
 #pragma unroll
-                for (int n = 0; n < 2; ++n) multiply<GPT, j>(x, e, w[i][n], sc[i][n], y[0][n]);
+                for (int n = 0; n < 2; ++n) multiply<GPT, j>(x, e, w[i][n], sc[i][n], y[n]);
             };
             half(std::integral_constant<int, 0>{});
             half(std::integral_constant<int, 1>{});
             // here, and not where they are read: carried on, the products' operands would take every register
-            asm volatile("" : "+v"(y[0][0]), "+v"(y[0][1]));
+            hold(y);
             __builtin_amdgcn_sched_barrier(0);
-            load_weights(s + i + FEW_W, i);
+            if (!REST) load_weights(s + FEW_W, i);
             if (i % CK == CK - 1) {
                 put((i / CK + 1 + turn) & 1);
                 __syncthreads();
             }
             __builtin_amdgcn_sched_barrier(0);
+        };
+        typedef std::integral_constant<bool, false> Loop;
+        typedef std::integral_constant<bool, true> Rest;
+        int s = 0;
+        for (; s + FEW_W <= steps; s += FEW_W) {
+            step(s, std::integral_constant<int, 0>{}, Loop{});
+            step(s + 1, std::integral_constant<int, 1>{}, Loop{});
+            step(s + 2, std::integral_constant<int, 2>{}, Loop{});
+            step(s + 3, std::integral_constant<int, 3>{}, Loop{});
+            if (CK == 4) turn ^= 1;
         }
-        if (CK == 4) turn ^= 1;
-    }
-    // hi's sums and lo's
+        if (s < steps) step(s, std::integral_constant<int, 0>{}, Rest{});
+        if (s + 1 < steps) step(s + 1, std::integral_constant<int, 1>{}, Rest{});
+        if (s + 2 < steps) step(s + 2, std::integral_constant<int, 2>{}, Rest{});
+        join_sums<KS, P>(y, reinterpret_cast<float*>(s_leave), p, kr, lane);
+        if constexpr (UP) {
+            store_h<P>(a.h, a.h_exps, a.n_out, tile.rows, [&](int m) { return tile.first + m; }, s_leave, y, p, kr == 0, group / GROUPS, group % GROUPS * (P / 2), THREADS);
+        } else if (kr == 0) {
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[0][n][i] += __shfl_xor(y[0][n][i], 32);
-    if constexpr (KS > 1) {                              // ranges of K meet in local memory, in their order
-        v4f* const part = reinterpret_cast<v4f*>(s_leave);         // [KS - 1][P][2][64]
-        if (kr > 0) {
-#pragma unroll
-            for (int n = 0; n < 2; ++n) part[(((kr - 1) * P + p) * 2 + n) * 64 + lane] = y[0][n];
-        }
-        __syncthreads();
-        if (kr == 0) {
-#pragma unroll
-            for (int k = 0; k < KS - 1; ++k)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) y[0][n] += part[((k * P + p) * 2 + n) * 64 + lane];
-        }
-        __syncthreads();
-    }
-    if constexpr (UP) {
-        store_h<1, P>(a.h, a.h_exps, a.n_out, tile.rows, [&](int m) { return tile.first + m; }, s_leave, y, p, kr == 0, group / GROUPS, group % GROUPS * (P / 2), THREADS);
-    } else if (kr == 0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int m = q * 4 + i;
-            if (m < tile.rows) {
-                float* const out = a.z + (int64_t)(tile.first + m) * a.n_out + pair * 32 + col;
-                out[0] = y[0][0][i];
-                out[16] = y[0][1][i];
+            for (int i = 0; i < L; ++i) {
+                const int m = q * L + i;
+                if (m < tile.rows) {
+                    float* const out = a.z + (int64_t)(tile.first + m) * a.n_out + pair * 32 + col;
+                    out[0] = y[0][i];
+                    out[16] = y[1][i];
+                }
             }
         }
-    }
+    });
 }
 
 // Many rows: bound by the matrix pipe.  A workgroup: four waves of 64 columns each (two pairs of blocks), up to 32 rows of
@@ -741,97 +794,87 @@ __global__ void __launch_bounds__(512, 2) moe_tiny_up_kernel(ExpertsArgs a, char
     if ((int)blockIdx.y >= c.tiles) return;
     const uint64_t mine = __ballot(c.tile == (int)blockIdx.y);
     const int rows = __popcll(mine), expert = __builtin_amdgcn_readlane(c.id, __ffsll((unsigned long long)mine) - 1);
-    const int p = wave % P, kr = wave / P;
-    const int steps = (n_kt + KS - 1) / KS, steps4 = (steps + TINY_W - 1) / TINY_W * TINY_W;
-    const int kt0 = kr * steps, my_steps = max(0, min(steps, n_kt - kt0));
-    const char* const blob = (const char*)a.e.gate_up + expert * a.e.gate_up_stride;
-    constexpr int GROUPS = 8 / P;       // pairs of a workgroup lie so that the units g and g + 4 of 128 numbers of h are both its own
-    struct Weights {                    // of the wave's first column block, its range of K; the second one follows
-        const char *codes, *scales;
-        int tiles;
-    };
-    auto weights_of = [&](int unit) {
-        const int group = blockIdx.x * units + unit;
-        const int pair = group / GROUPS * 8 + group % GROUPS * (P / 2) + p % (P / 2) + p / (P / 2) * 4;
-        const int64_t t = (int64_t)(2 * pair) * n_kt + kt0;
-        return Weights{blob + t * 1024, blob + a.up.codes_bytes + t * 32 * GPT, unit < units ? my_steps : 0};
-    };
-    v4i w[TINY_W][2];
-    typename Scales<GPT>::type sc[TINY_W][2];
-    auto load_weights = [&](const Weights& r, int s, int slot) {
+    with_rows(rows, [&](auto l_c) {
+        constexpr int L = decltype(l_c)::value;
+        const int p = wave % P, kr = wave / P;
+        const int steps = (n_kt + KS - 1) / KS, steps4 = (steps + TINY_W - 1) / TINY_W * TINY_W;
+        const int kt0 = kr * steps, my_steps = max(0, min(steps, n_kt - kt0));
+        const char* const blob = (const char*)a.e.gate_up + expert * a.e.gate_up_stride;
+        constexpr int GROUPS = 8 / P;       // pairs of a workgroup lie so that the units g and g + 4 of 128 numbers of h are both its own
+        struct Weights {                    // of the wave's first column block, its range of K; the second one follows
+            const char *codes, *scales;
+            int tiles;
+        };
+        auto weights_of = [&](int unit) {
+            const int group = blockIdx.x * units + unit;
+            const int pair = group / GROUPS * 8 + group % GROUPS * (P / 2) + p % (P / 2) + p / (P / 2) * 4;
+            const int64_t t = (int64_t)(2 * pair) * n_kt + kt0;
+            return Weights{blob + t * 1024, blob + a.up.codes_bytes + t * 32 * GPT, unit < units ? my_steps : 0};
+        };
+        v4i w[TINY_W][2];
+        typename Scales<GPT>::type sc[TINY_W][2];
+        auto load_weights = [&](const Weights& r, int s, int slot) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const __amdgpu_buffer_rsrc_t wr = resource32(r.codes + (int64_t)n * n_kt * 1024, r.tiles * 1024);
-            const __amdgpu_buffer_rsrc_t sr = resource32(r.scales + (int64_t)n * n_kt * 32 * GPT, r.tiles * 32 * GPT);
-            w[slot][n] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(wr, s * 1024 + lane * 16, 0, NT));
-            if constexpr (GPT == 2) sc[slot][n] = __builtin_amdgcn_raw_buffer_load_b32(sr, s * 64 + col * 4, 0, 0);
-            else sc[slot][n] = __builtin_bit_cast(Scales<4>::type, __builtin_amdgcn_raw_buffer_load_b64(sr, s * 128 + col * 8, 0, 0));
-        }
-    };
-    Weights now = weights_of(0);
-#pragma unroll
-    for (int i = 0; i < TINY_W; ++i) load_weights(now, i, i);
-
-    if (wave == 0 && c.tile == (int)blockIdx.y) s_row[c.row] = lane;
-    __syncthreads();
-    if (!early) {
-        bring(rows, [&](int r) { return (int64_t)(s_row[r] / a.top_k); });
-        __syncthreads();
-    }
-
-    const int nth = min(col & 7, rows - 1), row = early ? s_row[nth] / a.top_k : nth;         // (rows that are not there: the last one again)
-    const char* const at = s_mem + row * stride + (4 * (q & 1) + (q >> 1)) * 16 + (col >> 3) * 128;
-    const char* const at_e = s_exp + row * blocks + q * 2;
-    const int lo_exp = (col >> 3) * 0x0505;
-    for (int unit = 0; unit < units; ++unit) {
-        const Weights then = weights_of(unit + 1);
-        v4f y[1][2] = {};
-        for (int s = 0; s < steps4; s += TINY_W) {
-            const bool last = s + TINY_W >= steps4;
-            const Weights ahead = last ? then : now;
-            const int s_ahead = last ? 0 : s + TINY_W;
-#pragma unroll
-            for (int i = 0; i < TINY_W; ++i) {
-                asm volatile("" : "+v"(w[i][0]), "+v"(w[i][1]), "+v"(sc[i][0]), "+v"(sc[i][1]));
-                const int kt = min(kt0 + s + i, n_kt - 1);   // (past the range: weights of zero, and numbers that are there)
-                const char* const x0 = at + kt * 512;
-                const int e = *reinterpret_cast<const uint16_t*>(at_e + kt * 8) - lo_exp;
-                auto half = [&](auto jc) {
-                    constexpr int j = decltype(jc)::value;
-                    const v8i x = join(*reinterpret_cast<const v4i*>(x0 + j * 256), *reinterpret_cast<const v4i*>(x0 + j * 256 + 32));
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) multiply<GPT, j>(x, e, w[i][n], sc[i][n], y[0][n]);
-                };
-                half(std::integral_constant<int, 0>{});
-                half(std::integral_constant<int, 1>{});
-                asm volatile("" : "+v"(y[0][0]), "+v"(y[0][1]));
-                __builtin_amdgcn_sched_barrier(0);
-                load_weights(ahead, s_ahead + i, i);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int n = 0; n < 2; ++n) {
+                const __amdgpu_buffer_rsrc_t wr = resource32(r.codes + (int64_t)n * n_kt * 1024, r.tiles * 1024);
+                const __amdgpu_buffer_rsrc_t sr = resource32(r.scales + (int64_t)n * n_kt * 32 * GPT, r.tiles * 32 * GPT);
+                w[slot][n] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(wr, s * 1024 + lane * 16, 0, NT));
+                if constexpr (GPT == 2) sc[slot][n] = __builtin_amdgcn_raw_buffer_load_b32(sr, s * 64 + col * 4, 0, 0);
+                else sc[slot][n] = __builtin_bit_cast(Scales<4>::type, __builtin_amdgcn_raw_buffer_load_b64(sr, s * 128 + col * 8, 0, 0));
             }
+        };
+        Weights now = weights_of(0);
+#pragma unroll
+        for (int i = 0; i < TINY_W; ++i) {                       // in the order of the loop, whose waits count what is under way from either side
+            load_weights(now, i, i);
+            __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[0][n][i] += __shfl_xor(y[0][n][i], 32);
-        v4f* const part = reinterpret_cast<v4f*>(s_leave);   // [KS - 1][P][2][64]
-        if (kr > 0) {
-#pragma unroll
-            for (int n = 0; n < 2; ++n) part[(((kr - 1) * P + p) * 2 + n) * 64 + lane] = y[0][n];
+
+        if (wave == 0 && c.tile == (int)blockIdx.y) s_row[c.row] = lane;
+        __syncthreads();
+        if (!early) {
+            bring(rows, [&](int r) { return (int64_t)(s_row[r] / a.top_k); });
+            __syncthreads();
         }
-        __syncthreads();
-        if (kr == 0) {
+
+        const int lo_exp = (col >> 3) * 0x0505;
+        const int nth = min(row_of_lane<L>(col), rows - 1), row = early ? s_row[nth] / a.top_k : nth;         // (rows that are not there: the last one again)
+        const char* const at = s_mem + row * stride + (4 * (q & 1) + (q >> 1)) * 16 + (col >> 3) * 128;
+        const char* const at_e = s_exp + row * blocks + q * 2;
+        for (int unit = 0; unit < units; ++unit) {
+            const Weights then = weights_of(unit + 1);
+            float y[2][L] = {};
+            for (int s = 0; s < steps4; s += TINY_W) {
+                const bool last = s + TINY_W >= steps4;
+                const Weights ahead = last ? then : now;
+                const int s_ahead = last ? 0 : s + TINY_W;
 #pragma unroll
-            for (int k = 0; k < KS - 1; ++k)
+                for (int i = 0; i < TINY_W; ++i) {
+                    asm volatile("" : "+v"(w[i][0]), "+v"(w[i][1]), "+v"(sc[i][0]), "+v"(sc[i][1]));
+                    const int kt = min(kt0 + s + i, n_kt - 1);         // (past the range: weights of zero, and numbers that are there)
+                    const char* const x0 = at + kt * 512;
+                    const int e = *reinterpret_cast<const uint16_t*>(at_e + kt * 8) - lo_exp;
+                    auto half = [&](auto jc) {
+                        constexpr int j = decltype(jc)::value;
+                        const v8i x = join(*reinterpret_cast<const v4i*>(x0 + j * 256), *reinterpret_cast<const v4i*>(x0 + j * 256 + 32));
 #pragma unroll
-                for (int n = 0; n < 2; ++n) y[0][n] += part[((k * P + p) * 2 + n) * 64 + lane];
+                        for (int n = 0; n < 2; ++n) multiply<GPT, j>(x, e, w[i][n], sc[i][n], y[n]);
+                    };
+                    half(std::integral_constant<int, 0>{});
+                    half(std::integral_constant<int, 1>{});
+                    hold(y);
+                    __builtin_amdgcn_sched_barrier(0);
+                    load_weights(ahead, s_ahead + i, i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            join_sums<KS, P>(y, reinterpret_cast<float*>(s_leave), p, kr, lane);
+            const int group = blockIdx.x * units + unit;
+            store_h<P>(hs, he, (int)a.e.inter, rows, [&](int m) { return s_row[m]; }, s_leave, y, p, kr == 0, group / GROUPS, group % GROUPS * (P / 2), 512);
+            __syncthreads();
+            now = then;
         }
-        __syncthreads();
-        const int group = blockIdx.x * units + unit;
-        store_h<1, P>(hs, he, (int)a.e.inter, rows, [&](int m) { return s_row[m]; }, s_leave, y, p, kr == 0, group / GROUPS, group % GROUPS * (P / 2), 512);
-        __syncthreads();
-        now = then;
-    }
+    });
 }
 
 // A workgroup: one block of columns, eight waves.  All tiles one behind the other are a run of K that the waves share out; a wave adds
@@ -865,68 +908,77 @@ __global__ void __launch_bounds__(512, 2) moe_tiny_down_kernel(ExpertsArgs a, co
     const char* const scales = (const char*)a.e.down + a.down.codes_bytes + cb * n_kt * 32 * GPT + col * 2 * GPT;
     const int in_row = (4 * (q & 1) + (q >> 1)) * 16 + (col >> 3) * 128;
     const int lo_exp = (col >> 3) * 0x0505;
-    struct Slot {
-        v4i w, x[4];
-        typename Scales<GPT>::type sc;
-        int e;
-    } slot[TINY_W];
-    // the next step to load, its tile and what is its own
-    int next = begin, tile_l = begin / n_kt, kt_l = begin - tile_l * n_kt;
-    const char *codes_l = codes, *scales_l = scales, *x_l = hs, *e_l = he;
-    auto enter = [&]() {                // tile_l's weights and rows
-        const int expert = __builtin_amdgcn_readfirstlane(s_expert[tile_l]), row = s_row[tile_l][min(col & 7, s_rows[tile_l] - 1)];
-        codes_l = codes + expert * a.e.down_stride;
-        scales_l = scales + expert * a.e.down_stride;
-        x_l = hs + row * moe::row_bytes(a.e.inter) + in_row;
-        e_l = he + row * moe::exp_bytes(a.e.inter) + q * 2;
-    };
-    auto load = [&](Slot& t) {
-        if (next < end) {
-            t.w = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(codes_l + (int64_t)kt_l * 1024));
-            t.sc = *reinterpret_cast<const typename Scales<GPT>::type*>(scales_l + kt_l * 32 * GPT);
+    const int most = __ballot(c.id >= 0 && c.row >= 4) ? 8 : __ballot(c.id >= 0 && c.row >= 2) ? 4 : 2;      // rows of a tile
+    with_rows(most, [&](auto l_c) {
+        constexpr int L = decltype(l_c)::value;
+        const int nth = row_of_lane<L>(col);
+        struct Slot {
+            v4i w, x[4];
+            typename Scales<GPT>::type sc;
+            int e;
+        } slot[TINY_W];
+        // the next step to load, its tile and what is its own
+        int next = begin, tile_l = begin / n_kt, kt_l = begin - tile_l * n_kt;
+        const char *codes_l = codes, *scales_l = scales, *x_l = hs, *e_l = he;
+        auto enter = [&]() {                // tile_l's weights and rows
+            const int expert = __builtin_amdgcn_readfirstlane(s_expert[tile_l]), row = s_row[tile_l][min(nth, s_rows[tile_l] - 1)];
+            codes_l = codes + expert * a.e.down_stride;
+            scales_l = scales + expert * a.e.down_stride;
+            x_l = hs + row * moe::row_bytes(a.e.inter) + in_row;
+            e_l = he + row * moe::exp_bytes(a.e.inter) + q * 2;
+        };
+        auto load = [&](Slot& t) {
+            if (next < end) {
+                t.w = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(codes_l + (int64_t)kt_l * 1024));
+                t.sc = *reinterpret_cast<const typename Scales<GPT>::type*>(scales_l + kt_l * 32 * GPT);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) t.x[j] = *reinterpret_cast<const v4i*>(x_l + kt_l * 512 + j / 2 * 256 + j % 2 * 32);
-            t.e = load_exponents(e_l + kt_l * 8);
-            if (++next < end && ++kt_l == n_kt) {
-                kt_l = 0;
-                ++tile_l;
-                enter();
+                for (int j = 0; j < 4; ++j) t.x[j] = *reinterpret_cast<const v4i*>(x_l + kt_l * 512 + j / 2 * 256 + j % 2 * 32);
+                t.e = load_exponents(e_l + kt_l * 8);
+                if (++next < end && ++kt_l == n_kt) {
+                    kt_l = 0;
+                    ++tile_l;
+                    enter();
+                }
             }
-        }
-    };
-    if (begin < end) enter();
+        };
+        if (begin < end) enter();
 #pragma unroll
-    for (int i = 0; i < TINY_W; ++i) load(slot[i]);
-    v4f y = {};
-    int tile = begin / n_kt, left = n_kt - (begin - tile * n_kt);
-    for (int s = begin; s < end; s += TINY_W) {
+        for (int i = 0; i < TINY_W; ++i) load(slot[i]);
+        float y[L] = {};
+        int tile = begin / n_kt, left = n_kt - (begin - tile * n_kt);
+        for (int s = begin; s < end; s += TINY_W) {
 #pragma unroll
-        for (int i = 0; i < TINY_W; ++i) {
-            if (s + i < end) {
-                const int e = slot[i].e - lo_exp;
-                multiply<GPT, 0>(join(slot[i].x[0], slot[i].x[1]), e, slot[i].w, slot[i].sc, y);
-                multiply<GPT, 1>(join(slot[i].x[2], slot[i].x[3]), e, slot[i].w, slot[i].sc, y);
-                load(slot[i]);
-                if (--left == 0 || s + i + 1 == end) {       // the tile's rows, or the wave's share of them
+            for (int i = 0; i < TINY_W; ++i) {
+                if (s + i < end) {
+                    const int e = slot[i].e - lo_exp;
+                    multiply<GPT, 0>(join(slot[i].x[0], slot[i].x[1]), e, slot[i].w, slot[i].sc, y);
+                    multiply<GPT, 1>(join(slot[i].x[2], slot[i].x[3]), e, slot[i].w, slot[i].sc, y);
+                    load(slot[i]);
+                    if (--left == 0 || s + i + 1 == end) {   // the tile's rows, or the wave's share of them
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) y[r] += __shfl_xor(y[r], 32);
+                        for (int r = 0; r < L; ++r) y[r] += __shfl_xor(y[r], 32);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)              // four rows of the instruction and then the next: two may be one row of Y
-                        if (q == h) {
+                        for (int h = 0; h < 2; ++h) {        // the rows of a lane group and only then the next one's: two may be one row of Y
+                            if (q == h) {
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (4 * h + r < s_rows[tile]) {
-                                    const int at = s_row[tile][4 * h + r];
-                                    sums[at / a.top_k * 16 + col] += s_weight[at] * y[r];
-                                }
+                                for (int r = 0; r < L; ++r)
+                                    if (h * L + r < s_rows[tile]) {
+                                        const int at = s_row[tile][h * L + r];
+                                        sums[at / a.top_k * 16 + col] += s_weight[at] * y[r];
+                                    }
+                            }
+                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                            __builtin_amdgcn_wave_barrier();
                         }
-                    y = (v4f){0, 0, 0, 0};
-                    ++tile;
-                    left = n_kt;
+#pragma unroll
+                        for (int r = 0; r < L; ++r) y[r] = 0.0f;
+                        ++tile;
+                        left = n_kt;
+                    }
                 }
             }
         }
-    }
+    });
     __syncthreads();
     for (int i = tid; i < M * 16; i += 512) {
         const int64_t m = i / 16, n = cb * 16 + i % 16;
