@@ -608,35 +608,57 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
 #pragma unroll
         for (int i = 0; i < 4; ++i) at[i] = col * 256 + (((i >> 1) * 8 + unit + (i & 1) * 2) ^ col) * 16;
         v4f y[RT][4] = {};
-        auto stage = [&](int s, auto jc, Weights& wt) {
+        // Under way: the next column block's weights in four bits, and the last products, to be scaled and added.  Vector instructions
+        // of the block before and the block behind stand between a block's products (sched_barrier), so that neither waits for the other.
+        int b[4];
+        v4f p[RT] = {};
+        float p_scale = 0.0f;
+        auto add = [&](int r, int c) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[r][c][i] = fmaf(p[r][i], p_scale, y[r][c][i]);
+        };
+        auto stage = [&](int s, auto jc, const Weights& wt, const Weights& next) {       // next: the weights of the stage behind, half 1 - j
             constexpr int j = decltype(jc)::value;
             const char* const x = s_mem + (s & (RING - 1)) * BUFFER;
-            int b[4][4];
+            v8i hi[RT], lo[RT];
+            auto piece = [&](int r, int i) { return *reinterpret_cast<const v4i*>(x + r * 4096 + at[i]); };
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                to_fp4((uint32_t)wt.w[c][2 * j], b[c][0], b[c][1]);
-                to_fp4((uint32_t)wt.w[c][2 * j + 1], b[c][2], b[c][3]);
-            }
+            for (int r = 0; r < RT; ++r) lo[r] = join(piece(r, 2), piece(r, 3));
+#pragma unroll
+            for (int r = 0; r < RT; ++r) hi[r] = join(piece(r, 0), piece(r, 1));
+            __builtin_amdgcn_sched_barrier(0);
             const v4f zero = {0, 0, 0, 0};
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                auto piece = [&](int i) { return *reinterpret_cast<const v4i*>(x + r * 4096 + at[i]); };
-                const v8i hi = join(piece(0), piece(1)), lo = join(piece(2), piece(3));
-                const int eh = wt.e[r], el = wt.e[r] - 0x0505;
+            for (int c = 0; c < 4; ++c) {
+                const v4i& w = c < 3 ? wt.w[c + 1] : next.w[0];
+                const int half = c < 3 ? j : 1 - j;
+                int n[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    if constexpr (GPT == 2) y[r][c] += product<j>(hi, b[c], product<j>(lo, b[c], zero, el), eh) * scale_at(wt.sc[c], j);
-                    else {
-                        const int b0[4] = {b[c][0], b[c][1], 0, 0}, b1[4] = {0, 0, b[c][2], b[c][3]};
-                        y[r][c] += product<j>(hi, b0, product<j>(lo, b0, zero, el), eh) * scale_at(wt.sc[c], 2 * j);
-                        y[r][c] += product<j>(hi, b1, product<j>(lo, b1, zero, el), eh) * scale_at(wt.sc[c], 2 * j + 1);
+                for (int g = 0; g < GPT / 2; ++g) {
+                    const int bg[4] = {g == 0 ? b[0] : 0, g == 0 ? b[1] : 0, GPT == 2 || g ? b[2] : 0, GPT == 2 || g ? b[3] : 0};
+                    const int last = g ? c : (c + 3) % 4;
+                    v4f q[RT];
+                    q[0] = product<j>(lo[0], bg, zero, wt.e[0] - 0x0505);
+                    if (g == 0) to_fp4((uint32_t)w[2 * half], n[0], n[1]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (RT == 2) q[1] = product<j>(lo[1], bg, zero, wt.e[1] - 0x0505);
+                    if (g == GPT / 2 - 1) to_fp4((uint32_t)w[2 * half + 1], n[2], n[3]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    q[0] = product<j>(hi[0], bg, q[0], wt.e[0]);
+                    add(0, last);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (RT == 2) {
+                        q[1] = product<j>(hi[1], bg, q[1], wt.e[1]);
+                        add(1, last);
                     }
+                    p_scale = scale_at(wt.sc[c], GPT / 2 * j + g);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) p[r] = q[r];
                 }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[i] = n[i];
             }
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) asm volatile("" : "+v"(y[r][c]));          // here, not behind the barrier
             wait_loads<3 * RT + 8>();
             bare_barrier();
         };
@@ -647,25 +669,29 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
         for (int s = 0; s < RING - 1; ++s) load_rows(s);
         __builtin_amdgcn_sched_barrier(0);
         load_weights(1, wb);
+        to_fp4((uint32_t)wa.w[0][0], b[0], b[1]);
+        to_fp4((uint32_t)wa.w[0][1], b[2], b[3]);
         wait_loads<3 * RT + 8>();
         bare_barrier();
-        auto tile_of_k = [&](int kt, Weights& wt) {
+        auto tile_of_k = [&](int kt, Weights& wt, const Weights& next) {
             load_rows(2 * kt + 3);
             __builtin_amdgcn_sched_barrier(0);
-            stage(2 * kt, std::integral_constant<int, 0>{}, wt);
+            stage(2 * kt, std::integral_constant<int, 0>{}, wt, wt);
             load_rows(2 * kt + 4);
             __builtin_amdgcn_sched_barrier(0);
             // the second half of the tile needs its weights still: the next but one's follow it
-            stage(2 * kt + 1, std::integral_constant<int, 1>{}, wt);
+            stage(2 * kt + 1, std::integral_constant<int, 1>{}, wt, next);
             load_weights(kt + 2, wt);
             __builtin_amdgcn_sched_barrier(0);
         };
         int kt = 0;                     // (two at a time without a branch between them, past which the compiler would count fewer loads)
         for (; kt + 1 < a.n_kt; kt += 2) {
-            tile_of_k(kt, wa);
-            tile_of_k(kt + 1, wb);
+            tile_of_k(kt, wa, wb);
+            tile_of_k(kt + 1, wb, wa);
         }
-        if (kt < a.n_kt) tile_of_k(kt, wa);
+        if (kt < a.n_kt) tile_of_k(kt, wa, wb);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) add(r, 3);
         wait_loads<0>();                // what was asked for past the end has landed
         __syncthreads();
         if constexpr (UP) {
