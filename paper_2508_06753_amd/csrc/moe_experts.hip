@@ -6,8 +6,11 @@
 // significant bits and bf16 eight, so hi = round(x), lo = round(x - hi) is exact wherever lo's exponent reaches, which is down
 // to 2^-14 of the largest of the 32 numbers that share a power of two (off by 2^-22 of it below).  Against bf16 instructions
 // that is a third of the vector work per weight, and the products of hi and of lo together take no longer than one bf16
-// product (4300 TFLOP/s for both formats of eight and four bits, measured; half that for the pair).  What the instruction gives
-// away: of 8 neighbouring products, bits 13 places below the largest one's exponent are cut off.
+// product (4300 TFLOP/s for eight bits by four, measured; half that for the pair).  Its sums are not quite those of 32 bits: of 8
+// neighbouring products, bits 13 places below the largest one's exponent are cut off (measured), at most 7 * 2^-13 of the sum of magnitudes.
+//
+// Three ways through, by how many choices there are (moe_plan.h): up to 64 in two launches; few rows an expert, bound by the weights' way from
+// memory; many, bound by products.  The last two begin with a launch that sorts the choices and converts x, and end with one that sums.
 //
 // Rows in memory ("xs", "hs"): for every 256 k [2 halves of 128 k][hi, lo][8 units][16 bytes], a unit being 16 k in the order in which
 // the up-convert leaves the weights' nibbles, 0 8 1 9 2 10 3 11 4 12 5 13 6 14 7 15; exponents [4 g][2 halves] bytes beside
@@ -106,7 +109,8 @@ __device__ __forceinline__ uint64_t same_lanes(int id, bool live, int bits)
 // ---------------------------------------------------------------- before the products: who goes where, and x in two parts
 
 // Workgroup 0 sorts the choices by expert; the others convert x, a thread 32 numbers.  A choice's place among its expert's is
-// whichever it gets: what a row gives does not depend on the rows beside it, nor on where it stands.
+// whichever it gets from a counter in local memory: what a row gives does not depend on the rows beside it, nor on where it stands.
+// Bound by latency (384 choices: 4.6 us, two passes over ids that the L2 has), with many choices by the counters: 16384 take 16 us.
 __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* total_tiles, Tile* tiles, int64_t max_tiles, int rows_log2, Divider by_top_k,
                                                            int* tile_rows, int* place, char* xs, char* xe)
 {
@@ -370,7 +374,8 @@ __device__ __forceinline__ void join_sums(float (&y)[2][L], float* part, int p, 
     }
 }
 
-// Few rows: bound by the weights' way from memory.  A workgroup: four waves = 4 / KS pairs of column blocks times KS ranges of K, up to
+// Few rows: bound by the weights' way from memory (384 choices of 128 experts of 4096 x 1024, nearly all of which have some: 268 MB of gate and up in
+// 45 us, 6 TB/s, 134 MB of down in 27; the loads alone 42.6 and 22.8).  A workgroup: four waves = 4 / KS pairs of column blocks times KS ranges of K, up to
 // eight rows of one expert, hi in rows 0 to 7 of the instruction, lo in 8 to 15.  UP: a pair is a block of gate columns and one of up columns;
 // silu(gate) * up leaves in two parts.  Not UP: two blocks; sums leave in fp32.  The next four tiles of weights of each column block are
 // under way while one is multiplied; rows come through local memory, four tiles of K (over all ranges) at a time.  Every load
@@ -534,14 +539,22 @@ __global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kern
     });
 }
 
-// Many rows: bound by the matrix pipe.  A workgroup: four waves of 64 columns each (two pairs of blocks), up to 32 rows of
-// one expert.  As wide a wave as that because each wave reads every row's operands: with 32 columns a wave the local memory is
-// asked for as long as the matrix pipe is.  A stage is 128 of K: its rows go from global to local memory directly, three stages
-// ahead in a ring of four, a KiB (256 bytes of four rows) per instruction; the 16-byte piece p of row r stands at p ^ (r mod 16),
-// so that reads of 16 rows touch every bank once.  Weights and exponents of 256 of K are asked for two tiles ahead.
+// Many rows: bound by the matrix pipe and the vector instructions beside it.  A workgroup: four waves of 64 columns each (two pairs of
+// blocks), up to 32 rows of one expert (16, where there are no more: RT = 1).  As wide a wave as that because each wave reads every row's
+// operands: with 32 columns a wave 1806 choices of 64 experts of 2048 x 768 took 26.8 us for gate and up, not 24.3.  Tiles of 64 rows (two waves a
+// SIMD) took 175 and 108 us for the sizes below, those of 32 168 and 103 at that time.  A stage is 128 of K: its rows go from global to local memory directly, a KiB (256 bytes of four
+// rows) per instruction, in a ring of four; the 16-byte piece p of row r stands at p ^ (r mod 16), so that reads of 16 rows
+// touch every bank once.  Weights and exponents of 256 of K are asked for two tiles ahead.
 //
-// Waits (vector memory operations complete in order): behind stage s its successor's rows have landed, which were asked for in
-// stage s - 2.  Asked for since: rows of two more stages, and one tile's weights (4), scales (4) and exponents (RT).
+// Of a stage's column blocks the products of the last one begin behind the barrier at which the next stage's rows are there; those are read
+// into registers as the products let go of them.  Waits (vector memory operations complete in order): at the barrier of stage s the
+// rows of s + 1 have landed, which were asked for at that of s - 2.  Asked for since: rows of one more stage, and one tile's
+// weights (4), scales (4) and exponents (RT).  So no register may spill here: a load from scratch would be counted too.
+//
+// 16384 choices of 64 experts of 2048 x 1024: 142 to 161 us as the clock goes (1.6 to 2.1 GHz) for gate and up, 87 to 100 for down, of which the
+// products are 63 and 32 at 2.1 GHz (32 cycles each).  A workgroup takes 1.2 us to know its tile, 3.1 until rows are there, 15 for 2048 of K and 2.6 to leave;
+// a SIMD has two of its three waves in the loop at a time.  Neither the loads nor any one kind of vector instruction bounds the loop by itself
+// (left out one by one: 127 to 133 us for 132).
 constexpr int TILE_ROWS = 32, RING = 4;
 
 template <bool UP, int GPT>
@@ -575,12 +588,12 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
         constexpr int RT = decltype(rt_c)::value, BUFFER = RT * 16 * 256;
         const __amdgpu_buffer_rsrc_t rows = resource(a.rows, row_bytes_all);
         uint32_t src[RT];
-        const char* exps[RT];
+        uint32_t exps[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             const int row = (wave * RT + r) * 4 + q;         // of the KiB that this wave brings
             src[r] = (uint32_t)row_of(row) * (uint32_t)(a.n_kt * 512) + (col ^ (row & 15)) * 16;
-            exps[r] = a.exps + row_of(r * 16 + col) * (a.n_kt * 8) + q * 2;
+            exps[r] = (uint32_t)row_of(r * 16 + col) * (uint32_t)(a.n_kt * 8) + q * 2;
         }
         struct Weights {
             v4i w[4];
@@ -595,7 +608,7 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
                 r.sc[c] = *reinterpret_cast<const typename Scales<GPT>::type*>(scales[c] + (int64_t)kt * 32 * GPT + col * 2 * GPT);
             }
 #pragma unroll
-            for (int i = 0; i < RT; ++i) r.e[i] = load_exponents(exps[i] + (int64_t)kt * 8);
+            for (int i = 0; i < RT; ++i) r.e[i] = load_exponents(a.exps + (exps[i] + (uint32_t)kt * 8));
         };
         auto load_rows = [&](int stage) {
             char* const to = s_mem + (stage & (RING - 1)) * BUFFER + wave * RT * 1024;
@@ -617,19 +630,22 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[r][c][i] = fmaf(p[r][i], p_scale, y[r][c][i]);
         };
+        v8i hi[RT], lo[RT];
+        auto part = [&](int s, int r, int i) {
+            const char* const x = s_mem + (s & (RING - 1)) * BUFFER + r * 4096;
+            return join(*reinterpret_cast<const v4i*>(x + at[2 * i]), *reinterpret_cast<const v4i*>(x + at[2 * i + 1]));
+        };
         auto stage = [&](int s, auto jc, const Weights& wt, const Weights& next) {       // next: the weights of the stage behind, half 1 - j
             constexpr int j = decltype(jc)::value;
-            const char* const x = s_mem + (s & (RING - 1)) * BUFFER;
-            v8i hi[RT], lo[RT];
-            auto piece = [&](int r, int i) { return *reinterpret_cast<const v4i*>(x + r * 4096 + at[i]); };
-#pragma unroll
-            for (int r = 0; r < RT; ++r) lo[r] = join(piece(r, 2), piece(r, 3));
-#pragma unroll
-            for (int r = 0; r < RT; ++r) hi[r] = join(piece(r, 0), piece(r, 1));
-            __builtin_amdgcn_sched_barrier(0);
             const v4f zero = {0, 0, 0, 0};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
+                if (c == 3) {
+                    wait_loads<2 * RT + 8>();
+                    bare_barrier();
+                    load_rows(s + 3);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
                 const v4i& w = c < 3 ? wt.w[c + 1] : next.w[0];
                 const int half = c < 3 ? j : 1 - j;
                 int n[4];
@@ -644,6 +660,11 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
                     if constexpr (RT == 2) q[1] = product<j>(lo[1], bg, zero, wt.e[1] - 0x0505);
                     if (g == GPT / 2 - 1) to_fp4((uint32_t)w[2 * half + 1], n[2], n[3]);
                     __builtin_amdgcn_sched_barrier(0);
+                    if (c == 3 && g == GPT / 2 - 1) {
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) lo[r] = part(s + 1, r, 1);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                     q[0] = product<j>(hi[0], bg, q[0], wt.e[0]);
                     add(0, last);
                     __builtin_amdgcn_sched_barrier(0);
@@ -653,14 +674,17 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
                     }
                     p_scale = scale_at(wt.sc[c], GPT / 2 * j + g);
                     __builtin_amdgcn_sched_barrier(0);
+                    if (c == 3 && g == GPT / 2 - 1) {
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) hi[r] = part(s + 1, r, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
 #pragma unroll
                     for (int r = 0; r < RT; ++r) p[r] = q[r];
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) b[i] = n[i];
             }
-            wait_loads<3 * RT + 8>();
-            bare_barrier();
         };
         // in the order of the loop: stage 0's wait counts what the others do
         load_weights(0, wa);
@@ -673,12 +697,14 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
         to_fp4((uint32_t)wa.w[0][1], b[2], b[3]);
         wait_loads<3 * RT + 8>();
         bare_barrier();
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            lo[r] = part(0, r, 1);
+            hi[r] = part(0, r, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         auto tile_of_k = [&](int kt, Weights& wt, const Weights& next) {
-            load_rows(2 * kt + 3);
-            __builtin_amdgcn_sched_barrier(0);
             stage(2 * kt, std::integral_constant<int, 0>{}, wt, wt);
-            load_rows(2 * kt + 4);
-            __builtin_amdgcn_sched_barrier(0);
             // the second half of the tile needs its weights still: the next but one's follow it
             stage(2 * kt + 1, std::integral_constant<int, 1>{}, wt, next);
             load_weights(kt + 2, wt);
@@ -758,7 +784,8 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
 // ---------------------------------------------------------------- up to 64 choices in two launches
 
 // Every workgroup finds out for itself which rows share an expert: lane i of a wave holds choice i.  Tiles of up to eight
-// choices of one expert, in the order of their first ones.
+// choices of one expert, in the order of their first ones.  One row of 8 experts of 4096 x 1024 (25 MB, 3.8 us at the rate of a large read): 7.9 + 6.9 us,
+// launch and four trips to memory one behind the other (choices, rows or weights' addresses, weights, sums) each; four launches 21.5.
 struct Choice {
     int id, tile, row;                  // of lane i's choice: its expert (-1: none), its tile, its row there
     int tiles;                          // all of them
@@ -787,11 +814,11 @@ __device__ __forceinline__ Choice choose(const int32_t* ids, int A, int E)
     return c;
 }
 
-constexpr int TINY_EARLY = 2;
+constexpr int TINY_EARLY = 2;          // rows of x that are brought in before it is known whose they are
 constexpr int TINY_W = 4, TINY_KS = 4, TINY_P = 2;           // of the gate and up projection: 8 waves = 2 pairs of blocks times 4 ranges of K
 
 // A workgroup: a tile and `units` groups of two pairs of blocks.  It brings its rows into two parts in local memory itself, all of K,
-// and then streams weights past them; h leaves by the number of its choice.
+// and then streams weights past them, a group's end under the next one's loads; h leaves by the number of its choice.
 template <int GPT>
 __global__ void __launch_bounds__(512, 2) moe_tiny_up_kernel(ExpertsArgs a, char* hs, char* he, int units, int lds_rows)
 {
@@ -934,77 +961,74 @@ __global__ void __launch_bounds__(512, 2) moe_tiny_down_kernel(ExpertsArgs a, co
     const char* const scales = (const char*)a.e.down + a.down.codes_bytes + cb * n_kt * 32 * GPT + col * 2 * GPT;
     const int in_row = (4 * (q & 1) + (q >> 1)) * 16 + (col >> 3) * 128;
     const int lo_exp = (col >> 3) * 0x0505;
-    const int most = __ballot(c.id >= 0 && c.row >= 4) ? 8 : __ballot(c.id >= 0 && c.row >= 2) ? 4 : 2;      // rows of a tile
-    with_rows(most, [&](auto l_c) {
-        constexpr int L = decltype(l_c)::value;
-        const int nth = row_of_lane<L>(col);
-        struct Slot {
-            v4i w, x[4];
-            typename Scales<GPT>::type sc;
-            int e;
-        } slot[TINY_W];
-        // the next step to load, its tile and what is its own
-        int next = begin, tile_l = begin / n_kt, kt_l = begin - tile_l * n_kt;
-        const char *codes_l = codes, *scales_l = scales, *x_l = hs, *e_l = he;
-        auto enter = [&]() {                // tile_l's weights and rows
-            const int expert = __builtin_amdgcn_readfirstlane(s_expert[tile_l]), row = s_row[tile_l][min(nth, s_rows[tile_l] - 1)];
-            codes_l = codes + expert * a.e.down_stride;
-            scales_l = scales + expert * a.e.down_stride;
-            x_l = hs + row * moe::row_bytes(a.e.inter) + in_row;
-            e_l = he + row * moe::exp_bytes(a.e.inter) + q * 2;
-        };
-        auto load = [&](Slot& t) {
-            if (next < end) {
-                t.w = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(codes_l + (int64_t)kt_l * 1024));
-                t.sc = *reinterpret_cast<const typename Scales<GPT>::type*>(scales_l + kt_l * 32 * GPT);
+    constexpr int L = 4;                // (fewer for fewer rows: three times the code, and no faster)
+    const int nth = row_of_lane<L>(col);
+    struct Slot {
+        v4i w, x[4];
+        typename Scales<GPT>::type sc;
+        int e;
+    } slot[TINY_W];
+    // the next step to load, its tile and what is its own
+    int next = begin, tile_l = begin / n_kt, kt_l = begin - tile_l * n_kt;
+    const char *codes_l = codes, *scales_l = scales, *x_l = hs, *e_l = he;
+    auto enter = [&]() {                // tile_l's weights and rows
+        const int expert = __builtin_amdgcn_readfirstlane(s_expert[tile_l]), row = s_row[tile_l][min(nth, s_rows[tile_l] - 1)];
+        codes_l = codes + expert * a.e.down_stride;
+        scales_l = scales + expert * a.e.down_stride;
+        x_l = hs + row * moe::row_bytes(a.e.inter) + in_row;
+        e_l = he + row * moe::exp_bytes(a.e.inter) + q * 2;
+    };
+    auto load = [&](Slot& t) {
+        if (next < end) {
+            t.w = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(codes_l + (int64_t)kt_l * 1024));
+            t.sc = *reinterpret_cast<const typename Scales<GPT>::type*>(scales_l + kt_l * 32 * GPT);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) t.x[j] = *reinterpret_cast<const v4i*>(x_l + kt_l * 512 + j / 2 * 256 + j % 2 * 32);
-                t.e = load_exponents(e_l + kt_l * 8);
-                if (++next < end && ++kt_l == n_kt) {
-                    kt_l = 0;
-                    ++tile_l;
-                    enter();
-                }
+            for (int j = 0; j < 4; ++j) t.x[j] = *reinterpret_cast<const v4i*>(x_l + kt_l * 512 + j / 2 * 256 + j % 2 * 32);
+            t.e = load_exponents(e_l + kt_l * 8);
+            if (++next < end && ++kt_l == n_kt) {
+                kt_l = 0;
+                ++tile_l;
+                enter();
             }
-        };
-        if (begin < end) enter();
+        }
+    };
+    if (begin < end) enter();
 #pragma unroll
-        for (int i = 0; i < TINY_W; ++i) load(slot[i]);
-        float y[L] = {};
-        int tile = begin / n_kt, left = n_kt - (begin - tile * n_kt);
-        for (int s = begin; s < end; s += TINY_W) {
+    for (int i = 0; i < TINY_W; ++i) load(slot[i]);
+    float y[L] = {};
+    int tile = begin / n_kt, left = n_kt - (begin - tile * n_kt);
+    for (int s = begin; s < end; s += TINY_W) {
 #pragma unroll
-            for (int i = 0; i < TINY_W; ++i) {
-                if (s + i < end) {
-                    const int e = slot[i].e - lo_exp;
-                    multiply<GPT, 0>(join(slot[i].x[0], slot[i].x[1]), e, slot[i].w, slot[i].sc, y);
-                    multiply<GPT, 1>(join(slot[i].x[2], slot[i].x[3]), e, slot[i].w, slot[i].sc, y);
-                    load(slot[i]);
-                    if (--left == 0 || s + i + 1 == end) {   // the tile's rows, or the wave's share of them
+        for (int i = 0; i < TINY_W; ++i) {
+            if (s + i < end) {
+                const int e = slot[i].e - lo_exp;
+                multiply<GPT, 0>(join(slot[i].x[0], slot[i].x[1]), e, slot[i].w, slot[i].sc, y);
+                multiply<GPT, 1>(join(slot[i].x[2], slot[i].x[3]), e, slot[i].w, slot[i].sc, y);
+                load(slot[i]);
+                if (--left == 0 || s + i + 1 == end) {   // the tile's rows, or the wave's share of them
 #pragma unroll
-                        for (int r = 0; r < L; ++r) y[r] += __shfl_xor(y[r], 32);
+                    for (int r = 0; r < L; ++r) y[r] += __shfl_xor(y[r], 32);
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {        // the rows of a lane group and only then the next one's: two may be one row of Y
-                            if (q == h) {
+                    for (int h = 0; h < 2; ++h) {        // the rows of a lane group and only then the next one's: two may be one row of Y
+                        if (q == h) {
 #pragma unroll
-                                for (int r = 0; r < L; ++r)
-                                    if (h * L + r < s_rows[tile]) {
-                                        const int at = s_row[tile][h * L + r];
-                                        sums[at / a.top_k * 16 + col] += s_weight[at] * y[r];
-                                    }
-                            }
-                            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                            __builtin_amdgcn_wave_barrier();
+                            for (int r = 0; r < L; ++r)
+                                if (h * L + r < s_rows[tile]) {
+                                    const int at = s_row[tile][h * L + r];
+                                    sums[at / a.top_k * 16 + col] += s_weight[at] * y[r];
+                                }
                         }
-#pragma unroll
-                        for (int r = 0; r < L; ++r) y[r] = 0.0f;
-                        ++tile;
-                        left = n_kt;
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        __builtin_amdgcn_wave_barrier();
                     }
+#pragma unroll
+                    for (int r = 0; r < L; ++r) y[r] = 0.0f;
+                    ++tile;
+                    left = n_kt;
                 }
             }
         }
-    });
+    }
     __syncthreads();
     for (int i = tid; i < M * 16; i += 512) {
         const int64_t m = i / 16, n = cb * 16 + i % 16;
@@ -1015,7 +1039,8 @@ __global__ void __launch_bounds__(512, 2) moe_tiny_down_kernel(ExpertsArgs a, co
     }
 }
 
-// Y = base + the weighted rows of z, in the order of the slots; four rows of z under way together
+// Y = base + the weighted rows of z, in the order of the slots; four rows of z under way together.  Memory: 16384 rows of 2048 in fp16 13.5 us, 5.6 TB/s;
+// few rows: latency, 4.6 us.
 template <bool HALF>
 __global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const int* place, const float* z, const char* z_exps)
 {

@@ -17,6 +17,10 @@ typedef double v4d __attribute__((ext_vector_type(4)));
 
 constexpr int WAVES = 8;
 
+// Bound: many rows by the products (4095 rows, 4096 x 64: 2.1 GFLOP, 31 us at the 64-bit rate of the card, 46 with the choice; with bf16 products and
+// sums in 32 bits it would be the 7 us that x takes from memory, but see above); few by latency (1 row, 128 experts of 4096: 8.9 us for both launches;
+// 11.3 with vector instructions).  T = 2 (each number read meets twice as many) from 192 workgroups on.
+//
 // A workgroup: 16 T rows by 16 T experts, one of the parts of K, eight waves that share it out.  The matrix instruction is the one for
 // 64-bit numbers (16 x 16 x 4); a lane asks for 8 numbers of a row in a row of memory, and step i multiplies the i-th of
 // them: which of K's numbers those are is the same on both sides.  Sums of the waves meet in their order.
@@ -120,7 +124,8 @@ __device__ __forceinline__ double wave_total(double v)
 }
 
 // One wave: one row, expert e in lane e / PER; four rows a workgroup.  The largest key of the wave is found by its upper
-// 32 bits, moves that ride on the comparison, and by the lower ones where two lanes share those: a round of the choice is 150 cycles.
+// 32 bits, moves that ride on the comparison, and by the lower ones where two lanes share those: a round of the choice is 150 cycles
+// (53 rows, 8 of 256 experts in groups: 7 us for the scores and 8 here; 29.9 together with vector sums and a butterfly of 64-bit shuffles).
 template <int PER, bool GROUPS>
 __global__ void __launch_bounds__(256) route_select_kernel(RouteArgs a, const double* part, int parts)
 {
