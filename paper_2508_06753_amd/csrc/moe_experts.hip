@@ -284,10 +284,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource32(const void* p, int 
 // (the reciprocal is good to one step of fp32; an infinite exponential gives 0)
 __device__ __forceinline__ float silu_mul(float g, float u) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u; }
 
-__device__ __forceinline__ float finite_or_inf(float h)      // |h|, a NaN as the largest
+// |h| where it counts for the power of two that numbers share: infinities and NaN stay what they are beside any
+__device__ __forceinline__ float finite_or_zero(float h)
 {
     h = fabsf(h);
-    return h < INFINITY ? h : INFINITY;
+    return h < INFINITY ? h : 0.0f;
 }
 
 // exponent field of the largest of 16 lanes' numbers
@@ -319,7 +320,7 @@ __device__ __forceinline__ void store_h(char* hs, char* he, int inter, int rows,
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             h[i] = silu_mul(y[0][i], y[1][i]);
-            const int top = largest_field(finite_or_inf(h[i]));
+            const int top = largest_field(finite_or_zero(h[i]));
             if (col == 0) s_top[p * R + q * L + i] = top;
         }
     }
@@ -731,7 +732,7 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
                 for (int i = 0; i < 4; ++i) {
                     const int m = r * 16 + q * 4 + i;
                     const float h0 = silu_mul(y[r][0][i], y[r][1][i]), h1 = silu_mul(y[r][2][i], y[r][3][i]);
-                    const int ex = shared_exponent(largest_field(fmaxf(finite_or_inf(h0), finite_or_inf(h1))));
+                    const int ex = shared_exponent(largest_field(fmaxf(finite_or_zero(h0), finite_or_zero(h1))));
                     uint32_t hi, lo;
                     split2(h0, h1, scale_down(ex), hi, lo);
                     char* const to16 = s_out + m * 256 + wave * 16 + byte;
@@ -763,7 +764,7 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
 #pragma unroll
                     for (int n = 0; n < 2; ++n) {
                         const float u = y[r][2 * n][i], v = y[r][2 * n + 1][i];
-                        const int ex = half_exponent(largest_field(fmaxf(finite_or_inf(u), finite_or_inf(v))));
+                        const int ex = half_exponent(largest_field(fmaxf(finite_or_zero(u), finite_or_zero(v))));
                         const float f = half_scale(ex);
                         s_out[m * 256 + wave * 64 + n * 32 + col] = to_half(u * f);
                         s_out[m * 256 + wave * 64 + n * 32 + 16 + col] = to_half(v * f);

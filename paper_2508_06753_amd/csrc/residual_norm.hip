@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(NormArgs a, int64_t
     };
 
     float post = 1.0f;
-    if (a.p.post_norm) {
+    if (a.p.post_norm && a.y) {         // (none: zero, with eps = 0 too)
         float s = 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; ++v)

@@ -115,6 +115,9 @@ def test_norm_of_the_last_block_and_of_none(w2):
     """Only the residual, only x, only int8 rows: through the C entry; a NaN stays in its row."""
     lib, M, N = w2.raw(), 3, 512
     r, y = normal(1, M, N, dtype=torch.float32), normal(2, M, N)
+    w = torch.ones(N, dtype=torch.bfloat16, device="cuda")
+    x, r2 = w2.residual_norm(w2.Norm(w, post_weight=w, eps=0.0), r, None)       # no block: zero, not 0 / 0
+    assert torch.equal(r2, r) and torch.isfinite(x).all()
     norm = w2.Norm(block_scale=0.5)
     x, r2, xq, sx = w2.residual_norm(norm, r, y, quantize=True)
     s = torch.cuda.current_stream().cuda_stream
@@ -316,6 +319,27 @@ def test_experts_rows_do_not_meet(w2, M):
     bad[M // 2, 100] = float("inf")
     y = w2.moe_experts(bank.experts, bad, ids, w)
     assert torch.equal(y[keep], first[keep]) and not torch.isfinite(y[M // 2]).any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 5, 40, 150])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_experts_scales_that_are_no_numbers_stay_in_their_columns(w2, M, bad):
+    bank = Bank(w2, 512, 256, 6, 128, seed=7)
+    x, w, ids = normal(1, M, 512), mixing(M, 2, 2), choices(M, 6, 2, 3)
+    good = w2.moe_experts(bank.experts, x, ids, w).clone()
+    codes, scales = bank.parts[1]
+    e = int(ids[0, 0])
+    s = torch.from_numpy(scales[e]).bfloat16()
+    s[:, 5] = bad
+    down = bank.experts.down.clone()
+    size = w2.packed_size(256, 512, 128)
+    down[e, :size] = w2.prepack(torch.from_numpy(codes[e]).cuda(), s.cuda(), 128, 0)
+    y = w2.moe_experts(w2.Experts(bank.experts.gate_up, down, hidden=512, inter=256, G=128), x, ids, w)
+    hit = (ids == e).any(1)
+    assert not torch.isfinite(y[hit, 5]).any()
+    y[:, 5] = good[:, 5]
+    assert torch.equal(y, good)
 
 
 @pytest.mark.gpu
