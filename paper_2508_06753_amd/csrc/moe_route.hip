@@ -111,16 +111,40 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)           // the sa
     return max(max(r0, r1), max(r2, r3));
 }
 
+template <int CTRL>
+__device__ __forceinline__ double move(double v)
+{
+    const int64_t b = __double_as_longlong(v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, CTRL, 0xf, 0xf, true), hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, 0xf, 0xf, true);
+    return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+
+__device__ __forceinline__ double lane_of(double v, int lane)          // (lane: the same in every lane)
+{
+    const int64_t b = __double_as_longlong(v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)b, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), lane);
+    return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+
+// op over the lanes of a wave, the same in every lane: moves inside rows of 16, then the four rows' in their order
+template <typename F>
+__device__ __forceinline__ double over_wave(double v, F op)
+{
+    v = op(v, move<0xB1>(v));
+    v = op(v, move<0x4E>(v));
+    v = op(v, move<0x141>(v));
+    v = op(v, move<0x140>(v));
+    return op(op(lane_of(v, 0), lane_of(v, 16)), op(lane_of(v, 32), lane_of(v, 48)));
+}
+
 __device__ __forceinline__ double wave_max(double v)
 {
-    for (int off = 32; off; off >>= 1) v = fmax(v, __shfl_xor(v, off));
-    return v;
+    return over_wave(v, [](double a, double b) { return fmax(a, b); });
 }
 
 __device__ __forceinline__ double wave_total(double v)
 {
-    for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off);
-    return v;
+    return over_wave(v, [](double a, double b) { return a + b; });
 }
 
 // One wave: one row, expert e in lane e / PER; four rows a workgroup.  The largest key of the wave is found by its upper
@@ -205,7 +229,7 @@ __global__ void __launch_bounds__(256) route_select_kernel(RouteArgs a, const do
         const uint64_t score = sortable(a.r.group_top == 2 && size > 1 ? first + second : first);
         int better = 0;
         for (int o = 0; o < a.r.n_groups; ++o) {
-            const uint64_t other = __shfl((unsigned long long)score, o * lanes);
+            const uint64_t other = (uint64_t)__double_as_longlong(lane_of(__longlong_as_double((int64_t)score), o * lanes));
             better += other > score || (other == score && o < g);
         }
         const uint64_t open = __ballot(lane % lanes == 0 && g < a.r.n_groups && better < a.r.top_groups);
