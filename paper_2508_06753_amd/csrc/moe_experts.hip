@@ -110,7 +110,8 @@ __device__ __forceinline__ uint64_t same_lanes(int id, bool live, int bits)
 
 // Workgroup 0 sorts the choices by expert; the others convert x, a thread 32 numbers.  A choice's place among its expert's is
 // whichever it gets from a counter in local memory: what a row gives does not depend on the rows beside it, nor on where it stands.
-// Bound by latency (384 choices: 4.6 us, two passes over ids that the L2 has), with many choices by the counters: 16384 take 16 us.
+// Bound by latency (384 choices: 4.6 us), with many choices by the counters: 16384 take 13.5 us with 16 loads a thread at a time, 15.5 with 4 (2 are enough
+// up to 2048 choices, and less code).
 __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* total_tiles, Tile* tiles, int64_t max_tiles, int rows_log2, Divider by_top_k,
                                                            int* tile_rows, int* place, char* xs, char* xe)
 {
@@ -124,58 +125,71 @@ __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* t
         split_block(a.x + m * a.ldx, (int)b, xs + m * moe::row_bytes(a.e.hidden), xe + m * moe::exp_bytes(a.e.hidden));
         return;
     }
-    constexpr int AT_ONCE = 4;          // loads of 1024 choices under way together
     const int A = (int)(a.M * a.top_k), rows = 1 << rows_log2;
     s_next[tid] = 0;
     __syncthreads();
-    for (int i0 = tid; i0 < A; i0 += 1024 * AT_ONCE) {
-        int id[AT_ONCE];
+    auto sort = [&](auto at_once_c) {
+        constexpr int AT_ONCE = decltype(at_once_c)::value;  // loads of 1024 choices under way together; the first ones stay in registers
+        int kept[AT_ONCE], id[AT_ONCE];
+        auto ask = [&](int i0, int (&to)[AT_ONCE]) {
 #pragma unroll
-        for (int b = 0; b < AT_ONCE; ++b) id[b] = i0 + b * 1024 < A ? a.ids[i0 + b * 1024] : -1;
+            for (int b = 0; b < AT_ONCE; ++b) to[b] = i0 + b * 1024 < A ? a.ids[i0 + b * 1024] : -1;
+        };
+        auto count_them = [&](const int (&of)[AT_ONCE]) {
 #pragma unroll
-        for (int b = 0; b < AT_ONCE; ++b)
-            if ((unsigned)id[b] < (unsigned)E) atomicAdd(&s_next[id[b]], 1);
-    }
-    __syncthreads();
-    // thread e: expert e's rows, and where they and its tiles begin
-    const int count = s_next[tid], n_tiles = (count + rows - 1) >> rows_log2;
-    int first = count, tile = n_tiles;                       // inclusive sums over the experts
-    for (int off = 1; off < 64; off <<= 1) {
-        const int p = __shfl_up(first, off), q = __shfl_up(tile, off);
-        if (lane >= off) { first += p; tile += q; }
-    }
-    if (lane == 63) { s_sum[0][wave] = first; s_sum[1][wave] = tile; }
-    __syncthreads();
-    int all_tiles = 0;
-    for (int w = 0; w < 16; ++w) {
-        if (w < wave) { first += s_sum[0][w]; tile += s_sum[1][w]; }
-        all_tiles += s_sum[1][w];
-    }
-    first -= count;
-    tile -= n_tiles;
-    if (tid == 0) *total_tiles = all_tiles;
-    for (int t = 0; t < n_tiles; ++t) tiles[tile + t] = Tile{tid, first + t * rows, min(rows, count - t * rows), 0};
-    for (int64_t t = all_tiles + tid; t < max_tiles; t += 1024) tiles[t] = Tile{0, 0, 0, 0};
-    s_first[tid] = first;
-    s_tile[tid] = tile;
-    s_next[tid] = 0;
-    __syncthreads();
-    for (int i0 = tid; i0 < A; i0 += 1024 * AT_ONCE) {
-        int id[AT_ONCE];
-#pragma unroll
-        for (int b = 0; b < AT_ONCE; ++b) id[b] = i0 + b * 1024 < A ? a.ids[i0 + b * 1024] : -1;
-#pragma unroll
-        for (int b = 0; b < AT_ONCE; ++b) {
-            const int i = i0 + b * 1024;
-            const bool live = (unsigned)id[b] < (unsigned)E;
-            int n = 0;
-            if (live) {
-                n = atomicAdd(&s_next[id[b]], 1);
-                tile_rows[(s_tile[id[b]] << rows_log2) + n] = (int)divide((uint32_t)i, by_top_k);
-            }
-            if (i < A) place[i] = live ? s_first[id[b]] + n : -1;
+            for (int b = 0; b < AT_ONCE; ++b)
+                if ((unsigned)of[b] < (unsigned)E) atomicAdd(&s_next[of[b]], 1);
+        };
+        ask(tid, kept);
+        count_them(kept);
+        for (int i0 = tid + 1024 * AT_ONCE; i0 < A; i0 += 1024 * AT_ONCE) {
+            ask(i0, id);
+            count_them(id);
         }
-    }
+        __syncthreads();
+        // thread e: expert e's rows, and where they and its tiles begin
+        const int count = s_next[tid], n_tiles = (count + rows - 1) >> rows_log2;
+        int first = count, tile = n_tiles;                   // inclusive sums over the experts
+        for (int off = 1; off < 64; off <<= 1) {
+            const int p = __shfl_up(first, off), q = __shfl_up(tile, off);
+            if (lane >= off) { first += p; tile += q; }
+        }
+        if (lane == 63) { s_sum[0][wave] = first; s_sum[1][wave] = tile; }
+        __syncthreads();
+        int all_tiles = 0;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) { first += s_sum[0][w]; tile += s_sum[1][w]; }
+            all_tiles += s_sum[1][w];
+        }
+        first -= count;
+        tile -= n_tiles;
+        if (tid == 0) *total_tiles = all_tiles;
+        for (int t = 0; t < n_tiles; ++t) tiles[tile + t] = Tile{tid, first + t * rows, min(rows, count - t * rows), 0};
+        for (int64_t t = all_tiles + tid; t < max_tiles; t += 1024) tiles[t] = Tile{0, 0, 0, 0};
+        s_first[tid] = first;
+        s_tile[tid] = tile;
+        s_next[tid] = 0;
+        __syncthreads();
+        auto place_them = [&](int i0, const int (&of)[AT_ONCE]) {
+            int n[AT_ONCE];
+#pragma unroll
+            for (int b = 0; b < AT_ONCE; ++b) n[b] = (unsigned)of[b] < (unsigned)E ? atomicAdd(&s_next[of[b]], 1) : 0;
+#pragma unroll
+            for (int b = 0; b < AT_ONCE; ++b) {
+                const int i = i0 + b * 1024;
+                const bool live = (unsigned)of[b] < (unsigned)E;
+                if (live) tile_rows[(s_tile[of[b]] << rows_log2) + n[b]] = (int)divide((uint32_t)i, by_top_k);
+                if (i < A) place[i] = live ? s_first[of[b]] + n[b] : -1;
+            }
+        };
+        place_them(tid, kept);
+        for (int i0 = tid + 1024 * AT_ONCE; i0 < A; i0 += 1024 * AT_ONCE) {
+            ask(i0, id);
+            place_them(i0, id);
+        }
+    };
+    if (A <= 2048) sort(std::integral_constant<int, 2>{});
+    else sort(std::integral_constant<int, 16>{});
 }
 
 // ---------------------------------------------------------------- the products
