@@ -7,7 +7,8 @@ Bounds, with u = 2^-8 the relative error of one rounding to bf16 and e = 2^-24 t
 * moe_route: scores are sums in 64 bits: wherever two of them are further apart than 2^-40 the choice has to be exact; weights are
   rounded once to fp32 (2 e with the arithmetic before it);
 * moe_experts: a matrix instruction cuts each of 8 neighbouring products off 13 bits below the largest one's exponent: 7 * 2^-13 of the sum of
-  magnitudes at most, in either product; h is the sum of two numbers of four bits (u of it), Y is rounded once (u).  By norms: two
+  magnitudes at most, in either product; h is the sum of two numbers of four bits (2^-9 of it) and a row's sums may wait in fp16 (2^-11), together
+  less than u; Y is rounded once (u).  By norms: two
   independent roundings whose relative error is at most 2^-8 and, spread evenly over a step, 2^-8 / sqrt(3) in the mean square:
   0.0032 together, 0.0036 with what the products lose.
 """
