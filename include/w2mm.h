@@ -537,11 +537,11 @@ W2_API int w2_moe_experts_workspace_size(const w2_experts_t* experts, int64_t M,
  *   h[m,j] = silu(g) * u,  (g, u) = x[m] W_gate_up[ids[m,j]]           Y[m] = base[m] + sum_j weights[m,j] h[m,j] W_down[ids[m,j]]
  * Sums in fp32, one rounding of Y.  The matrix instructions multiply a weight's exact value with each number of x (or h) as the
  * sum of two e4m3 numbers, scaled by a power of two that 32 numbers share (k = 16 g .. 16 g + 15 and 64 + 16 g .. of each 128): a
- * bf16 number of x is exactly such a sum down to 2^-14 of the largest of its 32 and off by at most 2^-22 of that below, h is
- * rounded to one, by at most 2^-9 of itself or 2^-22 of that.  Of 8 neighbouring products the bits 13 places below the largest are cut off.  Where experts have
- * many rows each, the sums of a row's experts wait for each other rounded to 11 bits (2^-11 of
- * each).
- * What a row gives does not depend on which rows stand beside it, apart from their number.
+ * bf16 number of x is exactly such a sum down to 2^-14 of the largest of its 32 and off by at most 2^-22 of that below; h is
+ * rounded to one, by at most 2^-9 of itself or 2^-22 of that.  Of 8 neighbouring products the bits 13 places below the largest are
+ * cut off.  Where experts have many rows each, the sums of a row's experts wait for each other rounded by 2^-11 of each.
+ * The same call gives the same bits.  What other rows hold does not matter to a row; their number, and in calls of up to 64
+ * choices their ids, may change the order in which its sums are added.
  * x        dev, bf16 [M][hidden], row stride ldx;  a row with an infinity or NaN gives a row of NaN
  * ids      dev, int32 [M][top_k], any order, repetitions allowed; a number outside 0..n_experts-1 (-1): no expert, the slot adds
  *          nothing (its weight is not read)
