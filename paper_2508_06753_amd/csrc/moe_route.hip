@@ -17,7 +17,7 @@ typedef double v4d __attribute__((ext_vector_type(4)));
 
 constexpr int WAVES = 8;
 
-// Bound: many rows by the products (4095 rows, 4096 x 64: 2.1 GFLOP, 31 us at the 64-bit rate of the card, 46 with the choice; with bf16 products and
+// Bound: many rows by the products (4095 rows, 4096 x 64: 2.1 GFLOP, 31 us at the 64-bit rate of the card, 41 + 5 for the choice (43 with one block of K under way instead of four); with bf16 products and
 // sums in 32 bits it would be the 7 us that x takes from memory, but see above); few by latency (1 row, 128 experts of 4096: 8.9 us for both launches;
 // 11.3 with vector instructions).  T = 2 (each number read meets twice as many) from 192 workgroups on.
 //
@@ -41,35 +41,67 @@ __global__ void __launch_bounds__(WAVES * 64) route_logits_kernel(RouteArgs a, d
         w[t] = a.r.weight + (int64_t)min(e0 + t * 16 + col, E - 1) * a.r.ldw + q * 8;
     }
     v4d acc[T][T] = {};
-    uint4 xs[T], ws[T], xn[T], wn[T];
-    auto load = [&](int b, uint4 (&to_x)[T], uint4 (&to_w)[T]) {
-#pragma unroll
-        for (int t = 0; t < T; ++t) {
-            to_x[t] = to_w[t] = make_uint4(0, 0, 0, 0);
-            if (b * 32 + q * 8 < a.K) {                      // K % 8 == 0: eight numbers or none
-                to_x[t] = *reinterpret_cast<const uint4*>(x[t] + (int64_t)b * 32);
-                to_w[t] = *reinterpret_cast<const uint4*>(w[t] + (int64_t)b * 32);
-            }
-        }
-    };
     auto at = [](const uint4& v, int i) -> double {
         const uint32_t d = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
         return (double)__uint_as_float(i & 1 ? d & 0xffff0000u : d << 16);
     };
-    if (begin < end) load(begin, xn, wn);
-    for (int b = begin; b < end; ++b) {
-#pragma unroll
-        for (int t = 0; t < T; ++t) {
-            xs[t] = xn[t];
-            ws[t] = wn[t];
-        }
-        if (b + 1 < end) load(b + 1, xn, wn);
+    auto multiply = [&](const uint4 (&xs)[T], const uint4 (&ws)[T]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int r = 0; r < T; ++r)
 #pragma unroll
                 for (int c = 0; c < T; ++c) acc[r][c] = __builtin_amdgcn_mfma_f64_16x16x4f64(at(xs[r], i), at(ws[c], i), acc[r][c], 0, 0, 0);
+    };
+    auto load = [&](int b, uint4 (&to_x)[T], uint4 (&to_w)[T]) {
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            to_x[t] = *reinterpret_cast<const uint4*>(x[t] + (int64_t)b * 32);
+            to_w[t] = *reinterpret_cast<const uint4*>(w[t] + (int64_t)b * 32);
+        }
+    };
+    auto load_rest = [&](int b, uint4 (&to_x)[T], uint4 (&to_w)[T]) {            // K % 8 == 0: eight numbers or none
+#pragma unroll
+        for (int t = 0; t < T; ++t) to_x[t] = to_w[t] = make_uint4(0, 0, 0, 0);
+        if (b * 32 + q * 8 < a.K) load(b, to_x, to_w);
+    };
+    if constexpr (T == 1) {             // a few blocks a wave: one ahead, and little code to fetch
+        uint4 xs[T], ws[T], xn[T], wn[T];
+        if (begin < end) load_rest(begin, xn, wn);
+        for (int b = begin; b < end; ++b) {
+            xs[0] = xn[0];
+            ws[0] = wn[0];
+            if (b + 1 < end) load_rest(b + 1, xn, wn);
+            multiply(xs, ws);
+        }
+    } else {                            // all of K: whole blocks, four under way (past the last one that one again), then what is left
+        constexpr int AHEAD = 4;
+        const int whole = min(end, (int)(a.K / 32));
+        uint4 xs[AHEAD][T], ws[AHEAD][T];
+        if (begin < whole) {
+#pragma unroll
+            for (int d = 0; d < AHEAD; ++d) {
+                load(min(begin + d, whole - 1), xs[d], ws[d]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            int b = begin;
+            for (; b + AHEAD <= whole; b += AHEAD) {
+#pragma unroll
+                for (int d = 0; d < AHEAD; ++d) {
+                    multiply(xs[d], ws[d]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    load(min(b + d + AHEAD, whole - 1), xs[d], ws[d]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < AHEAD - 1; ++d)
+                if (b + d < whole) multiply(xs[d], ws[d]);
+        }
+        if (whole < end) {
+            load_rest(whole, xs[0], ws[0]);
+            multiply(xs[0], ws[0]);
+        }
     }
     // number i of a lane: row 4 i + q, column col
 #pragma unroll

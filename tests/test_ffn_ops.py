@@ -173,6 +173,13 @@ def test_route_row_counts(w2, M, K):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,E", [(2100, 72), (200, 1000)])   # enough tiles of 32 x 32 that K stays in one part
+@pytest.mark.parametrize("K", [8, 32, 72, 264, 1000, 4104])
+def test_route_many_rows(w2, M, E, K):
+    route_case(w2, M, K, E, 5, seed=M + K)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("group_top", [1, 2])
 @pytest.mark.parametrize("bias", [False, True])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
