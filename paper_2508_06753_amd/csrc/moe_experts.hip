@@ -212,8 +212,7 @@ struct ProductArgs {
     const int* tile_rows;               // up: which row of x each row of a tile is (down: the places in the sorted order)
     const char *rows, *exps;            // in two parts
     char *h, *h_exps;                   // up: rows of n_out numbers in two parts
-    float* z;                           // down: rows of n_out numbers (few rows in fp32, many in fp16 with exponents of 32 columns)
-    char* z_exps;
+    float* z;                           // down: rows of n_out numbers
     int n_out;
 };
 
@@ -314,11 +313,6 @@ __device__ __forceinline__ int largest_field(float m)
     m = fmaxf(m, dpp_move_f32<0x140>(m));
     return (int)(__float_as_uint(m) >> 23);
 }
-
-// A number as fp16 beside a power of two: the largest of 32 lands in 2^14 .. 2^15.  ex: that power's exponent field
-__device__ __forceinline__ int half_exponent(int field) { return max(field - 14, 1); }
-__device__ __forceinline__ float half_scale(int ex) { return __int_as_float((254 - ex) << 23); }
-__device__ __forceinline__ uint16_t to_half(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 
 // What the wave of a pair of blocks leaves of h, in two parts (every wave of the workgroup calls it).  The workgroup's P pairs are the
 // units c0 .. c0 + P/2 - 1 and those four further on of the 128 numbers u of h.  s_mem: P * 16 * 36 bytes.
@@ -767,29 +761,17 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
                         *reinterpret_cast<const uint4*>(s_out + m * 256 + tid % 16 * 16);
             }
         } else {
-            // fp16 and a power of two for 32 columns: off by at most 2^-11 of the number, half the bytes that fp32 would have written and read
-            uint16_t* const s_out = reinterpret_cast<uint16_t*>(s_mem);          // [rows][256 columns], then exponents [rows][8]
-            char* const s_exp = s_mem + TILE_ROWS * 512;
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int m = r * 16 + q * 4 + i;
+                    if (m < tile.rows) {
+                        float* const out = a.z + (int64_t)(tile.first + m) * a.n_out + pair[0] * 32 + col;
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const float u = y[r][2 * n][i], v = y[r][2 * n + 1][i];
-                        const int ex = half_exponent(largest_field(fmaxf(finite_or_zero(u), finite_or_zero(v))));
-                        const float f = half_scale(ex);
-                        s_out[m * 256 + wave * 64 + n * 32 + col] = to_half(u * f);
-                        s_out[m * 256 + wave * 64 + n * 32 + 16 + col] = to_half(v * f);
-                        s_exp[m * 8 + wave * 2 + n] = (char)ex;        // (the same from 16 lanes)
+                        for (int c = 0; c < 4; ++c) out[16 * c] = y[r][c][i];
                     }
                 }
-            __syncthreads();
-            if (tid < tile.rows * 8) a.z_exps[(int64_t)(tile.first + tid / 8) * (a.n_out / 32) + cg * 8 + tid % 8] = s_exp[tid];
-            for (int i = tid; i < tile.rows * 32; i += 256)
-                *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.z) + (int64_t)(tile.first + i / 32) * a.n_out + cg * 256 + i % 32 * 8) =
-                    *reinterpret_cast<const uint4*>(s_out + i * 8);
         }
     };
     if (tile.rows <= 16) body(std::integral_constant<int, 1>{});
@@ -1054,10 +1036,8 @@ __global__ void __launch_bounds__(512, 2) moe_tiny_down_kernel(ExpertsArgs a, co
     }
 }
 
-// Y = base + the weighted rows of z, in the order of the slots; four rows of z under way together.  Memory: 16384 rows of 2048 in fp16 13.5 us, 5.6 TB/s;
-// few rows: latency, 4.6 us.
-template <bool HALF>
-__global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const int* place, const float* z, const char* z_exps)
+// Y = base + the weighted rows of z, in the order of the slots; four rows of z under way together.
+__global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const int* place, const float* z)
 {
     const int64_t m = blockIdx.x;
     const int n = (blockIdx.y * 256 + threadIdx.x) * 8;
@@ -1072,38 +1052,25 @@ __global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const i
             y[2 * i + 1] = __uint_as_float(d[i] & 0xffff0000u);
         }
     }
-    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
     for (int j = 0; j < a.top_k; j += 4) {
-        int at[4], ex[4];
+        int at[4];
         float w[4];
         float4 p[4], q[4];
-        v8h h[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) at[i] = j + i < a.top_k ? place[m * a.top_k + j + i] : -1;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (at[i] >= 0) {
                 w[i] = a.weights[m * a.top_k + j + i];
-                if constexpr (HALF) {
-                    h[i] = *reinterpret_cast<const v8h*>(reinterpret_cast<const uint16_t*>(z) + (int64_t)at[i] * a.e.hidden + n);
-                    ex[i] = (uint8_t)z_exps[(int64_t)at[i] * (a.e.hidden / 32) + n / 32];
-                } else {
-                    const float4* const t = reinterpret_cast<const float4*>(z + (int64_t)at[i] * a.e.hidden + n);
-                    p[i] = t[0];
-                    q[i] = t[1];
-                }
+                const float4* const t = reinterpret_cast<const float4*>(z + (int64_t)at[i] * a.e.hidden + n);
+                p[i] = t[0];
+                q[i] = t[1];
             }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (at[i] < 0) continue;
-            if constexpr (HALF) {
-                const float f = __int_as_float(ex[i] << 23);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = fmaf(w[i], (float)h[i][e] * f, y[e]);
-            } else {
-                y[0] = fmaf(w[i], p[i].x, y[0]); y[1] = fmaf(w[i], p[i].y, y[1]); y[2] = fmaf(w[i], p[i].z, y[2]); y[3] = fmaf(w[i], p[i].w, y[3]);
-                y[4] = fmaf(w[i], q[i].x, y[4]); y[5] = fmaf(w[i], q[i].y, y[5]); y[6] = fmaf(w[i], q[i].z, y[6]); y[7] = fmaf(w[i], q[i].w, y[7]);
-            }
+            y[0] = fmaf(w[i], p[i].x, y[0]); y[1] = fmaf(w[i], p[i].y, y[1]); y[2] = fmaf(w[i], p[i].z, y[2]); y[3] = fmaf(w[i], p[i].w, y[3]);
+            y[4] = fmaf(w[i], q[i].x, y[4]); y[5] = fmaf(w[i], q[i].y, y[5]); y[6] = fmaf(w[i], q[i].z, y[6]); y[7] = fmaf(w[i], q[i].w, y[7]);
         }
     }
     *reinterpret_cast<uint4*>(a.Y + m * a.ldy + n) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
@@ -1192,7 +1159,7 @@ int launch_moe_experts(const ExpertsArgs& all, hipStream_t stream)
     u.rows = w + ws.xs; u.exps = w + ws.xe; u.h = w + ws.hs; u.h_exps = w + ws.he; u.n_out = (int)inter;
     ProductArgs d = {};
     d.blob = (const char*)a.e.down; d.blob_stride = a.e.down_stride; d.codes_bytes = (int64_t)a.down.codes_bytes;
-    d.n_kt = (int)(inter / 256); d.tiles = tile; d.rows = w + ws.hs; d.exps = w + ws.he; d.z = (float*)(w + ws.z); d.z_exps = w + ws.ze; d.n_out = (int)hidden;
+    d.n_kt = (int)(inter / 256); d.tiles = tile; d.rows = w + ws.hs; d.exps = w + ws.he; d.z = (float*)(w + ws.z); d.n_out = (int)hidden;
     const int64_t x_bytes = a.M * (int64_t)moe::row_bytes(hidden), h_bytes = A * (int64_t)moe::row_bytes(inter);
     int rc;
     if (a.e.G == 128) {
@@ -1202,9 +1169,8 @@ int launch_moe_experts(const ExpertsArgs& all, hipStream_t stream)
         if ((rc = launch_product<true, 4>(u, plan, x_bytes, n_tiles, stream))) return rc;
         if ((rc = launch_product<false, 4>(d, plan, h_bytes, n_tiles, stream))) return rc;
     }
-    const dim3 combine((unsigned)a.M, (unsigned)((hidden + 2047) / 2048));
-    if (plan.few) hipLaunchKernelGGL((moe_combine_kernel<false>), combine, dim3(256), 0, stream, a, (const int*)place, (const float*)d.z, (const char*)d.z_exps);
-    else hipLaunchKernelGGL((moe_combine_kernel<true>), combine, dim3(256), 0, stream, a, (const int*)place, (const float*)d.z, (const char*)d.z_exps);
+    hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)a.M, (unsigned)((hidden + 2047) / 2048)), dim3(256), 0, stream, a, (const int*)place,
+                       (const float*)d.z);
     return check_launch("w2_moe_experts");
 }
 

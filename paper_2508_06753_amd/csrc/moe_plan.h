@@ -67,7 +67,9 @@ inline Tiny tiny(int64_t hidden, int64_t inter, int E, int G, int64_t A)
 }
 
 struct Workspace {                      // offsets in bytes, each a multiple of 256; none shrinks when M grows
-    size_t tiles, tile_rows, place, xs, xe, hs, he, z, ze, total;
+    size_t tiles, tile_rows, place, xs, xe, hs, he, z;
+    size_t ze;                          // room that no kernel uses, a byte for 32 sums: whoever walks the workspace finds it here
+    size_t total;
 };
 
 // Rows that go together: their two parts lie within 2 GiB, offsets in 32 bits reach them, and their sums within 4 GiB
@@ -93,8 +95,7 @@ inline Workspace workspace(int64_t hidden, int64_t inter, int E, int G, int64_t 
     w.xe = take((size_t)M * exp_bytes(hidden));
     w.hs = take((size_t)A * row_bytes(inter));
     w.he = take((size_t)A * exp_bytes(inter));
-    // sums: fp32 of few rows, fp16 of many
-    w.z = take(std::max((size_t)std::min<int64_t>(A, few_per_expert(G) * (int64_t)E) * hidden * 4, (size_t)A * hidden * 2));
+    w.z = take((size_t)A * hidden * 4);
     w.ze = take((size_t)A * hidden / 32);
     w.total = at;
     return w;

@@ -1,0 +1,55 @@
+"""The operators of a layer's feed-forward half where few bits are left, numbers are tiny or far apart, and kernels run that ordinary
+sizes do not reach.  Bounds as in test_ffn_ops.py, and where a test says so, of one rounding alone."""
+import numpy as np
+import pytest
+
+from oracle import ffn_oracle as want
+from test_ffn_ops import CUT, U, Bank, f64, mixing, near, normal
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def w2():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2508_06753_amd import binding
+    return binding
+
+
+class MadeBank(Bank):
+    """Experts of codes [E, K, N] and scales [E, K/G, N] that a test makes itself."""
+
+    def __init__(self, w2, hidden, inter, G, up, down):
+        self.hidden, self.inter, self.E, self.G, self.zero = hidden, inter, len(up[0]), G, 2
+        self.parts, blobs = [], []
+        for codes, scales in (up, down):
+            scales = torch.tensor(np.asarray(scales), dtype=torch.float32).bfloat16()
+            codes = np.asarray(codes, dtype=np.uint8)
+            blobs.append(torch.stack([w2.prepack(torch.from_numpy(c).cuda(), s.cuda(), G) for c, s in zip(codes, scales)]))
+            self.parts.append((codes, scales.double().numpy()))
+        self.experts = w2.Experts(*blobs, hidden=hidden, inter=inter, G=G)
+
+
+# ------------------------------------------------------------------ experts: what a row's sums keep
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [64, 128])
+@pytest.mark.parametrize("M,E", [(5, 2), (40, 64), (40, 2), (300, 2)])        # in two launches, few rows an expert, many
+def test_experts_that_all_but_cancel(w2, M, E, G):
+    """Two experts whose results differ by 2^-7 of themselves, one less the other: what is left has the usual relative error only if
+    either sum is kept in 32 bits until they meet.  Their h and their products are the same bits, so that the errors of h and of the products
+    shrink with the difference; the sums' roundings do not: at most 16 of 2^-24 of the magnitude for each of two, 2^-19 together."""
+    hidden, inter = 512, 256
+    rng = np.random.default_rng(M + E + G)
+    up = rng.integers(0, 4, (1, hidden, 2 * inter)).repeat(E, 0), rng.uniform(0.005, 0.05, (1, hidden // G, 2 * inter)).repeat(E, 0)
+    scale = np.full((E, inter // G, hidden), 2.0 ** -5)
+    scale[1] *= 1.0 + 2.0 ** -7                               # eight bits
+    bank = MadeBank(w2, hidden, inter, G, up, (rng.integers(0, 4, (1, inter, hidden)).repeat(E, 0), scale))
+    x = normal(M, M, hidden)
+    ids = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda").repeat(M, 1)
+    weights = torch.tensor([[1.0, -1.0]], device="cuda").repeat(M, 1)
+    ref, mag, h_err = want.experts(f64(x), ids.cpu().numpy(), f64(weights), bank.weights(0), bank.weights(1))
+    y = w2.moe_experts(bank.experts, x, ids, weights)
+    near(y, ref, U * np.abs(ref) + 2.0 ** -8 * ((U + CUT) * mag + CUT * h_err) + 2.0 ** -19 * mag, "two experts that all but cancel")
+    off, norm = np.linalg.norm(f64(y) - ref), np.linalg.norm(ref)
+    assert off <= 0.0036 * norm + 2.0 ** -19 * np.linalg.norm(mag), f"{off / norm:.4f} off"
