@@ -812,17 +812,17 @@ __device__ __forceinline__ Choice choose(const int32_t* ids, int A, int E)
 }
 
 constexpr int TINY_EARLY = 2;          // rows of x that are brought in before it is known whose they are
-constexpr int TINY_W = 4, TINY_KS = 4, TINY_P = 2;           // of the gate and up projection: 8 waves = 2 pairs of blocks times 4 ranges of K
+constexpr int TINY_W = 4;              // tiles of weights under way
 
 // A workgroup: a tile and `units` groups of two pairs of blocks.  It brings its rows into two parts in local memory itself, all of K,
 // and then streams weights past them, a group's end under the next one's loads; h leaves by the number of its choice.
 template <int GPT>
 __global__ void __launch_bounds__(512, 2) moe_tiny_up_kernel(ExpertsArgs a, char* hs, char* he, int units, int lds_rows)
 {
-    constexpr int P = TINY_P, KS = TINY_KS;
-    extern __shared__ char s_mem[];                          // rows [lds_rows][2 K + 16], exponents [lds_rows][K / 32]
-    __shared__ __align__(16) char s_leave[(KS - 1) * P * 2048];
-    __shared__ int s_row[8];
+    constexpr int P = moe::TINY_P, KS = moe::TINY_KS;
+    extern __shared__ char s_all[];                          // what leaves, choices [8], rows [lds_rows][2 K + 16], exponents [lds_rows][K / 32]
+    char *const s_leave = s_all, *const s_mem = s_all + moe::TINY_LEAVE;
+    int* const s_row = reinterpret_cast<int*>(s_all + moe::TINY_SUMS);
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int A = (int)(a.M * a.top_k), n_kt = (int)(a.e.hidden / 256);
@@ -1111,9 +1111,9 @@ namespace {
 template <int GPT>
 int launch_tiny(const ExpertsArgs& a, const moe::Tiny& t, char* hs, char* he, hipStream_t stream)
 {
-    const int rc = ensure_dynamic_lds((const void*)moe_tiny_up_kernel<GPT>, t.lds, "w2_moe_experts");
+    const int rc = ensure_dynamic_lds((const void*)moe_tiny_up_kernel<GPT>, t.lds_all, "w2_moe_experts");
     if (rc) return rc;
-    hipLaunchKernelGGL((moe_tiny_up_kernel<GPT>), dim3((unsigned)(a.e.inter / 16 / TINY_P / t.units), (unsigned)t.tiles), dim3(512), t.lds, stream, a, hs,
+    hipLaunchKernelGGL((moe_tiny_up_kernel<GPT>), dim3((unsigned)(a.e.inter / 16 / moe::TINY_P / t.units), (unsigned)t.tiles), dim3(512), t.lds_all, stream, a, hs,
                        he, t.units, t.rows);
     hipLaunchKernelGGL((moe_tiny_down_kernel<GPT>), dim3((unsigned)(a.e.hidden / 16)), dim3(512), (size_t)a.M * 512, stream, a, (const char*)hs,
                        (const char*)he);

@@ -51,7 +51,14 @@ struct Tiny {
     int tiles, rows;                    // at most, and rows of a tile
     int units;                          // groups of two pairs of blocks that a workgroup takes one behind the other
     size_t lds;                         // rows and their exponents
+    size_t lds_all;                     // and what leaves: all that the gate and up launch asks for (its kernel declares none beside it)
 };
+
+// The gate and up launch's waves: two pairs of blocks times four ranges of K.  What leaves, in front of the rows: the sums of three ranges, or two
+// parts of h with the largest numbers (fewer), and the choice that each row is.
+constexpr int TINY_P = 2, TINY_KS = 4;
+constexpr size_t TINY_SUMS = (TINY_KS - 1) * TINY_P * 2048, TINY_LEAVE = TINY_SUMS + 8 * 4, TINY_MOST_ROWS = (size_t)128 << 10;
+static_assert(TINY_LEAVE % 16 == 0 && TINY_P * 16 * 36 <= TINY_SUMS && TINY_MOST_ROWS + TINY_LEAVE <= (size_t)160 << 10, "a CU's local memory");
 
 inline Tiny tiny(int64_t hidden, int64_t inter, int E, int G, int64_t A)
 {
@@ -59,7 +66,8 @@ inline Tiny tiny(int64_t hidden, int64_t inter, int E, int G, int64_t A)
     t.tiles = (int)most_tiles(A, E, 8);
     t.rows = (int)std::min<int64_t>(A, 8);                    // (or of x, where two of those are all)
     t.lds = (size_t)t.rows * (row_bytes(hidden) + 16 + exp_bytes(hidden));
-    t.fits = A <= 64 && t.lds <= (size_t)128 << 10 && t.tiles * hidden * inter <= (int64_t)1 << (G == 128 ? 27 : 26);
+    t.lds_all = t.lds + TINY_LEAVE;
+    t.fits = A <= 64 && t.lds <= TINY_MOST_ROWS && t.tiles * hidden * inter <= (int64_t)1 << (G == 128 ? 27 : 26);
     const int64_t groups = inter / 32;
     t.units = 1;
     while (t.units < 8 && groups % (2 * t.units) == 0 && t.tiles * (groups / (2 * t.units)) >= 512) t.units *= 2;

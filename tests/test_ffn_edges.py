@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import ffn_oracle as want
-from test_ffn_ops import CUT, U, Bank, f64, mixing, near, normal
+from test_ffn_ops import CUT, U, Bank, choices, experts_check, f64, mixing, near, normal
 
 torch = pytest.importorskip("torch")
 
@@ -53,3 +53,14 @@ def test_experts_that_all_but_cancel(w2, M, E, G):
     near(y, ref, U * np.abs(ref) + 2.0 ** -8 * ((U + CUT) * mag + CUT * h_err) + 2.0 ** -19 * mag, "two experts that all but cancel")
     off, norm = np.linalg.norm(f64(y) - ref), np.linalg.norm(ref)
     assert off <= 0.0036 * norm + 2.0 ** -19 * np.linalg.norm(mag), f"{off / norm:.4f} off"
+
+
+# ------------------------------------------------------------------ experts: up to 64 choices, local memory around 64 KiB
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [64, 128])
+@pytest.mark.parametrize("hidden,top", [(3584, 7), (3584, 8), (4096, 6), (4096, 7), (4096, 8), (5120, 5), (5120, 6), (7168, 4)])
+def test_experts_rows_around_64_kib(w2, hidden, top, G):
+    """One token and two: rows that fill 52 to 66 KiB of local memory, and 12 KiB beside them."""
+    bank = Bank(w2, hidden, 256, top + 1, G, seed=hidden + top)
+    for M in (1, 2):
+        experts_check(w2, bank, normal(M, M, hidden), choices(M, top + 1, top, M), mixing(M, top, M), what=f"hidden={hidden} top={top} M={M}")
