@@ -496,7 +496,8 @@ W2_API int w2_residual_norm(const w2_norm_t* norm, const void* residual, w2_dtyp
  *   c      = p + choice_bias             (choice_bias NULL: p)
  * With n_groups > 1 the experts are n_groups equal ranges, and only those of the top_groups ranges with the largest sum of
  * their group_top (1 or 2) largest c can be chosen.  Chosen are the top_k largest c, ties to the lower index (of groups too), in
- * falling order; their weights are scale * p, with renormalise != 0 divided by the sum of the chosen p.
+ * falling order; their weights are scale * p, with renormalise != 0 divided by the sum of the chosen p (also where every one of
+ * those is below what 64 bits hold: the quotients are those of the scores' exponentials).
  * Scores and choices are computed in 64 bits: two experts change places only where exact arithmetic would be in doubt too.  A
  * score that is NaN counts as lower than any number.
  * weight       dev, bf16 [n_experts][K], row stride ldw;  choice_bias  dev, fp32 [n_experts]

@@ -301,7 +301,20 @@ __global__ void __launch_bounds__(256) route_select_kernel(RouteArgs a, const do
             my_p = __longlong_as_double((int64_t)((uint64_t)p1 << 32 | p0));
         }
     }
-    const double total = a.r.renormalise ? wave_total(lane < a.r.top_k ? my_p : 0.0) : 1.0;
+    double total = a.r.renormalise ? wave_total(lane < a.r.top_k ? my_p : 0.0) : 1.0;
+    if (total < 0x1p-900) {
+        // All the chosen ones' p are next to nothing: quotients of their exponentials beside the largest one's.  (A sigmoid is exp(l) there to
+        // 2^-900 of itself; above, a p that lost digits is below 2^-100 of the sum.)
+        double my_l = 0.0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const double v = __shfl(l[j], my_id / PER);
+            if (my_id % PER == j) my_l = v;
+        }
+        const double largest = wave_max(lane < a.r.top_k ? my_l : -INFINITY);
+        my_p = exp(my_l - largest);
+        total = wave_total(lane < a.r.top_k ? my_p : 0.0);
+    }
     if (lane < a.r.top_k) {
         a.ids[m * a.r.top_k + lane] = my_id;
         a.weights[m * a.r.top_k + lane] = (float)(my_p / total * (double)a.r.scale);

@@ -64,3 +64,52 @@ def test_experts_rows_around_64_kib(w2, hidden, top, G):
     bank = Bank(w2, hidden, 256, top + 1, G, seed=hidden + top)
     for M in (1, 2):
         experts_check(w2, bank, normal(M, M, hidden), choices(M, top + 1, top, M), mixing(M, top, M), what=f"hidden={hidden} top={top} M={M}")
+
+
+# ------------------------------------------------------------------ the router where probabilities run out of 64 bits
+def renormalised(l, ids, scale):
+    """scale * exp(l - largest) / sum over the chosen ones: what p / (sum of p) is wherever every p is proportional to exp(l)."""
+    c = np.take_along_axis(l, ids, 1)
+    w = np.exp(c - c.max(1, keepdims=True))
+    return scale * w / w.sum(1, keepdims=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("E,top,groups", [(40, 5, 1), (128, 8, 1), (256, 8, 8), (1000, 64, 4)])
+@pytest.mark.parametrize("low", [-650.0, -720.0, -2000.0])
+def test_route_sigmoids_of_nothing_are_renormalised(w2, E, top, groups, low):
+    """Scores around -650 to -2000, where a sigmoid is exp(l) and below what 64 bits hold: the weights are their finite quotients."""
+    M, K = 9, 512
+    x, W = normal(1, M, K), normal(2, E, K, std=0.05)
+    x[:, 0], W[:, 0] = 1.0, low
+    ids, w = w2.moe_route(w2.Router(W, top, score="sigmoid", scale=2.5, n_groups=groups, top_groups=max(1, groups // 2)), x)
+    l = f64(x) @ f64(W).T
+    assert l.max() < low + 20 and np.ptp(l, axis=1).min() > 1
+    got = ids.cpu().numpy().astype(int)
+    near(w, renormalised(l, got, 2.5), 2.0 ** -22 * renormalised(l, got, 2.5) + 2.0 ** -149, "weights")
+    size = E // groups
+    for row, chosen in zip(l, got):                           # the largest ones of the groups with the largest
+        best = np.argsort(-row.reshape(groups, size).max(1), kind="stable")[:max(1, groups // 2)]
+        free = np.sort((best[:, None] * size + np.arange(size)).ravel())
+        assert chosen.tolist() == free[np.argsort(-row[free], kind="stable")[:top]].tolist()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_route_a_bias_that_chooses_experts_of_no_weight(w2, score):
+    """Experts whose p are 0 in 64 bits, chosen for their bias: the weights are the quotients of their exponentials, without NaN."""
+    M, K, E = 7, 256, 72
+    x, W = normal(3, M, K), normal(4, E, K, std=0.05)
+    x[:, 0] = 1.0
+    W[:, 0] = -1000.0
+    W[10, 0] = 1000.0                                         # has all of a softmax, and is not chosen
+    bias = torch.zeros(E, device="cuda")
+    bias[20:24] = torch.tensor([8.0, 7.0, 6.0, 5.0], device="cuda")
+    ids, w = w2.moe_route(w2.Router(W, 4, score=score, choice_bias=bias), x)
+    assert ids.tolist() == [[20, 21, 22, 23]] * M
+    ref = renormalised(f64(x) @ f64(W).T, ids.cpu().numpy().astype(int), 1.0)
+    near(w, ref, 2.0 ** -22 * ref, "weights")
+    ids, w = w2.moe_route(w2.Router(W, 5, score=score, choice_bias=bias), x)      # the fifth is the one with weight
+    assert ids.tolist() == [[20, 21, 22, 23, 10]] * M and w[:, 4].eq(1).all() and not w[:, :4].any()
+    ids, w = w2.moe_route(w2.Router(W, 4, score=score, choice_bias=bias, renormalise=False), x)
+    assert not w.any()                                        # p itself, which fp32 does not hold
