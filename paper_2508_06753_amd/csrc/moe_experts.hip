@@ -556,15 +556,16 @@ __global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kern
 // touch every bank once.  Weights and exponents of 256 of K are asked for two tiles ahead.
 //
 // Of a stage's column blocks the products of the last one begin behind the barrier at which the next stage's rows are there; those are read
-// into registers as the products let go of them.  Waits (vector memory operations complete in order): at the barrier of stage s the
-// rows of s + 1 have landed, which were asked for at that of s - 2.  Asked for since: rows of one more stage, and one tile's
-// weights (4), scales (4) and exponents (RT).  So no register may spill here: a load from scratch would be counted too.
+// into registers as the products let go of them.  What may be under way at a barrier is counted (moe_plan.h).  An operation more than counted makes
+// the wait longer; one fewer, a load that the compiler joins with another or drops, would let a barrier pass before its rows have landed.  So every load is
+// unconditional and none is made twice, and the compiled kernel's own order is walked by a test.
 //
 // 16384 choices of 64 experts of 2048 x 1024: 142 to 161 us as the clock goes (1.6 to 2.1 GHz) for gate and up, 87 to 100 for down, of which the
 // products are 63 and 32 at 2.1 GHz (32 cycles each).  A workgroup takes 1.2 us to know its tile, 3.1 until rows are there, 15 for 2048 of K and 2.6 to leave;
 // a SIMD has two of its three waves in the loop at a time.  Neither the loads nor any one kind of vector instruction bounds the loop by itself
 // (left out one by one: 127 to 133 us for 132).
-constexpr int TILE_ROWS = 32, RING = 4;
+constexpr int TILE_ROWS = 32, RING = moe::TILE_AHEAD + 1;
+static_assert((RING & (RING - 1)) == 0, "a stage's place in the ring");
 
 template <bool UP, int GPT>
 __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(ProductArgs a, int64_t row_bytes_all, const int* n_tiles, int col_groups)
@@ -650,9 +651,9 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 if (c == 3) {
-                    wait_loads<2 * RT + 8>();
+                    wait_loads<moe::tile_at_stage(RT)>();
                     bare_barrier();
-                    load_rows(s + 3);
+                    load_rows(s + moe::TILE_AHEAD);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 const v4i& w = c < 3 ? wt.w[c + 1] : next.w[0];
@@ -699,12 +700,12 @@ __global__ void __launch_bounds__(256, GPT == 2 ? 3 : 2) moe_tile_kernel(Product
         load_weights(0, wa);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int s = 0; s < RING - 1; ++s) load_rows(s);
+        for (int s = 0; s < moe::TILE_AHEAD; ++s) load_rows(s);
         __builtin_amdgcn_sched_barrier(0);
         load_weights(1, wb);
         to_fp4((uint32_t)wa.w[0][0], b[0], b[1]);
         to_fp4((uint32_t)wa.w[0][1], b[2], b[3]);
-        wait_loads<3 * RT + 8>();
+        wait_loads<moe::tile_at_start(RT)>();
         bare_barrier();
 #pragma unroll
         for (int r = 0; r < RT; ++r) {

@@ -74,6 +74,16 @@ inline Tiny tiny(int64_t hidden, int64_t inter, int E, int G, int64_t A)
     return t;
 }
 
+// Loads of a wave of the kernel for many rows that may still be under way at its counted waits (vector memory operations complete in order).  rt: row
+// tiles of 16, and so its loads of rows in a stage of 128 of K.  Rows are asked for three stages ahead, at a stage's barrier; a tile of 256 of K's weights
+// (4), scales (4) and exponents (rt) behind every second stage.
+constexpr int TILE_AHEAD = 3;
+constexpr int tile_weights(int rt) { return 8 + rt; }
+// before the first stage, whose rows have landed: those of two more, and the second tile's weights
+constexpr int tile_at_start(int rt) { return (TILE_AHEAD - 1) * rt + tile_weights(rt); }
+// at the barrier of stage s: the rows of s + 1 have landed, which were asked for at that of s - 2; those of s + 2 and one tile's weights since
+constexpr int tile_at_stage(int rt) { return (TILE_AHEAD - 2) * rt + tile_weights(rt); }
+
 struct Workspace {                      // offsets in bytes, each a multiple of 256; none shrinks when M grows
     size_t tiles, tile_rows, place, xs, xe, hs, he, z;
     size_t ze;                          // room that no kernel uses, a byte for 32 sums: whoever walks the workspace finds it here
