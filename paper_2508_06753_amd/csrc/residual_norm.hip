@@ -56,25 +56,40 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(NormArgs a, int64_t
     const int step = blockDim.x * 8;
     const int N = (int)a.N;
 
-    // everything the row needs is asked for before the first sum waits
-    uint4 y[NV], g[NV], w[NV], pw[NV], r0[NV], r1[NV];
+    // Everything the row needs is asked for before the first sum waits; of more than 4 vectors a thread only y, the others where they are
+    // used: together they would be up to 192 registers of the 128 that 1024 threads have (141 were spilled, and the row
+    // went to memory and back: 1000 gated rows of 65536, residual in 32 bits, 332 us; now 187, 4.9 TB/s).
+    constexpr bool EARLY = NV <= 4;
+    constexpr int NE = EARLY ? NV : 1;
+    uint4 y[NV], g[NE], w[NE], pw[NE], r0[NE], r1[NE];
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    auto load_others = [&](int e, int n) {
+        g[e] = pw[e] = r0[e] = r1[e] = zero;
+        if (n < N) {
+            if (a.residual) {
+                if constexpr (RBF) r0[e] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.residual) + m * a.ldr + n);
+                else {
+                    const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(a.residual) + m * a.ldr + n);
+                    r0[e] = p[0];
+                    r1[e] = p[1];
+                }
+            }
+            if (a.p.gate) g[e] = *reinterpret_cast<const uint4*>(a.p.gate + m * a.p.ld_gate + n);
+            if (a.p.post_weight) pw[e] = *reinterpret_cast<const uint4*>(a.p.post_weight + n);
+        }
+    };
+    auto load_weight = [&](int e, int n) {
+        w[e] = zero;
+        if (n < N && a.p.weight) w[e] = *reinterpret_cast<const uint4*>(a.p.weight + n);
+    };
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int n = tid * 8 + v * step;
-        y[v] = g[v] = w[v] = pw[v] = r0[v] = r1[v] = make_uint4(0, 0, 0, 0);
-        if (n < N) {
-            if (a.y) y[v] = *reinterpret_cast<const uint4*>(a.y + m * a.ldy + n);
-            if (a.residual) {
-                if constexpr (RBF) r0[v] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.residual) + m * a.ldr + n);
-                else {
-                    const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(a.residual) + m * a.ldr + n);
-                    r0[v] = p[0];
-                    r1[v] = p[1];
-                }
-            }
-            if (a.p.gate) g[v] = *reinterpret_cast<const uint4*>(a.p.gate + m * a.p.ld_gate + n);
-            if (a.p.post_weight) pw[v] = *reinterpret_cast<const uint4*>(a.p.post_weight + n);
-            if (a.p.weight) w[v] = *reinterpret_cast<const uint4*>(a.p.weight + n);
+        y[v] = zero;
+        if (n < N && a.y) y[v] = *reinterpret_cast<const uint4*>(a.y + m * a.ldy + n);
+        if constexpr (EARLY) {
+            load_others(v, n);
+            load_weight(v, n);
         }
     }
     auto total = [&](float s, int slot) -> float {
@@ -97,18 +112,19 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(NormArgs a, int64_t
     float r[NV][8], s = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
+        const int n = tid * 8 + v * step, e = EARLY ? v : 0;
+        if constexpr (!EARLY) load_others(e, n);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float b = bf16_at(y[v], i);
-            if (a.p.post_norm) b = a.p.post_weight ? b * post * (bf16_at(pw[v], i) + a.p.weight_offset) : b * post;
-            if (a.p.gate) b *= bf16_at(g[v], i);
+            if (a.p.post_norm) b = a.p.post_weight ? b * post * (bf16_at(pw[e], i) + a.p.weight_offset) : b * post;
+            if (a.p.gate) b *= bf16_at(g[e], i);
             float old;
-            if constexpr (RBF) old = bf16_at(r0[v], i);
-            else old = __uint_as_float(i < 4 ? (&r0[v].x)[i & 3] : (&r1[v].x)[i & 3]);
+            if constexpr (RBF) old = bf16_at(r0[e], i);
+            else old = __uint_as_float(i < 4 ? (&r0[e].x)[i & 3] : (&r1[e].x)[i & 3]);
             r[v][i] = fmaf(a.p.residual_scale, old, a.p.block_scale * b);
             s = fmaf(r[v][i], r[v][i], s);
         }
-        const int n = tid * 8 + v * step;
         if (a.residual_out && n < N) {
             if constexpr (RBF) {
                 *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.residual_out) + m * a.ldro + n) =
@@ -127,10 +143,11 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(NormArgs a, int64_t
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         float t[8];
+        const int n = tid * 8 + v * step, e = EARLY ? v : 0;
+        if constexpr (!EARLY) load_weight(e, n);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = a.p.weight ? r[v][i] * f * (bf16_at(w[v], i) + a.p.weight_offset) : r[v][i] * f;
+        for (int i = 0; i < 8; ++i) t[i] = a.p.weight ? r[v][i] * f * (bf16_at(w[e], i) + a.p.weight_offset) : r[v][i] * f;
         out[v] = make_uint4(pack_bf16(t[0], t[1]), pack_bf16(t[2], t[3]), pack_bf16(t[4], t[5]), pack_bf16(t[6], t[7]));
-        const int n = tid * 8 + v * step;
         if (n < N) {
             if (a.x) *reinterpret_cast<uint4*>(a.x + m * a.ldx + n) = out[v];
 #pragma unroll

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import ffn_oracle as want
-from test_ffn_ops import CUT, U, Bank, choices, experts_check, f64, mixing, near, normal
+from test_ffn_ops import CUT, U, Bank, choices, experts_check, f64, mixing, near, norm_case, normal
 
 torch = pytest.importorskip("torch")
 
@@ -113,3 +113,15 @@ def test_route_a_bias_that_chooses_experts_of_no_weight(w2, score):
     assert ids.tolist() == [[20, 21, 22, 23, 10]] * M and w[:, 4].eq(1).all() and not w[:, :4].any()
     ids, w = w2.moe_route(w2.Router(W, 4, score=score, choice_bias=bias, renormalise=False), x)
     assert not w.any()                                        # p itself, which fp32 does not hold
+
+
+# ------------------------------------------------------------------ between two blocks: rows of more than four vectors a thread
+@pytest.mark.gpu
+@pytest.mark.parametrize("N", [32776, 40960, 49160, 65528])
+@pytest.mark.parametrize("rdt", [torch.float32, torch.bfloat16])
+def test_norm_of_wide_rows(w2, N, rdt):
+    for post, gate, offset in ((True, "rows", 1.0), (True, "vector", 0.0), (False, "none", 0.5)):
+        norm_case(w2, 3, N, rdt, post=post, gate=gate, offset=offset, pad=8, scales=(0.5, 0.22), quantize=N % 256 == 0, seed=N)
+        norm_case(w2, 70, N, rdt, post=post, gate=gate, offset=offset, in_place=True, seed=N + 1)
+    norm_case(w2, 2, N, rdt, block=False, seed=N + 2)
+    norm_case(w2, 2, N, rdt, residual=False, post=True, seed=N + 3)

@@ -103,6 +103,11 @@ def test_kernel_for_many_rows_keeps_nothing_in_scratch(kernels):
         assert k[".private_segment_fixed_size"] == 0 and k[".vgpr_spill_count"] == 0 and k[".sgpr_spill_count"] == 0, n
 
 
+def test_norm_keeps_a_row_in_registers(kernels):
+    for n, k in named(kernels, "residual_norm_kernel").items():
+        assert k[".private_segment_fixed_size"] == 0 and k[".vgpr_spill_count"] == 0, n
+
+
 # ------------------------------------------------------------------ the counted waits of the kernel for many rows
 class Wave:
     """Vector memory operations in the order in which they are asked for, and so complete."""
