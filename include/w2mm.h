@@ -539,8 +539,8 @@ W2_API int w2_moe_experts_workspace_size(const w2_experts_t* experts, int64_t M,
  * Sums in fp32, one rounding of Y.  The matrix instructions multiply a weight's exact value with each number of x (or h) as the
  * sum of two e4m3 numbers, scaled by a power of two that 32 numbers share (k = 16 g .. 16 g + 15 and 64 + 16 g .. of each 128): a
  * bf16 number of x is exactly such a sum down to 2^-14 of the largest of its 32 and off by at most 2^-22 of that below; h is
- * rounded to one, by at most 2^-9 of itself or 2^-22 of that.  Of 8 neighbouring products the bits 13 places below the largest are
- * cut off.  The sums of a row's experts wait for each other in fp32.
+ * rounded to one, by at most 2^-9 of itself, 2^-22 of that, or 2^-137.  Of 8 neighbouring products the bits 13 places below the largest
+ * are cut off.  Denormal numbers count as what they are, in x, the sums and h.  The sums of a row's experts wait for each other in fp32.
  * The same call gives the same bits.  What other rows hold does not matter to a row; their number, and in calls of up to 64
  * choices their ids, may change the order in which its sums are added.
  * x        dev, bf16 [M][hidden], row stride ldx;  a row with an infinity or NaN gives a row of NaN

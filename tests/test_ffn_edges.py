@@ -125,3 +125,77 @@ def test_norm_of_wide_rows(w2, N, rdt):
         norm_case(w2, 70, N, rdt, post=post, gate=gate, offset=offset, in_place=True, seed=N + 1)
     norm_case(w2, 2, N, rdt, block=False, seed=N + 2)
     norm_case(w2, 2, N, rdt, residual=False, post=True, seed=N + 3)
+
+
+# ------------------------------------------------------------------ experts: what a row's numbers keep, on each of the three ways through
+WAYS = [(4, 2), (80, 64), (300, 2)]                           # rows, experts: two launches, few rows an expert, many
+
+
+def one_number(w2, E, G, up, down, hidden=256, inter=256):
+    """Experts with h = silu(g) u, g = u = up * (a row's first number) in every column, and Y = down * h[0] in every one."""
+    codes = np.full((E, hidden, 2 * inter), 2), np.full((E, inter, hidden), 2)
+    for c in codes:
+        c[:, 0] = 3
+    return MadeBank(w2, hidden, inter, G, (codes[0], np.full((E, hidden // G, 2 * inter), up)), (codes[1], np.full((E, inter // G, hidden), down)))
+
+
+def first_numbers(M, hidden, values):
+    x = torch.zeros(M, hidden, dtype=torch.float64)
+    x[:, 0] = torch.tensor([values[i % len(values)] for i in range(M)], dtype=torch.float64)
+    x = x.bfloat16()
+    return x.cuda(), x[:, 0].double().numpy()
+
+
+def through_one(w2, bank, x, base=None):
+    M = x.shape[0]
+    ids, weights = torch.zeros(M, 1, dtype=torch.int32, device="cuda"), torch.ones(M, 1, device="cuda")
+    return f64(w2.moe_experts(bank.experts, x, ids, weights, base=base))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [64, 128])
+@pytest.mark.parametrize("M,E", WAYS)
+def test_experts_round_h_by_half_a_step_of_nine_bits(w2, M, E, G):
+    """Y's own rounding does not hide h's: base is the negative of the result in bf16, so that what is left (exact in fp32) is their
+    difference, which 2^-8 of itself rounds.  h: 2^-9 of it, and 2^-20 for the exponential, the reciprocal and three products in 32 bits."""
+    bank = one_number(w2, E, G, 1.0, 1.0)
+    values = np.random.default_rng(M + G).uniform(0.25, 4.0, M) * np.random.default_rng(G).choice([-1.0, 1.0], M)
+    x, g = first_numbers(M, 256, list(values))
+    ref = g / (1.0 + np.exp(-g)) * g
+    b = torch.tensor(ref).bfloat16()
+    base = -b.cuda()[:, None].repeat(1, 256).contiguous()
+    left = (ref - b.double().numpy())[:, None].repeat(256, 1)
+    tol = (2.0 ** -9 + 2.0 ** -20) * np.abs(ref)[:, None]
+    near(through_one(w2, bank, x, base), left, tol + 2.0 ** -8 * (np.abs(left) + tol), "h")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [64, 128])
+@pytest.mark.parametrize("M,E", WAYS)
+def test_experts_smallest_numbers(w2, M, E, G):
+    """Rows of numbers down to bf16's smallest denormal, met by scales that bring them up: x is exact.  Then an h down to 2^-133: 2^-9 of it
+    or 2^-137, half a step of the second part at the smallest power of two.  Y: its rounding, u; 2^-16 for what is done in 32 bits."""
+    bank = one_number(w2, E, G, 2.0 ** 100, 2.0 ** 70)
+    x, g = first_numbers(M, 256, [2.0 ** -115, -2.0 ** -120, 255 * 2.0 ** -133, 1.5 * 2.0 ** -126, 2.0 ** -126, -2.0 ** -127, 3 * 2.0 ** -129, 2.0 ** -130, 5 * 2.0 ** -133, 2.0 ** -133])
+    g = g * 2.0 ** 100
+    ref = (g / (1.0 + np.exp(-g)) * g * 2.0 ** 70)[:, None].repeat(256, 1)
+    near(through_one(w2, bank, x), ref, (U + U / 2 + 2.0 ** -16) * np.abs(ref), "smallest x")
+    bank = one_number(w2, E, G, 1.0, 2.0 ** 100)
+    x, g = first_numbers(M, 256, [2.0 ** -57, -2.0 ** -60, 1.375 * 2.0 ** -60, 2.0 ** -62, 1.25 * 2.0 ** -62, 2.0 ** -63, 1.5 * 2.0 ** -64, 2.0 ** -65, -1.5 * 2.0 ** -66])
+    h = (g / (1.0 + np.exp(-g)) * g)[:, None].repeat(256, 1)
+    ref = h * 2.0 ** 100
+    near(through_one(w2, bank, x), ref, (U + 2.0 ** -16) * np.abs(ref) + np.maximum(U / 2 * np.abs(h), 2.0 ** -137) * (1 + U) * 2.0 ** 100, "smallest h")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [64, 128])
+@pytest.mark.parametrize("M,E", [(1, 6), (5, 6), (40, 64), (150, 6)])
+@pytest.mark.parametrize("f", [1e-16, 1e-18, 1e-30, 1e-37])
+def test_experts_rows_of_tiny_numbers(w2, M, E, G, f):
+    """Ordinary weights, rows of tiny numbers: finite, and near the definition beside what 32 bits hold of h and bf16 of Y.  Past the usual
+    bound: h's 2^-137 times inter * 2 slots * 0.1 (51 of them), half a step of Y's denormals (2^-134) and of 1000 operations' (2^-149): 2^-131."""
+    bank = Bank(w2, 512, 256, E, G, seed=E + G)
+    x, w = (normal(1, M, 512, dtype=torch.float32) * f).bfloat16(), mixing(M, 2, 2)
+    ids = choices(M, E, 2, 3)
+    ref, mag, h_err = want.experts(f64(x), ids.cpu().numpy(), f64(w), bank.weights(0), bank.weights(1))
+    near(w2.moe_experts(bank.experts, x, ids, w), ref, U * np.abs(ref) + (U + CUT) * mag + CUT * h_err + 2.0 ** -131, f"numbers of {f}")
