@@ -199,3 +199,30 @@ def test_experts_rows_of_tiny_numbers(w2, M, E, G, f):
     ids = choices(M, E, 2, 3)
     ref, mag, h_err = want.experts(f64(x), ids.cpu().numpy(), f64(w), bank.weights(0), bank.weights(1))
     near(w2.moe_experts(bank.experts, x, ids, w), ref, U * np.abs(ref) + (U + CUT) * mag + CUT * h_err + 2.0 ** -131, f"numbers of {f}")
+
+
+# ------------------------------------------------------------------ experts: kernels that ordinary sizes do not reach
+SPLIT = [(hidden, 256, 16, 8, 11) for hidden in (2048, 2304, 2560, 2816, 3328)] + [(256, inter, 16, 8, 11) for inter in (2048, 2304, 2560, 2816, 3328)] + \
+        [(2304, 2560, 12, 7, 10)]
+UNITS = [(256, 1024, 64, 8, 4, 2), (512, 1024, 64, 8, 8, 4), (256, 2048, 64, 8, 8, 8), (256, 1536, 64, 8, 6, 4)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [64, 128])
+@pytest.mark.parametrize("hidden,inter,E,k,M", SPLIT)
+def test_experts_few_rows_two_ranges_of_k(w2, G, hidden, inter, E, k, M):
+    """K of 8 to 13 tiles in two ranges: even ones, a shorter second one, one to three steps behind the last four."""
+    bank = Bank(w2, hidden, inter, E, G, seed=hidden + inter)
+    x, w = normal(M, M, hidden), mixing(M, k, M)
+    experts_check(w2, bank, x, choices(M, E, k, M), w, what=f"{hidden} x {inter}")
+    experts_check(w2, bank, x, choices(M, E, k, M, distinct=False), w, base=normal(2, M, hidden), what=f"{hidden} x {inter}, repeated")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [64, 128])
+@pytest.mark.parametrize("hidden,inter,E,k,M,units", UNITS)
+def test_experts_several_groups_of_blocks_a_workgroup(w2, G, hidden, inter, E, k, M, units):
+    bank = Bank(w2, hidden, inter, E, G, seed=hidden + inter)
+    x, w = normal(M, M, hidden), mixing(M, k, M)
+    experts_check(w2, bank, x, choices(M, E, k, M), w, what=f"{hidden} x {inter}")
+    experts_check(w2, bank, x, choices(M, E, k, M, skew=4.0), w, base=normal(2, M, hidden), what=f"{hidden} x {inter}, skewed")

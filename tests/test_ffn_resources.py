@@ -259,3 +259,46 @@ def test_built_kernel_for_many_rows_waits_for_its_rows(kernels, tmp_path):
             # both heights; 256 of K (two stages) and more, an odd number of them and an even one
             assert {(rt, n) for rt in (1, 2) for n in (2, 4, 6, 8, 10)} <= stages, sorted(stages)
     assert walked == len(names) == 4
+
+
+# ------------------------------------------------------------------ which kernels the tests' sizes reach
+REACH = r"""
+#include <cstdio>
+#include "%s/paper_2508_06753_amd/csrc/moe_plan.h"
+using namespace w2::moe;
+int main()
+{
+    long long hidden, inter, E, G, A;
+    while (scanf("%%lld %%lld %%lld %%lld %%lld", &hidden, &inter, &E, &G, &A) == 5) {
+        const Tiny t = tiny(hidden, inter, (int)E, (int)G, A);
+        const Plan p = plan(hidden, inter, (int)E, (int)G, A);
+        printf("%%d %%d %%d %%d %%d\n", t.fits, t.units, p.few, p.ks_up, p.ks_down);
+    }
+}
+"""
+
+
+def test_sizes_reach_the_kernels_that_they_are_for(tmp_path):
+    if shutil.which("g++") is None:
+        pytest.skip("no g++")
+    from test_ffn_edges import SPLIT, UNITS, WAYS
+    (tmp_path / "p.cpp").write_text(REACH % ROOT)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-o", str(tmp_path / "p"), str(tmp_path / "p.cpp")], check=True)
+
+    def reach(hidden, inter, E, G, A):
+        text = subprocess.run([str(tmp_path / "p")], input=f"{hidden} {inter} {E} {G} {A}", capture_output=True, text=True, check=True).stdout
+        return list(map(int, text.split()))
+
+    for G in (64, 128):
+        seen = set()
+        for hidden, inter, E, k, M in SPLIT:
+            fits, _, few, up, down = reach(hidden, inter, E, G, M * k)
+            assert not fits and few and (up, down) == (2 if hidden >= 2048 else 1, 2 if inter >= 2048 else 1)
+            seen |= {("up", hidden // 256)} if up == 2 else set()
+            seen |= {("down", inter // 256)} if down == 2 else set()
+        assert seen == {(which, n) for which in ("up", "down") for n in (8, 9, 10, 11, 13)}
+        for hidden, inter, E, k, M, units in UNITS:
+            fits, got, *_ = reach(hidden, inter, E, G, M * k)
+            assert fits and got == units, (hidden, inter, E, k, M, got)
+        ways = [reach(256, 256, E, G, M) for M, E in WAYS]
+        assert [(w[0], w[2]) for w in ways][0][0] == 1 and ways[1][0] == 0 and ways[1][2] == 1 and ways[2][0] == 0 and ways[2][2] == 0
