@@ -498,8 +498,9 @@ W2_API int w2_residual_norm(const w2_norm_t* norm, const void* residual, w2_dtyp
  * their group_top (1 or 2) largest c can be chosen.  Chosen are the top_k largest c, ties to the lower index (of groups too), in
  * falling order; their weights are scale * p, with renormalise != 0 divided by the sum of the chosen p (also where every one of
  * those is below what 64 bits hold: the quotients are those of the scores' exponentials).
- * Scores and choices are computed in 64 bits: two experts change places only where exact arithmetic would be in doubt too.  A
- * score that is NaN counts as lower than any number.
+ * Scores and choices are computed in 64 bits: two experts change places only where exact arithmetic would be in doubt too.  Without a
+ * choice_bias the order is that of l; with one, and for a group's sum of two, that of c in 64 bits: where sigmoids are 1 or p next to
+ * nothing, equal ones go to the lower index.  A score that is NaN counts as lower than any number.
  * weight       dev, bf16 [n_experts][K], row stride ldw;  choice_bias  dev, fp32 [n_experts]
  * n_experts up to 1024, n_groups a divisor of it up to 64, top_k <= 64 and <= the experts of top_groups groups. */
 typedef enum { W2_SCORE_SOFTMAX = 0, W2_SCORE_SIGMOID = 1 } w2_score_t;

@@ -228,8 +228,8 @@ __global__ void __launch_bounds__(256) route_select_kernel(RouteArgs a, const do
 #pragma unroll
         for (int j = 0; j < PER; ++j) p[j] = 1.0 / (1.0 + exp(-l[j]));
     }
-    // without a bias and without sums over groups the scores' own order decides: it does not run out of digits
-    const bool by_logit = !a.r.choice_bias && (!GROUPS || a.r.group_top == 1);
+    // without a bias the scores' own order decides, which does not run out of digits; a sum over a group is one of p
+    const bool by_logit = !a.r.choice_bias, group_by_logit = by_logit && a.r.group_top == 1;
     double* const s_val = s_all + wave * (64 * PER);
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -237,7 +237,10 @@ __global__ void __launch_bounds__(256) route_select_kernel(RouteArgs a, const do
         double c = by_logit ? l[j] : p[j];
         if (a.r.choice_bias && e < E) c += (double)a.r.choice_bias[e];
         key[j] = e < E ? sortable(c) : 0;
-        if constexpr (GROUPS) s_val[e] = c == c ? c : -INFINITY;
+        if constexpr (GROUPS) {
+            if (by_logit && !group_by_logit) c = p[j];
+            s_val[e] = c == c ? c : -INFINITY;
+        }
     }
     if constexpr (GROUPS) {
         // (a wave's own part of local memory, in order: no barrier)

@@ -226,3 +226,24 @@ def test_experts_several_groups_of_blocks_a_workgroup(w2, G, hidden, inter, E, k
     x, w = normal(M, M, hidden), mixing(M, k, M)
     experts_check(w2, bank, x, choices(M, E, k, M), w, what=f"{hidden} x {inter}")
     experts_check(w2, bank, x, choices(M, E, k, M, skew=4.0), w, base=normal(2, M, hidden), what=f"{hidden} x {inter}, skewed")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,groups,top_groups,top", [(32, 4, 2, 8), (256, 8, 8, 16), (60, 3, 3, 60)])
+def test_route_sums_of_groups_leave_the_scores_order(w2, score, E, groups, top_groups, top):
+    """Scores of 100 and more apart: sigmoids are 1 and a softmax has one number, so that sums over groups are equal and the lower ones go;
+    in them the scores' own order decides."""
+    x, W = normal(5, 6, 256), normal(6, E, 256, std=0.2)
+    x[:, 0] = 1.0
+    W[:, 0] = torch.tensor(np.random.default_rng(E).permutation(E) * 128.0 + 128.0).bfloat16()
+    ids, w = w2.moe_route(w2.Router(W, top, score=score, n_groups=groups, top_groups=top_groups, group_top=2), x)
+    l, size = f64(x) @ f64(W).T, E // groups
+    assert l.min() > 64
+    for row, chosen in zip(l, ids.cpu().numpy()):
+        p = 1.0 / (1.0 + np.exp(-row)) if score == "sigmoid" else np.exp(row - row.max())
+        best = np.sort(p.reshape(groups, size), 1)[:, -2:].sum(1)
+        kept = np.argsort(-best, kind="stable")[:top_groups]
+        free = np.sort((kept[:, None] * size + np.arange(size)).ravel())
+        assert chosen.tolist() == free[np.argsort(-row[free], kind="stable")[:top]].tolist()
+    assert torch.isfinite(w).all()
