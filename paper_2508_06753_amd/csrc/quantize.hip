@@ -14,15 +14,6 @@ namespace w2 {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// The definition's rounding and clamp, bits 0..7 of the result the int8 code: t = x * inv (one rounded multiply),
-// clamped to +-127, rounded half to even by adding 1.5 * 2^23 (|t| < 2^22: one more rounding).
-__device__ __forceinline__ uint32_t quant_bits(float x, float inv)
-{
-#pragma clang fp contract(off)
-    const float t = __builtin_amdgcn_fmed3f(x * inv, -127.0f, 127.0f);
-    return __float_as_uint(t + 12582912.0f);
-}
-
 // low bytes of a, b, c, d -> one dword
 __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
@@ -85,7 +76,7 @@ quantize_rows_kernel(const void* __restrict__ X, int64_t ldx, int8_t* __restrict
         const int64_t k = o / EB;
         uint32_t b[EPT];
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) b[e] = quant_bits(value(d, e), inv);
+        for (int e = 0; e < EPT; ++e) b[e] = quantised_bits(value(d, e), inv);
         const uint32_t p0 = pack4(b[0], b[1], b[2], b[3]);
         if constexpr (BF16) *reinterpret_cast<uint2*>(xq + m * K + k) = make_uint2(p0, pack4(b[4], b[5], b[6], b[7]));
         else *reinterpret_cast<uint32_t*>(xq + m * K + k) = p0;

@@ -39,14 +39,6 @@ __device__ __forceinline__ float bf16_at(const uint4& v, int i)
     return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
 }
 
-// the rounding of w2_quantize_rows, bits 0..7 the int8 code
-__device__ __forceinline__ uint32_t quant_bits(float x, float inv)
-{
-#pragma clang fp contract(off)
-    const float t = __builtin_amdgcn_fmed3f(x * inv, -127.0f, 127.0f);
-    return __float_as_uint(t + 12582912.0f);
-}
-
 template <int NV, bool RBF>
 __global__ void __launch_bounds__(1024) residual_norm_kernel(NormArgs a, int64_t m0, float inv_n)
 {
@@ -171,7 +163,7 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(NormArgs a, int64_t
         for (int h = 0; h < 2; ++h) {
             uint32_t b[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) b[i] = quant_bits(bf16_at(out[v], 4 * h + i), inv);
+            for (int i = 0; i < 4; ++i) b[i] = quantised_bits(bf16_at(out[v], 4 * h + i), inv);
             q[h] = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u) | __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
         }
         *reinterpret_cast<uint2*>(a.xq + m * N + n) = make_uint2(q[0], q[1]);

@@ -34,6 +34,16 @@ __device__ __forceinline__ float wave_max_f32(float m)
     return fmaxf(fmaxf(r0, r1), fmaxf(r2, r3));
 }
 
+// A row's quantisation, in w2_quantize_rows and for x's int8 rows in w2_residual_norm, which are the same bit for bit: the definition's
+// rounding and clamp, bits 0..7 of the result the int8 code: t = x * inv (one rounded multiply), clamped to +-127, rounded half to
+// even by adding 1.5 * 2^23 (|t| < 2^22: one more rounding).
+__device__ __forceinline__ uint32_t quantised_bits(float x, float inv)
+{
+#pragma clang fp contract(off)
+    const float t = __builtin_amdgcn_fmed3f(x * inv, -127.0f, 127.0f);
+    return __float_as_uint(t + 12582912.0f);
+}
+
 // Records `what` + the HIP error string as this thread's last error if the
 // preceding launches failed; returns a w2_status_t.
 int check_launch(const char* what);

@@ -247,3 +247,21 @@ def test_route_sums_of_groups_leave_the_scores_order(w2, score, E, groups, top_g
         free = np.sort((kept[:, None] * size + np.arange(size)).ravel())
         assert chosen.tolist() == free[np.argsort(-row[free], kind="stable")[:top]].tolist()
     assert torch.isfinite(w).all()
+
+
+# ------------------------------------------------------------------ between two blocks: int8 rows of numbers that are none
+@pytest.mark.gpu
+@pytest.mark.parametrize("N", [256, 5120])
+def test_norm_quantised_rows_where_numbers_are_not_finite(w2, N):
+    """x's int8 rows are those of quantize_rows for rows of NaN, of infinities, of the largest numbers and of denormals too."""
+    r = normal(7, 6, N, dtype=torch.float32)
+    weight = torch.ones(N, dtype=torch.bfloat16, device="cuda")
+    weight[3], weight[9], weight[11] = float("inf"), 3e38, float("nan")
+    r[0] *= 1e-38
+    r[1] = 0.0
+    r[2, 5] = float("nan")
+    r[3, 5] = float("inf")
+    for w in (None, weight):
+        x, _, xq, sx = w2.residual_norm(w2.Norm(w, eps=0.5), r, None, quantize=True)
+        bits, scale, _ = w2.quantize_rows(x)
+        assert torch.equal(xq, bits) and torch.equal(sx.view(torch.int32), scale.view(torch.int32))
