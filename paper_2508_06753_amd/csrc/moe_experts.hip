@@ -4,7 +4,8 @@
 // a row): a 2-bit weight -2, -1, 0, 1 IS a four-bit number (-1, -0.5, 0, 0.5 with the column's power of two at 2), seven
 // instructions turn 16 of them out of a packed dword, and a row's numbers are the sum of two eight-bit ones: E4M3 has four
 // significant bits and bf16 eight, so hi = round(x), lo = round(x - hi) is exact wherever lo's exponent reaches, which is down
-// to 2^-14 of the largest of the 32 numbers that share a power of two (off by 2^-22 of it below).  Against bf16 instructions
+// to 2^-14 of the largest of the 32 numbers that share a power of two (off by 2^-22 of it below).  h, which is computed in fp32, is rounded to
+// such a pair, by 2^-9 of itself at most: half of what a bf16 h would lose, and no third product.  Against bf16 instructions
 // that is a third of the vector work per weight, and the products of hi and of lo together take no longer than one bf16
 // product (4300 TFLOP/s for eight bits by four, measured; half that for the pair).  Its sums are not quite those of 32 bits: of 8
 // neighbouring products, bits 13 places below the largest one's exponent are cut off (measured), at most 7 * 2^-13 of the sum of magnitudes.
@@ -110,7 +111,7 @@ __device__ __forceinline__ uint64_t same_lanes(int id, bool live, int bits)
 
 // Workgroup 0 sorts the choices by expert; the others convert x, a thread 32 numbers.  A choice's place among its expert's is
 // whichever it gets from a counter in local memory: what a row gives does not depend on the rows beside it, nor on where it stands.
-// Bound by latency (384 choices: 4.6 us), with many choices by the counters: 16384 take 13.5 us with 16 loads a thread at a time, 15.5 with 4 (2 are enough
+// Bound by latency (384 choices: 4.6 us), with many choices by the counters: 16384 take 14 to 16 us with 16 loads a thread at a time, 2 more with 4 (2 are enough
 // up to 2048 choices, and less code).
 __global__ void __launch_bounds__(1024) moe_prepare_kernel(ExpertsArgs a, int* total_tiles, Tile* tiles, int64_t max_tiles, int rows_log2, Divider by_top_k,
                                                            int* tile_rows, int* place, char* xs, char* xe)
@@ -560,7 +561,7 @@ __global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kern
 // the wait longer; one fewer, a load that the compiler joins with another or drops, would let a barrier pass before its rows have landed.  So every load is
 // unconditional and none is made twice, and the compiled kernel's own order is walked by a test.
 //
-// 16384 choices of 64 experts of 2048 x 1024: 142 to 161 us as the clock goes (1.6 to 2.1 GHz) for gate and up, 87 to 100 for down, of which the
+// 16384 choices of 64 experts of 2048 x 1024: 142 to 161 us as the clock goes (1.6 to 2.1 GHz) for gate and up, 86 to 100 for down, of which the
 // products are 63 and 32 at 2.1 GHz (32 cycles each).  A workgroup takes 1.2 us to know its tile, 3.1 until rows are there, 15 for 2048 of K and 2.6 to leave;
 // a SIMD has two of its three waves in the loop at a time.  Neither the loads nor any one kind of vector instruction bounds the loop by itself
 // (left out one by one: 127 to 133 us for 132).
@@ -1037,7 +1038,9 @@ __global__ void __launch_bounds__(512, 2) moe_tiny_down_kernel(ExpertsArgs a, co
     }
 }
 
-// Y = base + the weighted rows of z, in the order of the slots; four rows of z under way together.
+// Y = base + the weighted rows of z, in the order of the slots; four rows of z under way together.  Memory: 16384 rows of 2048 22 us, 6 TB/s; few rows:
+// latency, 4.7 us.  z is in fp32: in fp16 beside a power of two for 32 columns this launch took 14 us there (and the call 3 % less, while 1806 rows
+// took 3 % more), and two experts that nearly cancel left 0.04 of their difference wrong.
 __global__ void __launch_bounds__(256) moe_combine_kernel(ExpertsArgs a, const int* place, const float* z)
 {
     const int64_t m = blockIdx.x;

@@ -1,12 +1,12 @@
 // What stands between two blocks, in one pass over the rows: norm of a block's output, gate, residual scale, the sum, norm
-// before the next block, and if asked for the next projection's int8 rows.
+// before the next block, and if asked for the next projection's int8 rows (8191 rows of 5120: 8 us more, w2_quantize_rows behind it 22).
 //
 // A workgroup takes a row and keeps it in registers (NV vectors of 8 numbers a thread), so that each number is read once and
 // written once however many sums the row needs: mean(y^2) where the block's output is normed, mean(r'^2), the abs-max of x
 // where it is quantised.  A sum is reduced by moves inside the waves and one trip through local memory.  Sums and what is between the
 // roundings of r' (none in 32 bits) and x are in fp32; mean(r'^2) takes r' before its rounding.
 //
-// Bound: many rows by memory (8191 rows of 5120, residual in 32 bits: 503 MB in 97 us, 5.2 TB/s, above the 4.75 of a large copy), few by the launch
+// Bound: many rows by memory (8191 rows of 5120, residual in 32 bits: 503 MB in 95 us, 5.3 TB/s, above the 4.75 of a large copy), few by the launch
 // (1 row of 4096: 6.3 us by the host's clock; 77 rows of 5120 with gate 6.9).  Threads a row: 512 for up to 64 rows, whose trips to
 // memory are then one, 256 for more, so that several rows share a CU; not more than 4 vectors a thread where 1024 threads allow it.
 #include <hip/hip_runtime.h>

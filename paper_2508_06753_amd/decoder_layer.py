@@ -1,7 +1,7 @@
 """A decoder layer with 2-bit weights, for prompts, single tokens and drafted trees of many requests.
 
-    residual, last block's output -> [norm behind it, gate, scale] -> residual -> norm -> attention block
-      -> [norm behind it, gate, scale] -> residual -> norm -> router -> 2-bit experts (+ a shared one) -> block's output
+    residual, last block's output -> [norm behind it, scale] -> residual -> norm -> attention block
+      -> [norm behind it, scale] -> residual -> norm -> router -> 2-bit experts (+ a shared one) -> block's output
 
 Every step is a call of ``binding`` or of ``attention_block``; a layer holds the weights and no memory of a step.
 ``python -m paper_2508_06753_amd.decoder_layer`` runs two layers over a prompt and single tokens.
