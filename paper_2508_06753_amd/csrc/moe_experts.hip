@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(FEW_WAVES * 64, GPT == 2 ? 4 : 3) moe_few_kern
 // Of a stage's column blocks the products of the last one begin behind the barrier at which the next stage's rows are there; those are read
 // into registers as the products let go of them.  What may be under way at a barrier is counted (moe_plan.h).  An operation more than counted makes
 // the wait longer; one fewer, a load that the compiler joins with another or drops, would let a barrier pass before its rows have landed.  So every load is
-// unconditional and none is made twice, and the compiled kernel's own order is walked by a test.
+// unconditional, and the compiled kernel's own order is walked by a test.
 //
 // 16384 choices of 64 experts of 2048 x 1024: 142 to 161 us as the clock goes (1.6 to 2.1 GHz) for gate and up, 86 to 100 for down, of which the
 // products are 63 and 32 at 2.1 GHz (32 cycles each).  A workgroup takes 1.2 us to know its tile, 3.1 until rows are there, 15 for 2048 of K and 2.6 to leave;

@@ -27,8 +27,9 @@ struct Plan {
 inline int ranges(int64_t used, int64_t pairs, int64_t n_kt) { return used * (pairs / 4) < 768 && n_kt >= 8 ? 2 : 1; }
 
 // Choices per expert up to which the kernel for few rows takes them.  It reads an expert's weights once for every eight rows,
-// the other one once for 32 and is bound by issue.  us a call at 6, 8 choices an expert (128 of 4096 x 1024, groups of 128): few 107, 122, many 112, 114; at 8, 16
-// with groups of 64, whose products the matrix pipe does in halves (32 of 5120 x 2048): 87, 131 and 102, 140.
+// the other one once for 32 and is bound by issue.  us a call at 6, 8 choices an expert (128 of 4096 x 1024, groups of 128): few 102, 114, many 101, 108; at 8, 16
+// with groups of 64, whose products the matrix pipe does in halves (32 of 5120 x 2048): 87, 131 and 91, 119 (so they cross between the two; 16 is from before
+// the kernel for many wrote its sums straight from registers, when it took 102 and 140).
 constexpr int few_per_expert(int G) { return G == 128 ? 6 : 16; }
 
 inline Plan plan(int64_t hidden, int64_t inter, int E, int G, int64_t A)
